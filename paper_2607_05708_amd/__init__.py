@@ -22,6 +22,12 @@ Names follow the C ABI in ``include/memattn.h``:
 * ``mem_append_chunks``   -- Insert with append-only page allocation
 * ``mem_compact_blocks``  -- background block compaction (Eq. 2, Algorithm 2)
 * ``mem_colocate``        -- association-aware relocation (Algorithm 2, online stage)
+
+and in ``include/memattn_kv.h``, over the same pages and directory:
+
+* ``KvCache``, ``mem_kv_page_bytes`` -- a paged cache of keys and values in 16, 8 or 4 bits
+* ``mem_kv_write`` / ``mem_kv_read`` -- quantise tokens into it, read them back
+* ``mem_attend``          -- attention of each request's new tokens over its chunks
 """
 from __future__ import annotations
 
@@ -35,11 +41,13 @@ __all__ = ["MemError", "MEM_F32", "MEM_BF16", "MEM_ORDER_RANK", "MEM_ORDER_TIME"
            "mem_build_relations", "mem_retrieve_topk_scoped",
            "mem_build_relations_scoped", "mem_workspace_bytes_grouped", "mem_retrieve_topk_grouped", "mem_gather_chunks", "mem_gather_budget", "mem_append_chunks",
            "mem_compact_workspace_bytes", "mem_compact_blocks", "mem_colocate_workspace_bytes", "mem_colocate",
-           "BankState"]
+           "BankState", "MEM_KV_BF16", "MEM_KV_FP8", "MEM_KV_FP4", "KvCache", "mem_kv_page_bytes", "mem_kv_write",
+           "mem_kv_read", "mem_attend_workspace_bytes", "mem_attend"]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 MEM_F32, MEM_BF16 = 0, 1
 MEM_ORDER_RANK, MEM_ORDER_TIME = 0, 1
+MEM_KV_BF16, MEM_KV_FP8, MEM_KV_FP4 = 0, 1, 2
 
 
 class MemBank(C.Structure):
@@ -66,6 +74,22 @@ class MemCompactResult(C.Structure):
 
 class MemColocateResult(C.Structure):
     _fields_ = [("moved_chunks", C.c_int64), ("groups", C.c_int64), ("next_free_page", C.c_int64)]
+
+
+class MemKv(C.Structure):
+    _fields_ = [("pages", MemPages), ("page_tokens", C.c_int32), ("heads", C.c_int32), ("head_dim", C.c_int32),
+                ("format", C.c_int32)]
+
+
+class MemKvRows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class MemAttendArgs(C.Structure):
+    _fields_ = [("tok_len", C.c_void_p), ("ids", C.c_void_p), ("m", C.c_int64), ("k", C.c_int32),
+                ("heads_q", C.c_int32), ("q_offsets", C.c_void_p), ("q_pos", C.c_void_p), ("scale", C.c_float),
+                ("softcap", C.c_float), ("slopes", C.c_void_p), ("causal", C.c_int32), ("window", C.c_int32),
+                ("prefix_len", C.c_void_p), ("chunk_ns", C.c_void_p), ("query_ns", C.c_void_p)]
 
 
 class MemError(RuntimeError):
@@ -126,6 +150,15 @@ def lib():
         L.mem_colocate.restype = C.c_int
         L.mem_append_chunks.argtypes = [C.POINTER(MemBank), i64, P, i64, i64, P, i32, C.POINTER(C.c_int64), i64, P]
         L.mem_append_chunks.restype = C.c_int
+        L.mem_kv_page_bytes.argtypes = [i32, i32, i32, i32]
+        L.mem_kv_page_bytes.restype = C.c_size_t
+        for f in (L.mem_kv_write, L.mem_kv_read):
+            f.argtypes = [C.POINTER(MemKv), C.POINTER(MemKvRows), C.POINTER(MemKvRows), i32, P, P, i64, P]
+            f.restype = C.c_int
+        L.mem_attend_workspace_bytes.argtypes = [C.POINTER(MemKv), i64, i32, i64, i32]
+        L.mem_attend_workspace_bytes.restype = C.c_size_t
+        L.mem_attend.argtypes = [C.POINTER(MemKv), C.POINTER(MemAttendArgs), P, i64, i64, i64, P, P, P, C.c_size_t, P]
+        L.mem_attend.restype = C.c_int
         L.mem_status_string.argtypes = [C.c_int]
         L.mem_status_string.restype = C.c_char_p
         L.mem_last_error.argtypes = []
@@ -500,3 +533,149 @@ def mem_append_chunks(state: BankState, new_emb: torch.Tensor, stream=None) -> B
                                                         state.n_pages_cap, _stream(stream)))
     state.n, state.next_free_page = int(b.n), int(nfp.value)
     return state
+
+
+def _used_on(stream, *tensors):
+    """Tensors allocated here on the current stream stay theirs until `stream` is done with them."""
+    if stream is not None and stream.cuda_stream != _stream(None):
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+
+
+def _i32(t: torch.Tensor | None, shape: tuple, name: str, dtype=torch.int32):
+    """Pointer of a contiguous GPU array of the given shape (None: NULL)."""
+    if t is None:
+        return None
+    if (not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != dtype or t.shape != shape
+            or not t.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous {dtype} {list(shape)} GPU tensor")
+    return t.data_ptr()
+
+
+def mem_kv_page_bytes(page_tokens: int, heads: int, head_dim: int, format: int) -> int:
+    """Bytes of one page of a key/value cache (0 on invalid sizes)."""
+    return int(lib().mem_kv_page_bytes(page_tokens, heads, head_dim, format))
+
+
+class KvCache:
+    """One layer's paged cache of keys and values over a page pool and its directory.
+
+    ``pool``: uint8 [n_pages, page_bytes] GPU tensor, page_bytes >= mem_kv_page_bytes(...);
+    ``table``: int32 [n_chunks, pages_per_chunk] GPU tensor; ``page_tokens`` tokens per page of ``heads`` heads of
+    ``head_dim``; ``format``: MEM_KV_BF16, MEM_KV_FP8 or MEM_KV_FP4.  The tensors are kept, not copied: pages may be
+    written, gathered, compacted and relocated by the other calls in between.
+    """
+
+    def __init__(self, pool: torch.Tensor, table: torch.Tensor, page_tokens: int, heads: int, head_dim: int,
+                 format: int):
+        _dev(pool, "pool")
+        if pool.dim() != 2 or not pool.is_contiguous():
+            raise ValueError("pool must be contiguous [n_pages, page_bytes]")
+        if table.dim() != 2:
+            raise ValueError("table must be int32 [n_chunks, pages_per_chunk]")
+        ptr = _i32(table, tuple(table.shape), "table")
+        if table.device != pool.device:
+            raise ValueError("table must be on the pool's device")
+        self.pool, self.table = pool, table
+        self.page_tokens, self.heads, self.head_dim, self.format = page_tokens, heads, head_dim, format
+        pages = MemPages(pool.data_ptr(), pool.shape[0], pool.shape[1] * pool.element_size(), ptr, table.shape[0],
+                         table.shape[1])
+        self._c = MemKv(pages, page_tokens, heads, head_dim, format)
+
+
+def _kv_rows(cache: KvCache, t: torch.Tensor, n: int, dtype, name: str) -> MemKvRows:
+    if (not isinstance(t, torch.Tensor) or t.device != cache.pool.device or t.dtype != dtype
+            or t.shape != (n, cache.heads, cache.head_dim) or (n and t.stride(2) != 1)):
+        raise ValueError(f"{name} must be {dtype} [{n}, {cache.heads}, {cache.head_dim}] on the cache's GPU with "
+                         "unit stride along the last dimension")
+    return MemKvRows(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _kv_dtype(dtype) -> int:
+    if dtype == torch.float32:
+        return MEM_F32
+    if dtype == torch.bfloat16:
+        return MEM_BF16
+    raise TypeError(f"keys and values must be float32 or bfloat16, got {dtype}")
+
+
+def mem_kv_write(cache: KvCache, k: torch.Tensor, v: torch.Tensor, chunk: torch.Tensor, pos: torch.Tensor, *,
+                 stream=None) -> None:
+    """Quantise tokens into the cache: rows i of ``k`` and ``v`` ([n, heads, head_dim], float32 or bfloat16, any
+    token and head strides) become token ``pos[i]`` of chunk ``chunk[i]`` (int32 [n]).  A chunk of -1 skips the
+    token; no two tokens may name one place."""
+    n, dt = k.shape[0], _kv_dtype(k.dtype)
+    kr, vr = _kv_rows(cache, k, n, k.dtype, "k"), _kv_rows(cache, v, n, k.dtype, "v")
+    _check("mem_kv_write", lib().mem_kv_write(C.byref(cache._c), C.byref(kr), C.byref(vr), dt,
+                                              _i32(chunk, (n,), "chunk"), _i32(pos, (n,), "pos"), n, _stream(stream)))
+
+
+def mem_kv_read(cache: KvCache, chunk: torch.Tensor, pos: torch.Tensor, *, dtype=torch.bfloat16, out=None,
+                stream=None):
+    """Tokens ``pos[i]`` of chunks ``chunk[i]`` (int32 [n]) as dense rows: (k, v), each [n, heads, head_dim] of
+    ``dtype`` (or written into ``out``, a pair of such tensors).  Both dtypes hold the cache's values exactly;
+    places outside the cache give zeros."""
+    n = chunk.shape[0]
+    if out is None:
+        out = tuple(torch.empty((n, cache.heads, cache.head_dim), dtype=dtype, device=cache.pool.device)
+                    for _ in range(2))
+        _used_on(stream, *out)
+    k, v = out
+    dt = _kv_dtype(k.dtype)
+    kr, vr = _kv_rows(cache, k, n, k.dtype, "out k"), _kv_rows(cache, v, n, k.dtype, "out v")
+    _check("mem_kv_read", lib().mem_kv_read(C.byref(cache._c), C.byref(kr), C.byref(vr), dt,
+                                            _i32(chunk, (n,), "chunk"), _i32(pos, (n,), "pos"), n, _stream(stream)))
+    return k, v
+
+
+def mem_attend_workspace_bytes(cache: KvCache, m: int, k: int, total_q: int, heads_q: int) -> int:
+    return int(lib().mem_attend_workspace_bytes(C.byref(cache._c), m, k, total_q, heads_q))
+
+
+def mem_attend(cache: KvCache, tok_len: torch.Tensor, ids: torch.Tensor, q: torch.Tensor, scale: float, *,
+               q_offsets: torch.Tensor | None = None, q_pos: torch.Tensor | None = None, causal: bool = False,
+               window: int = 0, prefix_len: torch.Tensor | None = None, chunk_ns: torch.Tensor | None = None,
+               query_ns: torch.Tensor | None = None, softcap: float = 0.0, slopes: torch.Tensor | None = None,
+               out=None, workspace: torch.Tensor | None = None, stream=None):
+    """Attention of each request's new tokens over its chunks: (out bfloat16 [total_q, heads_q, head_dim], lse
+    float32 [total_q, heads_q]).
+
+    ``tok_len`` int32 [n_chunks]: tokens held by each chunk; ``ids`` int32 [m, k]: each request's chunks in context
+    order (-1 = none); ``q`` bfloat16 [total_q, heads_q, head_dim], any token and head strides.  Request i's new
+    tokens are rows ``q_offsets[i]`` to ``q_offsets[i + 1]`` of q (int32 [m + 1]; None: total_q / m each) and are
+    the last of their context unless ``q_pos`` (int32 [total_q]) says where they are.  A token sees positions up to
+    its own with ``causal``, above its own minus ``window`` (0: all), always those below ``prefix_len`` (int32 [m]),
+    and only chunks whose ``chunk_ns`` (int32 [n_chunks], negative: deleted) equals its ``query_ns`` (int32
+    [total_q]).  Scores are ``softcap * tanh(scale <q, k> / softcap) - slopes[head] * distance`` (float32 [heads_q]).
+    A token that sees nothing gets zeros and an lse of -inf.
+    """
+    if ids.dim() != 2 or q.dim() != 3:
+        raise ValueError("ids must be int32 [m, k]; q bfloat16 [total_q, heads_q, head_dim]")
+    m, k = ids.shape
+    total_q, heads_q, d = q.shape
+    dev, n_chunks = cache.pool.device, cache.table.shape[0]
+    if q.dtype != torch.bfloat16 or q.device != dev or d != cache.head_dim or (total_q and q.stride(2) != 1):
+        raise ValueError(f"q must be bfloat16 [total_q, heads_q, {cache.head_dim}] on the cache's GPU with unit "
+                         "stride along the last dimension")
+    a = MemAttendArgs(_i32(tok_len, (n_chunks,), "tok_len"), _i32(ids, (m, k), "ids"), m, k, heads_q,
+                      _i32(q_offsets, (m + 1,), "q_offsets"), _i32(q_pos, (total_q,), "q_pos"), scale, softcap,
+                      _i32(slopes, (heads_q,), "slopes", torch.float32), 1 if causal else 0, window,
+                      _i32(prefix_len, (m,), "prefix_len"), _i32(chunk_ns, (n_chunks,), "chunk_ns"),
+                      _i32(query_ns, (total_q,), "query_ns"))
+    if out is None:
+        out = (torch.empty((total_q, heads_q, d), dtype=torch.bfloat16, device=dev),
+               torch.empty((total_q, heads_q), dtype=torch.float32, device=dev))
+        _used_on(stream, *out)
+    o, lse = out
+    if workspace is None:
+        size = mem_attend_workspace_bytes(cache, m, k, total_q, heads_q)
+        workspace = torch.empty(max(size, 1), dtype=torch.uint8, device=dev)
+        _used_on(stream, workspace)
+    _dev(workspace, "workspace")
+    _check("mem_attend", lib().mem_attend(C.byref(cache._c), C.byref(a), q.data_ptr(), total_q, q.stride(0),
+                                          q.stride(1), _i32(o, (total_q, heads_q, d), "out", torch.bfloat16),
+                                          _i32(lse, (total_q, heads_q), "out lse", torch.float32),
+                                          workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                                          _stream(stream)))
+    return o, lse

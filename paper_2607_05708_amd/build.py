@@ -1,6 +1,7 @@
 """Build the HIP libraries in-tree with hipcc for gfx950.
 
-* ``libmemattn.so``  -- the retrieval/gather library (C ABI in include/memattn.h)
+* ``libmemattn.so``  -- the retrieval/gather library (C ABI in include/memattn.h
+  and include/memattn_kv.h)
 * ``libmeminputs.so`` -- the device payload generator used to fill large
   synthetic page pools (input generation, not part of the method)
 
@@ -25,7 +26,7 @@ DEVICE_FLAGS = [f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-mcode-
 
 LIBS = {
     "libmemattn.so": ["csrc/api.cpp", "csrc/topk_valu.hip", "csrc/topk_score.hip", "csrc/topk_mfma.hip", "csrc/gather_append.hip",
-                      "csrc/compact.hip", "csrc/scope.hip"],
+                      "csrc/compact.hip", "csrc/scope.hip", "csrc/kv_api.cpp", "csrc/kv_cache.hip", "csrc/attend.hip"],
     "libmeminputs.so": ["inputs_hip/fill_payload.hip"],
 }
 

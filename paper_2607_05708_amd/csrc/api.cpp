@@ -12,6 +12,7 @@
 #include <string>
 
 #include "memattn.h"
+#include "error.h"
 #include "launch.h"
 
 namespace memattn {
@@ -20,7 +21,8 @@ namespace {
 
 thread_local std::string g_last_error;
 
-mem_status fail(mem_status s, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
+}  // namespace
+
 mem_status fail(mem_status s, const char* fmt, ...) {
   char buf[512];
   va_list ap;
@@ -35,6 +37,10 @@ mem_status device_status(hipError_t e, const char* what) {
   if (e == hipSuccess) return MEM_OK;
   return fail(MEM_ERR_DEVICE, "%s: %s", what, hipGetErrorString(e));
 }
+
+void clear_error() { g_last_error.clear(); }
+
+namespace {
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 size_t align256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }

@@ -1,0 +1,496 @@
+"""The key/value cache and the attention over it on the GPU, against the 64-bit
+model of kv_reference.py."""
+import itertools
+
+import numpy as np
+import pytest
+import torch
+
+import kv_reference as ref
+import paper_2607_05708_amd as pm
+
+pytestmark = pytest.mark.gpu
+
+FMTS = {"bf16": pm.MEM_KV_BF16, "fp8": pm.MEM_KV_FP8, "fp4": pm.MEM_KV_FP4}
+
+
+@pytest.fixture(scope="module", autouse=True)
+def dev():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+
+
+def up(a):
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+def host(t):
+    torch.cuda.synchronize()
+    return t.float().cpu().numpy().astype(np.float64)
+
+
+def new_cache(fmt, n_chunks, ppc, page_tokens, heads, d, seed=0, spare=0):
+    """A pool full of NaN patterns (all bits set), so that a place that should not be read shows."""
+    rng = np.random.default_rng(seed)
+    n_pages = n_chunks * ppc + spare
+    pool = np.full((n_pages, ref.page_bytes(fmt, page_tokens, heads, d)), 255, np.uint8)
+    table = rng.permutation(n_pages)[:n_chunks * ppc].reshape(n_chunks, ppc).astype(np.int32)
+    return pool, table
+
+
+# ---------------------------------------------------------------- writing and reading back
+
+def edge_rows(d, dtype):
+    """Rows that hold every place where rounding or the scale changes: the midpoints between codes and their
+    neighbours, at scales from the smallest to the largest, zeros, infinities and NaN."""
+    rows = []
+    for fmt in (ref.FP4, ref.FP8):
+        g = ref.GRID[fmt]
+        mids = (g[1:] + g[:-1]) / 2
+        pts = np.concatenate([g, mids, np.nextafter(mids.astype(np.float32), np.float32(0)).astype(np.float64),
+                              np.nextafter(mids.astype(np.float32), np.float32(1e9)).astype(np.float64)])
+        top = ref.TOP[fmt]
+        blocks = [np.append(pts[i:i + 31], np.zeros(max(0, 31 - len(pts[i:i + 31])))) for i in range(0, len(pts), 31)]
+        for e in (0, -3, 40, -100, -118, 115):
+            for lead in (g[-1], top):
+                rows += [np.append(b, lead) * 2.0 ** e for b in blocks[:6 if e else None]]
+        for a in (top, np.nextafter(np.float32(top), np.float32(1e9)), top / 2, 1.0, 1.999):
+            rows.append(np.append(np.linspace(-a, a, 31), a))
+    rows += [np.zeros(32), np.full(32, -0.0), np.full(32, 1e-40), np.full(32, 3.4e38),
+             np.append(np.ones(31), np.inf), np.append(np.ones(31), -np.inf), np.append(np.ones(31), np.nan),
+             np.append(np.full(31, np.inf), np.nan)]
+    x = np.stack(rows)
+    x = np.concatenate([x, -x])
+    if dtype == torch.bfloat16:
+        x = ref.to_bf16(x)
+    x = x.astype(np.float32)
+    n = -(-x.size // d)
+    return np.append(x.ravel(), np.zeros(n * d - x.size, np.float32)).reshape(n, d)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("name", list(FMTS))
+def test_round_trip_of_every_rounding_boundary(name, dtype):
+    fmt, d, heads = FMTS[name], 64, 1
+    x = edge_rows(d, dtype)
+    n = x.shape[0]
+    pool, table = new_cache(fmt, -(-n // 64), 2, 32, heads, d)
+    cache = pm.KvCache(up(pool), up(table), 32, heads, d, fmt)
+    k = up(x).to(dtype).view(n, 1, d)
+    chunk, pos = np.arange(n) // 64, np.arange(n) % 64
+    args = up(chunk.astype(np.int32)), up(pos.astype(np.int32))
+    pm.mem_kv_write(cache, k, -k, *args)
+    got = ref.views(fmt, 32, 1, d, cache.pool.cpu().numpy())
+    for sign, (gc, gs) in zip((1, -1), got):
+        c, s = (a[table[chunk, pos // 32], 0, pos % 32] for a in (gc, gs))
+        codes, scale = (a[:, 0] for a in ref.encode_rows(fmt, sign * x.astype(np.float64)[:, None, :]))
+        assert np.array_equal(s, scale), "scale bytes"
+        if fmt == ref.BF16:                                  # a NaN keeps being one, whichever
+            c, codes, dead = np.ascontiguousarray(c).view(np.uint16), codes.view(np.uint16), np.isnan(x)
+        else:
+            dead = np.repeat(scale == 255, c.shape[1] // scale.shape[1], -1)
+        assert np.array_equal(c[~dead], codes[~dead]), f"codes of rows {np.unique(np.argwhere((c != codes) & ~dead)[:, 0])}"
+    for out_dtype in (torch.float32, torch.bfloat16):
+        rk, rv = pm.mem_kv_read(cache, *args, dtype=out_dtype)
+        for sign, t in ((1, rk), (-1, rv)):
+            want = ref.decode_rows(fmt, *ref.encode_rows(fmt, sign * x.astype(np.float64)[:, None, :]))
+            assert np.array_equal(host(t), want, equal_nan=True)
+
+
+@pytest.mark.parametrize("n", [1, 7, 64, 333])
+@pytest.mark.parametrize("name,heads,d,page_tokens,ppc,dtype", [
+    ("fp4", 8, 128, 64, 2, torch.bfloat16), ("fp4", 3, 256, 32, 5, torch.float32), ("fp4", 1, 64, 96, 1, torch.bfloat16),
+    ("fp8", 5, 64, 32, 3, torch.float32), ("fp8", 2, 256, 128, 1, torch.bfloat16), ("bf16", 3, 128, 32, 4, torch.float32),
+    ("bf16", 12, 64, 64, 2, torch.bfloat16)])
+def test_round_trip_over_a_shuffled_directory(name, heads, d, page_tokens, ppc, dtype, n):
+    fmt = FMTS[name]
+    rng = np.random.default_rng(n)
+    cap = page_tokens * ppc
+    n_chunks = -(-n // cap) + 2
+    pool, table = new_cache(fmt, n_chunks, ppc, page_tokens, heads, d, n, spare=3)
+    cache = pm.KvCache(up(pool), up(table), page_tokens, heads, d, fmt)
+    at = rng.permutation(n_chunks * cap)[:n]
+    chunk, pos = (at // cap).astype(np.int32), (at % cap).astype(np.int32)
+    qkv = torch.randn((n, 2 * heads + 1, d), device="cuda").to(dtype)       # rows of a fused projection
+    k, v = qkv[:, 1:1 + heads], qkv[:, 1 + heads:]
+    pm.mem_kv_write(cache, k, v, up(chunk), up(pos))
+    expect = pool.copy()
+    kn, vn = host(k), host(v)
+    ref.put(fmt, page_tokens, expect, table[chunk, pos // page_tokens], pos % page_tokens, kn, vn)
+    assert np.array_equal(cache.pool.cpu().numpy(), expect)                 # and nothing else was touched
+    back = rng.permutation(n)
+    rk, rv = pm.mem_kv_read(cache, up(chunk[back]), up(pos[back]), dtype=dtype)
+    for t, which in ((rk, 0), (rv, 1)):
+        want = ref.get(fmt, page_tokens, heads, d, expect, table[chunk, pos // page_tokens], pos % page_tokens)[which]
+        assert np.array_equal(host(t), want[back])
+
+
+@pytest.mark.parametrize("name,dtype", itertools.product(FMTS, [torch.float32, torch.bfloat16]))
+def test_rows_with_odd_strides(name, dtype):
+    # rows that 16-byte accesses cannot reach, head-major input and a broadcast head
+    fmt, n, heads, d = FMTS[name], 21, 3, 64
+    pool, table = new_cache(fmt, 1, 1, 32, heads, d)
+    chunk, pos = np.zeros(n, np.int32), np.arange(n, dtype=np.int32)
+    flat = torch.randn(n * (heads * 65 + 3) + 1, device="cuda").to(dtype)
+    odd = flat[1:].view(n, heads * 65 + 3)[:, :heads * 65].view(n, heads, 65)[:, :, :d]
+    major = torch.randn((heads, n, d), device="cuda").to(dtype).transpose(0, 1)
+    one = torch.randn((n, 1, d), device="cuda").to(dtype).expand(n, heads, d)
+    for k, v in ((odd, major), (major, one)):
+        cache = pm.KvCache(up(pool), up(table), 32, heads, d, fmt)
+        pm.mem_kv_write(cache, k, v, up(chunk), up(pos))
+        expect = pool.copy()
+        ref.put(fmt, 32, expect, np.full(n, table[0, 0]), pos, host(k), host(v))
+        assert np.array_equal(cache.pool.cpu().numpy(), expect)
+        a, b = pm.mem_kv_read(cache, up(chunk), up(pos), dtype=dtype)
+        out = torch.full_like(flat, 7.0)
+        po = out[1:].view(n, heads * 65 + 3)[:, :heads * 65].view(n, heads, 65)[:, :, :d]
+        pv = torch.full((heads, n, d), 7.0, device="cuda", dtype=dtype).transpose(0, 1)
+        pm.mem_kv_read(cache, up(chunk), up(pos), out=(po, pv))
+        assert torch.equal(po, a) and torch.equal(pv, b)
+        kept = torch.ones_like(flat, dtype=torch.bool)
+        kept[1:].view(n, heads * 65 + 3)[:, :heads * 65].view(n, heads, 65)[:, :, :d] = False
+        assert (out[kept] == 7).all()
+
+
+def test_places_outside_the_cache_are_skipped_and_read_as_zeros():
+    fmt, heads, d, T, ppc = pm.MEM_KV_FP4, 2, 64, 32, 2
+    pool, table = new_cache(fmt, 4, ppc, T, heads, d)
+    table[1, 1], table[2, 0] = -1, 8                                        # no page, a page past the pool
+    chunk = np.array([0, -1, 4, 0, 0, 1, 1, 2, 2, -2 ** 31, 2 ** 31 - 1, 0], np.int32)
+    pos = np.array([5, 0, 0, -1, 64, 31, 32, 3, 40, 0, 0, 2 ** 31 - 1], np.int32)
+    ok = np.array([1, 0, 0, 0, 0, 1, 0, 0, 1, 0, 0, 0], bool)
+    n = len(chunk)
+    cache = pm.KvCache(up(pool), up(table), T, heads, d, fmt)
+    k, v = torch.randn((n, heads, d), device="cuda"), torch.randn((n, heads, d), device="cuda")
+    pm.mem_kv_write(cache, k, v, up(chunk), up(pos))
+    expect = pool.copy()
+    page, row = table[chunk[ok], pos[ok] // T], pos[ok] % T
+    ref.put(fmt, T, expect, page, row, host(k)[ok], host(v)[ok])
+    assert np.array_equal(cache.pool.cpu().numpy(), expect)
+    rk, rv = pm.mem_kv_read(cache, up(chunk), up(pos), dtype=torch.float32)
+    assert (host(rk)[~ok] == 0).all() and (host(rv)[~ok] == 0).all()
+    wk, wv = ref.get(fmt, T, heads, d, expect, page, row)
+    assert np.array_equal(host(rk)[ok], wk) and np.array_equal(host(rv)[ok], wv)
+
+
+def test_empty_calls():
+    pool, table = new_cache(pm.MEM_KV_FP4, 1, 1, 32, 1, 64)
+    cache = pm.KvCache(up(pool), up(table), 32, 1, 64, pm.MEM_KV_FP4)
+    none = torch.zeros(0, dtype=torch.int32, device="cuda")
+    x = torch.zeros((0, 1, 64), device="cuda")
+    pm.mem_kv_write(cache, x, x, none, none)
+    k, v = pm.mem_kv_read(cache, none, none)
+    assert k.shape == v.shape == (0, 1, 64)
+    assert np.array_equal(cache.pool.cpu().numpy(), pool)
+    o, l = pm.mem_attend(cache, none.new_zeros(1), none.new_zeros((3, 2)), torch.zeros((0, 2, 64), device="cuda",
+                                                                                   dtype=torch.bfloat16), 1.0)
+    assert o.shape == (0, 2, 64) and l.shape == (0, 2)
+
+
+# ---------------------------------------------------------------- attention
+
+class Problem:
+    """A seeded cache with `lens[i]` tokens in each chunk of request i, and queries over it."""
+
+    def __init__(self, seed, fmt, lens, nq, hq, heads, d, page_tokens=32, ppc=2, k=None, docs=0, holes=False,
+                 spread=1.0):
+        rng = np.random.default_rng(seed)
+        self.fmt, self.hq, self.heads, self.d, self.T, self.ppc = fmt, hq, heads, d, page_tokens, ppc
+        m, flat = len(lens), [x for r in lens for x in r]
+        n_chunks = len(flat) + 2
+        self.pool, self.table = new_cache(fmt, n_chunks, ppc, page_tokens, heads, d, seed, spare=2)
+        k = k or max(1, max(len(r) for r in lens))
+        self.ids = np.full((m, k), -1, np.int32)
+        self.tok_len = np.zeros(n_chunks, np.int32)
+        self.chunk_ns = rng.integers(-1, docs, n_chunks).astype(np.int32) if docs else None
+        order = rng.permutation(n_chunks)[:len(flat)]
+        at = 0
+        self.ctx = []                                       # per request: list of (page or -1, row, chunk)
+        for i, r in enumerate(lens):
+            slots = np.sort(rng.permutation(k)[:len(r)]) if holes else np.arange(len(r))
+            toks = []
+            for s, n in zip(slots, r):
+                c = order[at]
+                at += 1
+                self.ids[i, s] = c
+                self.tok_len[c] = n
+                t = np.arange(n)
+                page, row = self.table[c, t // page_tokens], t % page_tokens
+                toks += [(int(a), int(b), int(c)) for a, b in zip(page, row)]
+                x = rng.standard_normal((2, n, heads, d)) * spread
+                ref.put(fmt, page_tokens, self.pool, page, row, x[0], x[1])
+            self.ctx.append(toks)
+        if holes:
+            for i in range(m):
+                gone = self.ids[i] < 0
+                self.ids[i, gone] = rng.choice([-1, n_chunks, 2 ** 31 - 1, -2 ** 31], gone.sum())
+        self.nq = list(nq)
+        self.off = np.concatenate([[0], np.cumsum(self.nq)]).astype(np.int32)
+        total = int(self.off[-1])
+        self.q = torch.from_numpy(rng.standard_normal((total, hq, d)).astype(np.float32)).to(torch.bfloat16)
+        self.query_ns = rng.integers(-1, docs, total).astype(np.int32) if docs else None
+        self.slopes = (2.0 ** (-8.0 * (np.arange(hq) + 1) / hq)).astype(np.float32)
+        self.scale = float(np.float32(1.0 / np.sqrt(d) / spread))
+
+    def cache(self):
+        return pm.KvCache(up(self.pool), up(self.table), self.T, self.heads, self.d, self.fmt)
+
+    def gpu(self, causal=False, window=0, prefix=None, cap=0.0, bias=False, q_pos=None, offsets=True, q=None, **kw):
+        opt = lambda a, t=np.int32: None if a is None else up(np.asarray(a, t))  # noqa: E731
+        out = pm.mem_attend(kw.pop("cache", None) or self.cache(), up(self.tok_len), up(self.ids),
+                            self.q.cuda() if q is None else q, self.scale,
+                            q_offsets=up(self.off) if offsets else None, q_pos=opt(q_pos), causal=causal,
+                            window=window, prefix_len=opt(prefix), chunk_ns=opt(self.chunk_ns),
+                            query_ns=opt(self.query_ns), softcap=cap,
+                            slopes=opt(self.slopes, np.float32) if bias else None, **kw)
+        return host(out[0]), host(out[1])
+
+    def model(self, causal=False, window=0, prefix=None, cap=0.0, bias=False, q_pos=None):
+        parts = []
+        q = self.q.float().numpy().astype(np.float64)
+        for i, toks in enumerate(self.ctx):
+            a, b = self.off[i], self.off[i + 1]
+            n = len(toks)
+            page, row = (np.array([t[j] for t in toks], np.int64) for j in (0, 1))
+            present = (page >= 0) & (page < len(self.pool))
+            k, v = ref.get(self.fmt, self.T, self.heads, self.d, self.pool, np.where(present, page, 0), row)
+            doc = None if self.chunk_ns is None else np.array([self.chunk_ns[c] for _, _, c in toks], np.int64)
+            qpos = np.arange(b - a) + n - (b - a) if q_pos is None else np.asarray(q_pos[a:b], np.int64)
+            parts.append(ref.attend(q[a:b], k, v, doc, present, qpos,
+                                    None if doc is None else self.query_ns[a:b], self.scale, causal, window,
+                                    0 if prefix is None else prefix[i], cap, self.slopes if bias else None))
+        return [np.concatenate(x) for x in zip(*parts)]
+
+    def check(self, name, offsets=True, **masks):
+        out, lse = self.gpu(offsets=offsets, **masks)
+        ref.check_attend(name, out, lse, *self.model(**masks))
+
+
+SHAPES = [("fp4", 32, 8, 128), ("fp4", 5, 5, 64), ("fp4", 16, 1, 256), ("fp8", 12, 4, 128), ("fp8", 2, 1, 64),
+          ("fp8", 6, 2, 256), ("bf16", 16, 2, 128), ("bf16", 3, 3, 64), ("bf16", 8, 1, 256)]
+
+
+@pytest.mark.parametrize("name,hq,heads,d", SHAPES)
+def test_single_tokens(name, hq, heads, d):
+    # contexts of 0 tokens, 1 token, ends inside pages and tiles, chunks that hold nothing, holes in the lists
+    lens = [[], [1], [64, 31, 64], [33], [0, 64, 0, 5], [64] * 7, [32], [2, 63, 64, 17, 1]]
+    p = Problem(hq + d, FMTS[name], lens, [1] * len(lens), hq, heads, d, k=9, holes=True)
+    p.check("plain", offsets=False)
+    p.check("cap", cap=5.0)
+    p.check("bias, window", bias=True, window=40)
+
+
+@pytest.mark.parametrize("name,hq,heads,d", SHAPES)
+@pytest.mark.parametrize("masks", [dict(), dict(causal=True), dict(causal=True, window=37, cap=20.0),
+                                   dict(causal=True, window=9, bias=True, prefix=[3, 0, 70, 1000, 5]),
+                                   dict(window=1)])
+def test_several_tokens(name, hq, heads, d, masks):
+    lens = [[64, 64, 20], [5], [64, 1, 64, 64], [40, 33], []]
+    nq = [9, 5, 70, 0, 3]
+    p = Problem(3 * hq + d, FMTS[name], lens, nq, hq, heads, d)
+    p.check(str(masks), **masks)
+
+
+@pytest.mark.parametrize("name,hq,heads,d", SHAPES[:4] + SHAPES[6:8])
+def test_documents(name, hq, heads, d):
+    # chunks and tokens of three documents, deleted chunks, tokens that may see nothing
+    lens = [[64, 20, 64, 1, 64], [64, 64], [3, 64, 9], []]
+    p = Problem(hq * d, FMTS[name], lens, [40, 1, 17, 2], hq, heads, d, docs=3)
+    p.check("documents")
+    p.check("documents, causal", causal=True, prefix=[10, 0, 0, 0])
+    p.check("documents, window", window=30, cap=10.0)
+
+
+@pytest.mark.parametrize("nq", [1, 2, 4, 5, 16, 33, 64, 65, 128, 200])
+@pytest.mark.parametrize("group", [1, 3, 8, 16])
+def test_row_counts(nq, group):
+    # rows (tokens x heads of a group) around every tile's edge
+    p = Problem(nq * group, ref.FP4, [[64, 64, 64, 64, 50], [64, 30]], [nq, nq // 2], 2 * group, 2, 64)
+    p.check("causal", causal=True)
+
+
+@pytest.mark.parametrize("page_tokens,ppc", [(32, 1), (64, 3), (96, 2), (160, 1), (256, 2)])
+@pytest.mark.parametrize("name", list(FMTS))
+def test_page_sizes(name, page_tokens, ppc):
+    cap = page_tokens * ppc
+    lens = [[cap, cap - 1, cap], [1, cap // 2 + 1, cap], [cap]]
+    p = Problem(page_tokens + ppc, FMTS[name], lens, [1, 3, 20], 4, 2, 64, page_tokens=page_tokens, ppc=ppc)
+    p.check("pages", causal=True)
+
+
+def test_positions_given_by_the_caller():
+    lens = [[64, 64, 10], [30]]
+    p = Problem(5, ref.FP8, lens, [6, 4], 4, 2, 64)
+    pos = [0, 137, 138, 500, -1, 64, 29, 3, -2 ** 31, 2 ** 31 - 1]
+    p.check("any positions", causal=True, q_pos=pos)
+    p.check("any positions, window", window=20, q_pos=pos)
+    pos = [0, 137, 138, 500, -1, 64, 29, 3, -40, 1000]
+    p.check("any positions, bias", bias=True, q_pos=pos)
+
+
+@pytest.mark.parametrize("nq", [1, 40])
+def test_pages_outside_the_pool_are_not_seen(nq):
+    p = Problem(6, ref.FP4, [[64, 64, 64], [64, 7]], [nq, nq], 4, 2, 64)
+    for i, j, val in ((0, 0, -1), (0, 2, len(p.pool)), (1, 1, 2 ** 31 - 1)):
+        c = p.ids[i, j]
+        old = p.table[c, 0]
+        p.table[c, 0] = val
+        p.ctx[i] = [(val if page == old else page, r, cc) for page, r, cc in p.ctx[i]]
+    p.check("holes", causal=True)
+
+
+@pytest.mark.parametrize("name", list(FMTS))
+@pytest.mark.parametrize("nq", [1, 12, 90])
+def test_unseen_tokens_have_no_influence(name, nq):
+    # a NaN token, seen by the tokens behind it only; every other output is the one without it
+    fmt = FMTS[name]
+    p = Problem(7, fmt, [[64, 64]], [nq], 4, 2, 64)
+    masks = dict(causal=True, window=30)
+    clean = p.model(**masks)
+    at = 128 - nq // 2 - 1
+    page, row, _ = p.ctx[0][at]
+    nan = np.full((2, 64), np.nan)
+    ref.put(fmt, 32, p.pool, page, row, nan, nan)
+    out, lse = p.gpu(**masks)
+    qpos = np.arange(nq) + 128 - nq
+    sees = (qpos >= at) & (qpos - 30 < at)
+    live = [x[~sees] for x in (out, lse, *clean)]
+    if (~sees).any():
+        ref.check_attend("rows that do not see it", *live)
+    assert np.isnan(out[sees]).any(axis=-1).all(), "rows that see it show it"
+
+
+@pytest.mark.parametrize("nq", [1, 12, 90])
+def test_a_value_that_is_not_finite_reaches_the_rows_that_see_it(nq):
+    # infinite values (bf16 only), keys as they were
+    p = Problem(8, ref.BF16, [[64, 64]], [nq], 4, 2, 64)
+    clean = p.model(causal=True)
+    at = 128 - nq // 2 - 1
+    page, row, _ = p.ctx[0][at]
+    codes = ref.views(ref.BF16, 32, 2, 64, p.pool)[1][0]
+    codes[page, :, row, 10:12] = (0x80, 0x7F)                # element 5 of both heads' values: infinity
+    out, lse = p.gpu(causal=True)
+    sees = np.arange(nq) + 128 - nq >= at
+    if (~sees).any():
+        ref.check_attend("rows that do not see it", *[x[~sees] for x in (out, lse, *clean)])
+    assert (~np.isfinite(out[sees])).any(axis=-1).all()
+
+
+def test_odd_query_strides():
+    p = Problem(9, ref.FP4, [[64, 40], [64]], [3, 21], 4, 2, 64)
+    want = p.gpu(causal=True)
+    flat = torch.zeros(24 * (4 * 65 + 1) + 1, dtype=torch.bfloat16, device="cuda")
+    q = flat[1:].view(24, 4 * 65 + 1)[:, :260].view(24, 4, 65)[:, :, :64]
+    q.copy_(p.q)
+    got = p.gpu(causal=True, q=q)
+    assert np.array_equal(got[0], want[0]) and np.array_equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("nq", [1, 5, 40])
+def test_large_scores_and_equal_scores(nq):
+    # scores of some hundreds: the running maximum carries; and one repeated key: all weights equal
+    p = Problem(10, ref.FP8, [[64] * 5], [nq], 4, 2, 128)
+    p.scale = 30.0
+    p.check("large")
+    page, row, _ = np.array(p.ctx[0]).T
+    ref.put(ref.FP8, 32, p.pool, page, row, np.ones((len(page), 2, 128)), np.full((len(page), 2, 128), 3.0))
+    out, lse = p.gpu()
+    assert np.array_equal(out, np.full_like(out, 3.0))
+
+
+@pytest.mark.parametrize("nq", [1, 3, 70])
+def test_repeated_calls_and_a_captured_graph_agree(nq):
+    p = Problem(11, ref.FP4, [[64] * 9, [64, 3]], [nq, nq], 8, 2, 128)
+    cache, q = p.cache(), p.q.cuda()
+    tok, ids, off = up(p.tok_len), up(p.ids), up(p.off)
+    ws = torch.empty(max(1, pm.mem_attend_workspace_bytes(cache, 2, 9, 2 * nq, 8)), dtype=torch.uint8, device="cuda")
+    first = pm.mem_attend(cache, tok, ids, q, p.scale, q_offsets=off, causal=True, workspace=ws)
+    ws.fill_(255)                                            # whatever an earlier call left
+    out = tuple(torch.full_like(t, 7.0) for t in first)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        side.wait_stream(torch.cuda.default_stream())
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            pm.mem_attend(cache, tok, ids, q, p.scale, q_offsets=off, causal=True, workspace=ws, out=out)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for t in out:
+            t.fill_(7.0)
+        ws.fill_(129)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out[0], first[0]) and torch.equal(out[1], first[1])
+
+
+def test_long_list_of_small_chunks():
+    # 1,500 chunks of 32 tokens in a list of 2,000
+    fmt, heads, d = ref.FP4, 1, 64
+    rng = np.random.default_rng(12)
+    n_chunks, k = 1500, 2000
+    pool, table = new_cache(fmt, n_chunks, 1, 32, heads, d)
+    x = torch.randn((n_chunks * 32, 1, d), device="cuda", dtype=torch.float32,
+                    generator=torch.Generator("cuda").manual_seed(1))
+    y = torch.randn((n_chunks * 32, 1, d), device="cuda", dtype=torch.float32,
+                    generator=torch.Generator("cuda").manual_seed(2))
+    cache = pm.KvCache(up(pool), up(table), 32, heads, d, fmt)
+    chunk = np.repeat(np.arange(n_chunks), 32).astype(np.int32)
+    pos = np.tile(np.arange(32), n_chunks).astype(np.int32)
+    pm.mem_kv_write(cache, x, y, up(chunk), up(pos))
+    tok = rng.integers(0, 33, n_chunks).astype(np.int32)
+    ids = np.full((2, k), -1, np.int32)
+    at = np.sort(rng.permutation(k)[:n_chunks])
+    ids[0, at] = rng.permutation(n_chunks)
+    ids[1, 1999] = 7
+    rk, rv = (host(t) for t in pm.mem_kv_read(cache, up(chunk), up(pos), dtype=torch.float32))
+    for nq in (1, 6):
+        q = torch.randn((2 * nq, 4, d), device="cuda").to(torch.bfloat16)
+        out, lse = (host(t) for t in pm.mem_attend(cache, up(tok), up(ids), q, 0.125, causal=True))
+        for i in range(2):
+            rows = np.concatenate([np.arange(c * 32, c * 32 + tok[c]) for c in ids[i] if c >= 0])
+            n = len(rows)
+            want = ref.attend(host(q)[i * nq:(i + 1) * nq], rk[rows], rv[rows], None, np.ones(n, bool),
+                              np.arange(nq) + n - nq, None, 0.125, True, 0, 0, 0.0, None)
+            ref.check_attend(f"request {i}", out[i * nq:(i + 1) * nq], lse[i * nq:(i + 1) * nq], *want)
+
+
+def test_offsets_beyond_32_bits():
+    # a pool of 4.5 GiB whose last pages are used
+    fmt, heads, d, T = ref.BF16, 2, 128, 256
+    pb = ref.page_bytes(fmt, T, heads, d)
+    n_pages = (9 << 29) // pb
+    pool = torch.full((n_pages, pb), 255, dtype=torch.uint8, device="cuda")
+    assert pool.numel() > 1 << 32
+    table = np.array([[n_pages - 1, 0], [n_pages - 2, n_pages // 2]], np.int32)
+    cache = pm.KvCache(pool, up(table), T, heads, d, fmt)
+    n = 900
+    chunk, pos = (np.arange(n) // 512).astype(np.int32), (np.arange(n) % 512).astype(np.int32)
+    k = torch.randn((n, heads, d), device="cuda").to(torch.bfloat16)
+    v = torch.randn((n, heads, d), device="cuda").to(torch.bfloat16)
+    pm.mem_kv_write(cache, k, v, up(chunk), up(pos))
+    rk, rv = pm.mem_kv_read(cache, up(chunk), up(pos))
+    assert torch.equal(rk, k) and torch.equal(rv, v)
+    tok = np.array([512, n - 512], np.int32)
+    for nq in (1, 30):
+        q = torch.randn((nq, 4, d), device="cuda").to(torch.bfloat16)
+        out, lse = (host(t) for t in pm.mem_attend(cache, up(tok), up(np.array([[0, 1]], np.int32)), q, 0.1))
+        want = ref.attend(host(q), host(k), host(v), None, np.ones(n, bool), np.arange(nq), None, 0.1, False, 0, 0,
+                          0.0, None)
+        ref.check_attend(f"{nq} tokens", out, lse, *want)
+
+
+def test_pages_stay_a_cache_when_they_are_moved():
+    # relocation and compaction move pages; the cache reads the same afterwards
+    fmt, heads, d, T, ppc = ref.FP4, 2, 64, 32, 2
+    p = Problem(13, fmt, [[64, 64, 64, 64], [64, 64]], [2, 1], 4, heads, d)
+    spare = np.full((64, p.pool.shape[1]), 255, np.uint8)
+    first = p.pool.shape[0]
+    p.pool = np.concatenate([p.pool, spare])
+    cache = p.cache()
+    want = p.gpu(cache=cache, causal=True)
+    ids = up(p.ids[:1])
+    res = pm.mem_colocate(cache.pool, cache.table, ids, torch.ones_like(ids, dtype=torch.float32), 0.5, 2, first)
+    assert res["moved_chunks"] == 4
+    assert not np.array_equal(cache.table.cpu().numpy(), p.table)
+    got = p.gpu(cache=cache, causal=True)
+    assert np.array_equal(got[0], want[0]) and np.array_equal(got[1], want[1])
