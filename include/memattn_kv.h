@@ -144,8 +144,9 @@ MEMATTN_API size_t mem_attend_workspace_bytes(const mem_kv* kv, int64_t m, int32
  * read; out (device bf16) and lse (device fp32, nullable) are [total_q,
  * heads_q, head_dim] and [total_q, heads_q], contiguous; out is 16-byte
  * aligned.  Products are bf16 with fp32 sums; the softmax weights are rounded
- * to bf16 for the second product, their sum is not.  Rows of q that no request
- * owns are not written.  The context lengths are read on the device: nothing
+ * to bf16 for the second product and out is divided by the rounded weights'
+ * sum, lse is that of the unrounded ones.  Rows of q that no request owns are
+ * not written.  The context lengths are read on the device: nothing
  * is synchronised, and the call can be captured into a HIP graph.
  */
 MEMATTN_API mem_status mem_attend(const mem_kv* kv, const mem_attend_args* args, const void* q, int64_t total_q,

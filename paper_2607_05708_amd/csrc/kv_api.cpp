@@ -199,6 +199,8 @@ mem_status mem_attend(const mem_kv* kv, const mem_attend_args* a, const void* q,
     return fail(MEM_ERR_INVALID_ARG, "an int32 or float array is not 4-byte aligned");
   if (q_token_stride < 0 || q_head_stride < 0) return fail(MEM_ERR_INVALID_ARG, "negative stride of q");
   const int64_t capacity = static_cast<int64_t>(a->k) * kv->pages.pages_per_chunk * kv->page_tokens;
+  if (!attend_fits(a->m, capacity, total_q, kv->heads, a->heads_q, a->q_offsets != nullptr))
+    return fail(MEM_ERR_UNSUPPORTED, "too many requests and heads for one launch");
   const size_t need = attend_workspace_bytes(kv->head_dim, a->m, capacity, total_q, kv->heads, a->heads_q);
   if (need > 0 && !workspace) return fail(MEM_ERR_WORKSPACE, "workspace is NULL");
   if (need > 0 && !aligned(workspace, 16)) return fail(MEM_ERR_INVALID_ARG, "workspace must be 16-byte aligned");

@@ -169,8 +169,9 @@ def attend(q, k, v, doc, present, qpos, qdoc, scale, causal, window, prefix, cap
 
 
 def check_attend(name, got_out, got_lse, out, lse, mag, err):
-    """Compare a kernel's outputs with the model's.  A weight rounded to bf16 is off by 2^-9 of itself, so the sum by
-    2^-9 of the weighted |v|; the output's own rounding adds 2^-9 of it; a score that is off by e moves weights by
+    """Compare a kernel's outputs with the model's.  A weight rounded to bf16 is off by some 2^-9 of itself (half an
+    ulp is 2^-8 at most), which division by the rounded weights' sum partly cancels: 2^-9 of the weighted |v| is
+    allowed for; the output's own rounding adds at most 2^-8 of it; a score that is off by e moves weights by
     2 e; fp32 sums of the products stay below 2^-14 of the weighted |v| for the lengths used here."""
     empty = np.isneginf(lse)
     assert np.array_equal(np.isneginf(got_lse), empty), f"{name}: rows without a visible token"

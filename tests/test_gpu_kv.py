@@ -423,16 +423,14 @@ def test_repeated_calls_and_a_captured_graph_agree(nq):
         assert torch.equal(out[0], first[0]) and torch.equal(out[1], first[1])
 
 
-def test_long_list_of_small_chunks():
-    # 1,500 chunks of 32 tokens in a list of 2,000
-    fmt, heads, d = ref.FP4, 1, 64
+@pytest.mark.parametrize("d,n_chunks,k", [(64, 1500, 2000), (256, 700, 4096)])
+def test_long_list_of_small_chunks(d, n_chunks, k):
+    # chunks of up to 32 tokens in long lists with holes
+    fmt, heads = ref.FP4, 1
     rng = np.random.default_rng(12)
-    n_chunks, k = 1500, 2000
     pool, table = new_cache(fmt, n_chunks, 1, 32, heads, d)
-    x = torch.randn((n_chunks * 32, 1, d), device="cuda", dtype=torch.float32,
-                    generator=torch.Generator("cuda").manual_seed(1))
-    y = torch.randn((n_chunks * 32, 1, d), device="cuda", dtype=torch.float32,
-                    generator=torch.Generator("cuda").manual_seed(2))
+    x, y = (torch.randn((n_chunks * 32, 1, d), device="cuda", dtype=torch.float32,
+                        generator=torch.Generator("cuda").manual_seed(s)) for s in (1, 2))
     cache = pm.KvCache(up(pool), up(table), 32, heads, d, fmt)
     chunk = np.repeat(np.arange(n_chunks), 32).astype(np.int32)
     pos = np.tile(np.arange(32), n_chunks).astype(np.int32)
@@ -441,7 +439,7 @@ def test_long_list_of_small_chunks():
     ids = np.full((2, k), -1, np.int32)
     at = np.sort(rng.permutation(k)[:n_chunks])
     ids[0, at] = rng.permutation(n_chunks)
-    ids[1, 1999] = 7
+    ids[1, k - 1] = 7
     rk, rv = (host(t) for t in pm.mem_kv_read(cache, up(chunk), up(pos), dtype=torch.float32))
     for nq in (1, 6):
         q = torch.randn((2 * nq, 4, d), device="cuda").to(torch.bfloat16)
