@@ -5,24 +5,27 @@
 // tile of rows.  The context is walked in units of 32 tokens of one page, so
 // every unit is one page lookup and ends inside a tile only at the end of a
 // chunk.  A workgroup first turns its request's chunk list into units (a scan
-// of the chunk lengths, then one lookup per unit), then streams them; the
-// softmax keeps a running maximum and sum in the log2 domain, so keys and
-// values are read once.  Long contexts with few rows are split over
-// workgroups, whose partial results a second kernel joins in a fixed order.
+// of the chunk lengths, then one lookup per unit; units that no row can see
+// are left out), then streams them from the last to the first: where the
+// nearest tokens weigh most the running maximum of the softmax (log2 domain)
+// is found early.  Keys and values are read once.  Long contexts with few
+// rows are split over workgroups, whose partial results a second kernel joins
+// in a fixed order.
 //
 // Both kernels compute S^T = K Q^T and O^T = V^T P^T: the products' columns
 // are the rows, so the softmax of a row stays in the lanes that hold its
 // column, and the weights leave the first product in the layout in which the
 // second one reads them: P never moves between lanes.
 //
-//   attend_few_kernel   at most 16 rows a tile (single new tokens): 16x16x32
-//     products; each wave streams its own units with no barrier.  A lane
-//     loads a quarter of a token's row (16 bytes of 4-bit codes of 128
+//   attend_few_kernel   tiles of 16 rows (16x16x32 products) or 32 rows
+//     (32x32x16): each wave streams its own units with no barrier.  A lane
+//     loads quarters of a token's row (16 bytes of 4-bit codes of 128
 //     elements: exactly one block, so one scale) straight from the page into
 //     the operand of the first product; values go through the wave's own LDS
 //     rows once, as bf16, to be read back transposed.
-//   attend_tile_kernel  tiles of 128 rows: 32x32x16 products; the workgroup
-//     unpacks 64 tokens at a time into LDS for its four waves.
+//   attend_tile_kernel  tiles of 128 rows: the workgroup unpacks a step of 64
+//     tokens (32 of 256 elements) at a time into LDS for its four waves, into
+//     one half of a double buffer while the waves work on the other.
 #include "kv.h"
 #include "device_common.h"
 
@@ -37,12 +40,10 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
-constexpr int kUnit = 32;        // tokens per unit
-constexpr int kBatch = 512;      // units resolved at a time
-constexpr int kFewRows = 16;     // rows per tile of the few-rows kernel
-constexpr int kTileRows = 128;   // rows per tile of the tile kernel
-constexpr int kTileTokens = 64;  // tokens per step of the tile kernel
-constexpr int kFar = 1 << 30;    // above every position
+constexpr int kUnit = 32;       // tokens per unit
+constexpr int kTileRows = 128;  // rows per tile of the tile kernel
+constexpr int kFar = 1 << 30;   // above every position
+constexpr int kMaxSplits = 64;  // one lane of the join each
 
 // One unit of the context, resolved.
 struct Unit {
@@ -54,7 +55,7 @@ struct Unit {
 
 // How a call is spread over the GPU (shared by the workspace size and the launch).
 struct AttendPlan {
-  bool few;
+  int rows;       // rows per tile: 16, 32 (few-rows kernel) or 128 (tile kernel)
   int64_t tiles;  // row tiles (upper bound with ragged requests)
   int splits;
 };
@@ -71,13 +72,19 @@ struct Tile {
 
 // Request and rows of tile t.  With ragged requests tile t of request i is tile floor(q_offsets[i] G / R) + i + t:
 // these starts leave room for every request's ceil(n G / R) tiles without a scan; the tiles in between are empty.
-__device__ __forceinline__ bool find_tile(const AttendArgs& a, int64_t t, int group, int R, Tile* out) {
+// Every wave makes the search by itself, 64 probes at a time.
+template <int R>
+__device__ __forceinline__ bool find_tile(const AttendArgs& a, int64_t t, int group, Tile* out) {
   if (a.q_offsets) {
-    int64_t lo = 0, hi = a.m - 1;
-    while (lo < hi) {
-      const int64_t mid = (lo + hi + 1) >> 1;
-      const int64_t o = a.q_offsets[mid];
-      if (o * group / R + mid <= t) lo = mid; else hi = mid - 1;
+    const int lane = threadIdx.x & 63;
+    int64_t lo = 0, n = a.m;
+    while (n > 0) {
+      const int64_t step = (n + 63) >> 6, i = lane * step;
+      const bool before = i < n && (static_cast<int64_t>(a.q_offsets[lo + i]) * group) / R + lo + i <= t;
+      const int last = max(__builtin_popcountll(__ballot(before)) - 1, 0);  // the starts never fall
+      lo += last * step;
+      if (step == 1) break;
+      n = min(step, n - last * step);
     }
     const int64_t o = a.q_offsets[lo], e = a.q_offsets[lo + 1];
     if (o < 0 || e > a.total_q || o > e) return false;
@@ -100,18 +107,28 @@ __device__ __forceinline__ bool find_tile(const AttendArgs& a, int64_t t, int gr
   return true;
 }
 
-// Scan of the request's chunk list: ub[c] / tb[c] = units / tokens before entry c; index k holds the totals.
-__device__ __forceinline__ void scan_list(const AttendArgs& a, const int32_t* ids, int* ub, int* tb, int* tmp) {
+// The request's chunk list in LDS: cid[c] = chunk of entry c, ub[c] / tb[c] = units / tokens before it; index k of
+// the latter two holds the totals.
+struct ChunkList {
+  int *cid, *ub, *tb;
+  int k;
+};
+
+__device__ __forceinline__ ChunkList scan_list(const AttendArgs& a, int64_t req, int* lds, int* tmp) {
+  const int k = a.k;
+  const ChunkList L{lds, lds + k, lds + 2 * k + 1, k};
+  const int32_t* ids = a.ids + req * k;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int cap = a.kv.ppc * a.kv.page_tokens;
-  const int per = (a.k + kThreads - 1) / kThreads;
-  const int c0 = min(tid * per, a.k), c1 = min(c0 + per, a.k);
+  const int per = (k + kThreads - 1) / kThreads;
+  const int c0 = min(tid * per, k), c1 = min(c0 + per, k);
   int u = 0, t = 0;
   for (int c = c0; c < c1; ++c) {
     const int32_t id = ids[c];
     const int len = id >= 0 && id < a.kv.n_chunks ? min(max(a.tok_len[id], 0), cap) : 0;
-    ub[c] = u;
-    tb[c] = t;
+    L.cid[c] = id;
+    L.ub[c] = u;
+    L.tb[c] = t;
     u += (len + kUnit - 1) / kUnit;
     t += len;
   }
@@ -132,14 +149,15 @@ __device__ __forceinline__ void scan_list(const AttendArgs& a, const int32_t* id
     total_t += tmp[2 * w + 1];
   }
   for (int c = c0; c < c1; ++c) {
-    ub[c] += bu;
-    tb[c] += bt;
+    L.ub[c] += bu;
+    L.tb[c] += bt;
   }
   if (tid == 0) {
-    ub[a.k] = total_u;
-    tb[a.k] = total_t;
+    L.ub[k] = total_u;
+    L.tb[k] = total_t;
   }
   __syncthreads();
+  return L;
 }
 
 // Last entry c of b[0..k] with b[c] <= x, below k.
@@ -160,20 +178,20 @@ struct Span {
 };
 
 // The span for rows whose visible positions lie in [0, prefix) and [lo, hi].
-__device__ __forceinline__ Span visible_units(const int* ub, const int* tb, int k, int prefix, int lo, int hi) {
-  const int total = tb[k];
+__device__ __forceinline__ Span visible_units(const ChunkList& L, int prefix, int lo, int hi) {
+  const int total = L.tb[L.k], units = L.ub[L.k];
   auto unit_of = [&](int pos) {  // unit that holds position pos < total
-    const int c = find_entry(tb, k, pos);
-    return ub[c] + (pos - tb[c]) / kUnit;
+    const int c = find_entry(L.tb, L.k, pos);
+    return L.ub[c] + (pos - L.tb[c]) / kUnit;
   };
   Span s{0, 0, 0};
   hi = min(hi, total - 1);
   lo = max(lo, 0);
   if (lo <= hi) {
     s.b = lo > 0 ? unit_of(lo) : 0;
-    s.e = hi == total - 1 ? ub[k] : unit_of(hi) + 1;
+    s.e = hi == total - 1 ? units : unit_of(hi) + 1;
   }
-  const int p = prefix <= 0 ? 0 : prefix >= total ? ub[k] : unit_of(prefix - 1) + 1;
+  const int p = prefix <= 0 ? 0 : prefix >= total ? units : unit_of(prefix - 1) + 1;
   if (p >= s.b) {  // one range
     s.a = max(p, s.e);
     s.b = s.e = s.a;
@@ -181,27 +199,6 @@ __device__ __forceinline__ Span visible_units(const int* ub, const int* tb, int 
     s.a = p;
   }
   return s;
-}
-
-// Resolve units [first, first + n) of the span into `list`.
-__device__ __forceinline__ void resolve_units(const AttendArgs& a, const int32_t* ids, const int* ub, const int* tb,
-                                              const Span& span, int first, int n, Unit* list) {
-  for (int i = threadIdx.x; i < n; i += kThreads) {
-    const int u = span.unit(first + i);
-    const int c = find_entry(ub, a.k, u);
-    const int t = (u - ub[c]) * kUnit;
-    const int32_t id = ids[c];
-    const int p = t / a.kv.page_tokens;
-    const int32_t pg = a.kv.table[static_cast<int64_t>(id) * a.kv.ppc + p];
-    const bool ok = pg >= 0 && pg < a.kv.n_pages;
-    const int held = ok ? min(kUnit, tb[c + 1] - tb[c] - t) : 0;
-    Unit x;
-    x.page = ok ? pg : 0;
-    x.where = (t - p * a.kv.page_tokens) | held << 16;
-    x.pos = tb[c] + t;
-    x.ns = a.chunk_ns ? a.chunk_ns[id] : 0;
-    list[i] = x;
-  }
 }
 
 // What a row of the tile may see and how it is biased.
@@ -222,6 +219,106 @@ __device__ __forceinline__ RowRule row_rule(const AttendArgs& a, const Tile& t, 
   x.ns = a.chunk_ns ? a.query_ns[at] : 0;
   x.slope = a.slopes ? a.slopes[h] * kLog2e : 0.f;
   return x;
+}
+
+// What the rows of a tile see: any of them, and all of them.
+struct TileRule {
+  int lo, hi, ns_lo, ns_hi;  // some row sees positions lo .. hi, of documents ns_lo .. ns_hi
+  int lo_all, hi_all;        // every row sees positions lo_all .. hi_all
+  bool mixed;                // rows differ in their documents
+
+  // Whether every row sees 32 positions from p on.
+  __device__ __forceinline__ bool all_see(int p, int prefix) const {
+    return !mixed && (p + kUnit <= prefix || (p >= lo_all && p + kUnit - 1 <= hi_all));
+  }
+};
+
+// The rule of a tile whose rows are spread over the lanes of each wave (one or two a lane, repeats allowed).
+template <int R>
+__device__ __forceinline__ TileRule tile_rule(const AttendArgs& a, const Tile& t, int ctx, int g, int group) {
+  const int lane = threadIdx.x & 63;
+  TileRule x{kFar, -1, INT32_MAX, -1, 0, kFar, false};
+  bool none = false;
+#pragma unroll
+  for (int i = 0; i < (R + 63) / 64; ++i) {
+    const RowRule r = row_rule(a, t, ctx, g, group, t.r0 + min(lane + 64 * i, t.rows - 1));
+    x.lo = min(x.lo, r.lo);
+    x.hi = max(x.hi, r.hi);
+    x.lo_all = max(x.lo_all, r.lo);
+    x.hi_all = min(x.hi_all, r.hi);
+    none |= r.ns < 0;
+    if (r.ns >= 0) {
+      x.ns_lo = min(x.ns_lo, r.ns);
+      x.ns_hi = max(x.ns_hi, r.ns);
+    }
+  }
+  for (int off = 1; off < 64; off <<= 1) {
+    x.lo = min(x.lo, __shfl_xor(x.lo, off));
+    x.hi = max(x.hi, __shfl_xor(x.hi, off));
+    x.lo_all = max(x.lo_all, __shfl_xor(x.lo_all, off));
+    x.hi_all = min(x.hi_all, __shfl_xor(x.hi_all, off));
+    if (a.chunk_ns) {
+      x.ns_lo = min(x.ns_lo, __shfl_xor(x.ns_lo, off));
+      x.ns_hi = max(x.ns_hi, __shfl_xor(x.ns_hi, off));
+    }
+  }
+  x.mixed = __any(none) || x.ns_lo != x.ns_hi;
+  return x;
+}
+
+// Resolve units last, last - 1, ... (n of them, at most MAX) of the span into `list`, leaving out those that hold
+// nothing or are of no row's document.  Returns how many there are; ends with a barrier.
+template <int MAX>
+__device__ __forceinline__ int resolve_units(const AttendArgs& a, const ChunkList& L, const Span& span,
+                                             const TileRule& tr, int last, int n, Unit* list, int* counts) {
+  constexpr int kPer = MAX / kThreads;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  Unit x[kPer];
+  uint64_t kept[kPer];
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    const int i = j * kThreads + tid;
+    x[j] = Unit{0, 0, 0, 0};
+    if (i < n) {
+      const int u = span.unit(last - i);
+      const int c = find_entry(L.ub, L.k, u);
+      const int t = (u - L.ub[c]) * kUnit;
+      const int32_t id = L.cid[c];
+      const int p = t / a.kv.page_tokens;
+      const int32_t pg = a.kv.table[static_cast<int64_t>(id) * a.kv.ppc + p];
+      x[j].ns = a.chunk_ns ? a.chunk_ns[id] : 0;
+      const bool ok = pg >= 0 && pg < a.kv.n_pages && x[j].ns >= 0 && x[j].ns >= tr.ns_lo && x[j].ns <= tr.ns_hi;
+      x[j].page = ok ? pg : 0;
+      x[j].where = (t - p * a.kv.page_tokens) | (ok ? min(kUnit, L.tb[c + 1] - L.tb[c] - t) : 0) << 16;
+      x[j].pos = L.tb[c] + t;
+    }
+    kept[j] = __ballot((x[j].where >> 16) > 0);
+    if (lane == 0) counts[j * kWaves + wave] = __builtin_popcountll(kept[j]);
+  }
+  __syncthreads();
+  int total = 0, at[kPer];
+#pragma unroll
+  for (int j = 0; j < kPer; ++j)
+    for (int w = 0; w < kWaves; ++w) {
+      if (w == wave) at[j] = total;
+      total += counts[j * kWaves + w];
+    }
+#pragma unroll
+  for (int j = 0; j < kPer; ++j)
+    if ((x[j].where >> 16) > 0)
+      list[at[j] + __builtin_popcountll(kept[j] & ((uint64_t{1} << lane) - 1))] = x[j];
+  __syncthreads();
+  return total;
+}
+
+// A unit of the list in scalar registers.
+__device__ __forceinline__ Unit uniform_unit(const Unit& x) {
+  Unit u;
+  u.page = __builtin_amdgcn_readfirstlane(x.page);
+  u.where = __builtin_amdgcn_readfirstlane(x.where);
+  u.pos = __builtin_amdgcn_readfirstlane(x.pos);
+  u.ns = __builtin_amdgcn_readfirstlane(x.ns);
+  return u;
 }
 
 // ---------------------------------------------------------------- pieces of rows
@@ -333,402 +430,548 @@ __device__ __forceinline__ uint32_t pack2(float x, float y) {
   return bits_of(p);
 }
 
-// c plus both bf16 values of a word.
-__device__ __forceinline__ float add_pair(uint32_t pair, float c) {
-  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), __builtin_bit_cast(bf16x2, 0x3F803F80u), c,
-                                         false);
-}
-
 // What rounding x and y to the bf16 values of `pair` left, in bf16.
 __device__ __forceinline__ uint32_t rest2(float x, float y, uint32_t pair) {
   return pack2(x - __uint_as_float(pair << 16), y - __uint_as_float(pair & 0xFFFF0000u));
 }
 
-// Reductions over lanes l, l ^ 16, l ^ 32, l ^ 48 (column l & 15) and over l, l ^ 32.
-__device__ __forceinline__ float max_half(float x) {
+// Maximum that keeps a NaN: a score that is not a number must not be passed over.
+__device__ __forceinline__ float nan_max(float x, float y) { return __builtin_elementwise_maximum(x, y); }
+
+// Reductions over lanes l, l ^ 32, and with WIDTH 16 l ^ 16 and l ^ 48 too: the lanes that hold one row's scores.
+template <int WIDTH>
+__device__ __forceinline__ float max_column(float x) {
+  if constexpr (WIDTH == 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = nan_max(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  }
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  return nan_max(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
-__device__ __forceinline__ float sum_half(float x) {
+template <int WIDTH>
+__device__ __forceinline__ float sum_column(float x) {
+  if constexpr (WIDTH == 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  }
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
-__device__ __forceinline__ float max_rows(float x) {
-  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return max_half(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
-}
-__device__ __forceinline__ float sum_rows(float x) {
-  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return sum_half(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+template <int WIDTH>
+__device__ __forceinline__ bool any_column(bool x, int col) {
+  uint64_t v = __ballot(x);
+  v |= v >> 32;
+  if constexpr (WIDTH == 16) v |= v >> 16;
+  return (v >> col) & 1u;
 }
 
-// log2-domain score of a raw product: scale, cap, without the bias.  tanh(x) = 1 - 2 / (1 + e^2x).
+// ---------------------------------------------------------------- scores and their softmax
+
+// Offset in its unit of score j of a lane whose part (lane / WIDTH) is 0; part x adds 4 x.
+template <int WIDTH>
+__device__ constexpr int score_token(int j) {
+  return WIDTH == 16 ? 16 * (j >> 2) + (j & 3) : 8 * (j >> 2) + (j & 3);
+}
+
+// How raw products become scores in the log2 domain.
 struct Scores {
-  float c;     // scale * log2(e), or with a cap 2 * scale * log2(e) / cap
-  float cap2;  // cap * log2(e); 0: none
-  __device__ __forceinline__ float operator()(float s) const {
-    if (cap2 == 0.f) return s * c;
-    return cap2 - 2.f * cap2 * __builtin_amdgcn_rcpf(1.f + fast_exp2(s * c));
+  float c;      // scale * log2(e)
+  float x;      // scale / softcap
+  float cap2;   // softcap * log2(e); 0: none
+  bool bias;
+  bool causal;
+
+  __device__ __forceinline__ explicit Scores(const AttendArgs& a)
+      : c(a.scale * kLog2e), x(a.softcap > 0.f ? a.scale / a.softcap : 0.f), cap2(a.softcap * kLog2e),
+        bias(a.slopes != nullptr), causal(a.causal != 0) {}
+
+  // What scores still have to be multiplied by after `apply`: without cap and bias that waits for the exponential.
+  __device__ __forceinline__ float factor() const { return cap2 == 0.f && !bias ? c : 1.f; }
+
+  // tanh is 1 - 2 / (1 + e^2x), two transcendental operations of four times a product's cost each; where no score of
+  // the wave's unit is above a quarter of the cap its series to x^9 does as well (the next term is below 1e-8 of it).
+  template <int WIDTH, int N>
+  __device__ __forceinline__ void apply(float (&s)[N], const RowRule& rule, const TileRule& tr, int pos, int part) const {
+    if (cap2 != 0.f) {
+      float top = 0.f;
+#pragma unroll
+      for (int j = 0; j < N; ++j) top = fmaxf(top, fabsf(s[j]));
+      if (__any(top * x > 0.25f)) {
+        const float k2 = 2.f * x * kLog2e;
+#pragma unroll
+        for (int j = 0; j < N; ++j) s[j] = cap2 - 2.f * cap2 * __builtin_amdgcn_rcpf(1.f + fast_exp2(s[j] * k2));
+      } else {
+        const float c3 = cap2 * (-1.f / 3.f), c5 = cap2 * (2.f / 15.f), c7 = cap2 * (-17.f / 315.f),
+                    c9 = cap2 * (62.f / 2835.f);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+          const float t = s[j] * x, t2 = t * t;
+          s[j] = t * (cap2 + t2 * (c3 + t2 * (c5 + t2 * (c7 + t2 * c9))));
+        }
+      }
+    }
+    if (bias) {
+      const float f = cap2 == 0.f ? c : 1.f;
+      const float dist = static_cast<float>(rule.pos - pos - 4 * part);
+      if (causal && pos + kUnit - 1 <= tr.hi_all) {  // every token lies behind every row
+        const float near = -rule.slope * dist;
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+          s[j] = fmaf(s[j], f, fmaf(rule.slope, static_cast<float>(score_token<WIDTH>(j)), near));
+      } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+          s[j] = s[j] * f - rule.slope * fabsf(dist - static_cast<float>(score_token<WIDTH>(j)));
+      }
+    }
   }
 };
 
-__device__ __forceinline__ Scores scores_of(const AttendArgs& a) {
-  if (a.softcap > 0.f) return {2.f * a.scale * kLog2e / a.softcap, a.softcap * kLog2e};
-  return {a.scale * kLog2e, 0.f};
+// Masks of one unit's scores, looked at one by one.  Returns the scores that are seen as bits.
+template <int WIDTH, int N>
+__device__ __forceinline__ uint32_t mask_scores(float (&s)[N], const RowRule& rule, const Unit& u, int prefix, int part) {
+  const int held = u.where >> 16;
+  uint32_t seen = 0;
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    const int tok = score_token<WIDTH>(j) + 4 * part, p = u.pos + tok;
+    const bool see = tok < held && (p < prefix || (p >= rule.lo && p <= rule.hi)) && u.ns == rule.ns;
+    seen |= see ? 1u << j : 0u;
+    s[j] = see ? s[j] : -INFINITY;
+  }
+  return seen;
 }
 
+// Whether a seen score's token is among the unit's tokens with values that are not finite.
+template <int WIDTH, int N>
+__device__ __forceinline__ bool sees_bad(uint32_t seen, uint32_t bad, int part) {
+  bool hit = false;
+#pragma unroll
+  for (int j = 0; j < N; ++j) hit |= ((seen >> j) & 1u) && ((bad >> (score_token<WIDTH>(j) + 4 * part)) & 1u);
+  return hit;
+}
+
+// Running softmax of a row, in every lane that holds its scores: maximum (it may lag by kLag: weights up to 2^kLag
+// cost no precision and spare most rescalings) and the lane's part of the sum of weights.
+struct RowState {
+  float m;
+  float l;
+};
+constexpr float kLag = 8.f;
+// Scores this far (log2) below the maximum are left out: 2^24 of them change no fp32 sum.
+constexpr float kNothing = 48.f;
 // The weights are rounded to bf16 for the second product.  Where one weighs more than 1 / kHeavy of its lane's sum so
 // far, rounding it would show in the output, and the product is made a second time with what the rounding left (16
-// bits of weight in all); smaller weights' roundings average out.  Outputs are divided by the sum `lr` of the weights
-// as they were used, so that a common part of the rounding cancels; the lse takes the sum `l` of the unrounded ones.
+// bits of weight in all); smaller weights' roundings average out.  The sum is that of the unrounded ones.
 constexpr float kHeavy = 16.f;
 
-struct RowState {
-  float m;   // maximum so far (may lag, below)
-  float l;
-  float lr;
-};
-
-__device__ __forceinline__ float inverse_sum(float lr) { return lr > 0.f ? 1.f / lr : lr == 0.f ? 0.f : NAN; }
+__device__ __forceinline__ float inverse_sum(float l) { return l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN; }
 __device__ __forceinline__ float lse_of(float m, float l) {
   return l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
+__device__ __forceinline__ float finite_max(float m) { return m == -INFINITY ? 0.f : m; }
 
-// Running maxima may lag by this much (log2): weights up to 2^8 cost no precision and spare most rescalings.
-constexpr float kLag = 8.f;
+// Output rows of a wave: O^T in the layout of the products, `col` = row, NACC registers.
+template <int WIDTH, int D>
+struct Rows {
+  static constexpr int kBlocks = D / WIDTH;           // products along D
+  static constexpr int kRegs = WIDTH == 16 ? 4 : 16;  // registers per product
+  typedef float Acc __attribute__((ext_vector_type(kRegs)));
+  Acc o[kBlocks];
+
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int n = 0; n < kBlocks; ++n)
+#pragma unroll
+      for (int j = 0; j < kRegs; ++j) o[n][j] = 0.f;
+  }
+  __device__ __forceinline__ void scale(float f) {
+#pragma unroll
+    for (int n = 0; n < kBlocks; ++n) o[n] *= f;
+  }
+  // Four consecutive columns d = 4 part + (16 n, or 32 n + 8 y) at a time.
+  template <typename F>
+  __device__ __forceinline__ void each4(int part, F f) const {
+#pragma unroll
+    for (int n = 0; n < kBlocks; ++n)
+#pragma unroll
+      for (int y = 0; y < kRegs / 4; ++y)
+        f(n * WIDTH + 8 * y + 4 * part, f32x4{o[n][4 * y], o[n][4 * y + 1], o[n][4 * y + 2], o[n][4 * y + 3]});
+  }
+};
+
+// The scores of one row (N in this lane) into weights: updates the running state and the output's scale.  Returns
+// false if none of the wave's scores weighs anything.
+template <int WIDTH, int D, int N>
+__device__ __forceinline__ bool soften(float (&s)[N], float f, RowState& st, Rows<WIDTH, D>& rows, bool* heavy) {
+  float top = s[0];
+#pragma unroll
+  for (int j = 1; j < N; ++j) top = nan_max(top, s[j]);
+  top = max_column<WIDTH>(top) * f;
+  if (!__any(!(top <= st.m - kNothing))) return false;
+  if (__any(top > st.m + kLag)) {
+    const float mn = fmaxf(st.m, top);
+    const float r = mn == -INFINITY ? 1.f : fast_exp2(st.m - mn);
+    st.l *= r;
+    rows.scale(r);
+    st.m = mn;
+  }
+  const float ref = finite_max(st.m);
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    s[j] = fast_exp2(fmaf(s[j], f, -ref));
+    st.l += s[j];
+  }
+  *heavy = __any(fast_exp2(top - ref) * kHeavy > st.l);
+  return true;
+}
+
+// Write a row's output, or its part of a split context.
+template <int WIDTH, int D>
+__device__ __forceinline__ void write_rows(const AttendArgs& a, const Rows<WIDTH, D>& rows, RowState st, bool poison,
+                                           int64_t at, int part, int split, int splits, float* part_o,
+                                           RowState* part_ml) {
+  if (splits == 1) {
+    const float inv = poison ? NAN : inverse_sum(st.l);
+    uint16_t* dst = a.out + at * D;
+    rows.each4(part, [&](int d, f32x4 v) {
+      *reinterpret_cast<u32x2_t*>(dst + d) = u32x2_t{pack2(v[0] * inv, v[1] * inv), pack2(v[2] * inv, v[3] * inv)};
+    });
+    if (a.lse && part == 0) a.lse[at] = lse_of(st.m, st.l);
+  } else {
+    const int64_t slot = static_cast<int64_t>(split) * a.total_q * a.hq + at;
+    float* dst = part_o + slot * D;
+    rows.each4(part, [&](int d, f32x4 v) {
+      if (poison) v = f32x4{NAN, NAN, NAN, NAN};
+      *reinterpret_cast<f32x4*>(dst + d) = v;
+    });
+    if (part == 0) part_ml[slot] = st;
+  }
+}
+
+// The queries of a lane's row: kSteps operands of eight elements, `stride` elements apart.
+template <int STEPS>
+__device__ __forceinline__ void load_queries(const uint16_t* src, int stride, bf16x8 (&q)[STEPS]) {
+  const bool vec = (reinterpret_cast<uintptr_t>(src) & 15u) == 0;
+#pragma unroll
+  for (int i = 0; i < STEPS; ++i) {
+    union { u32x4_t v; uint16_t h[8]; } x;
+    if (vec) {
+      x.v = *reinterpret_cast<const u32x4_t*>(src + stride * i);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x.h[j] = src[stride * i + j];
+    }
+    q[i] = as_bf16x8(x.v);
+  }
+}
+
+// O^T += V^T P^T for the 32 tokens whose values lie in LDS rows at `v`, with the weights of the lane's row.
+template <int WIDTH, int D, int PITCH>
+__device__ __forceinline__ void add_values(Rows<WIDTH, D>& rows, const uint16_t* v, const u32x4_t* w, int lane) {
+  const int i = lane & 15;
+  if constexpr (WIDTH == 16) {
+    const uint16_t* src = v + (4 * (lane >> 4) + (i >> 2)) * PITCH + (i & 3) * 4;
+#pragma unroll
+    for (int n = 0; n < D / 16; ++n) {
+      const u32x2_t v0 = lds_transpose4(src + 16 * n);
+      const u32x2_t v1 = lds_transpose4(src + 16 * PITCH + 16 * n);
+      rows.o[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(u32x4_t{v0[0], v0[1], v1[0], v1[1]}),
+                                                          as_bf16x8(w[0]), rows.o[n], 0, 0, 0);
+    }
+  } else {
+    const uint16_t* src = v + (4 * (lane >> 5) + (i >> 2)) * PITCH + ((lane >> 4) & 1) * 16 + (i & 3) * 4;
+#pragma unroll
+    for (int n = 0; n < D / 32; ++n)
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const u32x2_t v0 = lds_transpose4(src + 16 * x * PITCH + 32 * n);
+        const u32x2_t v1 = lds_transpose4(src + (16 * x + 8) * PITCH + 32 * n);
+        rows.o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(u32x4_t{v0[0], v0[1], v1[0], v1[1]}),
+                                                            as_bf16x8(w[x]), rows.o[n], 0, 0, 0);
+      }
+  }
+}
+
+// N weights as operands of the second product, and what their rounding left.
+template <int N>
+__device__ __forceinline__ void pack_weights(const float (&s)[N], u32x4_t (&w)[N / 8]) {
+#pragma unroll
+  for (int j = 0; j < N / 2; ++j) w[j >> 2][j & 3] = pack2(s[2 * j], s[2 * j + 1]);
+}
+template <int N>
+__device__ __forceinline__ void pack_rests(const float (&s)[N], u32x4_t (&w)[N / 8]) {
+#pragma unroll
+  for (int j = 0; j < N / 2; ++j) w[j >> 2][j & 3] = rest2(s[2 * j], s[2 * j + 1], w[j >> 2][j & 3]);
+}
 
 // ---------------------------------------------------------------- few rows
 
-template <int FMT, int D>
+template <int FMT, int D, int R>
 struct FewShape {
-  static constexpr int kPitch = D + 16;                                   // bf16 elements between LDS rows
-  static constexpr int kWaveBytes = kUnit * kPitch * 2;                    // a wave's unpacked values
-  static constexpr int kJoinBytes = kWaves * kFewRows * D * 4;             // the waves' outputs at the end
+  static constexpr int kBatch = 512;                        // units resolved at a time
+  static constexpr int kPitch = D + 16;                     // bf16 elements between LDS rows
+  static constexpr int kWaveBytes = kUnit * kPitch * 2;     // a wave's unpacked values
+  static constexpr int kJoinBytes = 2 * R * D * 4;          // two waves' outputs at the end
   static constexpr int kArea = kWaves * kWaveBytes > kJoinBytes ? kWaves * kWaveBytes : kJoinBytes;
 };
 
-template <int FMT, int D>
-__global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_few_kernel(AttendArgs a, int splits, float* __restrict__ part_o,
-                                                              RowState* __restrict__ part_ml) {
+template <int FMT, int D, int R>
+__global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_few_kernel(AttendArgs a, int splits,
+                                                                                float* __restrict__ part_o,
+                                                                                RowState* __restrict__ part_ml) {
   using K = Dim<FMT, D>;
-  using S = FewShape<FMT, D>;
-  constexpr int kBlocks = D / 16;
-  extern __shared__ int dyn[];  // ub[k + 1], tb[k + 1]
+  using S = FewShape<FMT, D, R>;
+  constexpr int kParts = 64 / R;              // lanes that share a row's scores
+  constexpr int kScores = kUnit / kParts;     // scores per lane and unit
+  constexpr int kQSteps = D / (8 * kParts);   // operands of a row's queries per lane
+  extern __shared__ int dyn[];                // the chunk list: cid[k], ub[k + 1], tb[k + 1]
   __shared__ __align__(16) uint8_t area[S::kArea];
-  __shared__ Unit list[kBatch];
+  __shared__ Unit list[S::kBatch];
   __shared__ int tmp[2 * kWaves];
-  __shared__ RowState wave_ml[kWaves][kFewRows];
-  int* ub = dyn;
-  int* tb = dyn + a.k + 1;
+  __shared__ RowState joint[2][64];
+  __shared__ int joint_poison[2][64];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int col = lane & 15, quad = lane >> 4;
+  const int col = lane % R, part = lane / R;
   const int heads = a.kv.heads, group = a.hq / heads;
   int64_t b = blockIdx.x;
   const int g = static_cast<int>(b % heads);
   b /= heads;
   const int split = static_cast<int>(b % splits);
   Tile t;
-  if (!find_tile(a, b / splits, group, kFewRows, &t)) return;
-  const int32_t* ids = a.ids + t.req * a.k;
-  scan_list(a, ids, ub, tb, tmp);
-  const int ctx = tb[a.k];
+  if (!find_tile<R>(a, b / splits, group, &t)) return;
+  const ChunkList L = scan_list(a, t.req, dyn, tmp);
+  const int ctx = L.tb[a.k];
   const int prefix = a.prefix_len ? a.prefix_len[t.req] : 0;
-  const RowRule rule = row_rule(a, t, ctx, g, group, t.r0 + min(col, t.rows - 1));
-
-  // what the tile's rows see at most
-  int lo = rule.lo, hi = rule.hi;
-  for (int off = 1; off < 16; off <<= 1) {
-    lo = min(lo, __shfl_xor(lo, off));
-    hi = max(hi, __shfl_xor(hi, off));
-  }
-  int lo_all = rule.lo, hi_all = rule.hi;  // what all of them see
-  for (int off = 1; off < 16; off <<= 1) {
-    lo_all = max(lo_all, __shfl_xor(lo_all, off));
-    hi_all = min(hi_all, __shfl_xor(hi_all, off));
-  }
-  const Span span = visible_units(ub, tb, a.k, prefix, lo, hi);
+  const int my_row = t.r0 + min(col, t.rows - 1);
+  const RowRule rule = row_rule(a, t, ctx, g, group, my_row);
+  const TileRule tr = tile_rule<R>(a, t, ctx, g, group);
+  const Span span = visible_units(L, prefix, tr.lo, tr.hi);
   const int n_units = span.count();
   const int u0 = static_cast<int>(static_cast<int64_t>(n_units) * split / splits);
   const int u1 = static_cast<int>(static_cast<int64_t>(n_units) * (split + 1) / splits);
 
-  // the tile's queries: lane (col, quad) holds quarter `quad` of row `col`
-  bf16x8 q[K::kSteps];
-  {
-    const int r = t.r0 + min(col, t.rows - 1);
-    const uint16_t* src = a.q + (t.q0 + r / group) * a.q_ts + (g * group + r % group) * a.q_hs + quad * K::kElems;
-    const bool vec = (reinterpret_cast<uintptr_t>(src) & 15u) == 0;
-#pragma unroll
-    for (int i = 0; i < K::kSteps; ++i) {
-      union { u32x4_t v; uint16_t h[8]; } x;
-      if (vec) {
-        x.v = *reinterpret_cast<const u32x4_t*>(src + 8 * i);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x.h[j] = src[8 * i + j];
-      }
-      q[i] = as_bf16x8(x.v);
-    }
-  }
+  // lane (col, part) holds elements part D / kParts .. of row `col`
+  bf16x8 q[kQSteps];
+  load_queries(a.q + (t.q0 + my_row / group) * a.q_ts + (g * group + my_row % group) * a.q_hs + part * (D / kParts), 8, q);
 
-  const Scores score = scores_of(a);
+  const Scores scores(a);
   const int64_t T = a.kv.page_tokens;
   const int64_t head_at = static_cast<int64_t>(g) * 2 * T * (K::kRow + K::kSc);
-  const int my_codes = col * K::kRow + quad * K::kBytes;
-  const int my_scale = col * K::kSc + quad * K::kElems / kKvBlock;
+  // piece h of a lane: quarter `part` of row 16 h + col, or quarter 2 part + h of row `col`
+  const int row_step = R == 16 ? 16 : 0;
+  const int quarter = R == 16 ? part : 2 * part, quarter_step = R == 16 ? 0 : 1;
   uint16_t* vrows = reinterpret_cast<uint16_t*>(area + wave * S::kWaveBytes);
 
-  f32x4 acc[kBlocks];
-#pragma unroll
-  for (int n = 0; n < kBlocks; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float m = -INFINITY, l = 0.f, lr = 0.f;
+  Rows<R, D> rows;
+  rows.clear();
+  RowState st{-INFINITY, 0.f};
   bool poison = false;
 
-  struct Stage {
-    Piece<FMT, D> k[2], v[2];
-    Unit u;
-  };
-  auto load = [&](Stage& s, int i) {
-    Unit u = list[i];
-    u.page = __builtin_amdgcn_readfirstlane(u.page);
-    u.where = __builtin_amdgcn_readfirstlane(u.where);
-    u.pos = __builtin_amdgcn_readfirstlane(u.pos);
-    u.ns = __builtin_amdgcn_readfirstlane(u.ns);
-    s.u = u;
-    const int row = u.where & 0xFFFF;
-    const uint8_t* part = a.kv.pool + u.page * a.kv.page_bytes + head_at;
-    const uint8_t* kc = part + row * K::kRow + my_codes;
-    const uint8_t* ks = part + 2 * T * K::kRow + row * K::kSc + my_scale;
-    if ((u.where >> 16) == 0) return;  // no page: nothing of the unit is used
+  // Keys and values of the unit at hand.  Each is loaded again, for the wave's next unit, as soon as it has been used:
+  // a wave keeps nearly a whole unit in flight without a second set of registers.
+  Piece<FMT, D> pk[2], pv[2];
+  auto load = [&](Piece<FMT, D> (&p)[2], const Unit& u, bool is_v) {
+    const int row = (u.where & 0xFFFF) + col;
+    const uint8_t* base = a.kv.pool + u.page * a.kv.page_bytes + head_at;
+    const uint8_t* codes = base + (is_v ? T * K::kRow : 0) + row * K::kRow + quarter * K::kBytes;
+    const uint8_t* sc = base + 2 * T * K::kRow + (is_v ? T * K::kSc : 0) + row * K::kSc;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      load_piece<FMT, D>(s.k[h], kc + h * 16 * K::kRow, ks + h * 16 * K::kSc);
-      load_piece<FMT, D>(s.v[h], kc + T * K::kRow + h * 16 * K::kRow, ks + T * K::kSc + h * 16 * K::kSc);
-    }
+    for (int h = 0; h < 2; ++h)
+      load_piece<FMT, D>(p[h], codes + h * (row_step * K::kRow + quarter_step * K::kBytes),
+                         sc + h * row_step * K::kSc + (quarter + h * quarter_step) * K::kElems / kKvBlock);
   };
 
-  for (int first = u0; first < u1; first += kBatch) {
-    const int n = min(kBatch, u1 - first);
+  for (int last = u1 - 1; last >= u0; last -= S::kBatch) {
     __syncthreads();
-    resolve_units(a, ids, ub, tb, span, first, n, list);
-    __syncthreads();
-    Stage cur, next;
-    if (wave < n) load(cur, wave);
+    const int n = resolve_units<S::kBatch>(a, L, span, tr, last, min(S::kBatch, last - u0 + 1), list, tmp);
+    if (wave >= n) continue;
+    Unit u = uniform_unit(list[wave]);
+    load(pk, u, false);
+    load(pv, u, true);
     for (int i = wave; i < n; i += kWaves) {
-      if (i + kWaves < n) load(next, i + kWaves);
-      const Unit u = cur.u;
+      const bool more = i + kWaves < n;
+      const Unit next = uniform_unit(list[more ? i + kWaves : i]);
       const int held = u.where >> 16;
-      const int row_pos = u.pos + 4 * quad;  // position of the lane's first score
-      // S^T of two blocks of 16 tokens: lane (col, quad) gets tokens 4 quad .. 4 quad + 3 of each
-      f32x4 s[2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        s[h] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int x = 0; x < K::kSteps; ++x)
-          s[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(piece_step<FMT, D>(cur.k[h], x)), q[x], s[h], 0, 0, 0);
-      }
-      float x[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = score(s[j >> 2][j & 3]);
-      if (a.slopes) {
-        const float dist = static_cast<float>(rule.pos - row_pos);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] -= rule.slope * fabsf(dist - static_cast<float>(16 * (j >> 2) + (j & 3)));
-      }
-      // Masks: every token of the unit is seen by every row, or each score is looked at.
-      const bool inside = u.pos + kUnit <= prefix || (u.pos >= lo_all && u.pos + kUnit - 1 <= hi_all);
-      uint32_t bad = 0;  // tokens whose values are not finite
-      bool dead[2] = {false, false};  // this lane's value rows that are not read
-      uint32_t seen = 0xFFu;
-      if (held < kUnit || a.chunk_ns || !inside) {
-        seen = 0;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int tok = 16 * (j >> 2) + 4 * quad + (j & 3), p = u.pos + tok;
-          const bool see = tok < held && (p < prefix || (p >= rule.lo && p <= rule.hi)) && u.ns == rule.ns && u.ns >= 0;
-          seen |= see ? 1u << j : 0u;
-          x[j] = see ? x[j] : -INFINITY;
-        }
+      float s[kScores];
+      if constexpr (R == 16) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const bool out = 16 * h + col >= held;
-          const bool nf = !out && piece_bad<FMT, D>(cur.v[h]);
-          const uint64_t vote = __ballot(nf);
-          bad |= static_cast<uint32_t>((vote | vote >> 16 | vote >> 32 | vote >> 48) & 0xFFFFu) << (16 * h);
-          dead[h] = out || nf;
+          f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int y = 0; y < K::kSteps; ++y)
+            x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(piece_step<FMT, D>(pk[h], y)), q[y], x, 0, 0, 0);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) s[4 * h + j] = x[j];
+        }
+      } else {
+        f32x16 x;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) x[j] = 0.f;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int y = 0; y < K::kSteps; ++y)
+            x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(piece_step<FMT, D>(pk[h], y)), q[h * K::kSteps + y],
+                                                        x, 0, 0, 0);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) s[j] = x[j];
+      }
+      if (more) load(pk, next, false);
+      scores.template apply<R>(s, rule, tr, u.pos, part);
+      if (held < kUnit || !tr.all_see(u.pos, prefix)) {
+        const uint32_t seen = mask_scores<R>(s, rule, u, prefix, part);
+        uint32_t bad = 0;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int row = h * row_step + col;
+          const bool nf = row < held && piece_bad<FMT, D>(pv[h]);
+          uint64_t vote = __ballot(nf);
+          vote |= vote >> 32;
+          if (R == 16) vote |= vote >> 16;
+          bad |= static_cast<uint32_t>(R == 16 ? vote & 0xFFFFu : vote) << (h * row_step);
+          if (nf || row >= held) piece_clear<FMT, D>(pv[h]);
+        }
+        if (bad) poison |= sees_bad<R, kScores>(seen, bad, part);
+      }
+      bool heavy;
+      const bool counts = soften<R, D>(s, scores.factor(), st, rows, &heavy);
+      if (counts) {  // values: unpack into the wave's LDS rows, to be read back transposed
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint16_t* dst = vrows + (h * row_step + col) * S::kPitch + (quarter + h * quarter_step) * K::kElems;
+#pragma unroll
+          for (int y = 0; y < K::kSteps; ++y) *reinterpret_cast<u32x4_t*>(dst + 8 * y) = piece_step<FMT, D>(pv[h], y);
         }
       }
-      float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-      top = max_rows(top);
-      if (__any(top > m + kLag)) {
-        const float mn = fmaxf(m, top);
-        const float f = mn == -INFINITY ? 1.f : fast_exp2(m - mn);
-        l *= f;
-        lr *= f;
-#pragma unroll
-        for (int n2 = 0; n2 < kBlocks; ++n2) acc[n2] *= f;
-        m = mn;
-      }
-      const float ref = m == -INFINITY ? 0.f : m;
-      u32x4_t pw;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        x[j] = fast_exp2(x[j] - ref);
-        l += x[j];
-      }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        pw[j] = pack2(x[2 * j], x[2 * j + 1]);
-        lr = add_pair(pw[j], lr);
-      }
-      if (bad) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          poison |= ((seen >> j) & 1u) && ((bad >> (16 * (j >> 2) + 4 * quad + (j & 3))) & 1u);
-      }
-      // values: unpack into the wave's LDS rows, read back transposed
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        if (dead[h]) piece_clear<FMT, D>(cur.v[h]);
-        uint16_t* dst = vrows + (16 * h + col) * S::kPitch + quad * K::kElems;
-#pragma unroll
-        for (int y = 0; y < K::kSteps; ++y) *reinterpret_cast<u32x4_t*>(dst + 8 * y) = piece_step<FMT, D>(cur.v[h], y);
-      }
-      __builtin_amdgcn_wave_barrier();
-      const uint16_t* src = vrows + (4 * quad + (col >> 2)) * S::kPitch + (col & 3) * 4;
-      auto add_values = [&](const u32x4_t& w) {
-#pragma unroll
-        for (int n2 = 0; n2 < kBlocks; ++n2) {
-          const u32x2_t v0 = lds_transpose4(src + 16 * n2);
-          const u32x2_t v1 = lds_transpose4(src + 16 * S::kPitch + 16 * n2);
-          const u32x4_t v = {v0[0], v0[1], v1[0], v1[1]};
-          acc[n2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(v), as_bf16x8(w), acc[n2], 0, 0, 0);
+      if (more) load(pv, next, true);
+      if (counts) {
+        u32x4_t w[kScores / 8];
+        pack_weights(s, w);
+        __builtin_amdgcn_wave_barrier();
+        add_values<R, D, S::kPitch>(rows, vrows, w, lane);
+        if (heavy) {
+          pack_rests(s, w);
+          add_values<R, D, S::kPitch>(rows, vrows, w, lane);
         }
-      };
-      add_values(pw);
-      if (__any(fast_exp2(top - ref) * kHeavy > l)) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          pw[j] = rest2(x[2 * j], x[2 * j + 1], pw[j]);
-          lr = add_pair(pw[j], lr);
-        }
-        add_values(pw);
+        __builtin_amdgcn_wave_barrier();
       }
-      __builtin_amdgcn_wave_barrier();
-      cur = next;
+      u = next;
     }
   }
 
-  // join the waves in LDS, in wave order
-  l = sum_rows(l);
-  lr = sum_rows(lr);
-  {
-    const uint64_t v = __ballot(poison);
-    poison = ((v | v >> 16 | v >> 32 | v >> 48) >> col) & 1u;
-  }
-  __syncthreads();  // every wave is done with its rows of `area`
-  float* jo = reinterpret_cast<float*>(area);
-  if (quad == 0) wave_ml[wave][col] = RowState{m, l, lr};
+  // join the waves: 2 and 3 into 0 and 1, then 1 into 0 (a lane holds the same outputs in every wave)
+  st.l = sum_column<R>(st.l);
+  poison = any_column<R>(poison, col);
+  float* store = reinterpret_cast<float*>(area);
 #pragma unroll
-  for (int n = 0; n < kBlocks; ++n) {
-    f32x4 o = acc[n];
-    if (poison) o = f32x4{NAN, NAN, NAN, NAN};
-    *reinterpret_cast<f32x4*>(jo + (wave * kFewRows + col) * D + 16 * n + 4 * quad) = o;
-  }
-  __syncthreads();
-  constexpr int kPer = kFewRows * D / kThreads;  // outputs per thread, consecutive in a row
-  const int r = tid / (D / kPer), c0 = (tid % (D / kPer)) * kPer;
-  if (r >= t.rows) return;
-  float mm = -INFINITY;
-  for (int w = 0; w < kWaves; ++w) mm = fmaxf(mm, wave_ml[w][r].m);
-  const float ref = mm == -INFINITY ? 0.f : mm;
-  float ll = 0.f, llr = 0.f, o[kPer] = {};
-  for (int w = 0; w < kWaves; ++w) {
-    const RowState st = wave_ml[w][r];
-    const float f = fast_exp2(st.m - ref);
-    ll += f * st.l;
-    llr += f * st.lr;
-    for (int x = 0; x < kPer; ++x) o[x] += f * jo[(w * kFewRows + r) * D + c0 + x];
-  }
-  const int row = t.r0 + r;
-  const int64_t at = (t.q0 + row / group) * a.hq + g * group + row % group;
-  if (splits == 1) {
-    const float inv = inverse_sum(llr);
-    uint16_t* dst = a.out + at * D + c0;
-    for (int x = 0; x < kPer; x += 4) {
-      const u32x2_t v = {pack2(o[x] * inv, o[x + 1] * inv), pack2(o[x + 2] * inv, o[x + 3] * inv)};
-      *reinterpret_cast<u32x2_t*>(dst + x) = v;
+  for (int from = 2; from >= 1; --from) {
+    __syncthreads();  // what `area` held is done with
+    if (wave >= from && wave < 2 * from) {
+      float* dst = store + (wave - from) * R * D + lane * 4;
+      int x = 0;
+      rows.each4(part, [&](int, f32x4 v) { *reinterpret_cast<f32x4*>(dst + 256 * x++) = v; });
+      joint[wave - from][lane] = st;
+      joint_poison[wave - from][lane] = poison;
     }
-    if (a.lse && c0 == 0) a.lse[at] = lse_of(mm, ll);
-  } else {
-    const int64_t slot = static_cast<int64_t>(split) * a.total_q * a.hq + at;
-    for (int x = 0; x < kPer; x += 4)
-      *reinterpret_cast<f32x4*>(part_o + slot * D + c0 + x) = f32x4{o[x], o[x + 1], o[x + 2], o[x + 3]};
-    if (c0 == 0) part_ml[slot] = RowState{mm, ll, llr};
+    __syncthreads();
+    if (wave < from) {
+      const RowState other = joint[wave][lane];
+      poison |= joint_poison[wave][lane] != 0;
+      const float mn = fmaxf(st.m, other.m), ref = finite_max(mn);
+      const float f0 = fast_exp2(st.m - ref), f1 = fast_exp2(other.m - ref);
+      st.l = st.l * f0 + other.l * f1;
+      st.m = mn;
+      const float* src = store + wave * R * D + lane * 4;
+      constexpr int kQ = Rows<R, D>::kRegs / 4;
+#pragma unroll
+      for (int n = 0; n < Rows<R, D>::kBlocks; ++n)
+#pragma unroll
+        for (int y = 0; y < kQ; ++y) {
+          const f32x4 v = *reinterpret_cast<const f32x4*>(src + 256 * (n * kQ + y));
+#pragma unroll
+          for (int j = 0; j < 4; ++j) rows.o[n][4 * y + j] = rows.o[n][4 * y + j] * f0 + v[j] * f1;
+        }
+    }
   }
+  if (wave > 0 || col >= t.rows) return;
+  const int row = t.r0 + col;
+  write_rows<R, D>(a, rows, st, poison, (t.q0 + row / group) * a.hq + g * group + row % group, part, split, splits,
+                   part_o, part_ml);
 }
 
 // ---------------------------------------------------------------- joining splits
 
-// One wave per row: the splits' sums, weighted by their maxima, in split order.
+// One workgroup per row: lane s of every wave weighs split s, wave w adds splits w, w + 4, ..., then the waves' sums
+// are added in order.
 template <int D>
 __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a, int splits,
                                                                const float* __restrict__ part_o,
                                                                const RowState* __restrict__ part_ml) {
   constexpr int kPer = D / 64;
-  const int lane = threadIdx.x & 63;
-  const int64_t rows = a.total_q * a.hq;
-  const int64_t at = static_cast<int64_t>(blockIdx.x) * kWaves + (threadIdx.x >> 6);
-  if (at >= rows) return;
+  __shared__ float sums[kWaves][D];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t rows = a.total_q * a.hq, at = blockIdx.x;
   if (a.q_offsets) {  // rows that no request owns were not computed
     const int64_t j = at / a.hq;
     if (j < a.q_offsets[0] || j >= a.q_offsets[a.m]) return;
   }
-  float mm = -INFINITY;
-  for (int s = 0; s < splits; ++s) mm = fmaxf(mm, part_ml[s * rows + at].m);
-  const float ref = mm == -INFINITY ? 0.f : mm;
-  float ll = 0.f, llr = 0.f, o[kPer] = {};
-  for (int s = 0; s < splits; ++s) {
-    const RowState st = part_ml[s * rows + at];
-    const float f = fast_exp2(st.m - ref);
-    ll += f * st.l;
-    llr += f * st.lr;
+  RowState st{-INFINITY, 0.f};
+  if (lane < splits) st = part_ml[lane * rows + at];
+  const float m = wave_max_f32(st.m);
+  const float f = fast_exp2(st.m - finite_max(m));
+  float l = f * st.l;
+  for (int off = 1; off < 64; off <<= 1) l += __shfl_xor(l, off);
+  float o[kPer] = {};
+#pragma unroll 4
+  for (int s = wave; s < splits; s += kWaves) {
+    const float w = lane_f32(f, s);
     const float* src = part_o + (s * rows + at) * D + lane * kPer;
-    for (int x = 0; x < kPer; ++x) o[x] += f * src[x];
+#pragma unroll
+    for (int x = 0; x < kPer; ++x) o[x] += w * src[x];
   }
-  const float inv = inverse_sum(llr);
-  uint16_t* dst = a.out + at * D + lane * kPer;
-  for (int x = 0; x < kPer; ++x) dst[x] = static_cast<uint16_t>(pack2(o[x] * inv, 0.f) & 0xFFFFu);
-  if (a.lse && lane == 0) a.lse[at] = lse_of(mm, ll);
+#pragma unroll
+  for (int x = 0; x < kPer; ++x) sums[wave][lane * kPer + x] = o[x];
+  __syncthreads();
+  const float inv = inverse_sum(l);
+  const int d = 2 * threadIdx.x;
+  if (d < D) {
+    float v[2] = {0.f, 0.f};
+    for (int w = 0; w < kWaves; ++w) {
+      v[0] += sums[w][d];
+      v[1] += sums[w][d + 1];
+    }
+    *reinterpret_cast<uint32_t*>(a.out + at * D + d) = pack2(v[0] * inv, v[1] * inv);
+  }
+  if (a.lse && threadIdx.x == 0) a.lse[at] = lse_of(m, l);
 }
 
 // ---------------------------------------------------------------- tiles of rows
 
 template <int FMT, int D>
 struct TileShape {
-  static constexpr int kPitch = D + 8;                          // bf16 elements between LDS rows
-  static constexpr int kPart = kTileTokens * kPitch * 2;        // bytes of a step's keys or values
-  static constexpr int kLoads = kTileTokens * 4 / kThreads;     // quarter rows per thread, keys and values each
+  static constexpr int kBatch = 256;                          // units resolved at a time
+  static constexpr int kStepUnits = D == 256 ? 1 : 2;         // units per step
+  static constexpr int kTokens = kStepUnits * kUnit;
+  static constexpr int kPitch = D + 8;                        // bf16 elements between LDS rows
+  static constexpr int kPart = kTokens * kPitch;              // elements of a step's keys or values
+  static constexpr int kPieces = 2 * kTokens * 4 / kThreads;  // quarter rows per thread and step, keys then values
 };
 
 template <int FMT, int D>
-__global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile_kernel(AttendArgs a, int splits, int64_t tiles,
-                                                               float* __restrict__ part_o,
-                                                               RowState* __restrict__ part_ml) {
+__global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile_kernel(AttendArgs a, int splits,
+                                                                                 int64_t tiles,
+                                                                                 float* __restrict__ part_o,
+                                                                                 RowState* __restrict__ part_ml) {
   using K = Dim<FMT, D>;
   using S = TileShape<FMT, D>;
-  static_assert(S::kLoads == 1, "one quarter row of keys and one of values per thread and step");
-  constexpr int kBlocks = D / 32, kQSteps = D / 16;
-  extern __shared__ int dyn[];  // ub[k + 1], tb[k + 1]
-  __shared__ __align__(16) uint8_t area[2 * S::kPart];
-  __shared__ Unit list[kBatch];
+  constexpr int kQSteps = D / 16, kUnits = S::kStepUnits;
+  extern __shared__ int dyn[];  // the chunk list: cid[k], ub[k + 1], tb[k + 1]
+  __shared__ __align__(16) uint16_t area[2][2 * S::kPart];
+  __shared__ Unit list[S::kBatch + 1];
   __shared__ int tmp[2 * kWaves];
-  __shared__ uint32_t bad_tok[2][2];  // tokens whose values are not finite, of even and odd steps
-  int* ub = dyn;
-  int* tb = dyn + a.k + 1;
-  uint16_t* krows = reinterpret_cast<uint16_t*>(area);
-  uint16_t* vrows = reinterpret_cast<uint16_t*>(area + S::kPart);
+  __shared__ uint32_t bad_tok[3][2];  // tokens whose values are not finite: of this step, the next and the one after
 
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int col = lane & 31, half = lane >> 5;
@@ -738,276 +981,176 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile_kernel
   b /= heads;
   const int split = static_cast<int>(b % splits);
   Tile t;
-  if (!find_tile(a, tiles - 1 - b / splits, group, kTileRows, &t)) return;  // the latest rows see most: first
-  const int32_t* ids = a.ids + t.req * a.k;
-  scan_list(a, ids, ub, tb, tmp);
-  const int ctx = tb[a.k];
+  if (!find_tile<kTileRows>(a, tiles - 1 - b / splits, group, &t)) return;  // the latest rows see most: first
+  const ChunkList L = scan_list(a, t.req, dyn, tmp);
+  const int ctx = L.tb[a.k];
   const int prefix = a.prefix_len ? a.prefix_len[t.req] : 0;
-  const int my_row = min(32 * wave + col, t.rows - 1);
-  const RowRule rule = row_rule(a, t, ctx, g, group, t.r0 + my_row);
-
-  // what the tile's rows see at most, and what all of them see
-  int lo = kFar, hi = -1, lo_all = 0, hi_all = kFar;
-  for (int r = lane; r < t.rows; r += 64) {
-    const RowRule x = row_rule(a, t, ctx, g, group, t.r0 + r);
-    lo = min(lo, x.lo);
-    hi = max(hi, x.hi);
-    lo_all = max(lo_all, x.lo);
-    hi_all = min(hi_all, x.hi);
-  }
-  for (int off = 1; off < 64; off <<= 1) {
-    lo = min(lo, __shfl_xor(lo, off));
-    hi = max(hi, __shfl_xor(hi, off));
-    lo_all = max(lo_all, __shfl_xor(lo_all, off));
-    hi_all = min(hi_all, __shfl_xor(hi_all, off));
-  }
-  const Span span = visible_units(ub, tb, a.k, prefix, lo, hi);
+  const int my_row = t.r0 + min(32 * wave + col, t.rows - 1);
+  const bool works = 32 * wave < t.rows;  // this wave has rows
+  const RowRule rule = row_rule(a, t, ctx, g, group, my_row);
+  const TileRule tr = tile_rule<kTileRows>(a, t, ctx, g, group);
+  const Span span = visible_units(L, prefix, tr.lo, tr.hi);
   const int n_units = span.count();
   const int u0 = static_cast<int>(static_cast<int64_t>(n_units) * split / splits);
   const int u1 = static_cast<int>(static_cast<int64_t>(n_units) * (split + 1) / splits);
 
-  // queries: lane (col, half) holds elements 16 s + 8 half .. + 7 of row `col` of the wave
+  // lane (col, half) holds elements 16 s + 8 half .. + 7 of row `col` of the wave
   bf16x8 q[kQSteps];
-  {
-    const int r = t.r0 + my_row;
-    const uint16_t* src = a.q + (t.q0 + r / group) * a.q_ts + (g * group + r % group) * a.q_hs + 8 * half;
-    const bool vec = (reinterpret_cast<uintptr_t>(src) & 15u) == 0;
-#pragma unroll
-    for (int i = 0; i < kQSteps; ++i) {
-      union { u32x4_t v; uint16_t h[8]; } x;
-      if (vec) {
-        x.v = *reinterpret_cast<const u32x4_t*>(src + 16 * i);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x.h[j] = src[16 * i + j];
-      }
-      q[i] = as_bf16x8(x.v);
-    }
-  }
+  load_queries(a.q + (t.q0 + my_row / group) * a.q_ts + (g * group + my_row % group) * a.q_hs + 8 * half, 16, q);
 
-  const Scores score = scores_of(a);
+  const Scores scores(a);
   const int64_t T = a.kv.page_tokens;
   const int64_t head_at = static_cast<int64_t>(g) * 2 * T * (K::kRow + K::kSc);
-  const int my_tok = tid >> 2, my_quarter = tid & 3;  // the quarter row this thread unpacks
 
-  f32x16 acc[kBlocks];
-#pragma unroll
-  for (int n = 0; n < kBlocks; ++n)
-#pragma unroll
-    for (int j = 0; j < 16; ++j) acc[n][j] = 0.f;
-  float m = -INFINITY, l = 0.f, lr = 0.f;
+  Rows<32, D> rows;
+  rows.clear();
+  RowState st{-INFINITY, 0.f};
   bool poison = false;
-  if (tid < 2) bad_tok[0][tid] = 0;
-  int odd = 0;
+  if (tid < 6) bad_tok[tid >> 1][tid & 1] = 0;
+  int slot = 0;  // of the step at hand
 
-  for (int first = u0; first < u1; first += kBatch) {
-    const int n = min(kBatch, u1 - first);
+  for (int last = u1 - 1; last >= u0; last -= S::kBatch) {
     __syncthreads();
-    resolve_units(a, ids, ub, tb, span, first, n, list);
+    const int n = resolve_units<S::kBatch>(a, L, span, tr, last, min(S::kBatch, last - u0 + 1), list, tmp);
+    if (tid == 0) list[n] = Unit{0, 0, 0, -1};  // fills up the last step: holds nothing
     __syncthreads();
-    Piece<FMT, D> pk, pv;
-    bool out = true;
-    auto load = [&](int i) {
-      // the thread's token is in unit i + (my_tok >> 5); past the batch's end nothing is held
-      const int x = i + (my_tok >> 5);
-      const Unit u = list[min(x, n - 1)];
-      const int row = (u.where & 0xFFFF) + (my_tok & 31);
-      out = x >= n || (my_tok & 31) >= (u.where >> 16);
-      if (out) {
-        piece_clear<FMT, D>(pk);
-        piece_clear<FMT, D>(pv);
-        return;
+    Piece<FMT, D> piece[S::kPieces];
+    // Quarter row x of this thread: x = tid + 256 i; the first half of a step's are keys.
+    auto load = [&](int first) {
+#pragma unroll
+      for (int i = 0; i < S::kPieces; ++i) {
+        const int x = (tid + kThreads * i) % (4 * S::kTokens), tok = x >> 2, quarter = x & 3;
+        const bool is_v = tid + kThreads * i >= 4 * S::kTokens;
+        const Unit u = list[min(first + tok / kUnit, n)];
+        if (tok % kUnit >= (u.where >> 16)) {
+          piece_clear<FMT, D>(piece[i]);
+          continue;
+        }
+        const int row = (u.where & 0xFFFF) + tok % kUnit;
+        const uint8_t* base = a.kv.pool + u.page * a.kv.page_bytes + head_at;
+        load_piece<FMT, D>(piece[i], base + (is_v ? T * K::kRow : 0) + row * K::kRow + quarter * K::kBytes,
+                           base + 2 * T * K::kRow + (is_v ? T * K::kSc : 0) + row * K::kSc +
+                               quarter * K::kElems / kKvBlock);
       }
-      const uint8_t* part = a.kv.pool + u.page * a.kv.page_bytes + head_at;
-      const uint8_t* kc = part + row * K::kRow + my_quarter * K::kBytes;
-      const uint8_t* ks = part + 2 * T * K::kRow + row * K::kSc + my_quarter * K::kElems / kKvBlock;
-      load_piece<FMT, D>(pk, kc, ks);
-      load_piece<FMT, D>(pv, kc + T * K::kRow, ks + T * K::kSc);
     };
+    auto is_masked = [&](int first) {
+      bool m = false;
+#pragma unroll
+      for (int h = 0; h < kUnits; ++h) {
+        const Unit u = uniform_unit(list[min(first + h, n)]);
+        m |= (u.where >> 16) < kUnit || !tr.all_see(u.pos, prefix);
+      }
+      return m;
+    };
+    auto unpack = [&](int buffer, bool masked, uint32_t* bad) {
+#pragma unroll
+      for (int i = 0; i < S::kPieces; ++i) {
+        const int x = (tid + kThreads * i) % (4 * S::kTokens), tok = x >> 2, quarter = x & 3;
+        const bool is_v = tid + kThreads * i >= 4 * S::kTokens;
+        if (masked && is_v && piece_bad<FMT, D>(piece[i])) {
+          atomicOr(&bad[tok / kUnit], 1u << (tok % kUnit));
+          piece_clear<FMT, D>(piece[i]);
+        }
+        uint16_t* dst = area[buffer] + (is_v ? S::kPart : 0) + tok * S::kPitch + quarter * K::kElems;
+#pragma unroll
+        for (int y = 0; y < K::kSteps; ++y) *reinterpret_cast<u32x4_t*>(dst + 8 * y) = piece_step<FMT, D>(piece[i], y);
+      }
+    };
+    if (n == 0) continue;
     load(0);
-    for (int i = 0; i < n; i += 2) {
-      Unit u[2];
+    bool masked = is_masked(0);
+    unpack(0, masked, bad_tok[slot]);
+    if (kUnits < n) load(kUnits);
+    __syncthreads();
+    int buffer = 0;
+    for (int i = 0; i < n; i += kUnits, buffer ^= 1) {
+      const int slot1 = slot == 2 ? 0 : slot + 1, slot2 = slot1 == 2 ? 0 : slot1 + 1;
+      if (tid < 2) bad_tok[slot2][tid] = 0;
+      const uint16_t* keys = area[buffer];
+      const uint16_t* values = keys + S::kPart;
+      float s[16 * kUnits];
+      if (works) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        u[h] = list[min(i + h, n - 1)];
-        u[h].where = __builtin_amdgcn_readfirstlane(u[h].where);
-        u[h].pos = __builtin_amdgcn_readfirstlane(u[h].pos);
-        u[h].ns = __builtin_amdgcn_readfirstlane(u[h].ns);
-        if (i + h >= n) u[h].where = 0;
-      }
-      bool masked = a.chunk_ns != nullptr;
+        for (int h = 0; h < kUnits; ++h) {
+          f32x16 x;
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
-        masked |= (u[h].where >> 16) < kUnit ||
-                  !(u[h].pos + kUnit <= prefix || (u[h].pos >= lo_all && u[h].pos + kUnit - 1 <= hi_all));
-      __syncthreads();  // the last step's reads of the rows and of its bad_tok are done
-      if (tid < 2) bad_tok[odd ^ 1][tid] = 0;
-      if (masked && piece_bad<FMT, D>(pv)) {
-        atomicOr(&bad_tok[odd][my_tok >> 5], 1u << (my_tok & 31));
-        piece_clear<FMT, D>(pv);
-      }
-      uint16_t* kd = krows + my_tok * S::kPitch + my_quarter * K::kElems;
-      uint16_t* vd = vrows + my_tok * S::kPitch + my_quarter * K::kElems;
+          for (int j = 0; j < 16; ++j) x[j] = 0.f;
+          const uint16_t* kr = keys + (32 * h + col) * S::kPitch + 8 * half;
 #pragma unroll
-      for (int y = 0; y < K::kSteps; ++y) {
-        *reinterpret_cast<u32x4_t*>(kd + 8 * y) = piece_step<FMT, D>(pk, y);
-        *reinterpret_cast<u32x4_t*>(vd + 8 * y) = piece_step<FMT, D>(pv, y);
+          for (int y = 0; y < kQSteps; ++y)
+            x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                as_bf16x8(*reinterpret_cast<const u32x4_t*>(kr + 16 * y)), q[y], x, 0, 0, 0);
+#pragma unroll
+          for (int j = 0; j < 16; ++j) s[16 * h + j] = x[j];
+        }
       }
+      // the next step's rows go into the other buffer, and the loads of the one after start
+      bool next_masked = false;
+      if (i + kUnits < n) {
+        next_masked = is_masked(i + kUnits);
+        unpack(buffer ^ 1, next_masked, bad_tok[slot1]);
+        if (i + 2 * kUnits < n) load(i + 2 * kUnits);
+      }
+      if (works) {
+#pragma unroll
+        for (int h = 0; h < kUnits; ++h) {
+          const Unit u = uniform_unit(list[min(i + h, n)]);
+          float (&sh)[16] = *reinterpret_cast<float (*)[16]>(&s[16 * h]);
+          scores.template apply<32>(sh, rule, tr, u.pos, half);
+          if (masked) {
+            const uint32_t seen = mask_scores<32>(sh, rule, u, prefix, half);
+            const uint32_t bad = bad_tok[slot][h];
+            if (bad) poison |= sees_bad<32, 16>(seen, bad, half);
+          }
+        }
+        bool heavy;
+        if (soften<32, D>(s, scores.factor(), st, rows, &heavy)) {
+          u32x4_t w[2 * kUnits];
+          pack_weights(s, w);
+#pragma unroll
+          for (int h = 0; h < kUnits; ++h) add_values<32, D, S::kPitch>(rows, values + 32 * h * S::kPitch, w + 2 * h, lane);
+          if (heavy) {
+            pack_rests(s, w);
+#pragma unroll
+            for (int h = 0; h < kUnits; ++h)
+              add_values<32, D, S::kPitch>(rows, values + 32 * h * S::kPitch, w + 2 * h, lane);
+          }
+        }
+      }
+      masked = next_masked;
+      slot = slot1;
       __syncthreads();
-      if (i + 2 < n) load(i + 2);
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        if ((u[h].where >> 16) == 0) continue;
-        f32x16 s;
-#pragma unroll
-        for (int j = 0; j < 16; ++j) s[j] = 0.f;
-        const uint16_t* kr = krows + (32 * h + col) * S::kPitch + 8 * half;
-#pragma unroll
-        for (int x = 0; x < kQSteps; ++x)
-          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*reinterpret_cast<const u32x4_t*>(kr + 16 * x)), q[x],
-                                                      s, 0, 0, 0);
-        // lane (col, half) holds tokens 8 (j >> 2) + 4 half + (j & 3)
-#pragma unroll
-        for (int j = 0; j < 16; ++j) s[j] = score(s[j]);
-        if (a.slopes) {
-          const float dist = static_cast<float>(rule.pos - u[h].pos - 4 * half);
-#pragma unroll
-          for (int j = 0; j < 16; ++j)
-            s[j] -= rule.slope * fabsf(dist - static_cast<float>(8 * (j >> 2) + (j & 3)));
-        }
-        uint32_t seen = 0xFFFFu;
-        if (masked) {
-          const int held = u[h].where >> 16;
-          seen = 0;
-#pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            const int tok = 8 * (j >> 2) + 4 * half + (j & 3), p = u[h].pos + tok;
-            const bool see = tok < held && (p < prefix || (p >= rule.lo && p <= rule.hi)) && u[h].ns == rule.ns &&
-                             u[h].ns >= 0;
-            seen |= see ? 1u << j : 0u;
-            s[j] = see ? s[j] : -INFINITY;
-          }
-        }
-        float top = s[0];
-#pragma unroll
-        for (int j = 1; j < 16; ++j) top = fmaxf(top, s[j]);
-        top = max_half(top);
-        if (__any(top > m + kLag)) {
-          const float mn = fmaxf(m, top);
-          const float f = mn == -INFINITY ? 1.f : fast_exp2(m - mn);
-          l *= f;
-          lr *= f;
-#pragma unroll
-          for (int n2 = 0; n2 < kBlocks; ++n2) acc[n2] *= f;
-          m = mn;
-        }
-        const float ref = m == -INFINITY ? 0.f : m;
-        u32x4_t pw[2];
-#pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          s[j] = fast_exp2(s[j] - ref);
-          l += s[j];
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          pw[j >> 2][j & 3] = pack2(s[2 * j], s[2 * j + 1]);
-          lr = add_pair(pw[j >> 2][j & 3], lr);
-        }
-        if (masked && bad_tok[odd][h]) {
-          const uint32_t bad = bad_tok[odd][h];
-#pragma unroll
-          for (int j = 0; j < 16; ++j)
-            poison |= ((seen >> j) & 1u) && ((bad >> (8 * (j >> 2) + 4 * half + (j & 3))) & 1u);
-        }
-        // lane (16 x + i, half): rows 4 half + (i >> 2) (+ 8) of each 16 tokens, columns 16 x ..
-        const int i16 = lane & 15;
-        const uint16_t* vr = vrows + (32 * h + 4 * half + (i16 >> 2)) * S::kPitch + ((lane >> 4) & 1) * 16 + (i16 & 3) * 4;
-        auto add_values = [&]() {
-#pragma unroll
-          for (int n2 = 0; n2 < kBlocks; ++n2) {
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-              const u32x2_t v0 = lds_transpose4(vr + (16 * x) * S::kPitch + 32 * n2);
-              const u32x2_t v1 = lds_transpose4(vr + (16 * x + 8) * S::kPitch + 32 * n2);
-              const u32x4_t v = {v0[0], v0[1], v1[0], v1[1]};
-              acc[n2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(v), as_bf16x8(pw[x]), acc[n2], 0, 0, 0);
-            }
-          }
-        };
-        add_values();
-        if (__any(fast_exp2(top - ref) * kHeavy > l)) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            pw[j >> 2][j & 3] = rest2(s[2 * j], s[2 * j + 1], pw[j >> 2][j & 3]);
-            lr = add_pair(pw[j >> 2][j & 3], lr);
-          }
-          add_values();
-        }
-      }
-      odd ^= 1;
     }
   }
 
-  l = sum_half(l);
-  lr = sum_half(lr);
-  {
-    const uint64_t v = __ballot(poison);
-    poison = ((v | v >> 32) >> col) & 1u;
-  }
-  const int r = 32 * wave + col;
-  if (r >= t.rows) return;
-  const int row = t.r0 + r;
-  const int64_t at = (t.q0 + row / group) * a.hq + g * group + row % group;
-  float inv = inverse_sum(lr);
-  if (poison) inv = NAN;
-  if (splits == 1) {
-    uint16_t* dst = a.out + at * D + 4 * half;
-#pragma unroll
-    for (int n = 0; n < kBlocks; ++n)
-#pragma unroll
-      for (int y = 0; y < 4; ++y) {
-        const u32x2_t v = {pack2(acc[n][4 * y] * inv, acc[n][4 * y + 1] * inv),
-                           pack2(acc[n][4 * y + 2] * inv, acc[n][4 * y + 3] * inv)};
-        *reinterpret_cast<u32x2_t*>(dst + 32 * n + 8 * y) = v;
-      }
-    if (a.lse && half == 0) a.lse[at] = lse_of(m, l);
-  } else {
-    const int64_t slot = static_cast<int64_t>(split) * a.total_q * a.hq + at;
-    float* dst = part_o + slot * D + 4 * half;
-#pragma unroll
-    for (int n = 0; n < kBlocks; ++n)
-#pragma unroll
-      for (int y = 0; y < 4; ++y) {
-        f32x4 v = {acc[n][4 * y], acc[n][4 * y + 1], acc[n][4 * y + 2], acc[n][4 * y + 3]};
-        if (poison) v = f32x4{NAN, NAN, NAN, NAN};
-        *reinterpret_cast<f32x4*>(dst + 32 * n + 8 * y) = v;
-      }
-    if (half == 0) part_ml[slot] = RowState{m, l, lr};
-  }
+  st.l = sum_column<32>(st.l);
+  poison = any_column<32>(poison, col);
+  if (32 * wave + col >= t.rows) return;
+  write_rows<32, D>(a, rows, st, poison, (t.q0 + my_row / group) * a.hq + g * group + my_row % group, half, split,
+                    splits, part_o, part_ml);
 }
 
 // ---------------------------------------------------------------- launches
 
-int64_t tile_count(const int32_t* q_offsets, int64_t m, int64_t total_q, int group, int R) {
-  if (q_offsets) return total_q * group / R + m;
+int64_t tile_count(bool ragged, int64_t m, int64_t total_q, int group, int R) {
+  if (ragged) return total_q * group / R + m;
   return m * ((total_q / m * group + R - 1) / R);
 }
 
-// Rows per request decide the kernel: up to 16 (on average) the few-rows kernel.  A context is split when the tiles
-// alone leave CUs idle, into parts of at least kMinPart tokens.
+// Rows per request (on average) decide the kernel.  A context is split when the tiles alone leave CUs idle, into
+// parts of at least kMinPart tokens.
 constexpr int64_t kWantFew = 2048, kWantTile = 512;
 constexpr int64_t kMinPart = 512;
 
 AttendPlan make_plan(int64_t m, int64_t capacity, int64_t total_q, int heads, int heads_q, bool ragged) {
   AttendPlan p;
   const int group = heads_q / heads;
-  p.few = total_q * group <= kFewRows * m;
-  const int32_t some = 0;
-  p.tiles = tile_count(ragged ? &some : nullptr, m, total_q, group, p.few ? kFewRows : kTileRows);
-  const int64_t have = p.tiles * heads, want = p.few ? kWantFew : kWantTile;
+  p.rows = total_q * group <= 16 * m ? 16 : total_q * group <= 64 * m ? 32 : kTileRows;
+  p.tiles = tile_count(ragged, m, total_q, group, p.rows);
+  const int64_t have = p.tiles * heads, want = p.rows < kTileRows ? kWantFew : kWantTile;
   int64_t s = (want + have - 1) / have;
   s = s < capacity / kMinPart ? s : capacity / kMinPart;
-  p.splits = static_cast<int>(s < 1 ? 1 : s > 256 ? 256 : s);
+  p.splits = static_cast<int>(s < 1 ? 1 : s > kMaxSplits ? kMaxSplits : s);
   return p;
 }
 
@@ -1024,15 +1167,15 @@ hipError_t launch_dim(const AttendArgs& a, const AttendPlan& p, hipStream_t stre
                                                          partial_o_bytes(D, a.total_q, a.hq, p.splits))
                              : nullptr;
   const dim3 grid(static_cast<unsigned>(p.tiles * a.kv.heads * p.splits));
-  const size_t lds = static_cast<size_t>(2) * (a.k + 1) * sizeof(int);
-  if (p.few)
-    attend_few_kernel<FMT, D><<<grid, kThreads, lds, stream>>>(a, p.splits, po, pml);
+  const size_t lds = (3 * static_cast<size_t>(a.k) + 2) * sizeof(int);
+  if (p.rows == 16)
+    attend_few_kernel<FMT, D, 16><<<grid, kThreads, lds, stream>>>(a, p.splits, po, pml);
+  else if (p.rows == 32)
+    attend_few_kernel<FMT, D, 32><<<grid, kThreads, lds, stream>>>(a, p.splits, po, pml);
   else
     attend_tile_kernel<FMT, D><<<grid, kThreads, lds, stream>>>(a, p.splits, p.tiles, po, pml);
   if (hipError_t e = hipGetLastError(); e != hipSuccess || p.splits == 1) return e;
-  const int64_t rows = a.total_q * a.hq;
-  attend_join_kernel<D><<<dim3(static_cast<unsigned>((rows + kWaves - 1) / kWaves)), kThreads, 0, stream>>>(
-      a, p.splits, po, pml);
+  attend_join_kernel<D><<<dim3(static_cast<unsigned>(a.total_q * a.hq)), kThreads, 0, stream>>>(a, p.splits, po, pml);
   return hipGetLastError();
 }
 

@@ -1,10 +1,13 @@
 // Writing a quantised key/value cache and reading it back.
 //
 // Both move every byte once: a dense row in one direction, its codes and
-// scales in the other, and are bound by HBM.  A thread handles eight
-// consecutive elements (16 bytes of bf16, 4 bytes of 4-bit codes); the four
-// threads of a block of 32 share its largest magnitude through two
-// cross-lane steps, so a row is read once and nothing is staged.
+// scales in the other, and are bound by HBM.  An item is eight consecutive
+// elements (four to be read back as fp32); when writing, the four items of a
+// block of 32 are neighbouring lanes, which share its largest magnitude
+// through two cross-lane steps, so a row is read once and nothing is staged.
+// A workgroup first looks up the places of its tokens (chunk, position and
+// page: three dependent loads, made once per token and not once per item),
+// then keeps kInFlight items per thread in flight.
 #include "kv.h"
 #include "device_common.h"
 
@@ -13,44 +16,104 @@ namespace memattn {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kPiece = 8;  // elements per thread
+constexpr int kInFlight = 4;  // items per thread of large calls (small ones: 1, to use more CUs)
+constexpr int kMinItems = 16;  // items of a token of one head of 64: keys and values
+constexpr int kMaxTokens = kThreads * kInFlight / kMinItems + 2;  // tokens that a workgroup's items belong to
 
-// First byte of token (chunk, pos) of head 0's part, and its row in the page; false if the place does not exist.
-__device__ __forceinline__ bool kv_place(const KvView& kv, int32_t chunk, int32_t pos, int64_t* page, int* row) {
-  if (chunk < 0 || chunk >= kv.n_chunks || pos < 0) return false;
+// Page and row of a token; page -1: the place does not exist.
+struct Place {
+  int32_t page;
+  int32_t row;
+};
+
+__device__ __forceinline__ Place kv_place(const KvView& kv, int32_t chunk, int32_t pos) {
+  if (chunk < 0 || chunk >= kv.n_chunks || pos < 0) return {-1, 0};
   const int p = pos / kv.page_tokens;
-  if (p >= kv.ppc) return false;
+  if (p >= kv.ppc) return {-1, 0};
   const int32_t pg = kv.table[static_cast<int64_t>(chunk) * kv.ppc + p];
-  if (pg < 0 || pg >= kv.n_pages) return false;
-  *page = pg;
-  *row = pos - p * kv.page_tokens;
-  return true;
+  if (pg < 0 || pg >= kv.n_pages) return {-1, 0};
+  return {pg, pos - p * kv.page_tokens};
 }
 
-// Where piece `i` (elements 8 i ..) of a row lies: byte offsets of its codes and of its scale byte in the page.
-template <int FMT, int D>
+// A workgroup's share of the items, token by token.
+struct Share {
+  int64_t tok0;    // its first token
+  int skip;        // items of that token that belong to the workgroup before
+  int per_token;   // 2 * heads * head_dim / 8
+  uint64_t magic;  // ceil(2^40 / per_token): x / per_token = x * magic >> 40 for x < 2^18
+
+  // Token (from tok0) and item in it of item x.
+  __device__ __forceinline__ int token(int x, int* item) const {
+    const int t = static_cast<int>((static_cast<uint64_t>(x) * magic) >> 40);
+    *item = x - t * per_token;
+    return t;
+  }
+};
+
+// Look up the places of the workgroup's tokens (those past the last token count as missing).
+__device__ __forceinline__ Share open_share(const KvView& kv, int per_token, uint64_t magic, int items,
+                                            const int32_t* chunk, const int32_t* pos, int64_t n, Place* places) {
+  Share s;
+  const int64_t at = static_cast<int64_t>(blockIdx.x) * items;
+  s.tok0 = at / per_token;
+  s.skip = static_cast<int>(at - s.tok0 * per_token);
+  s.per_token = per_token;
+  s.magic = magic;
+  const int count = (s.skip + items - 1) / per_token + 1;
+  for (int t = threadIdx.x; t < count; t += kThreads) {
+    const int64_t tok = s.tok0 + t;
+    places[t] = tok < n ? kv_place(kv, chunk[tok], pos[tok]) : Place{-1, 0};
+  }
+  __syncthreads();
+  return s;
+}
+
+// Where item `i` of a row lies: byte offsets of its codes and of its scale byte in the page.
+template <int FMT, int D, int ITEM>
 __device__ __forceinline__ void kv_offsets(const KvView& kv, int head, bool is_v, int row, int i, int64_t* codes,
                                            int64_t* scale) {
   constexpr int kRow = kv_row_bytes(FMT, D), kSc = kv_scale_bytes(FMT, D);
   const int64_t t = kv.page_tokens;
   const int64_t base = static_cast<int64_t>(head) * 2 * t * (kRow + kSc);
-  *codes = base + (is_v ? t * kRow : 0) + static_cast<int64_t>(row) * kRow + i * (kRow / (D / kPiece));
-  *scale = base + 2 * t * kRow + (is_v ? t * kSc : 0) + static_cast<int64_t>(row) * kSc + i * kPiece / kKvBlock;
+  *codes = base + (is_v ? t * kRow : 0) + static_cast<int64_t>(row) * kRow + i * (kRow / (D / ITEM));
+  *scale = base + 2 * t * kRow + (is_v ? t * kSc : 0) + static_cast<int64_t>(row) * kSc + i * ITEM / kKvBlock;
 }
 
-template <typename T, bool VEC>
+// Elements per item: 16 bytes of a dense row read back, so that a wave's stores cover whole lines (with 32 bytes of
+// fp32 a lane, stored in two halves, non-temporal stores lose 11 %); 8 of a row to be written, which keeps a block in
+// one quad of lanes.
+template <bool WRITE, typename T>
+constexpr int kItem = WRITE ? 8 : 16 / static_cast<int>(sizeof(T));
+
+// 16 bytes; with NT past the caches, for large calls' dense rows, which no later part of the call touches.
+template <bool NT>
+__device__ __forceinline__ u32x4_t load16(const void* p) {
+  if constexpr (NT) return __builtin_nontemporal_load(static_cast<const u32x4_t*>(p));
+  return *static_cast<const u32x4_t*>(p);
+}
+template <bool NT>
+__device__ __forceinline__ void store16(void* p, u32x4_t v) {
+  if constexpr (NT)
+    __builtin_nontemporal_store(v, static_cast<u32x4_t*>(p));
+  else
+    *static_cast<u32x4_t*>(p) = v;
+}
+
+template <typename T, bool VEC, bool NT>
 __device__ __forceinline__ void load8(const T* p, float* x) {
   if constexpr (sizeof(T) == 4) {
     if constexpr (VEC) {
-      *reinterpret_cast<float4*>(x) = *reinterpret_cast<const float4*>(p);
-      *reinterpret_cast<float4*>(x + 4) = *reinterpret_cast<const float4*>(p + 4);
+      for (int h = 0; h < 2; ++h) {
+        const u32x4_t v = load16<NT>(p + 4 * h);
+        for (int j = 0; j < 4; ++j) x[4 * h + j] = __uint_as_float(v[j]);
+      }
     } else {
       for (int j = 0; j < 8; ++j) x[j] = p[j];
     }
   } else {
     union { u32x4_t v; uint16_t h[8]; } u;
     if constexpr (VEC) {
-      u.v = *reinterpret_cast<const u32x4_t*>(p);
+      u.v = load16<NT>(p);
     } else {
       for (int j = 0; j < 8; ++j) u.h[j] = p[j];
     }
@@ -64,57 +127,30 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   return __builtin_bit_cast(uint32_t, p);
 }
 
-template <typename T, bool VEC>
-__device__ __forceinline__ void store8(T* p, const float* x) {
-  if constexpr (sizeof(T) == 4) {
-    if constexpr (VEC) {
-      *reinterpret_cast<float4*>(p) = *reinterpret_cast<const float4*>(x);
-      *reinterpret_cast<float4*>(p + 4) = *reinterpret_cast<const float4*>(x + 4);
-    } else {
-      for (int j = 0; j < 8; ++j) p[j] = x[j];
-    }
+// 16 bytes of a dense row: 4 floats, or 8 rounded to bf16.
+template <typename T, bool VEC, bool NT>
+__device__ __forceinline__ void store_item(T* p, const float* x) {
+  union { u32x4_t v; T e[16 / sizeof(T)]; } u;
+  for (int j = 0; j < 4; ++j) u.v[j] = sizeof(T) == 4 ? __float_as_uint(x[j]) : pack_bf16(x[2 * j], x[2 * j + 1]);
+  if constexpr (VEC) {
+    store16<NT>(p, u.v);
   } else {
-    union { u32x4_t v; uint16_t h[8]; } u;
-    for (int j = 0; j < 4; ++j) u.v[j] = pack_bf16(x[2 * j], x[2 * j + 1]);
-    if constexpr (VEC) {
-      *reinterpret_cast<u32x4_t*>(p) = u.v;
-    } else {
-      for (int j = 0; j < 8; ++j) p[j] = u.h[j];
-    }
+    for (int j = 0; j < static_cast<int>(16 / sizeof(T)); ++j) p[j] = u.e[j];
   }
 }
 
-// Threads of a row stay together (D / 8 is a multiple of 8 and divides 64), so a block's four threads are lanes of
-// one quad and take the same branches.
-template <int FMT, int D, typename T, bool VEC>
-__global__ __launch_bounds__(kThreads) void kv_write_kernel(KvView kv, RowsView k, RowsView v,
-                                                            const int32_t* __restrict__ chunk,
-                                                            const int32_t* __restrict__ pos, int64_t n) {
-  constexpr int kPieces = D / kPiece;
-  const int64_t per_token = 2 * static_cast<int64_t>(kv.heads) * kPieces;
-  const int64_t at = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
-  const int64_t tok = at / per_token;
-  if (tok >= n) return;
-  const int rest = static_cast<int>(at - tok * per_token);
-  const int i = rest % kPieces, hv = rest / kPieces;
-  const bool is_v = hv >= kv.heads;
-  const int head = is_v ? hv - kv.heads : hv;
-  int64_t page;
-  int row;
-  if (!kv_place(kv, chunk[tok], pos[tok], &page, &row)) return;
-  const RowsView& src = is_v ? v : k;
-  float x[8];
-  load8<T, VEC>(static_cast<const T*>(src.data) + tok * src.ts + head * src.hs + i * kPiece, x);
-  int64_t co, so;
-  kv_offsets<FMT, D>(kv, head, is_v, row, i, &co, &so);
-  uint8_t* base = kv.pool + page * kv.page_bytes;
+// Codes of the block of which this lane holds eight elements, written to `codes`, and the scale byte.  A row's items
+// are consecutive and start at a multiple of 8, so the four items of a block are lanes of one quad.
+template <int FMT>
+__device__ __forceinline__ void encode_item(float* x, uint8_t* codes, uint8_t* scale, bool first, bool live) {
   if constexpr (FMT == MEM_KV_BF16) {
-    store8<uint16_t, true>(reinterpret_cast<uint16_t*>(base + co), x);
+    if (live) store_item<uint16_t, true, false>(reinterpret_cast<uint16_t*>(codes), x);
   } else {
     uint32_t amax = 0;
     for (int j = 0; j < 8; ++j) amax = max(amax, __float_as_uint(x[j]) & 0x7FFFFFFFu);
     amax = max(amax, dpp_u32<0xB1>(amax));
     amax = max(amax, dpp_u32<0x4E>(amax));
+    if (!live) return;
     const uint32_t byte = kv_scale_byte<FMT>(amax);
     const float inv = kv_inverse_scale(byte);
     constexpr float kTop = FMT == MEM_KV_FP4 ? 6.f : 448.f;
@@ -125,66 +161,135 @@ __global__ __launch_bounds__(kThreads) void kv_write_kernel(KvView kv, RowsView 
       c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[2], x[3], 1.f, 1);
       c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[4], x[5], 1.f, 2);
       c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[6], x[7], 1.f, 3);
-      *reinterpret_cast<uint32_t*>(base + co) = c;
+      *reinterpret_cast<uint32_t*>(codes) = c;
     } else {
       u32x2_t c;
       for (int w = 0; w < 2; ++w) {
-        int u = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * w], x[4 * w + 1], 0, false);
+        const int u = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * w], x[4 * w + 1], 0, false);
         c[w] = static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(x[4 * w + 2], x[4 * w + 3], u, true));
       }
-      *reinterpret_cast<u32x2_t*>(base + co) = c;
+      *reinterpret_cast<u32x2_t*>(codes) = c;
     }
-    if (i % 4 == 0) base[so] = static_cast<uint8_t>(byte);
+    if (first) *scale = static_cast<uint8_t>(byte);
   }
 }
 
-template <int FMT, int D, typename T, bool VEC>
-__global__ __launch_bounds__(kThreads) void kv_read_kernel(KvView kv, RowsView k, RowsView v,
-                                                           const int32_t* __restrict__ chunk,
-                                                           const int32_t* __restrict__ pos, int64_t n) {
-  constexpr int kPieces = D / kPiece;
-  const int64_t per_token = 2 * static_cast<int64_t>(kv.heads) * kPieces;
-  const int64_t at = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
-  const int64_t tok = at / per_token;
-  if (tok >= n) return;
-  const int rest = static_cast<int>(at - tok * per_token);
-  const int i = rest % kPieces, hv = rest / kPieces;
-  const bool is_v = hv >= kv.heads;
-  const int head = is_v ? hv - kv.heads : hv;
-  float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  int64_t page;
-  int row;
-  if (kv_place(kv, chunk[tok], pos[tok], &page, &row)) {
+template <int FMT, int D, typename T, bool VEC, int U>
+__global__ __launch_bounds__(kThreads) void kv_write_kernel(KvView kv, RowsView k, RowsView v,
+                                                            const int32_t* __restrict__ chunk,
+                                                            const int32_t* __restrict__ pos, int64_t n,
+                                                            int per_token, uint64_t magic) {
+  constexpr int kN = kItem<true, T>, kPieces = D / kN;
+  __shared__ Place places[kMaxTokens];
+  const Share sh = open_share(kv, per_token, magic, kThreads * U, chunk, pos, n, places);
+  float x[U][8];
+  uint8_t *codes[U], *scales[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    int item;
+    const int t = sh.token(sh.skip + threadIdx.x + u * kThreads, &item);
+    const int i = item % kPieces, hv = item / kPieces;
+    const bool is_v = hv >= kv.heads;
+    const int head = is_v ? hv - kv.heads : hv;
+    const Place p = places[t];
+    codes[u] = nullptr;
+    scales[u] = nullptr;
+    for (int j = 0; j < 8; ++j) x[u][j] = 0.f;
+    if (p.page < 0) continue;
+    const RowsView& src = is_v ? v : k;
+    load8<T, VEC, (U > 1)>(static_cast<const T*>(src.data) + (sh.tok0 + t) * src.ts + head * src.hs + i * kN, x[u]);
     int64_t co, so;
-    kv_offsets<FMT, D>(kv, head, is_v, row, i, &co, &so);
-    const uint8_t* base = kv.pool + page * kv.page_bytes;
-    if constexpr (FMT == MEM_KV_BF16) {
-      load8<uint16_t, true>(reinterpret_cast<const uint16_t*>(base + co), x);
-    } else {
-      const uint32_t byte = base[so];
-      const float s = kv_scale(byte);
-      f32x2 p[4];
-      if constexpr (FMT == MEM_KV_FP4) {
-        const uint32_t c = *reinterpret_cast<const uint32_t*>(base + co);
-        p[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 0);
-        p[1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 1);
-        p[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 2);
-        p[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 3);
-      } else {
-        const u32x2_t c = *reinterpret_cast<const u32x2_t*>(base + co);
-        for (int w = 0; w < 2; ++w) {
-          p[2 * w] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c[w], s, false);
-          p[2 * w + 1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c[w], s, true);
-        }
-      }
-      for (int j = 0; j < 4; ++j) {
-        x[2 * j] = byte == 255u ? __uint_as_float(0x7FC00000u) : p[j][0];
-        x[2 * j + 1] = byte == 255u ? __uint_as_float(0x7FC00000u) : p[j][1];
-      }
+    kv_offsets<FMT, D, kN>(kv, head, is_v, p.row, i, &co, &so);
+    uint8_t* base = kv.pool + p.page * kv.page_bytes;
+    codes[u] = base + co;
+    scales[u] = base + so;
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+    encode_item<FMT>(x[u], codes[u], scales[u], threadIdx.x % 4 == 0, codes[u] != nullptr);
+}
+
+// N elements (4 or 8) of a block from their codes.
+template <int FMT, int N>
+__device__ __forceinline__ void decode_item(const uint32_t* c, uint32_t byte, float* x) {
+  const float s = kv_scale(byte);
+  f32x2 p[N / 2];
+  if constexpr (FMT == MEM_KV_FP4) {
+    p[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[0], s, 0);
+    p[1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[0], s, 1);
+    if constexpr (N == 8) {
+      p[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[0], s, 2);
+      p[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[0], s, 3);
+    }
+  } else {
+    for (int w = 0; w < N / 4; ++w) {
+      p[2 * w] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c[w], s, false);
+      p[2 * w + 1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c[w], s, true);
     }
   }
-  const RowsView& dst = is_v ? v : k;
-  store8<T, VEC>(static_cast<T*>(dst.data) + tok * dst.ts + head * dst.hs + i * kPiece, x);
+  for (int j = 0; j < N / 2; ++j) {
+    x[2 * j] = byte == 255u ? __uint_as_float(0x7FC00000u) : p[j][0];
+    x[2 * j + 1] = byte == 255u ? __uint_as_float(0x7FC00000u) : p[j][1];
+  }
+}
+
+template <int FMT, int D, typename T, bool VEC, int U>
+__global__ __launch_bounds__(kThreads) void kv_read_kernel(KvView kv, RowsView k, RowsView v,
+                                                           const int32_t* __restrict__ chunk,
+                                                           const int32_t* __restrict__ pos, int64_t n,
+                                                           int per_token, uint64_t magic) {
+  constexpr int kN = kItem<false, T>, kPieces = D / kN;
+  constexpr int kBytes = kN * kv_row_bytes(FMT, D) / D, kWords = (kBytes + 3) / 4;  // of an item's codes
+  __shared__ Place places[kMaxTokens];
+  const Share sh = open_share(kv, per_token, magic, kThreads * U, chunk, pos, n, places);
+  uint32_t c[U][kWords], byte[U];
+  T* dst[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    int item;
+    const int t = sh.token(sh.skip + threadIdx.x + u * kThreads, &item);
+    const int i = item % kPieces, hv = item / kPieces;
+    const bool is_v = hv >= kv.heads;
+    const int head = is_v ? hv - kv.heads : hv;
+    const Place p = places[t];
+    const RowsView& to = is_v ? v : k;
+    const int64_t tok = sh.tok0 + t;
+    dst[u] = tok < n ? static_cast<T*>(to.data) + tok * to.ts + head * to.hs + i * kN : nullptr;
+    byte[u] = 127;
+    for (int w = 0; w < kWords; ++w) c[u][w] = 0;
+    if (p.page < 0) continue;  // reads as zeros
+    int64_t co, so;
+    kv_offsets<FMT, D, kN>(kv, head, is_v, p.row, i, &co, &so);
+    const uint8_t* base = kv.pool + p.page * kv.page_bytes;
+    const uint32_t* src = reinterpret_cast<const uint32_t*>(base + co);
+    if constexpr (kWords == 4) {
+      const u32x4_t w = *reinterpret_cast<const u32x4_t*>(src);
+      for (int j = 0; j < 4; ++j) c[u][j] = w[j];
+    } else if constexpr (kWords == 2) {
+      const u32x2_t w = *reinterpret_cast<const u32x2_t*>(src);
+      c[u][0] = w[0];
+      c[u][1] = w[1];
+    } else if constexpr (kBytes == 4) {
+      c[u][0] = *src;
+    } else {
+      c[u][0] = *reinterpret_cast<const uint16_t*>(src);
+    }
+    if constexpr (FMT != MEM_KV_BF16) byte[u] = base[so];
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    if (!dst[u]) continue;
+    float x[kN];
+    if constexpr (FMT == MEM_KV_BF16) {
+      for (int j = 0; j < kN / 2; ++j) {
+        x[2 * j] = __uint_as_float(c[u][j] << 16);
+        x[2 * j + 1] = __uint_as_float(c[u][j] & 0xFFFF0000u);
+      }
+    } else {
+      decode_item<FMT, kN>(c[u], byte[u], x);
+    }
+    store_item<T, VEC, (U > 1)>(dst[u], x);
+  }
 }
 
 // 16-byte accesses of the dense rows need aligned rows.
@@ -197,21 +302,22 @@ bool rows_aligned(const RowsView& r, int elem) {
 template <bool WRITE, int FMT, int D, typename T>
 hipError_t launch_typed(const KvView& kv, const RowsView& k, const RowsView& v, const int32_t* chunk,
                         const int32_t* pos, int64_t n, hipStream_t stream) {
-  const int64_t threads = n * 2 * kv.heads * (D / kPiece);
-  const dim3 grid(static_cast<unsigned>((threads + kThreads - 1) / kThreads));
   const bool vec = rows_aligned(k, sizeof(T)) && rows_aligned(v, sizeof(T));
-  if (WRITE) {
-    if (vec)
-      kv_write_kernel<FMT, D, T, true><<<grid, kThreads, 0, stream>>>(kv, k, v, chunk, pos, n);
-    else
-      kv_write_kernel<FMT, D, T, false><<<grid, kThreads, 0, stream>>>(kv, k, v, chunk, pos, n);
-  } else {
-    if (vec)
-      kv_read_kernel<FMT, D, T, true><<<grid, kThreads, 0, stream>>>(kv, k, v, chunk, pos, n);
-    else
-      kv_read_kernel<FMT, D, T, false><<<grid, kThreads, 0, stream>>>(kv, k, v, chunk, pos, n);
-  }
-  return hipGetLastError();
+  const int per_token = 2 * kv.heads * (D / kItem<WRITE, T>);
+  const uint64_t magic = ((uint64_t{1} << 40) + per_token - 1) / per_token;
+  const int64_t items = n * per_token;
+  // one item per thread until that alone fills the GPU (256 CUs of 2,048 threads)
+  const int u = items >= int64_t{256} * 2048 * kInFlight ? kInFlight : 1;
+  const dim3 grid(static_cast<unsigned>((items + kThreads * u - 1) / (kThreads * u)));
+  auto go = [&](auto write, auto read) {
+    (WRITE ? write : read)<<<grid, kThreads, 0, stream>>>(kv, k, v, chunk, pos, n, per_token, magic);
+    return hipGetLastError();
+  };
+  if (u == 1)
+    return vec ? go(kv_write_kernel<FMT, D, T, true, 1>, kv_read_kernel<FMT, D, T, true, 1>)
+               : go(kv_write_kernel<FMT, D, T, false, 1>, kv_read_kernel<FMT, D, T, false, 1>);
+  return vec ? go(kv_write_kernel<FMT, D, T, true, kInFlight>, kv_read_kernel<FMT, D, T, true, kInFlight>)
+             : go(kv_write_kernel<FMT, D, T, false, kInFlight>, kv_read_kernel<FMT, D, T, false, kInFlight>);
 }
 
 template <bool WRITE, int FMT, int D>

@@ -125,6 +125,29 @@ def test_round_trip_over_a_shuffled_directory(name, heads, d, page_tokens, ppc, 
         assert np.array_equal(host(t), want[back])
 
 
+@pytest.mark.parametrize("name,heads,d,n", [("fp4", 3, 64, 44001), ("fp8", 8, 128, 8195), ("bf16", 1, 256, 33003)])
+def test_large_calls(name, heads, d, n):
+    # enough items that threads take several each, an odd number of them per token
+    fmt, T = FMTS[name], 64
+    pool, table = new_cache(fmt, -(-n // 128), 2, T, heads, d)
+    cache = pm.KvCache(up(pool), up(table), T, heads, d, fmt)
+    at = np.random.default_rng(n).permutation(len(table) * 128)[:n]
+    chunk, pos = (at // 128).astype(np.int32), (at % 128).astype(np.int32)
+    chunk[::1000] = -1
+    ok = chunk >= 0
+    k = torch.randn((n, heads, d), device="cuda")
+    v = torch.randn((n, heads, d), device="cuda")
+    pm.mem_kv_write(cache, k, v, up(chunk), up(pos))
+    page, row = table[chunk[ok], pos[ok] // T], pos[ok] % T
+    ref.put(fmt, T, pool, page, row, host(k)[ok], host(v)[ok])
+    assert np.array_equal(cache.pool.cpu().numpy(), pool)
+    want = ref.get(fmt, T, heads, d, pool, page, row)
+    for dtype in (torch.float32, torch.bfloat16):
+        for t, w in zip(pm.mem_kv_read(cache, up(chunk), up(pos), dtype=dtype), want):
+            got = host(t)
+            assert np.array_equal(got[ok], w) and (got[~ok] == 0).all()
+
+
 @pytest.mark.parametrize("name,dtype", itertools.product(FMTS, [torch.float32, torch.bfloat16]))
 def test_rows_with_odd_strides(name, dtype):
     # rows that 16-byte accesses cannot reach, head-major input and a broadcast head
