@@ -103,7 +103,7 @@ __device__ __forceinline__ bool find_tile(const AttendArgs& a, int64_t t, int gr
   const int64_t r0 = t * R, rows = static_cast<int64_t>(out->nq) * group;
   if (t < 0 || r0 >= rows) return false;
   out->r0 = static_cast<int>(r0);
-  out->rows = static_cast<int>(min(static_cast<int64_t>(R), rows - r0));
+  out->rows = __builtin_amdgcn_readfirstlane(static_cast<int>(min(static_cast<int64_t>(R), rows - r0)));
   return true;
 }
 
@@ -204,7 +204,7 @@ __device__ __forceinline__ Span visible_units(const ChunkList& L, int prefix, in
 // What a row of the tile may see and how it is biased.
 struct RowRule {
   int64_t pos;   // its position
-  int lo, hi;    // visible positions besides the prefix
+  int lo, hi;    // visible positions besides the prefix (clamped to -1 .. kFar)
   int ns;        // its document (negative: none)
   float slope;   // log2(e) times the head's slope
 };
@@ -214,7 +214,7 @@ __device__ __forceinline__ RowRule row_rule(const AttendArgs& a, const Tile& t, 
   const int j = r / group, h = g * group + r % group;
   const int64_t at = t.q0 + j;
   x.pos = a.q_pos ? a.q_pos[at] : static_cast<int64_t>(ctx) - t.nq + j;
-  x.hi = a.causal ? static_cast<int>(min(x.pos, static_cast<int64_t>(kFar))) : kFar;
+  x.hi = a.causal ? static_cast<int>(min(max(x.pos, int64_t{-1}), static_cast<int64_t>(kFar))) : kFar;
   x.lo = a.window ? static_cast<int>(min(max(x.pos - a.window + 1, int64_t{0}), static_cast<int64_t>(kFar))) : 0;
   x.ns = a.chunk_ns ? a.query_ns[at] : 0;
   x.slope = a.slopes ? a.slopes[h] * kLog2e : 0.f;
@@ -262,6 +262,13 @@ __device__ __forceinline__ TileRule tile_rule(const AttendArgs& a, const Tile& t
       x.ns_hi = max(x.ns_hi, __shfl_xor(x.ns_hi, off));
     }
   }
+  // the same in every lane: scalar registers, and branches that the whole wave takes
+  x.lo = __builtin_amdgcn_readfirstlane(x.lo);
+  x.hi = __builtin_amdgcn_readfirstlane(x.hi);
+  x.lo_all = __builtin_amdgcn_readfirstlane(x.lo_all);
+  x.hi_all = __builtin_amdgcn_readfirstlane(x.hi_all);
+  x.ns_lo = __builtin_amdgcn_readfirstlane(x.ns_lo);
+  x.ns_hi = __builtin_amdgcn_readfirstlane(x.ns_hi);
   x.mixed = __any(none) || x.ns_lo != x.ns_hi;
   return x;
 }
@@ -308,7 +315,7 @@ __device__ __forceinline__ int resolve_units(const AttendArgs& a, const ChunkLis
     if ((x[j].where >> 16) > 0)
       list[at[j] + __builtin_popcountll(kept[j] & ((uint64_t{1} << lane) - 1))] = x[j];
   __syncthreads();
-  return total;
+  return __builtin_amdgcn_readfirstlane(total);
 }
 
 // A unit of the list in scalar registers.
@@ -473,56 +480,69 @@ __device__ constexpr int score_token(int j) {
   return WIDTH == 16 ? 16 * (j >> 2) + (j & 3) : 8 * (j >> 2) + (j & 3);
 }
 
-// How raw products become scores in the log2 domain.
+// How raw products become scores in the log2 domain: scaled, capped, biased.  The cap's tanh is
+// 1 - 2 / (1 + e^2x), with two transcendental operations of twice to three times a product's cost; where no score of a
+// wave's unit is above kSmall of the cap, its series to x^7 does as well (the next term is below 4e-8 of it).
 struct Scores {
-  float c;      // scale * log2(e)
-  float x;      // scale / softcap
-  float cap2;   // softcap * log2(e); 0: none
+  float c;     // scale * log2(e)
+  float k2;    // 2 * log2(e) * scale / softcap
+  float cap2;  // softcap * log2(e); 0: none
+  float limit; // raw products up to this magnitude are small
+  float s1, s3, s5, s7;  // the series in raw products
   bool bias;
   bool causal;
 
+  static constexpr float kSmall = 0.1875f;
+
   __device__ __forceinline__ explicit Scores(const AttendArgs& a)
-      : c(a.scale * kLog2e), x(a.softcap > 0.f ? a.scale / a.softcap : 0.f), cap2(a.softcap * kLog2e),
-        bias(a.slopes != nullptr), causal(a.causal != 0) {}
+      : c(a.scale * kLog2e), cap2(a.softcap * kLog2e), bias(a.slopes != nullptr), causal(a.causal != 0) {
+    const float x = a.softcap > 0.f ? a.scale / a.softcap : 0.f;
+    k2 = 2.f * kLog2e * x;
+    // (coefficients of a tiny x would lose bits as denormals)
+    limit = x > 1e-4f ? kSmall / x : -1.f;
+    s1 = cap2 * x;
+    s3 = cap2 * x * x * x * (-1.f / 3.f);
+    s5 = cap2 * x * x * x * x * x * (2.f / 15.f);
+    s7 = cap2 * x * x * x * x * x * x * x * (-17.f / 315.f);
+  }
 
-  // What scores still have to be multiplied by after `apply`: without cap and bias that waits for the exponential.
-  __device__ __forceinline__ float factor() const { return cap2 == 0.f && !bias ? c : 1.f; }
+  __device__ __forceinline__ float series(float s) const {  // capped score / s
+    const float t = s * s;
+    return s1 + t * (s3 + t * (s5 + t * s7));
+  }
+  __device__ __forceinline__ float fraction(float s) const { return __builtin_amdgcn_rcpf(1.f + fast_exp2(s * k2)); }
 
-  // tanh is 1 - 2 / (1 + e^2x), two transcendental operations of four times a product's cost each; where no score of
-  // the wave's unit is above a quarter of the cap its series to x^9 does as well (the next term is below 1e-8 of it).
+  template <int N>
+  __device__ __forceinline__ bool small(const float (&s)[N]) const {
+    float top = 0.f;
+#pragma unroll
+    for (int j = 0; j < N; ++j) top = fmaxf(top, fabsf(s[j]));
+    return !__any(top > limit);
+  }
+
+  // Scores of one unit made explicit: what masks and biases need.
   template <int WIDTH, int N>
   __device__ __forceinline__ void apply(float (&s)[N], const RowRule& rule, const TileRule& tr, int pos, int part) const {
     if (cap2 != 0.f) {
-      float top = 0.f;
 #pragma unroll
-      for (int j = 0; j < N; ++j) top = fmaxf(top, fabsf(s[j]));
-      if (__any(top * x > 0.25f)) {
-        const float k2 = 2.f * x * kLog2e;
-#pragma unroll
-        for (int j = 0; j < N; ++j) s[j] = cap2 - 2.f * cap2 * __builtin_amdgcn_rcpf(1.f + fast_exp2(s[j] * k2));
-      } else {
-        const float c3 = cap2 * (-1.f / 3.f), c5 = cap2 * (2.f / 15.f), c7 = cap2 * (-17.f / 315.f),
-                    c9 = cap2 * (62.f / 2835.f);
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-          const float t = s[j] * x, t2 = t * t;
-          s[j] = t * (cap2 + t2 * (c3 + t2 * (c5 + t2 * (c7 + t2 * c9))));
-        }
-      }
+      for (int j = 0; j < N; ++j) s[j] = cap2 - 2.f * cap2 * fraction(s[j]);
     }
-    if (bias) {
-      const float f = cap2 == 0.f ? c : 1.f;
-      const float dist = static_cast<float>(rule.pos - pos - 4 * part);
-      if (causal && pos + kUnit - 1 <= tr.hi_all) {  // every token lies behind every row
-        const float near = -rule.slope * dist;
+    const float f = cap2 == 0.f ? c : 1.f;
+    if (!bias) {
 #pragma unroll
-        for (int j = 0; j < N; ++j)
-          s[j] = fmaf(s[j], f, fmaf(rule.slope, static_cast<float>(score_token<WIDTH>(j)), near));
-      } else {
+      for (int j = 0; j < N; ++j) s[j] *= f;
+      return;
+    }
+    const float dist = static_cast<float>(rule.pos - pos - 4 * part);
+    if (causal && pos + kUnit - 1 <= tr.hi_all) {  // every token lies behind every row
+      const float near = -rule.slope * dist;
 #pragma unroll
-        for (int j = 0; j < N; ++j)
-          s[j] = s[j] * f - rule.slope * fabsf(dist - static_cast<float>(score_token<WIDTH>(j)));
-      }
+      for (int j = 0; j < N; ++j)
+        s[j] = fmaf(s[j], f, fmaf(rule.slope, static_cast<float>(score_token<WIDTH>(j)), near));
+    } else {
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        s[j] = s[j] * f - rule.slope * fabsf(dist - static_cast<float>(score_token<WIDTH>(j)));
     }
   }
 };
@@ -530,12 +550,14 @@ struct Scores {
 // Masks of one unit's scores, looked at one by one.  Returns the scores that are seen as bits.
 template <int WIDTH, int N>
 __device__ __forceinline__ uint32_t mask_scores(float (&s)[N], const RowRule& rule, const Unit& u, int prefix, int part) {
-  const int held = u.where >> 16;
+  const int first = u.pos + 4 * part;  // position of a score whose token offset is 0
+  const int held = (u.where >> 16) - 4 * part, pre = prefix - first, lo = rule.lo - first, hi = rule.hi - first;
+  const bool mine = u.ns == rule.ns;
   uint32_t seen = 0;
 #pragma unroll
   for (int j = 0; j < N; ++j) {
-    const int tok = score_token<WIDTH>(j) + 4 * part, p = u.pos + tok;
-    const bool see = tok < held && (p < prefix || (p >= rule.lo && p <= rule.hi)) && u.ns == rule.ns;
+    const int tok = score_token<WIDTH>(j);
+    const bool see = mine && tok < held && (tok < pre || (tok >= lo && tok <= hi));
     seen |= see ? 1u << j : 0u;
     s[j] = see ? s[j] : -INFINITY;
   }
@@ -545,10 +567,11 @@ __device__ __forceinline__ uint32_t mask_scores(float (&s)[N], const RowRule& ru
 // Whether a seen score's token is among the unit's tokens with values that are not finite.
 template <int WIDTH, int N>
 __device__ __forceinline__ bool sees_bad(uint32_t seen, uint32_t bad, int part) {
-  bool hit = false;
+  bad >>= 4 * part;
+  uint32_t hit = 0;
 #pragma unroll
-  for (int j = 0; j < N; ++j) hit |= ((seen >> j) & 1u) && ((bad >> (score_token<WIDTH>(j) + 4 * part)) & 1u);
-  return hit;
+  for (int j = 0; j < N; ++j) hit |= (seen >> j) & (bad >> score_token<WIDTH>(j)) & 1u;
+  return hit != 0;
 }
 
 // Running softmax of a row, in every lane that holds its scores: maximum (it may lag by kLag: weights up to 2^kLag
@@ -600,14 +623,21 @@ struct Rows {
   }
 };
 
-// The scores of one row (N in this lane) into weights: updates the running state and the output's scale.  Returns
-// false if none of the wave's scores weighs anything.
+// The scores of one row (N in this lane) into weights: updates the running state and the output's scale.  With
+// `ready` the scores are in the log2 domain, else they are raw products, unmasked and without a bias, whose scale or
+// cap goes into the exponential's argument.  Returns false if none of the wave's scores weighs anything.
 template <int WIDTH, int D, int N>
-__device__ __forceinline__ bool soften(float (&s)[N], float f, RowState& st, Rows<WIDTH, D>& rows, bool* heavy) {
+__device__ __forceinline__ bool soften(float (&s)[N], const Scores& sc, bool ready, RowState& st, Rows<WIDTH, D>& rows,
+                                       bool* heavy) {
+  const bool capped = !ready && sc.cap2 != 0.f;
+  const bool series = capped && sc.small(s);
+  const float f = ready ? 1.f : sc.c;
   float top = s[0];
 #pragma unroll
   for (int j = 1; j < N; ++j) top = nan_max(top, s[j]);
-  top = max_column<WIDTH>(top) * f;
+  top = max_column<WIDTH>(top);
+  // (both forms of the cap grow with the product, so the largest product has the largest score)
+  top = !capped ? top * f : series ? top * sc.series(top) : sc.cap2 - 2.f * sc.cap2 * sc.fraction(top);
   if (!__any(!(top <= st.m - kNothing))) return false;
   if (__any(top > st.m + kLag)) {
     const float mn = fmaxf(st.m, top);
@@ -617,11 +647,19 @@ __device__ __forceinline__ bool soften(float (&s)[N], float f, RowState& st, Row
     st.m = mn;
   }
   const float ref = finite_max(st.m);
+  if (!capped) {
 #pragma unroll
-  for (int j = 0; j < N; ++j) {
-    s[j] = fast_exp2(fmaf(s[j], f, -ref));
-    st.l += s[j];
+    for (int j = 0; j < N; ++j) s[j] = fast_exp2(fmaf(s[j], f, -ref));
+  } else if (series) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) s[j] = fast_exp2(fmaf(s[j], sc.series(s[j]), -ref));
+  } else {
+    const float base = sc.cap2 - ref, g = -2.f * sc.cap2;
+#pragma unroll
+    for (int j = 0; j < N; ++j) s[j] = fast_exp2(fmaf(sc.fraction(s[j]), g, base));
   }
+#pragma unroll
+  for (int j = 0; j < N; ++j) st.l += s[j];
   *heavy = __any(fast_exp2(top - ref) * kHeavy > st.l);
   return true;
 }
@@ -666,31 +704,78 @@ __device__ __forceinline__ void load_queries(const uint16_t* src, int stride, bf
   }
 }
 
-// O^T += V^T P^T for the 32 tokens whose values lie in LDS rows at `v`, with the weights of the lane's row.
-template <int WIDTH, int D, int PITCH>
-__device__ __forceinline__ void add_values(Rows<WIDTH, D>& rows, const uint16_t* v, const u32x4_t* w, int lane) {
-  const int i = lane & 15;
-  if constexpr (WIDTH == 16) {
-    const uint16_t* src = v + (4 * (lane >> 4) + (i >> 2)) * PITCH + (i & 3) * 4;
+// Values in LDS: bf16 rows whose pitch puts the four (WIDTH 32) or eight (16) rows that a transposing read takes
+// together on different banks; the 16-byte chunks of a row are exchanged within the 64 (32) bytes that such a read
+// takes of it, by the row's number shifted right by SHIFT, so that the writes meet different banks too.
+template <int WIDTH, int D>
+constexpr int kValuePitch = D + WIDTH;
+template <int WIDTH, int SHIFT>
+__device__ __forceinline__ int value_chunk(int row, int chunk) {
+  return chunk ^ ((row >> SHIFT) & (WIDTH == 32 ? 3 : 1));
+}
+
+// Transposed operands of the values of 32 tokens in LDS rows at `v`, for the output columns 128 half .. + 127 (or all
+// of fewer): loaded together, ahead of the products that use them, so that those do not wait for each.
+template <int WIDTH, int D>
+struct ValueOps {
+  static constexpr int kCols = D < 128 ? D : 128;
+  static constexpr int kOps = kCols / WIDTH * (WIDTH == 16 ? 1 : 2);
+  bf16x8 v[kOps];
+
+  template <int SHIFT>
+  __device__ __forceinline__ void load(const uint16_t* rows, int half, int lane) {
+    constexpr int P = kValuePitch<WIDTH, D>;
+    static_assert(WIDTH != 16 || SHIFT <= 3, "rows 16 apart have the same exchange");
+    const int i = lane & 15;
+    rows += half * kCols;
+    if constexpr (WIDTH == 16) {
+      const int r = 4 * (lane >> 4) + (i >> 2);  // rows r and r + 16, columns 16 n + 4 (i & 3)
+      const uint16_t* src = rows + r * P + 8 * value_chunk<16, SHIFT>(r, (i & 3) >> 1) + 4 * (i & 1);
 #pragma unroll
-    for (int n = 0; n < D / 16; ++n) {
-      const u32x2_t v0 = lds_transpose4(src + 16 * n);
-      const u32x2_t v1 = lds_transpose4(src + 16 * PITCH + 16 * n);
-      rows.o[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(u32x4_t{v0[0], v0[1], v1[0], v1[1]}),
-                                                          as_bf16x8(w[0]), rows.o[n], 0, 0, 0);
+      for (int n = 0; n < kOps; ++n) v[n] = pair(src + 16 * n, src + 16 * P + 16 * n);
+    } else {
+      // rows r + 8 y, columns 32 n + 16 (lane >> 4 & 1) + 4 (i & 3)
+      const int r = 4 * (lane >> 5) + (i >> 2), c = 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
+      const uint16_t* src[4];
+#pragma unroll
+      for (int y = 0; y < 4; ++y)
+        src[y] = rows + (r + 8 * y) * P + 8 * value_chunk<32, SHIFT>(r + 8 * y, c) + 4 * (i & 1);
+#pragma unroll
+      for (int n = 0; n < kOps; ++n) v[n] = pair(src[2 * (n & 1)] + 32 * (n >> 1), src[2 * (n & 1) + 1] + 32 * (n >> 1));
     }
-  } else {
-    const uint16_t* src = v + (4 * (lane >> 5) + (i >> 2)) * PITCH + ((lane >> 4) & 1) * 16 + (i & 3) * 4;
-#pragma unroll
-    for (int n = 0; n < D / 32; ++n)
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const u32x2_t v0 = lds_transpose4(src + 16 * x * PITCH + 32 * n);
-        const u32x2_t v1 = lds_transpose4(src + (16 * x + 8) * PITCH + 32 * n);
-        rows.o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(u32x4_t{v0[0], v0[1], v1[0], v1[1]}),
-                                                            as_bf16x8(w[x]), rows.o[n], 0, 0, 0);
-      }
   }
+  // O^T += V^T P^T with the weights of the lane's row.
+  __device__ __forceinline__ void multiply(Rows<WIDTH, D>& out, int half, const u32x4_t* w) const {
+#pragma unroll
+    for (int n = 0; n < kOps; ++n) {
+      if constexpr (WIDTH == 16) {
+        auto& o = out.o[half * kOps + n];
+        o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[n], as_bf16x8(w[0]), o, 0, 0, 0);
+      } else {
+        auto& o = out.o[half * (kOps / 2) + (n >> 1)];
+        o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[n], as_bf16x8(w[n & 1]), o, 0, 0, 0);
+      }
+    }
+  }
+
+ private:
+  static __device__ __forceinline__ bf16x8 pair(const uint16_t* p0, const uint16_t* p1) {
+    const u32x2_t v0 = lds_transpose4(p0), v1 = lds_transpose4(p1);
+    return as_bf16x8(u32x4_t{v0[0], v0[1], v1[0], v1[1]});
+  }
+};
+
+// Loads written before this stay before it, and what uses them behind.
+__device__ __forceinline__ void issue_first() { __builtin_amdgcn_sched_barrier(0); }
+
+// Unpack a quarter row of values into its LDS row.
+template <int WIDTH, int SHIFT, int FMT, int D>
+__device__ __forceinline__ void store_values(const Piece<FMT, D>& p, uint16_t* v, int row, int quarter) {
+  uint16_t* dst = v + row * kValuePitch<WIDTH, D>;
+#pragma unroll
+  for (int y = 0; y < Dim<FMT, D>::kSteps; ++y)
+    *reinterpret_cast<u32x4_t*>(dst + 8 * value_chunk<WIDTH, SHIFT>(row, quarter * Dim<FMT, D>::kSteps + y)) =
+        piece_step<FMT, D>(p, y);
 }
 
 // N weights as operands of the second product, and what their rounding left.
@@ -700,9 +785,9 @@ __device__ __forceinline__ void pack_weights(const float (&s)[N], u32x4_t (&w)[N
   for (int j = 0; j < N / 2; ++j) w[j >> 2][j & 3] = pack2(s[2 * j], s[2 * j + 1]);
 }
 template <int N>
-__device__ __forceinline__ void pack_rests(const float (&s)[N], u32x4_t (&w)[N / 8]) {
+__device__ __forceinline__ void pack_rests(const float (&s)[N], const u32x4_t (&w)[N / 8], u32x4_t (&rest)[N / 8]) {
 #pragma unroll
-  for (int j = 0; j < N / 2; ++j) w[j >> 2][j & 3] = rest2(s[2 * j], s[2 * j + 1], w[j >> 2][j & 3]);
+  for (int j = 0; j < N / 2; ++j) rest[j >> 2][j & 3] = rest2(s[2 * j], s[2 * j + 1], w[j >> 2][j & 3]);
 }
 
 // ---------------------------------------------------------------- few rows
@@ -710,8 +795,8 @@ __device__ __forceinline__ void pack_rests(const float (&s)[N], u32x4_t (&w)[N /
 template <int FMT, int D, int R>
 struct FewShape {
   static constexpr int kBatch = 512;                        // units resolved at a time
-  static constexpr int kPitch = D + 16;                     // bf16 elements between LDS rows
-  static constexpr int kWaveBytes = kUnit * kPitch * 2;     // a wave's unpacked values
+  static constexpr int kShift = R == 16 ? 3 : 2;            // exchange of chunks: a wave writes 16 rows at a time
+  static constexpr int kWaveBytes = kUnit * kValuePitch<R, D> * 2;  // a wave's unpacked values
   static constexpr int kJoinBytes = 2 * R * D * 4;          // two waves' outputs at the end
   static constexpr int kArea = kWaves * kWaveBytes > kJoinBytes ? kWaves * kWaveBytes : kJoinBytes;
 };
@@ -732,7 +817,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_few_kernel(
   __shared__ RowState joint[2][64];
   __shared__ int joint_poison[2][64];
 
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane % R, part = lane / R;
   const int heads = a.kv.heads, group = a.hq / heads;
   int64_t b = blockIdx.x;
@@ -743,12 +828,12 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_few_kernel(
   if (!find_tile<R>(a, b / splits, group, &t)) return;
   const ChunkList L = scan_list(a, t.req, dyn, tmp);
   const int ctx = L.tb[a.k];
-  const int prefix = a.prefix_len ? a.prefix_len[t.req] : 0;
+  const int prefix = a.prefix_len ? __builtin_amdgcn_readfirstlane(min(max(a.prefix_len[t.req], 0), kFar)) : 0;
   const int my_row = t.r0 + min(col, t.rows - 1);
   const RowRule rule = row_rule(a, t, ctx, g, group, my_row);
   const TileRule tr = tile_rule<R>(a, t, ctx, g, group);
   const Span span = visible_units(L, prefix, tr.lo, tr.hi);
-  const int n_units = span.count();
+  const int n_units = __builtin_amdgcn_readfirstlane(span.count());
   const int u0 = static_cast<int>(static_cast<int64_t>(n_units) * split / splits);
   const int u1 = static_cast<int>(static_cast<int64_t>(n_units) * (split + 1) / splits);
 
@@ -819,8 +904,9 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_few_kernel(
         for (int j = 0; j < 16; ++j) s[j] = x[j];
       }
       if (more) load(pk, next, false);
-      scores.template apply<R>(s, rule, tr, u.pos, part);
-      if (held < kUnit || !tr.all_see(u.pos, prefix)) {
+      const bool masked = held < kUnit || !tr.all_see(u.pos, prefix);
+      if (masked || scores.bias) scores.template apply<R>(s, rule, tr, u.pos, part);
+      if (masked) {
         const uint32_t seen = mask_scores<R>(s, rule, u, prefix, part);
         uint32_t bad = 0;
 #pragma unroll
@@ -836,24 +922,29 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_few_kernel(
         if (bad) poison |= sees_bad<R, kScores>(seen, bad, part);
       }
       bool heavy;
-      const bool counts = soften<R, D>(s, scores.factor(), st, rows, &heavy);
+      const bool counts = soften<R, D>(s, scores, masked || scores.bias, st, rows, &heavy);
       if (counts) {  // values: unpack into the wave's LDS rows, to be read back transposed
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint16_t* dst = vrows + (h * row_step + col) * S::kPitch + (quarter + h * quarter_step) * K::kElems;
-#pragma unroll
-          for (int y = 0; y < K::kSteps; ++y) *reinterpret_cast<u32x4_t*>(dst + 8 * y) = piece_step<FMT, D>(pv[h], y);
-        }
+        for (int h = 0; h < 2; ++h)
+          store_values<R, S::kShift>(pv[h], vrows, h * row_step + col, quarter + h * quarter_step);
       }
       if (more) load(pv, next, true);
       if (counts) {
-        u32x4_t w[kScores / 8];
-        pack_weights(s, w);
         __builtin_amdgcn_wave_barrier();
-        add_values<R, D, S::kPitch>(rows, vrows, w, lane);
-        if (heavy) {
-          pack_rests(s, w);
-          add_values<R, D, S::kPitch>(rows, vrows, w, lane);
+        u32x4_t w[kScores / 8], rest[kScores / 8];
+        ValueOps<R, D> ops;
+        ops.template load<S::kShift>(vrows, 0, lane);
+        issue_first();
+        pack_weights(s, w);
+        if (heavy) pack_rests(s, w, rest);
+#pragma unroll
+        for (int x = 0; x < D / ValueOps<R, D>::kCols; ++x) {
+          if (x > 0) {
+            ops.template load<S::kShift>(vrows, x, lane);
+            issue_first();
+          }
+          ops.multiply(rows, x, w);
+          if (heavy) ops.multiply(rows, x, rest);
         }
         __builtin_amdgcn_wave_barrier();
       }
@@ -952,10 +1043,12 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a, int
 template <int FMT, int D>
 struct TileShape {
   static constexpr int kBatch = 256;                          // units resolved at a time
-  static constexpr int kStepUnits = D == 256 ? 1 : 2;         // units per step
+  static constexpr int kStepUnits = D == 64 ? 2 : 1;          // units per step
   static constexpr int kTokens = kStepUnits * kUnit;
-  static constexpr int kPitch = D + 8;                        // bf16 elements between LDS rows
-  static constexpr int kPart = kTokens * kPitch;              // elements of a step's keys or values
+  static constexpr int kKeyPitch = D + 8;                     // bf16 elements between LDS rows of keys
+  static constexpr int kKeys = kTokens * kKeyPitch;           // elements of a step's keys
+  static constexpr int kValues = kTokens * kValuePitch<32, D>;
+  static constexpr int kShift = 0;                            // exchange of chunks: a wave writes 4 rows at a time
   static constexpr int kPieces = 2 * kTokens * 4 / kThreads;  // quarter rows per thread and step, keys then values
 };
 
@@ -968,12 +1061,12 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile_kernel
   using S = TileShape<FMT, D>;
   constexpr int kQSteps = D / 16, kUnits = S::kStepUnits;
   extern __shared__ int dyn[];  // the chunk list: cid[k], ub[k + 1], tb[k + 1]
-  __shared__ __align__(16) uint16_t area[2][2 * S::kPart];
+  __shared__ __align__(16) uint16_t area[2][S::kKeys + S::kValues];
   __shared__ Unit list[S::kBatch + 1];
   __shared__ int tmp[2 * kWaves];
   __shared__ uint32_t bad_tok[3][2];  // tokens whose values are not finite: of this step, the next and the one after
 
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 31, half = lane >> 5;
   const int heads = a.kv.heads, group = a.hq / heads;
   int64_t b = blockIdx.x;
@@ -984,13 +1077,13 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile_kernel
   if (!find_tile<kTileRows>(a, tiles - 1 - b / splits, group, &t)) return;  // the latest rows see most: first
   const ChunkList L = scan_list(a, t.req, dyn, tmp);
   const int ctx = L.tb[a.k];
-  const int prefix = a.prefix_len ? a.prefix_len[t.req] : 0;
+  const int prefix = a.prefix_len ? __builtin_amdgcn_readfirstlane(min(max(a.prefix_len[t.req], 0), kFar)) : 0;
   const int my_row = t.r0 + min(32 * wave + col, t.rows - 1);
   const bool works = 32 * wave < t.rows;  // this wave has rows
   const RowRule rule = row_rule(a, t, ctx, g, group, my_row);
   const TileRule tr = tile_rule<kTileRows>(a, t, ctx, g, group);
   const Span span = visible_units(L, prefix, tr.lo, tr.hi);
-  const int n_units = span.count();
+  const int n_units = __builtin_amdgcn_readfirstlane(span.count());
   const int u0 = static_cast<int>(static_cast<int64_t>(n_units) * split / splits);
   const int u1 = static_cast<int>(static_cast<int64_t>(n_units) * (split + 1) / splits);
 
@@ -1015,22 +1108,31 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile_kernel
     if (tid == 0) list[n] = Unit{0, 0, 0, -1};  // fills up the last step: holds nothing
     __syncthreads();
     Piece<FMT, D> piece[S::kPieces];
-    // Quarter row x of this thread: x = tid + 256 i; the first half of a step's are keys.
+    // Quarter row i of this thread: of the step's keys, then of its values.
+    struct Where {
+      int tok, quarter;
+      bool is_v;
+    };
+    auto where = [&](int i) {
+      const int x = (tid + kThreads * i) % (4 * S::kTokens);
+      // (a wave's quarter rows are all keys or all values)
+      return Where{x >> 2, x & 3, __builtin_amdgcn_readfirstlane(tid + kThreads * i) >= 4 * S::kTokens};
+    };
     auto load = [&](int first) {
 #pragma unroll
       for (int i = 0; i < S::kPieces; ++i) {
-        const int x = (tid + kThreads * i) % (4 * S::kTokens), tok = x >> 2, quarter = x & 3;
-        const bool is_v = tid + kThreads * i >= 4 * S::kTokens;
-        const Unit u = list[min(first + tok / kUnit, n)];
-        if (tok % kUnit >= (u.where >> 16)) {
+        const Where p = where(i);
+        const Unit u = kUnits == 1 ? uniform_unit(list[min(first, n)]) : list[min(first + p.tok / kUnit, n)];
+        if (p.tok % kUnit >= (u.where >> 16)) {
           piece_clear<FMT, D>(piece[i]);
           continue;
         }
-        const int row = (u.where & 0xFFFF) + tok % kUnit;
+        const int row = u.where & 0xFFFF;
         const uint8_t* base = a.kv.pool + u.page * a.kv.page_bytes + head_at;
-        load_piece<FMT, D>(piece[i], base + (is_v ? T * K::kRow : 0) + row * K::kRow + quarter * K::kBytes,
-                           base + 2 * T * K::kRow + (is_v ? T * K::kSc : 0) + row * K::kSc +
-                               quarter * K::kElems / kKvBlock);
+        const uint8_t* codes = base + (p.is_v ? T * K::kRow : 0) + row * K::kRow;
+        const uint8_t* sc = base + 2 * T * K::kRow + (p.is_v ? T * K::kSc : 0) + row * K::kSc;
+        load_piece<FMT, D>(piece[i], codes + (p.tok % kUnit * K::kRow + p.quarter * K::kBytes),
+                           sc + (p.tok % kUnit * K::kSc + p.quarter * K::kElems / kKvBlock));
       }
     };
     auto is_masked = [&](int first) {
@@ -1045,15 +1147,18 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile_kernel
     auto unpack = [&](int buffer, bool masked, uint32_t* bad) {
 #pragma unroll
       for (int i = 0; i < S::kPieces; ++i) {
-        const int x = (tid + kThreads * i) % (4 * S::kTokens), tok = x >> 2, quarter = x & 3;
-        const bool is_v = tid + kThreads * i >= 4 * S::kTokens;
-        if (masked && is_v && piece_bad<FMT, D>(piece[i])) {
-          atomicOr(&bad[tok / kUnit], 1u << (tok % kUnit));
-          piece_clear<FMT, D>(piece[i]);
-        }
-        uint16_t* dst = area[buffer] + (is_v ? S::kPart : 0) + tok * S::kPitch + quarter * K::kElems;
+        const Where p = where(i);
+        if (p.is_v) {
+          if (masked && piece_bad<FMT, D>(piece[i])) {
+            atomicOr(&bad[p.tok / kUnit], 1u << (p.tok % kUnit));
+            piece_clear<FMT, D>(piece[i]);
+          }
+          store_values<32, S::kShift>(piece[i], area[buffer] + S::kKeys, p.tok, p.quarter);
+        } else {
+          uint16_t* dst = area[buffer] + p.tok * S::kKeyPitch + p.quarter * K::kElems;
 #pragma unroll
-        for (int y = 0; y < K::kSteps; ++y) *reinterpret_cast<u32x4_t*>(dst + 8 * y) = piece_step<FMT, D>(piece[i], y);
+          for (int y = 0; y < K::kSteps; ++y) *reinterpret_cast<u32x4_t*>(dst + 8 * y) = piece_step<FMT, D>(piece[i], y);
+        }
       }
     };
     if (n == 0) continue;
@@ -1067,7 +1172,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile_kernel
       const int slot1 = slot == 2 ? 0 : slot + 1, slot2 = slot1 == 2 ? 0 : slot1 + 1;
       if (tid < 2) bad_tok[slot2][tid] = 0;
       const uint16_t* keys = area[buffer];
-      const uint16_t* values = keys + S::kPart;
+      const uint16_t* values = keys + S::kKeys;
       float s[16 * kUnits];
       if (works) {
 #pragma unroll
@@ -1075,11 +1180,19 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile_kernel
           f32x16 x;
 #pragma unroll
           for (int j = 0; j < 16; ++j) x[j] = 0.f;
-          const uint16_t* kr = keys + (32 * h + col) * S::kPitch + 8 * half;
+          const uint16_t* kr = keys + (32 * h + col) * S::kKeyPitch + 8 * half;
+          constexpr int kAhead = 8;  // operands loaded together
 #pragma unroll
-          for (int y = 0; y < kQSteps; ++y)
-            x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                as_bf16x8(*reinterpret_cast<const u32x4_t*>(kr + 16 * y)), q[y], x, 0, 0, 0);
+          for (int y0 = 0; y0 < kQSteps; y0 += kAhead) {
+            u32x4_t k[kAhead];
+#pragma unroll
+            for (int y = 0; y < kAhead && y0 + y < kQSteps; ++y)
+              k[y] = *reinterpret_cast<const u32x4_t*>(kr + 16 * (y0 + y));
+            issue_first();
+#pragma unroll
+            for (int y = 0; y < kAhead && y0 + y < kQSteps; ++y)
+              x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(k[y]), q[y0 + y], x, 0, 0, 0);
+          }
 #pragma unroll
           for (int j = 0; j < 16; ++j) s[16 * h + j] = x[j];
         }
@@ -1092,29 +1205,39 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile_kernel
         if (i + 2 * kUnits < n) load(i + 2 * kUnits);
       }
       if (works) {
+        const bool ready = masked || scores.bias;
+        if (ready) {
 #pragma unroll
-        for (int h = 0; h < kUnits; ++h) {
-          const Unit u = uniform_unit(list[min(i + h, n)]);
-          float (&sh)[16] = *reinterpret_cast<float (*)[16]>(&s[16 * h]);
-          scores.template apply<32>(sh, rule, tr, u.pos, half);
-          if (masked) {
-            const uint32_t seen = mask_scores<32>(sh, rule, u, prefix, half);
-            const uint32_t bad = bad_tok[slot][h];
-            if (bad) poison |= sees_bad<32, 16>(seen, bad, half);
+          for (int h = 0; h < kUnits; ++h) {
+            const Unit u = uniform_unit(list[min(i + h, n)]);
+            float (&sh)[16] = *reinterpret_cast<float (*)[16]>(&s[16 * h]);
+            scores.template apply<32>(sh, rule, tr, u.pos, half);
+            if (masked) {
+              const uint32_t seen = mask_scores<32>(sh, rule, u, prefix, half);
+              const uint32_t bad = bad_tok[slot][h];
+              if (bad) poison |= sees_bad<32, 16>(seen, bad, half);
+            }
           }
         }
+        ValueOps<32, D> ops;
+        ops.template load<S::kShift>(values, 0, lane);
+        issue_first();
         bool heavy;
-        if (soften<32, D>(s, scores.factor(), st, rows, &heavy)) {
-          u32x4_t w[2 * kUnits];
+        if (soften<32, D>(s, scores, ready, st, rows, &heavy)) {
+          u32x4_t w[2 * kUnits], rest[2 * kUnits];
           pack_weights(s, w);
+          if (heavy) pack_rests(s, w, rest);
 #pragma unroll
-          for (int h = 0; h < kUnits; ++h) add_values<32, D, S::kPitch>(rows, values + 32 * h * S::kPitch, w + 2 * h, lane);
-          if (heavy) {
-            pack_rests(s, w);
+          for (int h = 0; h < kUnits; ++h)
 #pragma unroll
-            for (int h = 0; h < kUnits; ++h)
-              add_values<32, D, S::kPitch>(rows, values + 32 * h * S::kPitch, w + 2 * h, lane);
-          }
+            for (int x = 0; x < D / ValueOps<32, D>::kCols; ++x) {
+              if (h + x > 0) {
+                ops.template load<S::kShift>(values + 32 * h * kValuePitch<32, D>, x, lane);
+                issue_first();
+              }
+              ops.multiply(rows, x, w + 2 * h);
+              if (heavy) ops.multiply(rows, x, rest + 2 * h);
+            }
         }
       }
       masked = next_masked;

@@ -347,6 +347,7 @@ def test_positions_given_by_the_caller():
     pos = [0, 137, 138, 500, -1, 64, 29, 3, -2 ** 31, 2 ** 31 - 1]
     p.check("any positions", causal=True, q_pos=pos)
     p.check("any positions, window", window=20, q_pos=pos)
+    p.check("any prefix", causal=True, q_pos=pos, prefix=[-2 ** 31, 2 ** 31 - 1])
     pos = [0, 137, 138, 500, -1, 64, 29, 3, -40, 1000]
     p.check("any positions, bias", bias=True, q_pos=pos)
 
