@@ -23,9 +23,12 @@
 //     elements: exactly one block, so one scale) straight from the page into
 //     the operand of the first product; values go through the wave's own LDS
 //     rows once, as bf16, to be read back transposed.
-//   attend_tile_kernel  tiles of 128 rows: the workgroup unpacks a step of 64
-//     tokens (32 of 256 elements) at a time into LDS for its four waves, into
-//     one half of a double buffer while the waves work on the other.
+//   attend_tile_kernel  tiles of 128 rows: the workgroup unpacks a unit at a
+//     time into LDS for its four waves, into one half of a double buffer while
+//     they work on the other; each wave's matrix products run beside the
+//     exponentials of the unit before and the unpacking of the one after.
+#include <type_traits>
+
 #include "kv.h"
 #include "device_common.h"
 
@@ -47,10 +50,15 @@ constexpr int kMaxSplits = 64;  // one lane of the join each
 
 // One unit of the context, resolved.
 struct Unit {
-  int32_t page;   // page of the pool (0 if `count` is 0)
-  int32_t where;  // first row in the page | tokens held << 16
+  int64_t at;     // byte of the pool at which its first key's codes start (of the workgroup's head)
+  int32_t where;  // first row in the page | tokens held << 16 | kMasked
   int32_t pos;    // position of its first token
   int32_t ns;     // document of its chunk
+
+  static constexpr int kMasked = 1 << 24;  // some row does not see some of its 32 tokens
+  __device__ __forceinline__ int row() const { return where & 0xFFFF; }
+  __device__ __forceinline__ int held() const { return (where >> 16) & 63; }
+  __device__ __forceinline__ bool masked() const { return (where & kMasked) != 0; }
 };
 
 // How a call is spread over the GPU (shared by the workspace size and the launch).
@@ -274,10 +282,12 @@ __device__ __forceinline__ TileRule tile_rule(const AttendArgs& a, const Tile& t
 }
 
 // Resolve units last, last - 1, ... (n of them, at most MAX) of the span into `list`, leaving out those that hold
-// nothing or are of no row's document.  Returns how many there are; ends with a barrier.
+// nothing or are of no row's document.  Returns how many there are; ends with a barrier.  head_at: start of the
+// workgroup's head in a page, `row_bytes`: of a row's codes.
 template <int MAX>
 __device__ __forceinline__ int resolve_units(const AttendArgs& a, const ChunkList& L, const Span& span,
-                                             const TileRule& tr, int last, int n, Unit* list, int* counts) {
+                                             const TileRule& tr, int prefix, int64_t head_at, int row_bytes, int last,
+                                             int n, Unit* list, int* counts) {
   constexpr int kPer = MAX / kThreads;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   Unit x[kPer];
@@ -286,6 +296,7 @@ __device__ __forceinline__ int resolve_units(const AttendArgs& a, const ChunkLis
   for (int j = 0; j < kPer; ++j) {
     const int i = j * kThreads + tid;
     x[j] = Unit{0, 0, 0, 0};
+    bool ok = false;
     if (i < n) {
       const int u = span.unit(last - i);
       const int c = find_entry(L.ub, L.k, u);
@@ -293,13 +304,14 @@ __device__ __forceinline__ int resolve_units(const AttendArgs& a, const ChunkLis
       const int32_t id = L.cid[c];
       const int p = t / a.kv.page_tokens;
       const int32_t pg = a.kv.table[static_cast<int64_t>(id) * a.kv.ppc + p];
+      const int row = t - p * a.kv.page_tokens, held = min(kUnit, L.tb[c + 1] - L.tb[c] - t);
       x[j].ns = a.chunk_ns ? a.chunk_ns[id] : 0;
-      const bool ok = pg >= 0 && pg < a.kv.n_pages && x[j].ns >= 0 && x[j].ns >= tr.ns_lo && x[j].ns <= tr.ns_hi;
-      x[j].page = ok ? pg : 0;
-      x[j].where = (t - p * a.kv.page_tokens) | (ok ? min(kUnit, L.tb[c + 1] - L.tb[c] - t) : 0) << 16;
       x[j].pos = L.tb[c] + t;
+      x[j].at = pg * a.kv.page_bytes + head_at + row * row_bytes;
+      x[j].where = row | held << 16 | (held < kUnit || !tr.all_see(x[j].pos, prefix) ? Unit::kMasked : 0);
+      ok = pg >= 0 && pg < a.kv.n_pages && x[j].ns >= 0 && x[j].ns >= tr.ns_lo && x[j].ns <= tr.ns_hi;
     }
-    kept[j] = __ballot((x[j].where >> 16) > 0);
+    kept[j] = __ballot(ok);
     if (lane == 0) counts[j * kWaves + wave] = __builtin_popcountll(kept[j]);
   }
   __syncthreads();
@@ -312,8 +324,7 @@ __device__ __forceinline__ int resolve_units(const AttendArgs& a, const ChunkLis
     }
 #pragma unroll
   for (int j = 0; j < kPer; ++j)
-    if ((x[j].where >> 16) > 0)
-      list[at[j] + __builtin_popcountll(kept[j] & ((uint64_t{1} << lane) - 1))] = x[j];
+    if ((kept[j] >> lane) & 1u) list[at[j] + __builtin_popcountll(kept[j] & ((uint64_t{1} << lane) - 1))] = x[j];
   __syncthreads();
   return __builtin_amdgcn_readfirstlane(total);
 }
@@ -321,7 +332,9 @@ __device__ __forceinline__ int resolve_units(const AttendArgs& a, const ChunkLis
 // A unit of the list in scalar registers.
 __device__ __forceinline__ Unit uniform_unit(const Unit& x) {
   Unit u;
-  u.page = __builtin_amdgcn_readfirstlane(x.page);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(x.at));
+  const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(x.at >> 32));
+  u.at = static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
   u.where = __builtin_amdgcn_readfirstlane(x.where);
   u.pos = __builtin_amdgcn_readfirstlane(x.pos);
   u.ns = __builtin_amdgcn_readfirstlane(x.ns);
@@ -481,14 +494,16 @@ __device__ constexpr int score_token(int j) {
 }
 
 // How raw products become scores in the log2 domain: scaled, capped, biased.  The cap's tanh is
-// 1 - 2 / (1 + e^2x), with two transcendental operations of twice to three times a product's cost; where no score of a
-// wave's unit is above kSmall of the cap, its series to x^7 does as well (the next term is below 4e-8 of it).
+// 1 - 2 / (1 + e^2x), with two transcendental operations of twice to three times a product's cost each.  Where no score
+// of a wave's unit is above kSmall of the cap, tanh(x) / x as a polynomial of degree 2 in t = x^2 does as well: its
+// series 1 - t / 3 + 2 t^2 / 15 - 17 t^3 / 315 with t^3 replaced by the quadratic that is nearest to it on
+// [0, kSmall^2], off by at most kSmall^6 / 32 (Chebyshev).  With the series' next term that is 1.1e-7 of the score.
 struct Scores {
   float c;     // scale * log2(e)
   float k2;    // 2 * log2(e) * scale / softcap
   float cap2;  // softcap * log2(e); 0: none
   float limit; // raw products up to this magnitude are small
-  float s1, s3, s5, s7;  // the series in raw products
+  float s0, s1, s2;  // the polynomial in squared raw products, times scale * log2(e)
   bool bias;
   bool causal;
 
@@ -498,27 +513,18 @@ struct Scores {
       : c(a.scale * kLog2e), cap2(a.softcap * kLog2e), bias(a.slopes != nullptr), causal(a.causal != 0) {
     const float x = a.softcap > 0.f ? a.scale / a.softcap : 0.f;
     k2 = 2.f * kLog2e * x;
-    // (coefficients of a tiny x would lose bits as denormals)
-    limit = x > 1e-4f ? kSmall / x : -1.f;
-    s1 = cap2 * x;
-    s3 = cap2 * x * x * x * (-1.f / 3.f);
-    s5 = cap2 * x * x * x * x * x * (2.f / 15.f);
-    s7 = cap2 * x * x * x * x * x * x * x * (-17.f / 315.f);
+    limit = x > 1e-4f ? kSmall / x : -1.f;  // (coefficients of a tiny x would lose bits as denormals)
+    constexpr float kT = kSmall * kSmall, kCubic = 17.f / 315.f;
+    s0 = c * (1.f - kCubic * kT * kT * kT / 32.f);
+    s1 = c * x * x * (-1.f / 3.f + kCubic * kT * kT * (9.f / 16.f));
+    s2 = c * x * x * x * x * (2.f / 15.f - kCubic * kT * 1.5f);
   }
 
   __device__ __forceinline__ float series(float s) const {  // capped score / s
     const float t = s * s;
-    return s1 + t * (s3 + t * (s5 + t * s7));
+    return s0 + t * (s1 + t * s2);
   }
   __device__ __forceinline__ float fraction(float s) const { return __builtin_amdgcn_rcpf(1.f + fast_exp2(s * k2)); }
-
-  template <int N>
-  __device__ __forceinline__ bool small(const float (&s)[N]) const {
-    float top = 0.f;
-#pragma unroll
-    for (int j = 0; j < N; ++j) top = fmaxf(top, fabsf(s[j]));
-    return !__any(top > limit);
-  }
 
   // Scores of one unit made explicit: what masks and biases need.
   template <int WIDTH, int N>
@@ -551,7 +557,7 @@ struct Scores {
 template <int WIDTH, int N>
 __device__ __forceinline__ uint32_t mask_scores(float (&s)[N], const RowRule& rule, const Unit& u, int prefix, int part) {
   const int first = u.pos + 4 * part;  // position of a score whose token offset is 0
-  const int held = (u.where >> 16) - 4 * part, pre = prefix - first, lo = rule.lo - first, hi = rule.hi - first;
+  const int held = u.held() - 4 * part, pre = prefix - first, lo = rule.lo - first, hi = rule.hi - first;
   const bool mine = u.ns == rule.ns;
   uint32_t seen = 0;
 #pragma unroll
@@ -623,21 +629,27 @@ struct Rows {
   }
 };
 
-// The scores of one row (N in this lane) into weights: updates the running state and the output's scale.  With
-// `ready` the scores are in the log2 domain, else they are raw products, unmasked and without a bias, whose scale or
-// cap goes into the exponential's argument.  Returns false if none of the wave's scores weighs anything.
-template <int WIDTH, int D, int N>
-__device__ __forceinline__ bool soften(float (&s)[N], const Scores& sc, bool ready, RowState& st, Rows<WIDTH, D>& rows,
-                                       bool* heavy) {
-  const bool capped = !ready && sc.cap2 != 0.f;
-  const bool series = capped && sc.small(s);
-  const float f = ready ? 1.f : sc.c;
-  float top = s[0];
-#pragma unroll
-  for (int j = 1; j < N; ++j) top = nan_max(top, s[j]);
-  top = max_column<WIDTH>(top);
-  // (both forms of the cap grow with the product, so the largest product has the largest score)
-  top = !capped ? top * f : series ? top * sc.series(top) : sc.cap2 - 2.f * sc.cap2 * sc.fraction(top);
+// How a unit's scores become weights 2^(score - ref): from numbers that only want a factor (scores in the log2 domain,
+// or raw products without a cap), or from raw products whose cap (by series or exactly) goes into the exponential's
+// argument.
+enum Mode { kLinear, kSeries, kExact };
+
+template <Mode MODE>
+__device__ __forceinline__ float weigh(float s, float f, const Scores& sc, float ref) {
+  if constexpr (MODE == kLinear) return fast_exp2(fmaf(s, f, -ref));
+  if constexpr (MODE == kSeries) return fast_exp2(fmaf(s, sc.series(s), -ref));
+  return fast_exp2(fmaf(sc.fraction(s), -2.f * sc.cap2, sc.cap2 - ref));
+}
+
+// The largest score of a row from the largest number (the cap grows with the product).
+__device__ __forceinline__ float top_score(float top, float f, const Scores& sc, Mode mode) {
+  if (mode == kLinear) return top * f;
+  return mode == kSeries ? top * sc.series(top) : sc.cap2 - 2.f * sc.cap2 * sc.fraction(top);
+}
+
+// Whether a unit with this largest score weighs anything in the wave; raises the running maximum if it has to.
+template <int WIDTH, int D>
+__device__ __forceinline__ bool raise(float top, RowState& st, Rows<WIDTH, D>& rows) {
   if (!__any(!(top <= st.m - kNothing))) return false;
   if (__any(top > st.m + kLag)) {
     const float mn = fmaxf(st.m, top);
@@ -646,22 +658,18 @@ __device__ __forceinline__ bool soften(float (&s)[N], const Scores& sc, bool rea
     rows.scale(r);
     st.m = mn;
   }
-  const float ref = finite_max(st.m);
-  if (!capped) {
-#pragma unroll
-    for (int j = 0; j < N; ++j) s[j] = fast_exp2(fmaf(s[j], f, -ref));
-  } else if (series) {
-#pragma unroll
-    for (int j = 0; j < N; ++j) s[j] = fast_exp2(fmaf(s[j], sc.series(s[j]), -ref));
-  } else {
-    const float base = sc.cap2 - ref, g = -2.f * sc.cap2;
-#pragma unroll
-    for (int j = 0; j < N; ++j) s[j] = fast_exp2(fmaf(sc.fraction(s[j]), g, base));
-  }
-#pragma unroll
-  for (int j = 0; j < N; ++j) st.l += s[j];
-  *heavy = __any(fast_exp2(top - ref) * kHeavy > st.l);
   return true;
+}
+__device__ __forceinline__ bool is_heavy(float top, const RowState& st) {
+  return __any(fast_exp2(top - finite_max(st.m)) * kHeavy > st.l);
+}
+
+template <int N>
+__device__ __forceinline__ float max_of(const float (&s)[N]) {
+  float top = s[0];
+#pragma unroll
+  for (int j = 1; j < N; ++j) top = nan_max(top, s[j]);
+  return top;
 }
 
 // Write a row's output, or its part of a split context.
@@ -714,47 +722,39 @@ __device__ __forceinline__ int value_chunk(int row, int chunk) {
   return chunk ^ ((row >> SHIFT) & (WIDTH == 32 ? 3 : 1));
 }
 
-// Transposed operands of the values of 32 tokens in LDS rows at `v`, for the output columns 128 half .. + 127 (or all
-// of fewer): loaded together, ahead of the products that use them, so that those do not wait for each.
-template <int WIDTH, int D>
+// Transposed operands of the values of 32 tokens in LDS rows at `rows`: operand n of WIDTH 16 is for the output columns
+// 16 n .. + 15, of 32 for the columns 32 (n / 2) .. + 31 and every second 16 tokens.
+template <int WIDTH, int D, int SHIFT>
 struct ValueOps {
-  static constexpr int kCols = D < 128 ? D : 128;
-  static constexpr int kOps = kCols / WIDTH * (WIDTH == 16 ? 1 : 2);
-  bf16x8 v[kOps];
+  static constexpr int kOps = D / WIDTH * (WIDTH == 16 ? 1 : 2);
+  static constexpr int P = kValuePitch<WIDTH, D>;
+  const uint16_t* src[WIDTH == 16 ? 1 : 4];
 
-  template <int SHIFT>
-  __device__ __forceinline__ void load(const uint16_t* rows, int half, int lane) {
-    constexpr int P = kValuePitch<WIDTH, D>;
+  __device__ __forceinline__ ValueOps(const uint16_t* rows, int lane) {
     static_assert(WIDTH != 16 || SHIFT <= 3, "rows 16 apart have the same exchange");
     const int i = lane & 15;
-    rows += half * kCols;
     if constexpr (WIDTH == 16) {
       const int r = 4 * (lane >> 4) + (i >> 2);  // rows r and r + 16, columns 16 n + 4 (i & 3)
-      const uint16_t* src = rows + r * P + 8 * value_chunk<16, SHIFT>(r, (i & 3) >> 1) + 4 * (i & 1);
-#pragma unroll
-      for (int n = 0; n < kOps; ++n) v[n] = pair(src + 16 * n, src + 16 * P + 16 * n);
+      src[0] = rows + r * P + 8 * value_chunk<16, SHIFT>(r, (i & 3) >> 1) + 4 * (i & 1);
     } else {
       // rows r + 8 y, columns 32 n + 16 (lane >> 4 & 1) + 4 (i & 3)
       const int r = 4 * (lane >> 5) + (i >> 2), c = 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
-      const uint16_t* src[4];
 #pragma unroll
       for (int y = 0; y < 4; ++y)
         src[y] = rows + (r + 8 * y) * P + 8 * value_chunk<32, SHIFT>(r + 8 * y, c) + 4 * (i & 1);
-#pragma unroll
-      for (int n = 0; n < kOps; ++n) v[n] = pair(src[2 * (n & 1)] + 32 * (n >> 1), src[2 * (n & 1) + 1] + 32 * (n >> 1));
     }
   }
-  // O^T += V^T P^T with the weights of the lane's row.
-  __device__ __forceinline__ void multiply(Rows<WIDTH, D>& out, int half, const u32x4_t* w) const {
-#pragma unroll
-    for (int n = 0; n < kOps; ++n) {
-      if constexpr (WIDTH == 16) {
-        auto& o = out.o[half * kOps + n];
-        o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[n], as_bf16x8(w[0]), o, 0, 0, 0);
-      } else {
-        auto& o = out.o[half * (kOps / 2) + (n >> 1)];
-        o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[n], as_bf16x8(w[n & 1]), o, 0, 0, 0);
-      }
+  __device__ __forceinline__ bf16x8 operator[](int n) const {
+    if constexpr (WIDTH == 16) return pair(src[0] + 16 * n, src[0] + 16 * P + 16 * n);
+    else return pair(src[2 * (n & 1)] + 32 * (n >> 1), src[2 * (n & 1) + 1] + 32 * (n >> 1));
+  }
+  // O^T += V^T P^T for operand n, with the weights of the lane's row.
+  static __device__ __forceinline__ void multiply(Rows<WIDTH, D>& out, int n, bf16x8 v, const u32x4_t* w) {
+    if constexpr (WIDTH == 16) {
+      out.o[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, as_bf16x8(w[0]), out.o[n], 0, 0, 0);
+    } else {
+      auto& o = out.o[n >> 1];
+      o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, as_bf16x8(w[n & 1]), o, 0, 0, 0);
     }
   }
 
@@ -765,7 +765,7 @@ struct ValueOps {
   }
 };
 
-// Loads written before this stay before it, and what uses them behind.
+// What is written before this is issued before it.
 __device__ __forceinline__ void issue_first() { __builtin_amdgcn_sched_barrier(0); }
 
 // Unpack a quarter row of values into its LDS row.
@@ -794,7 +794,7 @@ __device__ __forceinline__ void pack_rests(const float (&s)[N], const u32x4_t (&
 
 template <int FMT, int D, int R>
 struct FewShape {
-  static constexpr int kBatch = 512;                        // units resolved at a time
+  static constexpr int kBatch = 256;                        // units resolved at a time
   static constexpr int kShift = R == 16 ? 3 : 2;            // exchange of chunks: a wave writes 16 rows at a time
   static constexpr int kWaveBytes = kUnit * kValuePitch<R, D> * 2;  // a wave's unpacked values
   static constexpr int kJoinBytes = 2 * R * D * 4;          // two waves' outputs at the end
@@ -857,20 +857,20 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_few_kernel(
   // Keys and values of the unit at hand.  Each is loaded again, for the wave's next unit, as soon as it has been used:
   // a wave keeps nearly a whole unit in flight without a second set of registers.
   Piece<FMT, D> pk[2], pv[2];
+  const int my_codes = col * K::kRow + quarter * K::kBytes;
   auto load = [&](Piece<FMT, D> (&p)[2], const Unit& u, bool is_v) {
-    const int row = (u.where & 0xFFFF) + col;
-    const uint8_t* base = a.kv.pool + u.page * a.kv.page_bytes + head_at;
-    const uint8_t* codes = base + (is_v ? T * K::kRow : 0) + row * K::kRow + quarter * K::kBytes;
-    const uint8_t* sc = base + 2 * T * K::kRow + (is_v ? T * K::kSc : 0) + row * K::kSc;
+    const uint8_t* codes = a.kv.pool + u.at + (is_v ? T * K::kRow : 0);
+    const uint8_t* sc = a.kv.pool + u.at + (2 * T * K::kRow - u.row() * (K::kRow - K::kSc)) + (is_v ? T * K::kSc : 0);
 #pragma unroll
     for (int h = 0; h < 2; ++h)
-      load_piece<FMT, D>(p[h], codes + h * (row_step * K::kRow + quarter_step * K::kBytes),
-                         sc + h * row_step * K::kSc + (quarter + h * quarter_step) * K::kElems / kKvBlock);
+      load_piece<FMT, D>(p[h], codes + (my_codes + h * (row_step * K::kRow + quarter_step * K::kBytes)),
+                         sc + ((col + h * row_step) * K::kSc + (quarter + h * quarter_step) * K::kElems / kKvBlock));
   };
 
   for (int last = u1 - 1; last >= u0; last -= S::kBatch) {
     __syncthreads();
-    const int n = resolve_units<S::kBatch>(a, L, span, tr, last, min(S::kBatch, last - u0 + 1), list, tmp);
+    const int n = resolve_units<S::kBatch>(a, L, span, tr, prefix, head_at, K::kRow, last,
+                                             min(S::kBatch, last - u0 + 1), list, tmp);
     if (wave >= n) continue;
     Unit u = uniform_unit(list[wave]);
     load(pk, u, false);
@@ -878,7 +878,6 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_few_kernel(
     for (int i = wave; i < n; i += kWaves) {
       const bool more = i + kWaves < n;
       const Unit next = uniform_unit(list[more ? i + kWaves : i]);
-      const int held = u.where >> 16;
       float s[kScores];
       if constexpr (R == 16) {
 #pragma unroll
@@ -904,9 +903,10 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_few_kernel(
         for (int j = 0; j < 16; ++j) s[j] = x[j];
       }
       if (more) load(pk, next, false);
-      const bool masked = held < kUnit || !tr.all_see(u.pos, prefix);
-      if (masked || scores.bias) scores.template apply<R>(s, rule, tr, u.pos, part);
-      if (masked) {
+      const bool ready = u.masked() || scores.bias;
+      if (ready) scores.template apply<R>(s, rule, tr, u.pos, part);
+      if (u.masked()) {
+        const int held = u.held();
         const uint32_t seen = mask_scores<R>(s, rule, u, prefix, part);
         uint32_t bad = 0;
 #pragma unroll
@@ -921,8 +921,30 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_few_kernel(
         }
         if (bad) poison |= sees_bad<R, kScores>(seen, bad, part);
       }
-      bool heavy;
-      const bool counts = soften<R, D>(s, scores, masked || scores.bias, st, rows, &heavy);
+      bool small = false;
+      if (!ready && scores.cap2 != 0.f) {
+        float most = 0.f;
+#pragma unroll
+        for (int j = 0; j < kScores; ++j) most = fmaxf(most, fabsf(s[j]));
+        small = !__any(most > scores.limit);
+      }
+      const Mode mode = ready || scores.cap2 == 0.f ? kLinear : small ? kSeries : kExact;
+      const float f = ready ? 1.f : scores.c;
+      const float top = top_score(max_column<R>(max_of(s)), f, scores, mode);
+      const bool counts = raise<R, D>(top, st, rows);
+      if (counts) {
+        const float ref = finite_max(st.m);
+        auto weigh_all = [&](auto m) {
+#pragma unroll
+          for (int j = 0; j < kScores; ++j) {
+            s[j] = weigh<decltype(m)::value>(s[j], f, scores, ref);
+            st.l += s[j];
+          }
+        };
+        if (mode == kLinear) weigh_all(std::integral_constant<Mode, kLinear>{});
+        else if (mode == kSeries) weigh_all(std::integral_constant<Mode, kSeries>{});
+        else weigh_all(std::integral_constant<Mode, kExact>{});
+      }
       if (counts) {  // values: unpack into the wave's LDS rows, to be read back transposed
 #pragma unroll
         for (int h = 0; h < 2; ++h)
@@ -932,19 +954,25 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_few_kernel(
       if (counts) {
         __builtin_amdgcn_wave_barrier();
         u32x4_t w[kScores / 8], rest[kScores / 8];
-        ValueOps<R, D> ops;
-        ops.template load<S::kShift>(vrows, 0, lane);
-        issue_first();
-        pack_weights(s, w);
-        if (heavy) pack_rests(s, w, rest);
+        const bool heavy = is_heavy(top, st);
+        const ValueOps<R, D, S::kShift> ops(vrows, lane);
+        constexpr int kOps = ValueOps<R, D, S::kShift>::kOps, kTogether = 8;  // operands loaded ahead of their products
 #pragma unroll
-        for (int x = 0; x < D / ValueOps<R, D>::kCols; ++x) {
-          if (x > 0) {
-            ops.template load<S::kShift>(vrows, x, lane);
-            issue_first();
+        for (int n0 = 0; n0 < kOps; n0 += kTogether) {
+          bf16x8 v[kTogether];
+#pragma unroll
+          for (int x = 0; x < kTogether && n0 + x < kOps; ++x) v[x] = ops[n0 + x];
+          issue_first();
+          if (n0 == 0) {
+            pack_weights(s, w);
+            if (heavy) pack_rests(s, w, rest);
           }
-          ops.multiply(rows, x, w);
-          if (heavy) ops.multiply(rows, x, rest);
+#pragma unroll
+          for (int x = 0; x < kTogether && n0 + x < kOps; ++x) ops.multiply(rows, n0 + x, v[x], w);
+          if (heavy) {
+#pragma unroll
+            for (int x = 0; x < kTogether && n0 + x < kOps; ++x) ops.multiply(rows, n0 + x, v[x], rest);
+          }
         }
         __builtin_amdgcn_wave_barrier();
       }
@@ -1042,16 +1070,18 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a, int
 
 template <int FMT, int D>
 struct TileShape {
-  static constexpr int kBatch = 256;                          // units resolved at a time
-  static constexpr int kStepUnits = D == 64 ? 2 : 1;          // units per step
-  static constexpr int kTokens = kStepUnits * kUnit;
-  static constexpr int kKeyPitch = D + 8;                     // bf16 elements between LDS rows of keys
-  static constexpr int kKeys = kTokens * kKeyPitch;           // elements of a step's keys
-  static constexpr int kValues = kTokens * kValuePitch<32, D>;
-  static constexpr int kShift = 0;                            // exchange of chunks: a wave writes 4 rows at a time
-  static constexpr int kPieces = 2 * kTokens * 4 / kThreads;  // quarter rows per thread and step, keys then values
+  static constexpr int kBatch = 256;                        // units resolved at a time
+  static constexpr int kKeyPitch = D + 8;                   // bf16 elements between LDS rows of keys
+  static constexpr int kKeys = kUnit * kKeyPitch;           // elements of a unit's keys
+  static constexpr int kValues = kUnit * kValuePitch<32, D>;
+  static constexpr int kShift = 0;                          // exchange of chunks: a wave writes 4 rows at a time
+  static_assert(kThreads == 2 * 4 * kUnit, "a quarter row of keys or of values per thread");
 };
 
+// Iteration i of a wave: the weights of unit i beside the first product of unit i + 1, then the second product of
+// unit i beside the unpacking of keys i + 2 (waves 0, 1) and values i + 1 (waves 2, 3).  A wave issues in order, so
+// the matrix products only overlap with what stands between them: both stretches are written as groups of one matrix
+// instruction and a share of the other work.
 template <int FMT, int D>
 __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile_kernel(AttendArgs a, int splits,
                                                                                  int64_t tiles,
@@ -1059,12 +1089,13 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile_kernel
                                                                                  RowState* __restrict__ part_ml) {
   using K = Dim<FMT, D>;
   using S = TileShape<FMT, D>;
-  constexpr int kQSteps = D / 16, kUnits = S::kStepUnits;
+  constexpr int kQSteps = D / 16;
   extern __shared__ int dyn[];  // the chunk list: cid[k], ub[k + 1], tb[k + 1]
-  __shared__ __align__(16) uint16_t area[2][S::kKeys + S::kValues];
-  __shared__ Unit list[S::kBatch + 1];
+  __shared__ __align__(16) uint16_t key_rows[2][S::kKeys];
+  __shared__ __align__(16) uint16_t value_rows[2][S::kValues];
+  __shared__ Unit list[S::kBatch];
   __shared__ int tmp[2 * kWaves];
-  __shared__ uint32_t bad_tok[3][2];  // tokens whose values are not finite: of this step, the next and the one after
+  __shared__ uint32_t bad_tok[2];  // tokens of a masked unit whose values are not finite
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 31, half = lane >> 5;
@@ -1099,149 +1130,186 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile_kernel
   rows.clear();
   RowState st{-INFINITY, 0.f};
   bool poison = false;
-  if (tid < 6) bad_tok[tid >> 1][tid & 1] = 0;
-  int slot = 0;  // of the step at hand
+
+  // the quarter row that this thread unpacks of every unit: keys (waves 0, 1) or values
+  const bool is_v = wave >= 2;
+  const int lead = is_v ? 1 : 2;  // units ahead of the one at hand
+  const int tok = (tid & 127) >> 2, quarter = tid & 3;
+  const uint32_t my_codes = tok * K::kRow + quarter * K::kBytes;
+  const uint32_t my_scale = tok * K::kSc + quarter * K::kElems / kKvBlock;
+  const int64_t codes_at = is_v ? T * K::kRow : 0, scales_at = 2 * T * K::kRow + (is_v ? T * K::kSc : 0);
+  Piece<FMT, D> piece;
 
   for (int last = u1 - 1; last >= u0; last -= S::kBatch) {
     __syncthreads();
-    const int n = resolve_units<S::kBatch>(a, L, span, tr, last, min(S::kBatch, last - u0 + 1), list, tmp);
-    if (tid == 0) list[n] = Unit{0, 0, 0, -1};  // fills up the last step: holds nothing
-    __syncthreads();
-    Piece<FMT, D> piece[S::kPieces];
-    // Quarter row i of this thread: of the step's keys, then of its values.
-    struct Where {
-      int tok, quarter;
-      bool is_v;
-    };
-    auto where = [&](int i) {
-      const int x = (tid + kThreads * i) % (4 * S::kTokens);
-      // (a wave's quarter rows are all keys or all values)
-      return Where{x >> 2, x & 3, __builtin_amdgcn_readfirstlane(tid + kThreads * i) >= 4 * S::kTokens};
-    };
-    auto load = [&](int first) {
-#pragma unroll
-      for (int i = 0; i < S::kPieces; ++i) {
-        const Where p = where(i);
-        const Unit u = kUnits == 1 ? uniform_unit(list[min(first, n)]) : list[min(first + p.tok / kUnit, n)];
-        if (p.tok % kUnit >= (u.where >> 16)) {
-          piece_clear<FMT, D>(piece[i]);
-          continue;
-        }
-        const int row = u.where & 0xFFFF;
-        const uint8_t* base = a.kv.pool + u.page * a.kv.page_bytes + head_at;
-        const uint8_t* codes = base + (p.is_v ? T * K::kRow : 0) + row * K::kRow;
-        const uint8_t* sc = base + 2 * T * K::kRow + (p.is_v ? T * K::kSc : 0) + row * K::kSc;
-        load_piece<FMT, D>(piece[i], codes + (p.tok % kUnit * K::kRow + p.quarter * K::kBytes),
-                           sc + (p.tok % kUnit * K::kSc + p.quarter * K::kElems / kKvBlock));
-      }
-    };
-    auto is_masked = [&](int first) {
-      bool m = false;
-#pragma unroll
-      for (int h = 0; h < kUnits; ++h) {
-        const Unit u = uniform_unit(list[min(first + h, n)]);
-        m |= (u.where >> 16) < kUnit || !tr.all_see(u.pos, prefix);
-      }
-      return m;
-    };
-    auto unpack = [&](int buffer, bool masked, uint32_t* bad) {
-#pragma unroll
-      for (int i = 0; i < S::kPieces; ++i) {
-        const Where p = where(i);
-        if (p.is_v) {
-          if (masked && piece_bad<FMT, D>(piece[i])) {
-            atomicOr(&bad[p.tok / kUnit], 1u << (p.tok % kUnit));
-            piece_clear<FMT, D>(piece[i]);
-          }
-          store_values<32, S::kShift>(piece[i], area[buffer] + S::kKeys, p.tok, p.quarter);
-        } else {
-          uint16_t* dst = area[buffer] + p.tok * S::kKeyPitch + p.quarter * K::kElems;
-#pragma unroll
-          for (int y = 0; y < K::kSteps; ++y) *reinterpret_cast<u32x4_t*>(dst + 8 * y) = piece_step<FMT, D>(piece[i], y);
-        }
-      }
-    };
+    const int n = resolve_units<S::kBatch>(a, L, span, tr, prefix, head_at, K::kRow, last,
+                                           min(S::kBatch, last - u0 + 1), list, tmp);
     if (n == 0) continue;
+    auto load = [&](int i) {
+      if (i >= n) return;
+      const Unit u = uniform_unit(list[i]);
+      if (tok < u.held()) {
+        load_piece<FMT, D>(piece, a.kv.pool + (u.at + codes_at) + my_codes,
+                           a.kv.pool + (u.at + scales_at - u.row() * (K::kRow - K::kSc)) + my_scale);
+      } else {
+        piece_clear<FMT, D>(piece);
+      }
+    };
+    // step y of unpacking the piece into the buffers of unit i
+    auto unpack = [&](int i, int y) {
+      const u32x4_t v = piece_step<FMT, D>(piece, y);
+      uint16_t* dst = is_v ? value_rows[i & 1] + tok * kValuePitch<32, D> +
+                                 8 * value_chunk<32, S::kShift>(tok, quarter * K::kSteps + y)
+                           : key_rows[i & 1] + tok * S::kKeyPitch + quarter * K::kElems + 8 * y;
+      *reinterpret_cast<u32x4_t*>(dst) = v;
+    };
+    // values of a masked unit that are not finite are noted and left out (every thread of the workgroup calls this)
+    auto check_bad = [&](int i) {
+      if (tid == 0) bad_tok[i & 1] = 0;
+      __syncthreads();
+      if (is_v && piece_bad<FMT, D>(piece)) {
+        atomicOr(&bad_tok[i & 1], 1u << tok);
+        piece_clear<FMT, D>(piece);
+      }
+    };
+    auto is_masked = [&](int i) { return i < n && (__builtin_amdgcn_readfirstlane(list[i].where) & Unit::kMasked) != 0; };
+
+    // keys 0 and 1, values 0, and the loads of the next ones
     load(0);
-    bool masked = is_masked(0);
-    unpack(0, masked, bad_tok[slot]);
-    if (kUnits < n) load(kUnits);
+    if (is_masked(0)) check_bad(0);
+#pragma unroll
+    for (int y = 0; y < K::kSteps; ++y) unpack(0, y);
+    load(1);
+    if (!is_v) {
+#pragma unroll
+      for (int y = 0; y < K::kSteps; ++y) unpack(1, y);
+      load(2);
+    }
     __syncthreads();
-    int buffer = 0;
-    for (int i = 0; i < n; i += kUnits, buffer ^= 1) {
-      const int slot1 = slot == 2 ? 0 : slot + 1, slot2 = slot1 == 2 ? 0 : slot1 + 1;
-      if (tid < 2) bad_tok[slot2][tid] = 0;
-      const uint16_t* keys = area[buffer];
-      const uint16_t* values = keys + S::kKeys;
-      float s[16 * kUnits];
+
+    float s[16], raw[16];  // of the unit at hand: scores, then weights; of the next: raw products
+    float most = 0.f, top = -INFINITY;  // of the raw products: largest magnitude, largest
+    const int key_at = col * S::kKeyPitch + 8 * half;
+    auto products = [&](int i) {  // S^T of unit i, by itself
+      f32x16 x;
+#pragma unroll
+      for (int j = 0; j < 16; ++j) x[j] = 0.f;
+#pragma unroll
+      for (int y = 0; y < kQSteps; ++y)
+        x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+            as_bf16x8(*reinterpret_cast<const u32x4_t*>(key_rows[i & 1] + key_at + 16 * y)), q[y], x, 0, 0, 0);
+#pragma unroll
+      for (int j = 0; j < 16; ++j) raw[j] = x[j];
+    };
+    auto bounds = [&]() {
+      top = max_of(raw);
+      most = 0.f;
+#pragma unroll
+      for (int j = 0; j < 16; ++j) most = fmaxf(most, fabsf(raw[j]));
+    };
+    if (works) {
+      products(0);
+      bounds();
+    }
+    for (int i = 0; i < n; ++i) {
       if (works) {
+        const Unit u = uniform_unit(list[i]);
+        const bool ready = u.masked() || scores.bias;
 #pragma unroll
-        for (int h = 0; h < kUnits; ++h) {
-          f32x16 x;
+        for (int j = 0; j < 16; ++j) s[j] = raw[j];
+        if (ready) {
+          scores.template apply<32>(s, rule, tr, u.pos, half);
+          if (u.masked()) {
+            const uint32_t seen = mask_scores<32>(s, rule, u, prefix, half);
+            const uint32_t bad = __builtin_amdgcn_readfirstlane(bad_tok[i & 1]);
+            if (bad) poison |= sees_bad<32, 16>(seen, bad, half);
+          }
+          top = max_of(s);
+        }
+        const Mode mode = ready || scores.cap2 == 0.f ? kLinear : __any(most > scores.limit) ? kExact : kSeries;
+        const float f = ready ? 1.f : scores.c;
+        const float high = top_score(max_column<32>(top), f, scores, mode);
+        const bool counts = raise<32, D>(high, st, rows);
+        const float ref = finite_max(st.m);
+        u32x4_t w[2];
+        // the weights of this unit beside the first product of the next
+        {
+          auto weights_and_products = [&](auto m) {
+            constexpr int kPer = 16 / kQSteps > 0 ? 16 / kQSteps : 1, kAhead = 4;
+            const uint16_t* keys = key_rows[(i + 1) & 1] + key_at;
+            f32x16 x;
 #pragma unroll
-          for (int j = 0; j < 16; ++j) x[j] = 0.f;
-          const uint16_t* kr = keys + (32 * h + col) * S::kKeyPitch + 8 * half;
-          constexpr int kAhead = 8;  // operands loaded together
+            for (int j = 0; j < 16; ++j) x[j] = 0.f;
+            u32x4_t k[kQSteps];
 #pragma unroll
-          for (int y0 = 0; y0 < kQSteps; y0 += kAhead) {
-            u32x4_t k[kAhead];
-#pragma unroll
-            for (int y = 0; y < kAhead && y0 + y < kQSteps; ++y)
-              k[y] = *reinterpret_cast<const u32x4_t*>(kr + 16 * (y0 + y));
+            for (int y = 0; y < kAhead && y < kQSteps; ++y) k[y] = *reinterpret_cast<const u32x4_t*>(keys + 16 * y);
             issue_first();
 #pragma unroll
-            for (int y = 0; y < kAhead && y0 + y < kQSteps; ++y)
-              x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(k[y]), q[y0 + y], x, 0, 0, 0);
-          }
+            for (int y = 0; y < kQSteps; ++y) {
+              if (y + kAhead < kQSteps) k[y + kAhead] = *reinterpret_cast<const u32x4_t*>(keys + 16 * (y + kAhead));
+              x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(k[y]), q[y], x, 0, 0, 0);
 #pragma unroll
-          for (int j = 0; j < 16; ++j) s[16 * h + j] = x[j];
-        }
-      }
-      // the next step's rows go into the other buffer, and the loads of the one after start
-      bool next_masked = false;
-      if (i + kUnits < n) {
-        next_masked = is_masked(i + kUnits);
-        unpack(buffer ^ 1, next_masked, bad_tok[slot1]);
-        if (i + 2 * kUnits < n) load(i + 2 * kUnits);
-      }
-      if (works) {
-        const bool ready = masked || scores.bias;
-        if (ready) {
-#pragma unroll
-          for (int h = 0; h < kUnits; ++h) {
-            const Unit u = uniform_unit(list[min(i + h, n)]);
-            float (&sh)[16] = *reinterpret_cast<float (*)[16]>(&s[16 * h]);
-            scores.template apply<32>(sh, rule, tr, u.pos, half);
-            if (masked) {
-              const uint32_t seen = mask_scores<32>(sh, rule, u, prefix, half);
-              const uint32_t bad = bad_tok[slot][h];
-              if (bad) poison |= sees_bad<32, 16>(seen, bad, half);
-            }
-          }
-        }
-        ValueOps<32, D> ops;
-        ops.template load<S::kShift>(values, 0, lane);
-        issue_first();
-        bool heavy;
-        if (soften<32, D>(s, scores, ready, st, rows, &heavy)) {
-          u32x4_t w[2 * kUnits], rest[2 * kUnits];
-          pack_weights(s, w);
-          if (heavy) pack_rests(s, w, rest);
-#pragma unroll
-          for (int h = 0; h < kUnits; ++h)
-#pragma unroll
-            for (int x = 0; x < D / ValueOps<32, D>::kCols; ++x) {
-              if (h + x > 0) {
-                ops.template load<S::kShift>(values + 32 * h * kValuePitch<32, D>, x, lane);
-                issue_first();
+              for (int j = kPer * y; j < kPer * (y + 1); ++j) {
+                s[j] = weigh<decltype(m)::value>(s[j], f, scores, ref);
+                st.l += s[j];
+                if (j & 1) w[j >> 3][(j >> 1) & 3] = pack2(s[j - 1], s[j]);
               }
-              ops.multiply(rows, x, w + 2 * h);
-              if (heavy) ops.multiply(rows, x, rest + 2 * h);
+              issue_first();
             }
+#pragma unroll
+            for (int j = 0; j < 16; ++j) raw[j] = x[j];
+          };
+          if (mode == kLinear) weights_and_products(std::integral_constant<Mode, kLinear>{});
+          else if (mode == kSeries) weights_and_products(std::integral_constant<Mode, kSeries>{});
+          else weights_and_products(std::integral_constant<Mode, kExact>{});
         }
+        if (is_masked(i + 1)) check_bad(i + 1);
+        // the second product beside the unpacking and the next products' bounds (two ifs that the compiler does not see
+        // to be one: with an else it keeps the accumulators twice)
+        int counts_too = __builtin_amdgcn_readfirstlane(counts);
+        asm volatile("" : "+s"(counts_too));
+        if (!counts) {
+#pragma unroll
+          for (int y = 0; y < K::kSteps; ++y) unpack(i + lead, y);
+          bounds();
+        }
+        if (counts_too) {
+          const ValueOps<32, D, S::kShift> ops(value_rows[i & 1], lane);
+          constexpr int kOps = ValueOps<32, D, S::kShift>::kOps, kAhead = 3;
+          bf16x8 v[kOps];
+#pragma unroll
+          for (int x = 0; x < kAhead; ++x) v[x] = ops[x];
+          issue_first();
+          top = -INFINITY;
+          most = 0.f;
+#pragma unroll
+          for (int x = 0; x < kOps; ++x) {
+            if (x + kAhead < kOps) v[x + kAhead] = ops[x + kAhead];
+            ops.multiply(rows, x, v[x], w);
+            if (x % 2 == 1) {
+              unpack(i + lead, x / 2);
+#pragma unroll
+              for (int j = 0; j < 32 / kOps; ++j) {
+                const float r = raw[(x / 2) * (32 / kOps) + j];
+                top = nan_max(top, r);
+                most = fmaxf(most, fabsf(r));
+              }
+            }
+            issue_first();
+          }
+          if (is_heavy(high, st)) {
+            u32x4_t rest[2];
+            pack_rests(s, w, rest);
+#pragma unroll
+            for (int x = 0; x < kOps; ++x) ops.multiply(rows, x, ops[x], rest);
+          }
+        }
+      } else {
+        if (is_masked(i + 1)) check_bad(i + 1);
+#pragma unroll
+        for (int y = 0; y < K::kSteps; ++y) unpack(i + lead, y);
       }
-      masked = next_masked;
-      slot = slot1;
+      load(i + lead + 1);
       __syncthreads();
     }
   }
@@ -1260,20 +1328,33 @@ int64_t tile_count(bool ragged, int64_t m, int64_t total_q, int group, int R) {
   return m * ((total_q / m * group + R - 1) / R);
 }
 
-// Rows per request (on average) decide the kernel.  A context is split when the tiles alone leave CUs idle, into
-// parts of at least kMinPart tokens.
-constexpr int64_t kWantFew = 2048, kWantTile = 512;
-constexpr int64_t kMinPart = 512;
+// Workgroups that run together on the 256 CUs, by what a kernel's registers and LDS allow.
+int64_t slots_of(int rows, int d) {
+  const int per_cu = d == 256 ? 1 : rows != 16 ? 2 : d == 128 ? 3 : 4;
+  return int64_t{256} * per_cu;
+}
 
-AttendPlan make_plan(int64_t m, int64_t capacity, int64_t total_q, int heads, int heads_q, bool ragged) {
+// Rows per request (on average) decide the kernel.  The context is split so that the rounds of workgroups take least,
+// a workgroup being taken to cost its units and kStart more: finding its units, its start and its end.  Tiles of 128
+// rows that fill the GPU are left whole: causal ones are of unequal length, and even out by themselves.
+constexpr int64_t kStart = 16;
+
+AttendPlan make_plan(int d, int64_t m, int64_t units, int64_t total_q, int heads, int heads_q, bool ragged) {
   AttendPlan p;
   const int group = heads_q / heads;
   p.rows = total_q * group <= 16 * m ? 16 : total_q * group <= 64 * m ? 32 : kTileRows;
   p.tiles = tile_count(ragged, m, total_q, group, p.rows);
-  const int64_t have = p.tiles * heads, want = p.rows < kTileRows ? kWantFew : kWantTile;
-  int64_t s = (want + have - 1) / have;
-  s = s < capacity / kMinPart ? s : capacity / kMinPart;
-  p.splits = static_cast<int>(s < 1 ? 1 : s > kMaxSplits ? kMaxSplits : s);
+  const int64_t work = p.tiles * heads, slots = slots_of(p.rows, d);
+  int64_t best = INT64_MAX;
+  p.splits = 1;
+  const int64_t most = p.rows == kTileRows && work >= slots ? 1 : kMaxSplits;
+  for (int64_t s = 1; s <= most && (s == 1 || units / s >= kWaves); ++s) {
+    const int64_t cost = (work * s + slots - 1) / slots * ((units + s - 1) / s + kStart) + (s > 1 ? s / 4 : 0);
+    if (cost < best) {
+      best = cost;
+      p.splits = static_cast<int>(s);
+    }
+  }
   return p;
 }
 
@@ -1314,11 +1395,11 @@ hipError_t launch_fmt(const AttendArgs& a, const AttendPlan& p, int d, hipStream
 }  // namespace
 
 // The larger of the two forms of a call (ragged or not), so that one size serves both.
-size_t attend_workspace_bytes(int d, int64_t m, int64_t capacity, int64_t total_q, int heads, int heads_q) {
+size_t attend_workspace_bytes(int d, int64_t m, int64_t units, int64_t total_q, int heads, int heads_q) {
   size_t need = 0;
   for (int ragged = 0; ragged < 2; ++ragged) {
     if (!ragged && total_q % m != 0) continue;
-    const int s = make_plan(m, capacity, total_q, heads, heads_q, ragged != 0).splits;
+    const int s = make_plan(d, m, units, total_q, heads, heads_q, ragged != 0).splits;
     if (s == 1) continue;
     const size_t b = partial_o_bytes(d, total_q, heads_q, s) +
                      align256(static_cast<size_t>(s) * total_q * heads_q * sizeof(RowState));
@@ -1327,14 +1408,14 @@ size_t attend_workspace_bytes(int d, int64_t m, int64_t capacity, int64_t total_
   return need;
 }
 
-bool attend_fits(int64_t m, int64_t capacity, int64_t total_q, int heads, int heads_q, bool ragged) {
-  const AttendPlan p = make_plan(m, capacity, total_q, heads, heads_q, ragged);
+bool attend_fits(int d, int64_t m, int64_t units, int64_t total_q, int heads, int heads_q, bool ragged) {
+  const AttendPlan p = make_plan(d, m, units, total_q, heads, heads_q, ragged);
   return p.tiles * p.splits <= INT32_MAX / heads;
 }
 
 hipError_t launch_attend(const AttendArgs& a, int fmt, int d, hipStream_t stream) {
-  const int64_t capacity = static_cast<int64_t>(a.k) * a.kv.ppc * a.kv.page_tokens;
-  const AttendPlan p = make_plan(a.m, capacity, a.total_q, a.kv.heads, a.hq, a.q_offsets != nullptr);
+  const int64_t units = static_cast<int64_t>(a.k) * a.kv.ppc * a.kv.page_tokens / kUnit;
+  const AttendPlan p = make_plan(d, a.m, units, a.total_q, a.kv.heads, a.hq, a.q_offsets != nullptr);
   switch (fmt) {
     case MEM_KV_BF16: return launch_fmt<MEM_KV_BF16>(a, p, d, stream);
     case MEM_KV_FP8: return launch_fmt<MEM_KV_FP8>(a, p, d, stream);
