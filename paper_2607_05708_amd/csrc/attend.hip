@@ -23,10 +23,10 @@
 //     elements: exactly one block, so one scale) straight from the page into
 //     the operand of the first product; values go through the wave's own LDS
 //     rows once, as bf16, to be read back transposed.
-//   attend_tile_kernel  tiles of 128 rows: the workgroup unpacks a unit at a
-//     time into LDS for its four waves, into one half of a double buffer while
-//     they work on the other; each wave's matrix products run beside the
-//     exponentials of the unit before and the unpacking of the one after.
+//   attend_tile_kernel  tiles of 128 rows: the workgroup unpacks two units at
+//     a time into LDS for its four waves, into one half of a double buffer
+//     while they work on the other; a wave's matrix products are interleaved
+//     with the exponentials and the unpacking.
 #include <type_traits>
 
 #include "kv.h"
@@ -288,7 +288,7 @@ template <int MAX>
 __device__ __forceinline__ int resolve_units(const AttendArgs& a, const ChunkList& L, const Span& span,
                                              const TileRule& tr, int prefix, int64_t head_at, int row_bytes, int last,
                                              int n, Unit* list, int* counts) {
-  constexpr int kPer = MAX / kThreads;
+  constexpr int kPer = (MAX + kThreads - 1) / kThreads;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   Unit x[kPer];
   uint64_t kept[kPer];
@@ -1070,32 +1070,35 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a, int
 
 template <int FMT, int D>
 struct TileShape {
-  static constexpr int kBatch = 256;                        // units resolved at a time
+  static constexpr int kBatch = 128;                        // units resolved at a time
+  static constexpr int kTokens = 2 * kUnit;                 // tokens of a step
   static constexpr int kKeyPitch = D + 8;                   // bf16 elements between LDS rows of keys
-  static constexpr int kKeys = kUnit * kKeyPitch;           // elements of a unit's keys
-  static constexpr int kValues = kUnit * kValuePitch<32, D>;
+  static constexpr int kKeys = kTokens * kKeyPitch;         // elements of a step's keys
+  static constexpr int kValues = kTokens * kValuePitch<32, D>;
   static constexpr int kShift = 0;                          // exchange of chunks: a wave writes 4 rows at a time
-  static_assert(kThreads == 2 * 4 * kUnit, "a quarter row of keys or of values per thread");
+  static_assert(kThreads == 4 * kTokens, "a quarter row of keys and one of values per thread");
 };
 
-// Iteration i of a wave: the weights of unit i beside the first product of unit i + 1, then the second product of
-// unit i beside the unpacking of keys i + 2 (waves 0, 1) and values i + 1 (waves 2, 3).  A wave issues in order, so
-// the matrix products only overlap with what stands between them: both stretches are written as groups of one matrix
-// instruction and a share of the other work.
-template <int FMT, int D>
+// A wave issues in order, so its matrix products only overlap with what stands between them: the second product of a
+// step's first unit is written in groups of one matrix instruction and a share of the second unit's exponentials, the
+// second unit's with a share of the unpacking.  (Two units a step: of one unit's 1.59 us, 0.65 went into the step
+// itself -- barrier, list, maximum -- whatever it did.)  CAPPED: the scores are capped; a kernel has one way to
+// weigh scores in those groups, and takes the rare others apart from them.
+template <int FMT, int D, bool CAPPED>
 __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile_kernel(AttendArgs a, int splits,
                                                                                  int64_t tiles,
                                                                                  float* __restrict__ part_o,
                                                                                  RowState* __restrict__ part_ml) {
   using K = Dim<FMT, D>;
   using S = TileShape<FMT, D>;
+  using Ops = ValueOps<32, D, S::kShift>;
   constexpr int kQSteps = D / 16;
   extern __shared__ int dyn[];  // the chunk list: cid[k], ub[k + 1], tb[k + 1]
   __shared__ __align__(16) uint16_t key_rows[2][S::kKeys];
   __shared__ __align__(16) uint16_t value_rows[2][S::kValues];
-  __shared__ Unit list[S::kBatch];
+  __shared__ Unit list[S::kBatch + 6];  // (read some steps ahead)
   __shared__ int tmp[2 * kWaves];
-  __shared__ uint32_t bad_tok[2];  // tokens of a masked unit whose values are not finite
+  __shared__ uint32_t bad_tok[2][2];  // tokens of a masked step's units whose values are not finite
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 31, half = lane >> 5;
@@ -1131,185 +1134,198 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile_kernel
   RowState st{-INFINITY, 0.f};
   bool poison = false;
 
-  // the quarter row that this thread unpacks of every unit: keys (waves 0, 1) or values
-  const bool is_v = wave >= 2;
-  const int lead = is_v ? 1 : 2;  // units ahead of the one at hand
-  const int tok = (tid & 127) >> 2, quarter = tid & 3;
-  const uint32_t my_codes = tok * K::kRow + quarter * K::kBytes;
-  const uint32_t my_scale = tok * K::kSc + quarter * K::kElems / kKvBlock;
-  const int64_t codes_at = is_v ? T * K::kRow : 0, scales_at = 2 * T * K::kRow + (is_v ? T * K::kSc : 0);
-  Piece<FMT, D> piece;
+  // the quarter row that this thread unpacks, keys and values, of every step (a wave's are of one unit)
+  const int tok = tid >> 2, quarter = tid & 3, my_unit = wave >> 1;
+  const uint32_t my_codes = tok % kUnit * K::kRow + quarter * K::kBytes;
+  const uint32_t my_scale = tok % kUnit * K::kSc + quarter * K::kElems / kKvBlock;
+  Piece<FMT, D> pk, pv;
 
   for (int last = u1 - 1; last >= u0; last -= S::kBatch) {
     __syncthreads();
     const int n = resolve_units<S::kBatch>(a, L, span, tr, prefix, head_at, K::kRow, last,
                                            min(S::kBatch, last - u0 + 1), list, tmp);
     if (n == 0) continue;
-    auto load = [&](int i) {
-      if (i >= n) return;
-      const Unit u = uniform_unit(list[i]);
-      if (tok < u.held()) {
-        load_piece<FMT, D>(piece, a.kv.pool + (u.at + codes_at) + my_codes,
-                           a.kv.pool + (u.at + scales_at - u.row() * (K::kRow - K::kSc)) + my_scale);
+    if (tid == 0) list[n] = Unit{0, Unit::kMasked, 0, -1};  // fills up the last step: holds nothing
+    __syncthreads();
+    const int steps = (n + 1) / 2;
+    auto load = [&](const Unit& u) {
+      if (tok % kUnit < u.held()) {
+        const uint8_t* codes = a.kv.pool + u.at;
+        const uint8_t* sc = codes + (2 * T * K::kRow - u.row() * (K::kRow - K::kSc));
+        load_piece<FMT, D>(pk, codes + my_codes, sc + my_scale);
+        load_piece<FMT, D>(pv, codes + T * K::kRow + my_codes, sc + T * K::kSc + my_scale);
       } else {
-        piece_clear<FMT, D>(piece);
+        piece_clear<FMT, D>(pk);
+        piece_clear<FMT, D>(pv);
       }
     };
-    // step y of unpacking the piece into the buffers of unit i
+    // part y of unpacking into the buffers of step i: keys first, then values
     auto unpack = [&](int i, int y) {
-      const u32x4_t v = piece_step<FMT, D>(piece, y);
-      uint16_t* dst = is_v ? value_rows[i & 1] + tok * kValuePitch<32, D> +
-                                 8 * value_chunk<32, S::kShift>(tok, quarter * K::kSteps + y)
-                           : key_rows[i & 1] + tok * S::kKeyPitch + quarter * K::kElems + 8 * y;
-      *reinterpret_cast<u32x4_t*>(dst) = v;
-    };
-    // values of a masked unit that are not finite are noted and left out (every thread of the workgroup calls this)
-    auto check_bad = [&](int i) {
-      if (tid == 0) bad_tok[i & 1] = 0;
-      __syncthreads();
-      if (is_v && piece_bad<FMT, D>(piece)) {
-        atomicOr(&bad_tok[i & 1], 1u << tok);
-        piece_clear<FMT, D>(piece);
+      if (y < K::kSteps) {
+        *reinterpret_cast<u32x4_t*>(key_rows[i & 1] + tok * S::kKeyPitch + quarter * K::kElems + 8 * y) =
+            piece_step<FMT, D>(pk, y);
+      } else {
+        y -= K::kSteps;
+        *reinterpret_cast<u32x4_t*>(value_rows[i & 1] + tok * kValuePitch<32, D> +
+                                    8 * value_chunk<32, S::kShift>(tok, quarter * K::kSteps + y)) =
+            piece_step<FMT, D>(pv, y);
       }
     };
-    auto is_masked = [&](int i) { return i < n && (__builtin_amdgcn_readfirstlane(list[i].where) & Unit::kMasked) != 0; };
+    // values of a masked step that are not finite are noted and left out (every thread of the workgroup calls this)
+    auto check_bad = [&](int i) {
+      if (tid < 2) bad_tok[i & 1][tid] = 0;
+      __syncthreads();
+      if (piece_bad<FMT, D>(pv)) {
+        atomicOr(&bad_tok[i & 1][my_unit], 1u << (tok % kUnit));
+        piece_clear<FMT, D>(pv);
+      }
+    };
 
-    // keys 0 and 1, values 0, and the loads of the next ones
-    load(0);
-    if (is_masked(0)) check_bad(0);
+    // the first step's rows, and the loads of the second
+    Unit ua = uniform_unit(list[0]), ub = uniform_unit(list[1]);  // units of the step at hand
+    load(my_unit ? ub : ua);
+    if (ua.masked() || ub.masked()) check_bad(0);
 #pragma unroll
-    for (int y = 0; y < K::kSteps; ++y) unpack(0, y);
-    load(1);
-    if (!is_v) {
-#pragma unroll
-      for (int y = 0; y < K::kSteps; ++y) unpack(1, y);
-      load(2);
-    }
+    for (int y = 0; y < 2 * K::kSteps; ++y) unpack(0, y);
+    Unit na = uniform_unit(list[2]), nb = uniform_unit(list[3]);  // of the next
+    if (n == 3) nb = uniform_unit(list[n]);
+    if (steps > 1) load(my_unit ? nb : na);
     __syncthreads();
 
-    float s[16], raw[16];  // of the unit at hand: scores, then weights; of the next: raw products
-    float most = 0.f, top = -INFINITY;  // of the raw products: largest magnitude, largest
     const int key_at = col * S::kKeyPitch + 8 * half;
-    auto products = [&](int i) {  // S^T of unit i, by itself
-      f32x16 x;
-#pragma unroll
-      for (int j = 0; j < 16; ++j) x[j] = 0.f;
-#pragma unroll
-      for (int y = 0; y < kQSteps; ++y)
-        x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-            as_bf16x8(*reinterpret_cast<const u32x4_t*>(key_rows[i & 1] + key_at + 16 * y)), q[y], x, 0, 0, 0);
-#pragma unroll
-      for (int j = 0; j < 16; ++j) raw[j] = x[j];
-    };
-    auto bounds = [&]() {
-      top = max_of(raw);
-      most = 0.f;
-#pragma unroll
-      for (int j = 0; j < 16; ++j) most = fmaxf(most, fabsf(raw[j]));
-    };
-    if (works) {
-      products(0);
-      bounds();
-    }
-    for (int i = 0; i < n; ++i) {
+    for (int i = 0; i < steps; ++i) {
+      // lists are read two steps ahead, for the end of this one
+      const int at2 = 2 * i + 4;
+      const Unit next_a = list[min(at2, n)], next_b = list[min(at2 + 1, n)];
+      const bool more = i + 1 < steps;
+      if (more && (na.masked() || nb.masked())) check_bad(i + 1);
       if (works) {
-        const Unit u = uniform_unit(list[i]);
-        const bool ready = u.masked() || scores.bias;
+        const uint16_t* keys = key_rows[i & 1] + key_at;
+        const uint16_t* values = value_rows[i & 1];
+        const bool masked = ua.masked() || ub.masked(), ready = masked || scores.bias;
+        // S^T of both units; operands are read kAhead products ahead
+        float s[2][16];
+        float top = -INFINITY, most = 0.f;  // largest product or score, largest magnitude of a product
+        {
+          constexpr int kAhead = 4, kAll = 2 * kQSteps;
+          auto key = [&](int y) {
+            return *reinterpret_cast<const u32x4_t*>(keys + y / kQSteps * kUnit * S::kKeyPitch + 16 * (y % kQSteps));
+          };
+          u32x4_t k[kAll];
+          f32x16 x[2];
 #pragma unroll
-        for (int j = 0; j < 16; ++j) s[j] = raw[j];
-        if (ready) {
-          scores.template apply<32>(s, rule, tr, u.pos, half);
-          if (u.masked()) {
-            const uint32_t seen = mask_scores<32>(s, rule, u, prefix, half);
-            const uint32_t bad = __builtin_amdgcn_readfirstlane(bad_tok[i & 1]);
-            if (bad) poison |= sees_bad<32, 16>(seen, bad, half);
+          for (int y = 0; y < kAhead; ++y) k[y] = key(y);
+#pragma unroll
+          for (int j = 0; j < 16; ++j) x[0][j] = x[1][j] = 0.f;
+          issue_first();
+#pragma unroll
+          for (int y = 0; y < kAll; ++y) {
+            if (y + kAhead < kAll) k[y + kAhead] = key(y + kAhead);
+            f32x16& acc = x[y / kQSteps];
+            acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(k[y]), q[y % kQSteps], acc, 0, 0, 0);
+            issue_first();
           }
-          top = max_of(s);
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            s[0][j] = x[0][j];
+            s[1][j] = x[1][j];
+          }
         }
-        const Mode mode = ready || scores.cap2 == 0.f ? kLinear : __any(most > scores.limit) ? kExact : kSeries;
+        if (ready) {
+          scores.template apply<32>(s[0], rule, tr, ua.pos, half);
+          scores.template apply<32>(s[1], rule, tr, ub.pos, half);
+          if (masked) {
+            const uint32_t seen_a = mask_scores<32>(s[0], rule, ua, prefix, half);
+            const uint32_t seen_b = mask_scores<32>(s[1], rule, ub, prefix, half);
+            const uint32_t bad_a = __builtin_amdgcn_readfirstlane(bad_tok[i & 1][0]);
+            const uint32_t bad_b = __builtin_amdgcn_readfirstlane(bad_tok[i & 1][1]);
+            if (bad_a) poison |= sees_bad<32, 16>(seen_a, bad_a, half);
+            if (bad_b) poison |= sees_bad<32, 16>(seen_b, bad_b, half);
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+          top = nan_max(top, s[j >> 4][j & 15]);
+          if (CAPPED) most = fmaxf(most, fabsf(s[j >> 4][j & 15]));
+        }
+        const Mode mode = !CAPPED || ready ? kLinear : __any(most > scores.limit) ? kExact : kSeries;
         const float f = ready ? 1.f : scores.c;
         const float high = top_score(max_column<32>(top), f, scores, mode);
         const bool counts = raise<32, D>(high, st, rows);
         const float ref = finite_max(st.m);
-        u32x4_t w[2];
-        // the weights of this unit beside the first product of the next
-        {
-          auto weights_and_products = [&](auto m) {
-            constexpr int kPer = 16 / kQSteps > 0 ? 16 / kQSteps : 1, kAhead = 4;
-            const uint16_t* keys = key_rows[(i + 1) & 1] + key_at;
-            f32x16 x;
-#pragma unroll
-            for (int j = 0; j < 16; ++j) x[j] = 0.f;
-            u32x4_t k[kQSteps];
-#pragma unroll
-            for (int y = 0; y < kAhead && y < kQSteps; ++y) k[y] = *reinterpret_cast<const u32x4_t*>(keys + 16 * y);
-            issue_first();
-#pragma unroll
-            for (int y = 0; y < kQSteps; ++y) {
-              if (y + kAhead < kQSteps) k[y + kAhead] = *reinterpret_cast<const u32x4_t*>(keys + 16 * (y + kAhead));
-              x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(k[y]), q[y], x, 0, 0, 0);
-#pragma unroll
-              for (int j = kPer * y; j < kPer * (y + 1); ++j) {
-                s[j] = weigh<decltype(m)::value>(s[j], f, scores, ref);
-                st.l += s[j];
-                if (j & 1) w[j >> 3][(j >> 1) & 3] = pack2(s[j - 1], s[j]);
-              }
-              issue_first();
-            }
-#pragma unroll
-            for (int j = 0; j < 16; ++j) raw[j] = x[j];
-          };
-          if (mode == kLinear) weights_and_products(std::integral_constant<Mode, kLinear>{});
-          else if (mode == kSeries) weights_and_products(std::integral_constant<Mode, kSeries>{});
-          else weights_and_products(std::integral_constant<Mode, kExact>{});
-        }
-        if (is_masked(i + 1)) check_bad(i + 1);
-        // the second product beside the unpacking and the next products' bounds (two ifs that the compiler does not see
-        // to be one: with an else it keeps the accumulators twice)
-        int counts_too = __builtin_amdgcn_readfirstlane(counts);
-        asm volatile("" : "+s"(counts_too));
-        if (!counts) {
-#pragma unroll
-          for (int y = 0; y < K::kSteps; ++y) unpack(i + lead, y);
-          bounds();
-        }
-        if (counts_too) {
-          const ValueOps<32, D, S::kShift> ops(value_rows[i & 1], lane);
-          constexpr int kOps = ValueOps<32, D, S::kShift>::kOps, kAhead = 3;
-          bf16x8 v[kOps];
+        auto weigh_score = [&](auto m, float& x) {
+          x = weigh<decltype(m)::value>(x, f, scores, ref);
+          st.l += x;
+        };
+        // O^T += V^T P^T of one unit, a product at a time, each with its share of other work
+        auto add_values = [&](int unit, const u32x4_t (&w)[2], auto share) {
+          const Ops ops(values + unit * kUnit * kValuePitch<32, D>, lane);
+          constexpr int kAhead = 3;
+          bf16x8 v[Ops::kOps];
 #pragma unroll
           for (int x = 0; x < kAhead; ++x) v[x] = ops[x];
           issue_first();
-          top = -INFINITY;
-          most = 0.f;
 #pragma unroll
-          for (int x = 0; x < kOps; ++x) {
-            if (x + kAhead < kOps) v[x + kAhead] = ops[x + kAhead];
+          for (int x = 0; x < Ops::kOps; ++x) {
+            if (x + kAhead < Ops::kOps) v[x + kAhead] = ops[x + kAhead];
             ops.multiply(rows, x, v[x], w);
-            if (x % 2 == 1) {
-              unpack(i + lead, x / 2);
-#pragma unroll
-              for (int j = 0; j < 32 / kOps; ++j) {
-                const float r = raw[(x / 2) * (32 / kOps) + j];
-                top = nan_max(top, r);
-                most = fmaxf(most, fabsf(r));
-              }
-            }
+            share(x);
             issue_first();
           }
-          if (is_heavy(high, st)) {
-            u32x4_t rest[2];
-            pack_rests(s, w, rest);
+        };
+        // The usual way is the second block; the first is for steps that weigh nothing and for those with a heavy
+        // weight or, where scores are capped, with a mask, a bias or a large score.  (Two flags that the compiler does
+        // not know to be one: with an if and an else over the same accumulators it keeps them twice.)
+        constexpr Mode kUsual = CAPPED ? kSeries : kLinear;
+        const bool usual = counts && mode == kUsual && !is_heavy(high, st);
+        int usual_too = __builtin_amdgcn_readfirstlane(usual);
+        asm volatile("" : "+s"(usual_too));
+        if (!usual) {
+          if (counts) {
+            if (mode == kLinear) {
 #pragma unroll
-            for (int x = 0; x < kOps; ++x) ops.multiply(rows, x, ops[x], rest);
+              for (int j = 0; j < 32; ++j) weigh_score(std::integral_constant<Mode, kLinear>{}, s[j >> 4][j & 15]);
+            } else {
+#pragma unroll
+              for (int j = 0; j < 32; ++j) weigh_score(std::integral_constant<Mode, kExact>{}, s[j >> 4][j & 15]);
+            }
+            u32x4_t w[2], rest[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              pack_weights(s[h], w);
+              pack_rests(s[h], w, rest);
+              add_values(h, w, [](int) {});
+              add_values(h, rest, [](int) {});
+            }
           }
+#pragma unroll
+          for (int y = 0; y < 2 * K::kSteps; ++y) unpack(i + 1, y);
+        }
+        if (usual_too) {
+          const std::integral_constant<Mode, kUsual> m;
+          u32x4_t w[2][2];
+#pragma unroll
+          for (int j = 0; j < 16; ++j) weigh_score(m, s[0][j]);
+          pack_weights(s[0], w[0]);
+          add_values(0, w[0], [&](int x) {
+            constexpr int kPer = 16 / Ops::kOps;
+#pragma unroll
+            for (int j = kPer * x; j < kPer * (x + 1); ++j) {
+              weigh_score(m, s[1][j]);
+              if (j & 1) w[1][j >> 3][(j >> 1) & 3] = pack2(s[1][j - 1], s[1][j]);
+            }
+          });
+          add_values(1, w[1], [&](int x) { unpack(i + 1, x); });
         }
       } else {
-        if (is_masked(i + 1)) check_bad(i + 1);
 #pragma unroll
-        for (int y = 0; y < K::kSteps; ++y) unpack(i + lead, y);
+        for (int y = 0; y < 2 * K::kSteps; ++y) unpack(i + 1, y);
       }
-      load(i + lead + 1);
+      ua = na;
+      ub = nb;
+      na = uniform_unit(next_a);
+      nb = uniform_unit(next_b);
+      if (i + 2 < steps) load(my_unit ? nb : na);
       __syncthreads();
     }
   }
@@ -1377,7 +1393,9 @@ hipError_t launch_dim(const AttendArgs& a, const AttendPlan& p, hipStream_t stre
   else if (p.rows == 32)
     attend_few_kernel<FMT, D, 32><<<grid, kThreads, lds, stream>>>(a, p.splits, po, pml);
   else
-    attend_tile_kernel<FMT, D><<<grid, kThreads, lds, stream>>>(a, p.splits, p.tiles, po, pml);
+    (a.softcap > 0.f ? attend_tile_kernel<FMT, D, true> : attend_tile_kernel<FMT, D, false>)<<<grid, kThreads, lds,
+                                                                                               stream>>>(
+        a, p.splits, p.tiles, po, pml);
   if (hipError_t e = hipGetLastError(); e != hipSuccess || p.splits == 1) return e;
   attend_join_kernel<D><<<dim3(static_cast<unsigned>(a.total_q * a.hq)), kThreads, 0, stream>>>(a, p.splits, po, pml);
   return hipGetLastError();
