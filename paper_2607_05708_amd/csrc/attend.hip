@@ -527,8 +527,8 @@ struct Scores {
   __device__ __forceinline__ float fraction(float s) const { return __builtin_amdgcn_rcpf(1.f + fast_exp2(s * k2)); }
 
   // Scores of one unit made explicit: what masks and biases need.
-  template <int WIDTH, int N>
-  __device__ __forceinline__ void apply(float (&s)[N], const RowRule& rule, const TileRule& tr, int pos, int part) const {
+  template <int WIDTH, int N, typename V>
+  __device__ __forceinline__ void apply(V& s, const RowRule& rule, const TileRule& tr, int pos, int part) const {
     if (cap2 != 0.f) {
 #pragma unroll
       for (int j = 0; j < N; ++j) s[j] = cap2 - 2.f * cap2 * fraction(s[j]);
@@ -554,8 +554,8 @@ struct Scores {
 };
 
 // Masks of one unit's scores, looked at one by one.  Returns the scores that are seen as bits.
-template <int WIDTH, int N>
-__device__ __forceinline__ uint32_t mask_scores(float (&s)[N], const RowRule& rule, const Unit& u, int prefix, int part) {
+template <int WIDTH, int N, typename V>
+__device__ __forceinline__ uint32_t mask_scores(V& s, const RowRule& rule, const Unit& u, int prefix, int part) {
   const int first = u.pos + 4 * part;  // position of a score whose token offset is 0
   const int held = u.held() - 4 * part, pre = prefix - first, lo = rule.lo - first, hi = rule.hi - first;
   const bool mine = u.ns == rule.ns;
@@ -592,7 +592,7 @@ constexpr float kNothing = 48.f;
 // The weights are rounded to bf16 for the second product.  Where one weighs more than 1 / kHeavy of its lane's sum so
 // far, rounding it would show in the output, and the product is made a second time with what the rounding left (16
 // bits of weight in all); smaller weights' roundings average out.  The sum is that of the unrounded ones.
-constexpr float kHeavy = 16.f;
+constexpr float kHeavy = 4.f;
 
 __device__ __forceinline__ float inverse_sum(float l) { return l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN; }
 __device__ __forceinline__ float lse_of(float m, float l) {
@@ -779,13 +779,13 @@ __device__ __forceinline__ void store_values(const Piece<FMT, D>& p, uint16_t* v
 }
 
 // N weights as operands of the second product, and what their rounding left.
-template <int N>
-__device__ __forceinline__ void pack_weights(const float (&s)[N], u32x4_t (&w)[N / 8]) {
+template <int N, typename V>
+__device__ __forceinline__ void pack_weights(const V& s, u32x4_t (&w)[N / 8]) {
 #pragma unroll
   for (int j = 0; j < N / 2; ++j) w[j >> 2][j & 3] = pack2(s[2 * j], s[2 * j + 1]);
 }
-template <int N>
-__device__ __forceinline__ void pack_rests(const float (&s)[N], const u32x4_t (&w)[N / 8], u32x4_t (&rest)[N / 8]) {
+template <int N, typename V>
+__device__ __forceinline__ void pack_rests(const V& s, const u32x4_t (&w)[N / 8], u32x4_t (&rest)[N / 8]) {
 #pragma unroll
   for (int j = 0; j < N / 2; ++j) rest[j >> 2][j & 3] = rest2(s[2 * j], s[2 * j + 1], w[j >> 2][j & 3]);
 }
@@ -904,10 +904,10 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_few_kernel(
       }
       if (more) load(pk, next, false);
       const bool ready = u.masked() || scores.bias;
-      if (ready) scores.template apply<R>(s, rule, tr, u.pos, part);
+      if (ready) scores.template apply<R, kScores>(s, rule, tr, u.pos, part);
       if (u.masked()) {
         const int held = u.held();
-        const uint32_t seen = mask_scores<R>(s, rule, u, prefix, part);
+        const uint32_t seen = mask_scores<R, kScores>(s, rule, u, prefix, part);
         uint32_t bad = 0;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -964,8 +964,8 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_few_kernel(
           for (int x = 0; x < kTogether && n0 + x < kOps; ++x) v[x] = ops[n0 + x];
           issue_first();
           if (n0 == 0) {
-            pack_weights(s, w);
-            if (heavy) pack_rests(s, w, rest);
+            pack_weights<kScores>(s, w);
+            if (heavy) pack_rests<kScores>(s, w, rest);
           }
 #pragma unroll
           for (int x = 0; x < kTogether && n0 + x < kOps; ++x) ops.multiply(rows, n0 + x, v[x], w);
@@ -1085,7 +1085,7 @@ struct TileShape {
 // itself -- barrier, list, maximum -- whatever it did.)  CAPPED: the scores are capped; a kernel has one way to
 // weigh scores in those groups, and takes the rare others apart from them.
 template <int FMT, int D, bool CAPPED>
-__global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile_kernel(AttendArgs a, int splits,
+__global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 3) void attend_tile_kernel(AttendArgs a, int splits,
                                                                                  int64_t tiles,
                                                                                  float* __restrict__ part_o,
                                                                                  RowState* __restrict__ part_ml) {
@@ -1203,40 +1203,37 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile_kernel
         const uint16_t* keys = key_rows[i & 1] + key_at;
         const uint16_t* values = value_rows[i & 1];
         const bool masked = ua.masked() || ub.masked(), ready = masked || scores.bias;
-        // S^T of both units; operands are read kAhead products ahead
-        float s[2][16];
+        // S^T of both units; operands are read kAhead products ahead.  (The other parts of a step have priority over
+        // the other workgroup's wave: it is then at its matrix products while this one is at its exponentials.)
+        f32x16 s[2];
         float top = -INFINITY, most = 0.f;  // largest product or score, largest magnitude of a product
         {
-          constexpr int kAhead = 4, kAll = 2 * kQSteps;
+          constexpr int kAhead = 2, kAll = 2 * kQSteps;
           auto key = [&](int y) {
             return *reinterpret_cast<const u32x4_t*>(keys + y / kQSteps * kUnit * S::kKeyPitch + 16 * (y % kQSteps));
           };
           u32x4_t k[kAll];
-          f32x16 x[2];
 #pragma unroll
           for (int y = 0; y < kAhead; ++y) k[y] = key(y);
 #pragma unroll
-          for (int j = 0; j < 16; ++j) x[0][j] = x[1][j] = 0.f;
+          for (int j = 0; j < 16; ++j) s[0][j] = s[1][j] = 0.f;
+          __builtin_amdgcn_s_setprio(0);
           issue_first();
 #pragma unroll
           for (int y = 0; y < kAll; ++y) {
             if (y + kAhead < kAll) k[y + kAhead] = key(y + kAhead);
-            f32x16& acc = x[y / kQSteps];
+            f32x16& acc = s[y / kQSteps];
             acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(k[y]), q[y % kQSteps], acc, 0, 0, 0);
             issue_first();
           }
-#pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            s[0][j] = x[0][j];
-            s[1][j] = x[1][j];
-          }
+          __builtin_amdgcn_s_setprio(1);
         }
         if (ready) {
-          scores.template apply<32>(s[0], rule, tr, ua.pos, half);
-          scores.template apply<32>(s[1], rule, tr, ub.pos, half);
+          scores.template apply<32, 16>(s[0], rule, tr, ua.pos, half);
+          scores.template apply<32, 16>(s[1], rule, tr, ub.pos, half);
           if (masked) {
-            const uint32_t seen_a = mask_scores<32>(s[0], rule, ua, prefix, half);
-            const uint32_t seen_b = mask_scores<32>(s[1], rule, ub, prefix, half);
+            const uint32_t seen_a = mask_scores<32, 16>(s[0], rule, ua, prefix, half);
+            const uint32_t seen_b = mask_scores<32, 16>(s[1], rule, ub, prefix, half);
             const uint32_t bad_a = __builtin_amdgcn_readfirstlane(bad_tok[i & 1][0]);
             const uint32_t bad_b = __builtin_amdgcn_readfirstlane(bad_tok[i & 1][1]);
             if (bad_a) poison |= sees_bad<32, 16>(seen_a, bad_a, half);
@@ -1253,14 +1250,15 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile_kernel
         const float high = top_score(max_column<32>(top), f, scores, mode);
         const bool counts = raise<32, D>(high, st, rows);
         const float ref = finite_max(st.m);
-        auto weigh_score = [&](auto m, float& x) {
-          x = weigh<decltype(m)::value>(x, f, scores, ref);
+        auto weigh_score = [&](auto m, int j) {  // score j of both units' 32
+          const float x = weigh<decltype(m)::value>(s[j >> 4][j & 15], f, scores, ref);
+          s[j >> 4][j & 15] = x;
           st.l += x;
         };
         // O^T += V^T P^T of one unit, a product at a time, each with its share of other work
         auto add_values = [&](int unit, const u32x4_t (&w)[2], auto share) {
           const Ops ops(values + unit * kUnit * kValuePitch<32, D>, lane);
-          constexpr int kAhead = 3;
+          constexpr int kAhead = 2;
           bf16x8 v[Ops::kOps];
 #pragma unroll
           for (int x = 0; x < kAhead; ++x) v[x] = ops[x];
@@ -1284,16 +1282,16 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile_kernel
           if (counts) {
             if (mode == kLinear) {
 #pragma unroll
-              for (int j = 0; j < 32; ++j) weigh_score(std::integral_constant<Mode, kLinear>{}, s[j >> 4][j & 15]);
+              for (int j = 0; j < 32; ++j) weigh_score(std::integral_constant<Mode, kLinear>{}, j);
             } else {
 #pragma unroll
-              for (int j = 0; j < 32; ++j) weigh_score(std::integral_constant<Mode, kExact>{}, s[j >> 4][j & 15]);
+              for (int j = 0; j < 32; ++j) weigh_score(std::integral_constant<Mode, kExact>{}, j);
             }
             u32x4_t w[2], rest[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-              pack_weights(s[h], w);
-              pack_rests(s[h], w, rest);
+              pack_weights<16>(s[h], w);
+              pack_rests<16>(s[h], w, rest);
               add_values(h, w, [](int) {});
               add_values(h, rest, [](int) {});
             }
@@ -1305,13 +1303,13 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile_kernel
           const std::integral_constant<Mode, kUsual> m;
           u32x4_t w[2][2];
 #pragma unroll
-          for (int j = 0; j < 16; ++j) weigh_score(m, s[0][j]);
-          pack_weights(s[0], w[0]);
+          for (int j = 0; j < 16; ++j) weigh_score(m, j);
+          pack_weights<16>(s[0], w[0]);
           add_values(0, w[0], [&](int x) {
             constexpr int kPer = 16 / Ops::kOps;
 #pragma unroll
             for (int j = kPer * x; j < kPer * (x + 1); ++j) {
-              weigh_score(m, s[1][j]);
+              weigh_score(m, 16 + j);
               if (j & 1) w[1][j >> 3][(j >> 1) & 3] = pack2(s[1][j - 1], s[1][j]);
             }
           });
@@ -1346,7 +1344,7 @@ int64_t tile_count(bool ragged, int64_t m, int64_t total_q, int group, int R) {
 
 // Workgroups that run together on the 256 CUs, by what a kernel's registers and LDS allow.
 int64_t slots_of(int rows, int d) {
-  const int per_cu = d == 256 ? 1 : rows != 16 ? 2 : d == 128 ? 3 : 4;
+  const int per_cu = d == 256 ? 1 : d == 64 ? 3 : rows == 16 ? 3 : 2;
   return int64_t{256} * per_cu;
 }
 
