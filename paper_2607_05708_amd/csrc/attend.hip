@@ -71,8 +71,8 @@ struct AttendPlan {
 // ---------------------------------------------------------------- a workgroup's request, rows and units
 
 struct Tile {
-  int64_t req;
-  int64_t q0;     // first query token of the request
+  int req;
+  int q0;         // first query token of the request
   int nq;         // its new tokens
   int r0;         // first row of the tile among the request's rows
   int rows;       // rows in the tile
@@ -82,38 +82,68 @@ struct Tile {
 // these starts leave room for every request's ceil(n G / R) tiles without a scan; the tiles in between are empty.
 // Every wave makes the search by itself, 64 probes at a time.
 template <int R>
-__device__ __forceinline__ bool find_tile(const AttendArgs& a, int64_t t, int group, Tile* out) {
+__device__ __forceinline__ bool find_tile(const AttendArgs& a, uint32_t t, int group, Tile* out) {
+  const int m = static_cast<int>(a.m), total = static_cast<int>(a.total_q);
   if (a.q_offsets) {
+    auto start = [&](int i) { return static_cast<int64_t>(a.q_offsets[i]) * group / R + i; };
     const int lane = threadIdx.x & 63;
-    int64_t lo = 0, n = a.m;
+    int lo = 0, n = m;
     while (n > 0) {
-      const int64_t step = (n + 63) >> 6, i = lane * step;
-      const bool before = i < n && (static_cast<int64_t>(a.q_offsets[lo + i]) * group) / R + lo + i <= t;
+      const int step = (n + 63) >> 6, i = lane * step;
+      const bool before = i < n && start(lo + i) <= t;
       const int last = max(__builtin_popcountll(__ballot(before)) - 1, 0);  // the starts never fall
       lo += last * step;
       if (step == 1) break;
       n = min(step, n - last * step);
     }
-    const int64_t o = a.q_offsets[lo], e = a.q_offsets[lo + 1];
-    if (o < 0 || e > a.total_q || o > e) return false;
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    const int o = a.q_offsets[lo], e = a.q_offsets[lo + 1];
+    if (o < 0 || e > total || o > e || start(lo) > t) return false;
     out->req = lo;
     out->q0 = o;
-    out->nq = static_cast<int>(e - o);
-    t -= o * group / R + lo;
+    out->nq = e - o;
+    t -= static_cast<uint32_t>(start(lo));
   } else {
-    const int64_t nq = a.total_q / a.m;
-    const int64_t per = (nq * group + R - 1) / R;
-    out->req = t / per;
-    out->q0 = out->req * nq;
+    const uint32_t nq = static_cast<uint32_t>(total) / static_cast<uint32_t>(m);
+    const uint32_t per = (nq * group + R - 1) / R;
+    out->req = static_cast<int>(t / per);
+    out->q0 = out->req * static_cast<int>(nq);
     out->nq = static_cast<int>(nq);
     t -= out->req * per;
   }
-  const int64_t r0 = t * R, rows = static_cast<int64_t>(out->nq) * group;
-  if (t < 0 || r0 >= rows) return false;
-  out->r0 = static_cast<int>(r0);
-  out->rows = __builtin_amdgcn_readfirstlane(static_cast<int>(min(static_cast<int64_t>(R), rows - r0)));
+  const int rows = out->nq * group;
+  if (t >= static_cast<uint32_t>((rows + R - 1) / R)) return false;
+  out->r0 = static_cast<int>(t) * R;
+  out->rows = min(R, rows - out->r0);
   return true;
 }
+
+// Sum over the lanes up to this one (row by row, then across rows: no trip through the LDS unit).
+__device__ __forceinline__ int wave_prefix_sum(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
+  const int lane = threadIdx.x & 63;
+  const int r0 = __builtin_amdgcn_readlane(x, 15), r1 = __builtin_amdgcn_readlane(x, 31),
+            r2 = __builtin_amdgcn_readlane(x, 47);
+  return x + (lane >= 48 ? r0 + r1 + r2 : lane >= 32 ? r0 + r1 : lane >= 16 ? r0 : 0);
+}
+
+// Smallest and largest over a fully active wave, in a scalar register.
+template <int CTRL>
+__device__ __forceinline__ int dpp_i32(int x) {
+  return __builtin_amdgcn_update_dpp(0, x, CTRL, 0xF, 0xF, false);
+}
+__device__ __forceinline__ int wave_min(int x) {
+  x = min(x, dpp_i32<0xB1>(x));
+  x = min(x, dpp_i32<0x4E>(x));
+  x = min(x, dpp_i32<0x141>(x));
+  x = min(x, dpp_i32<0x140>(x));
+  return min(min(__builtin_amdgcn_readlane(x, 0), __builtin_amdgcn_readlane(x, 16)),
+             min(__builtin_amdgcn_readlane(x, 32), __builtin_amdgcn_readlane(x, 48)));
+}
+__device__ __forceinline__ int wave_max(int x) { return ~wave_min(~x); }
 
 // The request's chunk list in LDS: cid[c] = chunk of entry c, ub[c] / tb[c] = units / tokens before it; index k of
 // the latter two holds the totals.
@@ -122,10 +152,10 @@ struct ChunkList {
   int k;
 };
 
-__device__ __forceinline__ ChunkList scan_list(const AttendArgs& a, int64_t req, int* lds, int* tmp) {
+__device__ __forceinline__ ChunkList scan_list(const AttendArgs& a, int req, int* lds, int* tmp) {
   const int k = a.k;
   const ChunkList L{lds, lds + k, lds + 2 * k + 1, k};
-  const int32_t* ids = a.ids + req * k;
+  const int32_t* ids = a.ids + static_cast<int64_t>(req) * k;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int cap = a.kv.ppc * a.kv.page_tokens;
   const int per = (k + kThreads - 1) / kThreads;
@@ -140,11 +170,7 @@ __device__ __forceinline__ ChunkList scan_list(const AttendArgs& a, int64_t req,
     u += (len + kUnit - 1) / kUnit;
     t += len;
   }
-  int su = u, st = t;
-  for (int off = 1; off < 64; off <<= 1) {
-    const int pu = __shfl_up(su, off), pt = __shfl_up(st, off);
-    if (lane >= off) { su += pu; st += pt; }
-  }
+  const int su = wave_prefix_sum(u), st = wave_prefix_sum(t);
   if (lane == 63) {
     tmp[2 * wave] = su;
     tmp[2 * wave + 1] = st;
@@ -220,7 +246,7 @@ struct RowRule {
 __device__ __forceinline__ RowRule row_rule(const AttendArgs& a, const Tile& t, int ctx, int g, int group, int r) {
   RowRule x;
   const int j = r / group, h = g * group + r % group;
-  const int64_t at = t.q0 + j;
+  const int at = t.q0 + j;
   x.pos = a.q_pos ? a.q_pos[at] : static_cast<int64_t>(ctx) - t.nq + j;
   x.hi = a.causal ? static_cast<int>(min(max(x.pos, int64_t{-1}), static_cast<int64_t>(kFar))) : kFar;
   x.lo = a.window ? static_cast<int>(min(max(x.pos - a.window + 1, int64_t{0}), static_cast<int64_t>(kFar))) : 0;
@@ -244,8 +270,9 @@ struct TileRule {
 // The rule of a tile whose rows are spread over the lanes of each wave (one or two a lane, repeats allowed).
 template <int R>
 __device__ __forceinline__ TileRule tile_rule(const AttendArgs& a, const Tile& t, int ctx, int g, int group) {
-  const int lane = threadIdx.x & 63;
   TileRule x{kFar, -1, INT32_MAX, -1, 0, kFar, false};
+  if (!a.causal && !a.window && !a.chunk_ns) return TileRule{0, kFar, 0, 0, 0, kFar, false};
+  const int lane = threadIdx.x & 63;
   bool none = false;
 #pragma unroll
   for (int i = 0; i < (R + 63) / 64; ++i) {
@@ -260,23 +287,13 @@ __device__ __forceinline__ TileRule tile_rule(const AttendArgs& a, const Tile& t
       x.ns_hi = max(x.ns_hi, r.ns);
     }
   }
-  for (int off = 1; off < 64; off <<= 1) {
-    x.lo = min(x.lo, __shfl_xor(x.lo, off));
-    x.hi = max(x.hi, __shfl_xor(x.hi, off));
-    x.lo_all = max(x.lo_all, __shfl_xor(x.lo_all, off));
-    x.hi_all = min(x.hi_all, __shfl_xor(x.hi_all, off));
-    if (a.chunk_ns) {
-      x.ns_lo = min(x.ns_lo, __shfl_xor(x.ns_lo, off));
-      x.ns_hi = max(x.ns_hi, __shfl_xor(x.ns_hi, off));
-    }
-  }
   // the same in every lane: scalar registers, and branches that the whole wave takes
-  x.lo = __builtin_amdgcn_readfirstlane(x.lo);
-  x.hi = __builtin_amdgcn_readfirstlane(x.hi);
-  x.lo_all = __builtin_amdgcn_readfirstlane(x.lo_all);
-  x.hi_all = __builtin_amdgcn_readfirstlane(x.hi_all);
-  x.ns_lo = __builtin_amdgcn_readfirstlane(x.ns_lo);
-  x.ns_hi = __builtin_amdgcn_readfirstlane(x.ns_hi);
+  x.lo = wave_min(x.lo);
+  x.hi = wave_max(x.hi);
+  x.lo_all = wave_max(x.lo_all);
+  x.hi_all = wave_min(x.hi_all);
+  x.ns_lo = wave_min(x.ns_lo);
+  x.ns_hi = wave_max(x.ns_hi);
   x.mixed = __any(none) || x.ns_lo != x.ns_hi;
   return x;
 }
@@ -820,12 +837,10 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_few_kernel(
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane % R, part = lane / R;
   const int heads = a.kv.heads, group = a.hq / heads;
-  int64_t b = blockIdx.x;
-  const int g = static_cast<int>(b % heads);
-  b /= heads;
-  const int split = static_cast<int>(b % splits);
+  const uint32_t b = blockIdx.x / static_cast<uint32_t>(heads), tile = b / static_cast<uint32_t>(splits);
+  const int g = static_cast<int>(blockIdx.x - b * heads), split = static_cast<int>(b - tile * splits);
   Tile t;
-  if (!find_tile<R>(a, b / splits, group, &t)) return;
+  if (!find_tile<R>(a, tile, group, &t)) return;
   const ChunkList L = scan_list(a, t.req, dyn, tmp);
   const int ctx = L.tb[a.k];
   const int prefix = a.prefix_len ? __builtin_amdgcn_readfirstlane(min(max(a.prefix_len[t.req], 0), kFar)) : 0;
@@ -839,7 +854,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_few_kernel(
 
   // lane (col, part) holds elements part D / kParts .. of row `col`
   bf16x8 q[kQSteps];
-  load_queries(a.q + (t.q0 + my_row / group) * a.q_ts + (g * group + my_row % group) * a.q_hs + part * (D / kParts), 8, q);
+  load_queries(a.q + static_cast<int64_t>(t.q0 + my_row / group) * a.q_ts + (g * group + my_row % group) * a.q_hs + part * (D / kParts), 8, q);
 
   const Scores scores(a);
   const int64_t T = a.kv.page_tokens;
@@ -876,8 +891,9 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_few_kernel(
     load(pk, u, false);
     load(pv, u, true);
     for (int i = wave; i < n; i += kWaves) {
-      const bool more = i + kWaves < n;
-      const Unit next = uniform_unit(list[more ? i + kWaves : i]);
+      // (loads are not behind a condition, so that the compiler knows how many are in flight behind the one that it
+      // waits for: the last unit is loaded again instead)
+      const Unit next = uniform_unit(list[i + kWaves < n ? i + kWaves : i]);
       float s[kScores];
       if constexpr (R == 16) {
 #pragma unroll
@@ -902,7 +918,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_few_kernel(
 #pragma unroll
         for (int j = 0; j < 16; ++j) s[j] = x[j];
       }
-      if (more) load(pk, next, false);
+      load(pk, next, false);
       const bool ready = u.masked() || scores.bias;
       if (ready) scores.template apply<R, kScores>(s, rule, tr, u.pos, part);
       if (u.masked()) {
@@ -950,7 +966,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_few_kernel(
         for (int h = 0; h < 2; ++h)
           store_values<R, S::kShift>(pv[h], vrows, h * row_step + col, quarter + h * quarter_step);
       }
-      if (more) load(pv, next, true);
+      load(pv, next, true);
       if (counts) {
         __builtin_amdgcn_wave_barrier();
         u32x4_t w[kScores / 8], rest[kScores / 8];
@@ -1016,7 +1032,8 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_few_kernel(
   }
   if (wave > 0 || col >= t.rows) return;
   const int row = t.r0 + col;
-  write_rows<R, D>(a, rows, st, poison, (t.q0 + row / group) * a.hq + g * group + row % group, part, split, splits,
+  write_rows<R, D>(a, rows, st, poison, static_cast<int64_t>(t.q0 + row / group) * a.hq + g * group + row % group, part,
+                   split, splits,
                    part_o, part_ml);
 }
 
@@ -1103,12 +1120,10 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 3) void att
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 31, half = lane >> 5;
   const int heads = a.kv.heads, group = a.hq / heads;
-  int64_t b = blockIdx.x;
-  const int g = static_cast<int>(b % heads);
-  b /= heads;
-  const int split = static_cast<int>(b % splits);
+  const uint32_t b = blockIdx.x / static_cast<uint32_t>(heads), tile = b / static_cast<uint32_t>(splits);
+  const int g = static_cast<int>(blockIdx.x - b * heads), split = static_cast<int>(b - tile * splits);
   Tile t;
-  if (!find_tile<kTileRows>(a, tiles - 1 - b / splits, group, &t)) return;  // the latest rows see most: first
+  if (!find_tile<kTileRows>(a, static_cast<uint32_t>(tiles) - 1 - tile, group, &t)) return;  // the latest rows see most: first
   const ChunkList L = scan_list(a, t.req, dyn, tmp);
   const int ctx = L.tb[a.k];
   const int prefix = a.prefix_len ? __builtin_amdgcn_readfirstlane(min(max(a.prefix_len[t.req], 0), kFar)) : 0;
@@ -1123,7 +1138,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 3) void att
 
   // lane (col, half) holds elements 16 s + 8 half .. + 7 of row `col` of the wave
   bf16x8 q[kQSteps];
-  load_queries(a.q + (t.q0 + my_row / group) * a.q_ts + (g * group + my_row % group) * a.q_hs + 8 * half, 16, q);
+  load_queries(a.q + static_cast<int64_t>(t.q0 + my_row / group) * a.q_ts + (g * group + my_row % group) * a.q_hs + 8 * half, 16, q);
 
   const Scores scores(a);
   const int64_t T = a.kv.page_tokens;
@@ -1331,7 +1346,8 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 3) void att
   st.l = sum_column<32>(st.l);
   poison = any_column<32>(poison, col);
   if (32 * wave + col >= t.rows) return;
-  write_rows<32, D>(a, rows, st, poison, (t.q0 + my_row / group) * a.hq + g * group + my_row % group, half, split,
+  write_rows<32, D>(a, rows, st, poison,
+                    static_cast<int64_t>(t.q0 + my_row / group) * a.hq + g * group + my_row % group, half, split,
                     splits, part_o, part_ml);
 }
 
