@@ -543,13 +543,11 @@ def _used_on(stream, *tensors):
                 t.record_stream(stream)
 
 
-def _i32(t: torch.Tensor | None, shape: tuple, name: str, dtype=torch.int32):
-    """Pointer of a contiguous GPU array of the given shape (None: NULL)."""
-    if t is None:
-        return None
-    if (not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != dtype or t.shape != shape
+def _array(t: torch.Tensor, shape: tuple, name: str, dev: int, dtype=torch.int32) -> int:
+    """Pointer of a contiguous array of the given shape on GPU `dev`."""
+    if (not isinstance(t, torch.Tensor) or t.get_device() != dev or t.dtype is not dtype or t.shape != shape
             or not t.is_contiguous()):
-        raise ValueError(f"{name} must be a contiguous {dtype} {list(shape)} GPU tensor")
+        raise ValueError(f"{name} must be a contiguous {dtype} {list(shape)} tensor on the cache's GPU")
     return t.data_ptr()
 
 
@@ -574,30 +572,34 @@ class KvCache:
             raise ValueError("pool must be contiguous [n_pages, page_bytes]")
         if table.dim() != 2:
             raise ValueError("table must be int32 [n_chunks, pages_per_chunk]")
-        ptr = _i32(table, tuple(table.shape), "table")
-        if table.device != pool.device:
-            raise ValueError("table must be on the pool's device")
+        self._dev = pool.get_device()
+        ptr = _array(table, tuple(table.shape), "table", self._dev)
         self.pool, self.table = pool, table
         self.page_tokens, self.heads, self.head_dim, self.format = page_tokens, heads, head_dim, format
         pages = MemPages(pool.data_ptr(), pool.shape[0], pool.shape[1] * pool.element_size(), ptr, table.shape[0],
                          table.shape[1])
         self._c = MemKv(pages, page_tokens, heads, head_dim, format)
+        self._ref = C.byref(self._c)
 
 
-def _kv_rows(cache: KvCache, t: torch.Tensor, n: int, dtype, name: str) -> MemKvRows:
-    if (not isinstance(t, torch.Tensor) or t.device != cache.pool.device or t.dtype != dtype
-            or t.shape != (n, cache.heads, cache.head_dim) or (n and t.stride(2) != 1)):
-        raise ValueError(f"{name} must be {dtype} [{n}, {cache.heads}, {cache.head_dim}] on the cache's GPU with "
-                         "unit stride along the last dimension")
-    return MemKvRows(t.data_ptr(), t.stride(0), t.stride(1))
+_KV_DTYPES = {torch.float32: MEM_F32, torch.bfloat16: MEM_BF16}
+
+
+def _kv_rows(cache: KvCache, t: torch.Tensor, n: int, dtype, name: str):
+    if (not isinstance(t, torch.Tensor) or t.get_device() != cache._dev or t.dtype is not dtype
+            or t.shape != (n, cache.heads, cache.head_dim)):
+        raise ValueError(f"{name} must be {dtype} [{n}, {cache.heads}, {cache.head_dim}] on the cache's GPU")
+    token, head, one = t.stride()
+    if one != 1 and n:
+        raise ValueError(f"{name} must have unit stride along its last dimension")
+    return C.byref(MemKvRows(t.data_ptr(), token, head))
 
 
 def _kv_dtype(dtype) -> int:
-    if dtype == torch.float32:
-        return MEM_F32
-    if dtype == torch.bfloat16:
-        return MEM_BF16
-    raise TypeError(f"keys and values must be float32 or bfloat16, got {dtype}")
+    code = _KV_DTYPES.get(dtype)
+    if code is None:
+        raise TypeError(f"keys and values must be float32 or bfloat16, got {dtype}")
+    return code
 
 
 def mem_kv_write(cache: KvCache, k: torch.Tensor, v: torch.Tensor, chunk: torch.Tensor, pos: torch.Tensor, *,
@@ -605,10 +607,11 @@ def mem_kv_write(cache: KvCache, k: torch.Tensor, v: torch.Tensor, chunk: torch.
     """Quantise tokens into the cache: rows i of ``k`` and ``v`` ([n, heads, head_dim], float32 or bfloat16, any
     token and head strides) become token ``pos[i]`` of chunk ``chunk[i]`` (int32 [n]).  A chunk of -1 skips the
     token; no two tokens may name one place."""
-    n, dt = k.shape[0], _kv_dtype(k.dtype)
-    kr, vr = _kv_rows(cache, k, n, k.dtype, "k"), _kv_rows(cache, v, n, k.dtype, "v")
-    _check("mem_kv_write", lib().mem_kv_write(C.byref(cache._c), C.byref(kr), C.byref(vr), dt,
-                                              _i32(chunk, (n,), "chunk"), _i32(pos, (n,), "pos"), n, _stream(stream)))
+    n, dtype, dev = k.shape[0], k.dtype, cache._dev
+    status = lib().mem_kv_write(cache._ref, _kv_rows(cache, k, n, dtype, "k"), _kv_rows(cache, v, n, dtype, "v"),
+                                _kv_dtype(dtype), _array(chunk, (n,), "chunk", dev), _array(pos, (n,), "pos", dev), n,
+                                _stream(stream))
+    _check("mem_kv_write", status)
 
 
 def mem_kv_read(cache: KvCache, chunk: torch.Tensor, pos: torch.Tensor, *, dtype=torch.bfloat16, out=None,
@@ -616,21 +619,23 @@ def mem_kv_read(cache: KvCache, chunk: torch.Tensor, pos: torch.Tensor, *, dtype
     """Tokens ``pos[i]`` of chunks ``chunk[i]`` (int32 [n]) as dense rows: (k, v), each [n, heads, head_dim] of
     ``dtype`` (or written into ``out``, a pair of such tensors).  Both dtypes hold the cache's values exactly;
     places outside the cache give zeros."""
-    n = chunk.shape[0]
+    n, dev = chunk.shape[0], cache._dev
     if out is None:
-        out = tuple(torch.empty((n, cache.heads, cache.head_dim), dtype=dtype, device=cache.pool.device)
-                    for _ in range(2))
-        _used_on(stream, *out)
-    k, v = out
-    dt = _kv_dtype(k.dtype)
-    kr, vr = _kv_rows(cache, k, n, k.dtype, "out k"), _kv_rows(cache, v, n, k.dtype, "out v")
-    _check("mem_kv_read", lib().mem_kv_read(C.byref(cache._c), C.byref(kr), C.byref(vr), dt,
-                                            _i32(chunk, (n,), "chunk"), _i32(pos, (n,), "pos"), n, _stream(stream)))
+        k = torch.empty((n, cache.heads, cache.head_dim), dtype=dtype, device=cache.pool.device)
+        v = torch.empty_like(k)
+        _used_on(stream, k, v)
+    else:
+        k, v = out
+        dtype = k.dtype
+    status = lib().mem_kv_read(cache._ref, _kv_rows(cache, k, n, dtype, "out k"),
+                               _kv_rows(cache, v, n, dtype, "out v"), _kv_dtype(dtype),
+                               _array(chunk, (n,), "chunk", dev), _array(pos, (n,), "pos", dev), n, _stream(stream))
+    _check("mem_kv_read", status)
     return k, v
 
 
 def mem_attend_workspace_bytes(cache: KvCache, m: int, k: int, total_q: int, heads_q: int) -> int:
-    return int(lib().mem_attend_workspace_bytes(C.byref(cache._c), m, k, total_q, heads_q))
+    return int(lib().mem_attend_workspace_bytes(cache._ref, m, k, total_q, heads_q))
 
 
 def mem_attend(cache: KvCache, tok_len: torch.Tensor, ids: torch.Tensor, q: torch.Tensor, scale: float, *,
@@ -654,28 +659,34 @@ def mem_attend(cache: KvCache, tok_len: torch.Tensor, ids: torch.Tensor, q: torc
         raise ValueError("ids must be int32 [m, k]; q bfloat16 [total_q, heads_q, head_dim]")
     m, k = ids.shape
     total_q, heads_q, d = q.shape
-    dev, n_chunks = cache.pool.device, cache.table.shape[0]
-    if q.dtype != torch.bfloat16 or q.device != dev or d != cache.head_dim or (total_q and q.stride(2) != 1):
+    dev, n_chunks = cache._dev, cache.table.shape[0]
+    token, head, one = q.stride()
+    if q.dtype is not torch.bfloat16 or q.get_device() != dev or d != cache.head_dim or (total_q and one != 1):
         raise ValueError(f"q must be bfloat16 [total_q, heads_q, {cache.head_dim}] on the cache's GPU with unit "
                          "stride along the last dimension")
-    a = MemAttendArgs(_i32(tok_len, (n_chunks,), "tok_len"), _i32(ids, (m, k), "ids"), m, k, heads_q,
-                      _i32(q_offsets, (m + 1,), "q_offsets"), _i32(q_pos, (total_q,), "q_pos"), scale, softcap,
-                      _i32(slopes, (heads_q,), "slopes", torch.float32), 1 if causal else 0, window,
-                      _i32(prefix_len, (m,), "prefix_len"), _i32(chunk_ns, (n_chunks,), "chunk_ns"),
-                      _i32(query_ns, (total_q,), "query_ns"))
+    a = MemAttendArgs(
+        _array(tok_len, (n_chunks,), "tok_len", dev), _array(ids, (m, k), "ids", dev), m, k, heads_q,
+        None if q_offsets is None else _array(q_offsets, (m + 1,), "q_offsets", dev),
+        None if q_pos is None else _array(q_pos, (total_q,), "q_pos", dev), scale, softcap,
+        None if slopes is None else _array(slopes, (heads_q,), "slopes", dev, torch.float32), 1 if causal else 0, window,
+        None if prefix_len is None else _array(prefix_len, (m,), "prefix_len", dev),
+        None if chunk_ns is None else _array(chunk_ns, (n_chunks,), "chunk_ns", dev),
+        None if query_ns is None else _array(query_ns, (total_q,), "query_ns", dev))
     if out is None:
-        out = (torch.empty((total_q, heads_q, d), dtype=torch.bfloat16, device=dev),
-               torch.empty((total_q, heads_q), dtype=torch.float32, device=dev))
-        _used_on(stream, *out)
-    o, lse = out
+        o = torch.empty((total_q, heads_q, d), dtype=torch.bfloat16, device=q.device)
+        lse = torch.empty((total_q, heads_q), dtype=torch.float32, device=q.device)
+        _used_on(stream, o, lse)
+        o_ptr, lse_ptr = o.data_ptr(), lse.data_ptr()
+    else:
+        o, lse = out
+        o_ptr = _array(o, (total_q, heads_q, d), "out", dev, torch.bfloat16)
+        lse_ptr = None if lse is None else _array(lse, (total_q, heads_q), "out lse", dev, torch.float32)
     if workspace is None:
-        size = mem_attend_workspace_bytes(cache, m, k, total_q, heads_q)
-        workspace = torch.empty(max(size, 1), dtype=torch.uint8, device=dev)
+        workspace = torch.empty(max(mem_attend_workspace_bytes(cache, m, k, total_q, heads_q), 1), dtype=torch.uint8,
+                                device=q.device)
         _used_on(stream, workspace)
     _dev(workspace, "workspace")
-    _check("mem_attend", lib().mem_attend(C.byref(cache._c), C.byref(a), q.data_ptr(), total_q, q.stride(0),
-                                          q.stride(1), _i32(o, (total_q, heads_q, d), "out", torch.bfloat16),
-                                          _i32(lse, (total_q, heads_q), "out lse", torch.float32),
-                                          workspace.data_ptr(), workspace.numel() * workspace.element_size(),
-                                          _stream(stream)))
+    status = lib().mem_attend(cache._ref, C.byref(a), q.data_ptr(), total_q, token, head, o_ptr, lse_ptr,
+                              workspace.data_ptr(), workspace.nbytes, _stream(stream))
+    _check("mem_attend", status)
     return o, lse
