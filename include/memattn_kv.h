@@ -138,15 +138,16 @@ MEMATTN_API size_t mem_attend_workspace_bytes(const mem_kv* kv, int64_t m, int32
  *   out   = sum over a(p) of exp(s(p) - lse) * V_pg
  * A token that sees nothing gets out = 0 and lse = -inf, and so does every
  * token of an empty context.  Tokens that a query does not see have no
- * influence on it, whatever they hold; a non-finite value among those that it
- * does see makes its output non-finite.
+ * influence on it, whatever they hold; a value that is not finite among those
+ * that it does see makes its output so, however small its weight (keys that
+ * only make a score -inf hide their token).
  * q (device bf16, [total_q, heads_q, head_dim] with the strides given) is only
  * read; out (device bf16) and lse (device fp32, nullable) are [total_q,
  * heads_q, head_dim] and [total_q, heads_q], contiguous; out is 16-byte
  * aligned.  Products are bf16 with fp32 sums; the softmax weights are rounded
- * to bf16 for the second product and out is divided by the rounded weights'
- * sum, lse is that of the unrounded ones.  Rows of q that no request owns are
- * not written.  The context lengths are read on the device: nothing
+ * to bf16 for the second product (heavy ones to 16 bits) and out is divided by
+ * the unrounded weights' sum, which is also lse's.  Rows of q that no request
+ * owns are not written.  The context lengths are read on the device: nothing
  * is synchronised, and the call can be captured into a HIP graph.
  */
 MEMATTN_API mem_status mem_attend(const mem_kv* kv, const mem_attend_args* args, const void* q, int64_t total_q,

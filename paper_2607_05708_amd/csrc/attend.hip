@@ -40,6 +40,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
@@ -440,9 +441,11 @@ __device__ __forceinline__ bool piece_bad(const Piece<FMT, D>& p) {
       bad |= (((p.w[i] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) != 0;
   }
   if constexpr (FMT == MEM_KV_BF16) {
+    u16x2 most = {0, 0};
 #pragma unroll
     for (int i = 0; i < Dim<FMT, D>::kWords; ++i)
-      bad |= (p.w[i] & 0x7F80u) == 0x7F80u || (p.w[i] & 0x7F800000u) == 0x7F800000u;
+      most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, p.w[i] & 0x7FFF7FFFu));
+    bad = most[0] >= 0x7F80u || most[1] >= 0x7F80u;
   }
   return bad;
 }
@@ -604,8 +607,6 @@ struct RowState {
   float l;
 };
 constexpr float kLag = 8.f;
-// Scores this far (log2) below the maximum are left out: 2^24 of them change no fp32 sum.
-constexpr float kNothing = 48.f;
 // The weights are rounded to bf16 for the second product.  Where one weighs more than 1 / kHeavy of its lane's sum so
 // far, rounding it would show in the output, and the product is made a second time with what the rounding left (16
 // bits of weight in all); smaller weights' roundings average out.  The sum is that of the unrounded ones.
@@ -664,10 +665,11 @@ __device__ __forceinline__ float top_score(float top, float f, const Scores& sc,
   return mode == kSeries ? top * sc.series(top) : sc.cap2 - 2.f * sc.cap2 * sc.fraction(top);
 }
 
-// Whether a unit with this largest score weighs anything in the wave; raises the running maximum if it has to.
+// Whether some row of the wave sees something of a unit with this largest score (what weighs little is not left out:
+// its values may be large, or no numbers); raises the running maximum if it has to.
 template <int WIDTH, int D>
 __device__ __forceinline__ bool raise(float top, RowState& st, Rows<WIDTH, D>& rows) {
-  if (!__any(!(top <= st.m - kNothing))) return false;
+  if (!__any(top != -INFINITY)) return false;
   if (__any(top > st.m + kLag)) {
     const float mn = fmaxf(st.m, top);
     const float r = mn == -INFINITY ? 1.f : fast_exp2(st.m - mn);
@@ -1369,10 +1371,21 @@ int64_t slots_of(int rows, int d) {
 // rows that fill the GPU are left whole: causal ones are of unequal length, and even out by themselves.
 constexpr int64_t kStart = 16;
 
-AttendPlan make_plan(int d, int64_t m, int64_t units, int64_t total_q, int heads, int heads_q, bool ragged) {
+// Bytes of LDS that a workgroup's chunk list takes.
+size_t list_bytes(int k) { return (3 * static_cast<size_t>(k) + 2) * sizeof(int); }
+
+// Tiles of 128 rows of heads of 256 leave 18 KB of a CU's 160 KB for the chunk list: calls with longer lists (more than
+// 1,535 chunks a request) take the tiles of 32 rows, whose values leave 77 KB (the longest list takes 48).
+bool list_fits_tiles(int d, int k) { return d < 256 || list_bytes(k) <= 18 * 1024; }
+static_assert(2 * sizeof(uint16_t) * (TileShape<MEM_KV_BF16, 256>::kKeys + TileShape<MEM_KV_BF16, 256>::kValues) +
+                      (TileShape<MEM_KV_BF16, 256>::kBatch + 6) * sizeof(Unit) + 128 + 18 * 1024 <=
+                  160 * 1024,
+              "a workgroup's LDS");
+
+AttendPlan make_plan(int d, int64_t m, int k, int64_t units, int64_t total_q, int heads, int heads_q, bool ragged) {
   AttendPlan p;
   const int group = heads_q / heads;
-  p.rows = total_q * group <= 16 * m ? 16 : total_q * group <= 64 * m ? 32 : kTileRows;
+  p.rows = total_q * group <= 16 * m ? 16 : total_q * group <= 64 * m || !list_fits_tiles(d, k) ? 32 : kTileRows;
   p.tiles = tile_count(ragged, m, total_q, group, p.rows);
   const int64_t work = p.tiles * heads, slots = slots_of(p.rows, d);
   int64_t best = INT64_MAX;
@@ -1401,7 +1414,7 @@ hipError_t launch_dim(const AttendArgs& a, const AttendPlan& p, hipStream_t stre
                                                          partial_o_bytes(D, a.total_q, a.hq, p.splits))
                              : nullptr;
   const dim3 grid(static_cast<unsigned>(p.tiles * a.kv.heads * p.splits));
-  const size_t lds = (3 * static_cast<size_t>(a.k) + 2) * sizeof(int);
+  const size_t lds = list_bytes(a.k);
   if (p.rows == 16)
     attend_few_kernel<FMT, D, 16><<<grid, kThreads, lds, stream>>>(a, p.splits, po, pml);
   else if (p.rows == 32)
@@ -1427,11 +1440,11 @@ hipError_t launch_fmt(const AttendArgs& a, const AttendPlan& p, int d, hipStream
 }  // namespace
 
 // The larger of the two forms of a call (ragged or not), so that one size serves both.
-size_t attend_workspace_bytes(int d, int64_t m, int64_t units, int64_t total_q, int heads, int heads_q) {
+size_t attend_workspace_bytes(int d, int64_t m, int k, int64_t units, int64_t total_q, int heads, int heads_q) {
   size_t need = 0;
   for (int ragged = 0; ragged < 2; ++ragged) {
     if (!ragged && total_q % m != 0) continue;
-    const int s = make_plan(d, m, units, total_q, heads, heads_q, ragged != 0).splits;
+    const int s = make_plan(d, m, k, units, total_q, heads, heads_q, ragged != 0).splits;
     if (s == 1) continue;
     const size_t b = partial_o_bytes(d, total_q, heads_q, s) +
                      align256(static_cast<size_t>(s) * total_q * heads_q * sizeof(RowState));
@@ -1440,14 +1453,14 @@ size_t attend_workspace_bytes(int d, int64_t m, int64_t units, int64_t total_q, 
   return need;
 }
 
-bool attend_fits(int d, int64_t m, int64_t units, int64_t total_q, int heads, int heads_q, bool ragged) {
-  const AttendPlan p = make_plan(d, m, units, total_q, heads, heads_q, ragged);
+bool attend_fits(int d, int64_t m, int k, int64_t units, int64_t total_q, int heads, int heads_q, bool ragged) {
+  const AttendPlan p = make_plan(d, m, k, units, total_q, heads, heads_q, ragged);
   return p.tiles * p.splits <= INT32_MAX / heads;
 }
 
 hipError_t launch_attend(const AttendArgs& a, int fmt, int d, hipStream_t stream) {
   const int64_t units = static_cast<int64_t>(a.k) * a.kv.ppc * a.kv.page_tokens / kUnit;
-  const AttendPlan p = make_plan(d, a.m, units, a.total_q, a.kv.heads, a.hq, a.q_offsets != nullptr);
+  const AttendPlan p = make_plan(d, a.m, a.k, units, a.total_q, a.kv.heads, a.hq, a.q_offsets != nullptr);
   switch (fmt) {
     case MEM_KV_BF16: return launch_fmt<MEM_KV_BF16>(a, p, d, stream);
     case MEM_KV_FP8: return launch_fmt<MEM_KV_FP8>(a, p, d, stream);

@@ -68,9 +68,9 @@ hipError_t launch_kv_write(const KvView& kv, int fmt, int d, const RowsView& k, 
 hipError_t launch_kv_read(const KvView& kv, int fmt, int d, const RowsView& k, const RowsView& v, int dtype,
                           const int32_t* chunk, const int32_t* pos, int64_t n, hipStream_t stream);
 // `units`: blocks of 32 tokens that a request's chunks can hold.
-size_t attend_workspace_bytes(int d, int64_t m, int64_t units, int64_t total_q, int heads, int heads_q);
+size_t attend_workspace_bytes(int d, int64_t m, int k, int64_t units, int64_t total_q, int heads, int heads_q);
 // Whether the call's workgroups fit one launch.
-bool attend_fits(int d, int64_t m, int64_t units, int64_t total_q, int heads, int heads_q, bool ragged);
+bool attend_fits(int d, int64_t m, int k, int64_t units, int64_t total_q, int heads, int heads_q, bool ragged);
 hipError_t launch_attend(const AttendArgs& a, int fmt, int d, hipStream_t stream);
 
 #ifdef __HIPCC__

@@ -168,7 +168,7 @@ size_t mem_attend_workspace_bytes(const mem_kv* kv, int64_t m, int32_t k, int64_
   clear_error();
   if (check_sizes(kv, m, k, total_q, heads_q) != MEM_OK || m == 0 || total_q == 0) return 0;
   const int64_t units = static_cast<int64_t>(k) * kv->pages.pages_per_chunk * kv->page_tokens / 32;
-  return attend_workspace_bytes(kv->head_dim, m, units, total_q, kv->heads, heads_q);
+  return attend_workspace_bytes(kv->head_dim, m, k, units, total_q, kv->heads, heads_q);
 }
 
 mem_status mem_attend(const mem_kv* kv, const mem_attend_args* a, const void* q, int64_t total_q,
@@ -199,9 +199,9 @@ mem_status mem_attend(const mem_kv* kv, const mem_attend_args* a, const void* q,
     return fail(MEM_ERR_INVALID_ARG, "an int32 or float array is not 4-byte aligned");
   if (q_token_stride < 0 || q_head_stride < 0) return fail(MEM_ERR_INVALID_ARG, "negative stride of q");
   const int64_t units = static_cast<int64_t>(a->k) * kv->pages.pages_per_chunk * kv->page_tokens / 32;
-  if (!attend_fits(kv->head_dim, a->m, units, total_q, kv->heads, a->heads_q, a->q_offsets != nullptr))
+  if (!attend_fits(kv->head_dim, a->m, a->k, units, total_q, kv->heads, a->heads_q, a->q_offsets != nullptr))
     return fail(MEM_ERR_UNSUPPORTED, "too many requests and heads for one launch");
-  const size_t need = attend_workspace_bytes(kv->head_dim, a->m, units, total_q, kv->heads, a->heads_q);
+  const size_t need = attend_workspace_bytes(kv->head_dim, a->m, a->k, units, total_q, kv->heads, a->heads_q);
   if (need > 0 && !workspace) return fail(MEM_ERR_WORKSPACE, "workspace is NULL");
   if (need > 0 && !aligned(workspace, 16)) return fail(MEM_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
   if (ws_bytes < need) return fail(MEM_ERR_WORKSPACE, "workspace of %zu bytes < %zu needed", ws_bytes, need);

@@ -400,6 +400,32 @@ def test_a_value_that_is_not_finite_reaches_the_rows_that_see_it(nq):
     assert (~np.isfinite(out[sees])).any(axis=-1).all()
 
 
+@pytest.mark.parametrize("name,value", [("bf16", np.inf), ("fp8", np.nan), ("fp4", np.nan)])
+@pytest.mark.parametrize("nq", [1, 12, 90])
+def test_a_value_that_is_not_finite_shows_from_afar(name, value, nq):
+    # a distance bias so steep that the token's weight is zero in fp32: zero times its value is no number
+    fmt = FMTS[name]
+    p = Problem(14, fmt, [[64] * 9], [nq], 4, 2, 64)
+    p.slopes[:] = 8.0
+    p.check("far tokens", causal=True, bias=True)
+    page, row, _ = p.ctx[0][100]
+    x = np.ones((2, 64))
+    x[:, 5] = value
+    ref.put(fmt, 32, p.pool, page, row, np.zeros((2, 64)), x)
+    out, _ = p.gpu(causal=True, bias=True)
+    assert (~np.isfinite(out)).any(axis=-1).all()
+
+
+@pytest.mark.parametrize("nq", [1, 12, 90])
+def test_a_large_value_counts_at_a_small_weight(nq):
+    # 1e32 with weights from e^-75 on, and less the further a token is from it
+    p = Problem(15, ref.BF16, [[64] * 3], [nq], 4, 2, 64)
+    p.slopes[:] = 1.0
+    page, row, _ = p.ctx[0][192 - nq - 75]
+    ref.put(ref.BF16, 32, p.pool, page, row, np.zeros((2, 64)), np.full((2, 64), 1e32))
+    p.check("far value", causal=True, bias=True)
+
+
 def test_odd_query_strides():
     p = Problem(9, ref.FP4, [[64, 40], [64]], [3, 21], 4, 2, 64)
     want = p.gpu(causal=True)
@@ -474,6 +500,15 @@ def test_long_list_of_small_chunks(d, n_chunks, k):
             want = ref.attend(host(q)[i * nq:(i + 1) * nq], rk[rows], rv[rows], None, np.ones(n, bool),
                               np.arange(nq) + n - nq, None, 0.125, True, 0, 0, 0.0, None)
             ref.check_attend(f"request {i}", out[i * nq:(i + 1) * nq], lse[i * nq:(i + 1) * nq], *want)
+
+
+@pytest.mark.parametrize("d,k", [(256, 1535), (256, 1536), (256, 4096), (128, 4096)])
+def test_many_rows_behind_a_long_list(d, k):
+    # a list that does not fit beside the tiles of wide heads in LDS
+    rng = np.random.default_rng(k)
+    lens = [[int(x) for x in rng.integers(0, 33, 40)], [32, 7]]
+    p = Problem(k, ref.FP4, lens, [40, 9], 8, 1, d, ppc=1, k=k, holes=True)
+    p.check("long list", causal=True)
 
 
 def test_offsets_beyond_32_bits():
