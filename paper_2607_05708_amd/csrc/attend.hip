@@ -79,13 +79,54 @@ struct Tile {
   int rows;       // rows in the tile
 };
 
-// Request and rows of tile t.  With ragged requests tile t of request i is tile floor(q_offsets[i] G / R) + i + t:
-// these starts leave room for every request's ceil(n G / R) tiles without a scan; the tiles in between are empty.
-// Every wave makes the search by itself, 64 probes at a time.
+// Sum over the lanes up to this one (row by row, then across rows: no trip through the LDS unit).
+__device__ __forceinline__ int wave_prefix_sum(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
+  const int lane = threadIdx.x & 63;
+  const int r0 = __builtin_amdgcn_readlane(x, 15), r1 = __builtin_amdgcn_readlane(x, 31),
+            r2 = __builtin_amdgcn_readlane(x, 47);
+  return x + (lane >= 48 ? r0 + r1 + r2 : lane >= 32 ? r0 + r1 : lane >= 16 ? r0 : 0);
+}
+
+// Request and rows of tile t.  With ragged requests there are ceil(n G / R) tiles for each; every wave adds them up by
+// itself, 64 requests at a time, as long as there are few (kCounted) requests.  With more, tile t of request i is tile
+// floor(q_offsets[i] G / R) + i + t: these starts leave room for every request's tiles and can be searched without a
+// sum, 64 probes at a time; some of the tiles are empty.  (Empty tiles between the others cost more than their start:
+// workgroups go to the XCDs and their shader engines in turn, and with one empty tile for each that is not only half
+// of them got work: 64 requests of 128 rows over 16,384 tokens 1.20 ms, added up 0.66 ms.)
+constexpr int kCounted = 512;
 template <int R>
 __device__ __forceinline__ bool find_tile(const AttendArgs& a, uint32_t t, int group, Tile* out) {
   const int m = static_cast<int>(a.m), total = static_cast<int>(a.total_q);
-  if (a.q_offsets) {
+  if (a.q_offsets && m <= kCounted) {
+    const int lane = threadIdx.x & 63;
+    int at = -1, first = 0, o = 0, e = 0;  // request, its first tile, its tokens
+    for (int i0 = 0; i0 < m && at < 0; i0 += 64) {
+      const int i = i0 + lane;
+      const int from = i < m ? a.q_offsets[i] : 0, to = i < m ? a.q_offsets[i + 1] : 0;
+      const int64_t n = min(max(static_cast<int64_t>(to) - from, int64_t{0}), a.total_q);
+      const int mine = static_cast<int>((n * group + R - 1) / R);
+      const int upto = wave_prefix_sum(mine);
+      const uint64_t after = __ballot(first + upto > static_cast<int64_t>(t));
+      if (after) {
+        const int l = __builtin_ctzll(after);
+        at = i0 + l;
+        o = __builtin_amdgcn_readlane(from, l);
+        e = __builtin_amdgcn_readlane(to, l);
+        first += __builtin_amdgcn_readlane(upto - mine, l);
+      } else {
+        first += __builtin_amdgcn_readlane(upto, 63);
+      }
+    }
+    if (at < 0 || o < 0 || e > total || o > e) return false;
+    out->req = at;
+    out->q0 = o;
+    out->nq = e - o;
+    t -= static_cast<uint32_t>(first);
+  } else if (a.q_offsets) {
     auto start = [&](int i) { return static_cast<int64_t>(a.q_offsets[i]) * group / R + i; };
     const int lane = threadIdx.x & 63;
     int lo = 0, n = m;
@@ -117,18 +158,6 @@ __device__ __forceinline__ bool find_tile(const AttendArgs& a, uint32_t t, int g
   out->r0 = static_cast<int>(t) * R;
   out->rows = min(R, rows - out->r0);
   return true;
-}
-
-// Sum over the lanes up to this one (row by row, then across rows: no trip through the LDS unit).
-__device__ __forceinline__ int wave_prefix_sum(int x) {
-  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
-  const int lane = threadIdx.x & 63;
-  const int r0 = __builtin_amdgcn_readlane(x, 15), r1 = __builtin_amdgcn_readlane(x, 31),
-            r2 = __builtin_amdgcn_readlane(x, 47);
-  return x + (lane >= 48 ? r0 + r1 + r2 : lane >= 32 ? r0 + r1 : lane >= 16 ? r0 : 0);
 }
 
 // Smallest and largest over a fully active wave, in a scalar register.
@@ -573,31 +602,23 @@ struct Scores {
   }
 };
 
-// Masks of one unit's scores, looked at one by one.  Returns the scores that are seen as bits.
-template <int WIDTH, int N, typename V>
-__device__ __forceinline__ uint32_t mask_scores(V& s, const RowRule& rule, const Unit& u, int prefix, int part) {
-  const int first = u.pos + 4 * part;  // position of a score whose token offset is 0
-  const int held = u.held() - 4 * part, pre = prefix - first, lo = rule.lo - first, hi = rule.hi - first;
-  const bool mine = u.ns == rule.ns;
-  uint32_t seen = 0;
-#pragma unroll
-  for (int j = 0; j < N; ++j) {
-    const int tok = score_token<WIDTH>(j);
-    const bool see = mine && tok < held && (tok < pre || (tok >= lo && tok <= hi));
-    seen |= see ? 1u << j : 0u;
-    s[j] = see ? s[j] : -INFINITY;
-  }
-  return seen;
+// Tokens of a unit that a row sees, as bits.
+__device__ __forceinline__ uint32_t visible_tokens(const RowRule& rule, const Unit& u, int prefix) {
+  auto below = [](int n) { return n <= 0 ? 0u : n >= kUnit ? ~0u : (1u << n) - 1; };
+  const uint32_t near = below(rule.hi - u.pos + 1) & ~below(rule.lo - u.pos);
+  return u.ns == rule.ns ? (near | below(prefix - u.pos)) & below(u.held()) : 0;
 }
 
-// Whether a seen score's token is among the unit's tokens with values that are not finite.
-template <int WIDTH, int N>
-__device__ __forceinline__ bool sees_bad(uint32_t seen, uint32_t bad, int part) {
-  bad >>= 4 * part;
-  uint32_t hit = 0;
+// Scores of the tokens that a row does not see become -inf.
+template <int WIDTH, int N, typename V>
+__device__ __forceinline__ void mask_scores(V& s, uint32_t seen, int part) {
+  seen >>= 4 * part;
 #pragma unroll
-  for (int j = 0; j < N; ++j) hit |= (seen >> j) & (bad >> score_token<WIDTH>(j)) & 1u;
-  return hit != 0;
+  for (int j = 0; j < N; ++j) {
+    const uint32_t keep = static_cast<uint32_t>(static_cast<int32_t>(seen << (31 - score_token<WIDTH>(j))) >> 31);
+    const float x = s[j];
+    s[j] = __uint_as_float((__float_as_uint(x) & keep) | (0xFF800000u & ~keep));
+  }
 }
 
 // Running softmax of a row, in every lane that holds its scores: maximum (it may lag by kLag: weights up to 2^kLag
@@ -925,7 +946,8 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_few_kernel(
       if (ready) scores.template apply<R, kScores>(s, rule, tr, u.pos, part);
       if (u.masked()) {
         const int held = u.held();
-        const uint32_t seen = mask_scores<R, kScores>(s, rule, u, prefix, part);
+        const uint32_t seen = visible_tokens(rule, u, prefix);
+        mask_scores<R, kScores>(s, seen, part);
         uint32_t bad = 0;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -937,7 +959,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_few_kernel(
           bad |= static_cast<uint32_t>(R == 16 ? vote & 0xFFFFu : vote) << (h * row_step);
           if (nf || row >= held) piece_clear<FMT, D>(pv[h]);
         }
-        if (bad) poison |= sees_bad<R, kScores>(seen, bad, part);
+        poison |= (seen & bad) != 0;
       }
       bool small = false;
       if (!ready && scores.cap2 != 0.f) {
@@ -1117,7 +1139,9 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 3) void att
   __shared__ __align__(16) uint16_t value_rows[2][S::kValues];
   __shared__ Unit list[S::kBatch + 6];  // (read some steps ahead)
   __shared__ int tmp[2 * kWaves];
-  __shared__ uint32_t bad_tok[2][2];  // tokens of a masked step's units whose values are not finite
+  // Tokens of a masked step's units whose values are not finite: of the step at hand, of the next, and of the one
+  // after that, which is cleared (so that a barrier stands between clearing and noting, and between noting and reading).
+  __shared__ uint32_t bad_tok[3][2];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 31, half = lane >> 5;
@@ -1163,6 +1187,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 3) void att
                                            min(S::kBatch, last - u0 + 1), list, tmp);
     if (n == 0) continue;
     if (tid == 0) list[n] = Unit{0, Unit::kMasked, 0, -1};  // fills up the last step: holds nothing
+    if (tid < 4) bad_tok[tid >> 1][tid & 1] = 0;
     __syncthreads();
     const int steps = (n + 1) / 2;
     auto load = [&](const Unit& u) {
@@ -1188,12 +1213,10 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 3) void att
             piece_step<FMT, D>(pv, y);
       }
     };
-    // values of a masked step that are not finite are noted and left out (every thread of the workgroup calls this)
-    auto check_bad = [&](int i) {
-      if (tid < 2) bad_tok[i & 1][tid] = 0;
-      __syncthreads();
+    // values of a masked step that are not finite are noted and left out
+    auto check_bad = [&](int to) {
       if (piece_bad<FMT, D>(pv)) {
-        atomicOr(&bad_tok[i & 1][my_unit], 1u << (tok % kUnit));
+        atomicOr(&bad_tok[to][my_unit], 1u << (tok % kUnit));
         piece_clear<FMT, D>(pv);
       }
     };
@@ -1210,12 +1233,15 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 3) void att
     __syncthreads();
 
     const int key_at = col * S::kKeyPitch + 8 * half;
+    int slot = 0;  // i mod 3
     for (int i = 0; i < steps; ++i) {
       // lists are read two steps ahead, for the end of this one
       const int at2 = 2 * i + 4;
       const Unit next_a = list[min(at2, n)], next_b = list[min(at2 + 1, n)];
       const bool more = i + 1 < steps;
-      if (more && (na.masked() || nb.masked())) check_bad(i + 1);
+      const bool next_masked = more && (na.masked() || nb.masked());
+      const int slot1 = slot == 2 ? 0 : slot + 1;
+      if (tid < 2) bad_tok[slot == 0 ? 2 : slot - 1][tid] = 0;
       if (works) {
         const uint16_t* keys = key_rows[i & 1] + key_at;
         const uint16_t* values = value_rows[i & 1];
@@ -1249,12 +1275,10 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 3) void att
           scores.template apply<32, 16>(s[0], rule, tr, ua.pos, half);
           scores.template apply<32, 16>(s[1], rule, tr, ub.pos, half);
           if (masked) {
-            const uint32_t seen_a = mask_scores<32, 16>(s[0], rule, ua, prefix, half);
-            const uint32_t seen_b = mask_scores<32, 16>(s[1], rule, ub, prefix, half);
-            const uint32_t bad_a = __builtin_amdgcn_readfirstlane(bad_tok[i & 1][0]);
-            const uint32_t bad_b = __builtin_amdgcn_readfirstlane(bad_tok[i & 1][1]);
-            if (bad_a) poison |= sees_bad<32, 16>(seen_a, bad_a, half);
-            if (bad_b) poison |= sees_bad<32, 16>(seen_b, bad_b, half);
+            const uint32_t seen_a = visible_tokens(rule, ua, prefix), seen_b = visible_tokens(rule, ub, prefix);
+            mask_scores<32, 16>(s[0], seen_a, half);
+            mask_scores<32, 16>(s[1], seen_b, half);
+            poison |= ((seen_a & bad_tok[slot][0]) | (seen_b & bad_tok[slot][1])) != 0;
           }
         }
 #pragma unroll
@@ -1291,6 +1315,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 3) void att
         // The usual way is the second block; the first is for steps that weigh nothing and for those with a heavy
         // weight or, where scores are capped, with a mask, a bias or a large score.  (Two flags that the compiler does
         // not know to be one: with an if and an else over the same accumulators it keeps them twice.)
+        if (next_masked) check_bad(slot1);
         constexpr Mode kUsual = CAPPED ? kSeries : kLinear;
         const bool usual = counts && mode == kUsual && !is_heavy(high, st);
         int usual_too = __builtin_amdgcn_readfirstlane(usual);
@@ -1333,9 +1358,11 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 3) void att
           add_values(1, w[1], [&](int x) { unpack(i + 1, x); });
         }
       } else {
+        if (next_masked) check_bad(slot1);
 #pragma unroll
         for (int y = 0; y < 2 * K::kSteps; ++y) unpack(i + 1, y);
       }
+      slot = slot1;
       ua = na;
       ub = nb;
       na = uniform_unit(next_a);
@@ -1387,7 +1414,8 @@ AttendPlan make_plan(int d, int64_t m, int k, int64_t units, int64_t total_q, in
   const int group = heads_q / heads;
   p.rows = total_q * group <= 16 * m ? 16 : total_q * group <= 64 * m || !list_fits_tiles(d, k) ? 32 : kTileRows;
   p.tiles = tile_count(ragged, m, total_q, group, p.rows);
-  const int64_t work = p.tiles * heads, slots = slots_of(p.rows, d);
+  const int64_t filled = ragged ? (total_q * group + p.rows - 1) / p.rows + m / 2 : p.tiles;  // about
+  const int64_t work = filled * heads, slots = slots_of(p.rows, d);
   int64_t best = INT64_MAX;
   p.splits = 1;
   const int64_t most = p.rows == kTileRows && work >= slots ? 1 : kMaxSplits;
