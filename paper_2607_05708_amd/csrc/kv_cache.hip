@@ -1,13 +1,14 @@
 // Writing a quantised key/value cache and reading it back.
 //
 // Both move every byte once: a dense row in one direction, its codes and
-// scales in the other, and are bound by HBM.  An item is eight consecutive
-// elements (four to be read back as fp32); when writing, the four items of a
-// block of 32 are neighbouring lanes, which share its largest magnitude
-// through two cross-lane steps, so a row is read once and nothing is staged.
-// A workgroup first looks up the places of its tokens (chunk, position and
-// page: three dependent loads, made once per token and not once per item),
-// then keeps kInFlight items per thread in flight.
+// scales in the other, and are bound by HBM (5.4 to 5.9 TB/s in large calls,
+// where a plain copy reaches 5.1; one token of 64 sessions takes 3.2 us).  An
+// item is eight consecutive elements (four to be read back as fp32); when
+// writing, the four items of a block of 32 are neighbouring lanes, which share
+// its largest magnitude through two cross-lane steps, so a row is read once
+// and nothing is staged.  A workgroup first looks up the places of its tokens
+// (chunk, position and page: three dependent loads, made once per token and
+// not once per item), then keeps kInFlight items per thread in flight.
 #include "kv.h"
 #include "device_common.h"
 
@@ -17,8 +18,12 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kInFlight = 4;  // items per thread of large calls (small ones: 1, to use more CUs)
-constexpr int kMinItems = 16;  // items of a token of one head of 64: keys and values
-constexpr int kMaxTokens = kThreads * kInFlight / kMinItems + 2;  // tokens that a workgroup's items belong to
+constexpr int kTokenGroup = 32;  // consecutive tokens of a head moved together in large calls
+constexpr int kMinItems = 8;   // items of a row of 64
+
+// Tokens whose rows a workgroup moves (at most): U items a thread, groups of GROUP tokens of a row or more each.
+template <int U, int GROUP>
+constexpr int kMaxTokens = (kThreads * U / kMinItems / GROUP + 2) * GROUP;
 
 // Page and row of a token; page -1: the place does not exist.
 struct Place {
@@ -35,31 +40,43 @@ __device__ __forceinline__ Place kv_place(const KvView& kv, int32_t chunk, int32
   return {pg, pos - p * kv.page_tokens};
 }
 
-// A workgroup's share of the items, token by token.
+// A workgroup's share of the rows, of keys or of values: a call moves all keys, then all values.  (Dense keys and
+// values are arrays of one size, often a power of two apart: written together, both streams meet the same channels and
+// banks.  131,071 tokens read back from 4 bits: token by token with keys and values side by side 192 us, so 125 us,
+// 5.4 TB/s.)  Within them rows go by groups of GROUP consecutive tokens, head by head: consecutive tokens are mostly
+// neighbours in a page, where heads lie apart, so that a workgroup moves whole stretches of codes and scales (65,536
+// fp32 tokens to 8 bits and back: 244 -> 232 us).  GROUP is 1 in small calls, where a group would be mostly empty.
+template <int GROUP>
 struct Share {
-  int64_t tok0;    // its first token
-  int skip;        // items of that token that belong to the workgroup before
-  int per_token;   // 2 * heads * head_dim / 8
-  uint64_t magic;  // ceil(2^40 / per_token): x / per_token = x * magic >> 40 for x < 2^18
+  int64_t tok0;      // first token of its first group
+  int skip;          // rows of that group that belong to the workgroups before
+  int group_rows;    // heads * GROUP
+  uint64_t magic;    // ceil(2^40 / heads): x / heads = x * magic >> 40 for x < 2^18
+  bool is_v;
 
-  // Token (from tok0) and item in it of item x.
-  __device__ __forceinline__ int token(int x, int* item) const {
-    const int t = static_cast<int>((static_cast<uint64_t>(x) * magic) >> 40);
-    *item = x - t * per_token;
-    return t;
+  // Token (from tok0) and head of the workgroup's row r.
+  __device__ __forceinline__ int token(int r, int* head) const {
+    r += skip;
+    const int x = r / GROUP, g = static_cast<int>((static_cast<uint64_t>(x) * magic) >> 40);
+    *head = x - g * (group_rows / GROUP);
+    return g * GROUP + r % GROUP;
   }
 };
 
 // Look up the places of the workgroup's tokens (those past the last token count as missing).
-__device__ __forceinline__ Share open_share(const KvView& kv, int per_token, uint64_t magic, int items,
-                                            const int32_t* chunk, const int32_t* pos, int64_t n, Place* places) {
-  Share s;
-  const int64_t at = static_cast<int64_t>(blockIdx.x) * items;
-  s.tok0 = at / per_token;
-  s.skip = static_cast<int>(at - s.tok0 * per_token);
-  s.per_token = per_token;
+template <int GROUP>
+__device__ __forceinline__ Share<GROUP> open_share(const KvView& kv, uint64_t magic, int rows, const int32_t* chunk,
+                                                   const int32_t* pos, int64_t n, Place* places) {
+  Share<GROUP> s;
+  s.group_rows = kv.heads * GROUP;
+  const uint32_t half = gridDim.x / 2;
+  s.is_v = blockIdx.x >= half;
+  const int64_t at = static_cast<int64_t>(s.is_v ? blockIdx.x - half : blockIdx.x) * rows;
+  const int64_t group = at / s.group_rows;
+  s.tok0 = group * GROUP;
+  s.skip = static_cast<int>(at - group * s.group_rows);
   s.magic = magic;
-  const int count = (s.skip + items - 1) / per_token + 1;
+  const int count = ((s.skip + rows - 1) / s.group_rows + 1) * GROUP;
   for (int t = threadIdx.x; t < count; t += kThreads) {
     const int64_t tok = s.tok0 + t;
     places[t] = tok < n ? kv_place(kv, chunk[tok], pos[tok]) : Place{-1, 0};
@@ -178,28 +195,26 @@ template <int FMT, int D, typename T, bool VEC, int U>
 __global__ __launch_bounds__(kThreads) void kv_write_kernel(KvView kv, RowsView k, RowsView v,
                                                             const int32_t* __restrict__ chunk,
                                                             const int32_t* __restrict__ pos, int64_t n,
-                                                            int per_token, uint64_t magic) {
-  constexpr int kN = kItem<true, T>, kPieces = D / kN;
-  __shared__ Place places[kMaxTokens];
-  const Share sh = open_share(kv, per_token, magic, kThreads * U, chunk, pos, n, places);
+                                                            uint64_t magic) {
+  constexpr int kN = kItem<true, T>, kPieces = D / kN, kGroup = U > 1 ? kTokenGroup : 1;
+  __shared__ Place places[kMaxTokens<U, kGroup>];
+  const auto sh = open_share<kGroup>(kv, magic, kThreads * U / kPieces, chunk, pos, n, places);
   float x[U][8];
   uint8_t *codes[U], *scales[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    int item;
-    const int t = sh.token(sh.skip + threadIdx.x + u * kThreads, &item);
-    const int i = item % kPieces, hv = item / kPieces;
-    const bool is_v = hv >= kv.heads;
-    const int head = is_v ? hv - kv.heads : hv;
+    const int at = threadIdx.x + u * kThreads, i = at % kPieces;
+    int head;
+    const int t = sh.token(at / kPieces, &head);
     const Place p = places[t];
     codes[u] = nullptr;
     scales[u] = nullptr;
     for (int j = 0; j < 8; ++j) x[u][j] = 0.f;
     if (p.page < 0) continue;
-    const RowsView& src = is_v ? v : k;
+    const RowsView& src = sh.is_v ? v : k;
     load8<T, VEC, (U > 1)>(static_cast<const T*>(src.data) + (sh.tok0 + t) * src.ts + head * src.hs + i * kN, x[u]);
     int64_t co, so;
-    kv_offsets<FMT, D, kN>(kv, head, is_v, p.row, i, &co, &so);
+    kv_offsets<FMT, D, kN>(kv, head, sh.is_v, p.row, i, &co, &so);
     uint8_t* base = kv.pool + p.page * kv.page_bytes;
     codes[u] = base + co;
     scales[u] = base + so;
@@ -237,29 +252,27 @@ template <int FMT, int D, typename T, bool VEC, int U>
 __global__ __launch_bounds__(kThreads) void kv_read_kernel(KvView kv, RowsView k, RowsView v,
                                                            const int32_t* __restrict__ chunk,
                                                            const int32_t* __restrict__ pos, int64_t n,
-                                                           int per_token, uint64_t magic) {
-  constexpr int kN = kItem<false, T>, kPieces = D / kN;
+                                                           uint64_t magic) {
+  constexpr int kN = kItem<false, T>, kPieces = D / kN, kGroup = U > 1 ? kTokenGroup : 1;
   constexpr int kBytes = kN * kv_row_bytes(FMT, D) / D, kWords = (kBytes + 3) / 4;  // of an item's codes
-  __shared__ Place places[kMaxTokens];
-  const Share sh = open_share(kv, per_token, magic, kThreads * U, chunk, pos, n, places);
+  __shared__ Place places[kMaxTokens<U, kGroup>];
+  const auto sh = open_share<kGroup>(kv, magic, kThreads * U / kPieces, chunk, pos, n, places);
   uint32_t c[U][kWords], byte[U];
   T* dst[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    int item;
-    const int t = sh.token(sh.skip + threadIdx.x + u * kThreads, &item);
-    const int i = item % kPieces, hv = item / kPieces;
-    const bool is_v = hv >= kv.heads;
-    const int head = is_v ? hv - kv.heads : hv;
+    const int at = threadIdx.x + u * kThreads, i = at % kPieces;
+    int head;
+    const int t = sh.token(at / kPieces, &head);
     const Place p = places[t];
-    const RowsView& to = is_v ? v : k;
+    const RowsView& to = sh.is_v ? v : k;
     const int64_t tok = sh.tok0 + t;
     dst[u] = tok < n ? static_cast<T*>(to.data) + tok * to.ts + head * to.hs + i * kN : nullptr;
     byte[u] = 127;
     for (int w = 0; w < kWords; ++w) c[u][w] = 0;
     if (p.page < 0) continue;  // reads as zeros
     int64_t co, so;
-    kv_offsets<FMT, D, kN>(kv, head, is_v, p.row, i, &co, &so);
+    kv_offsets<FMT, D, kN>(kv, head, sh.is_v, p.row, i, &co, &so);
     const uint8_t* base = kv.pool + p.page * kv.page_bytes;
     const uint32_t* src = reinterpret_cast<const uint32_t*>(base + co);
     if constexpr (kWords == 4) {
@@ -303,14 +316,16 @@ template <bool WRITE, int FMT, int D, typename T>
 hipError_t launch_typed(const KvView& kv, const RowsView& k, const RowsView& v, const int32_t* chunk,
                         const int32_t* pos, int64_t n, hipStream_t stream) {
   const bool vec = rows_aligned(k, sizeof(T)) && rows_aligned(v, sizeof(T));
-  const int per_token = 2 * kv.heads * (D / kItem<WRITE, T>);
-  const uint64_t magic = ((uint64_t{1} << 40) + per_token - 1) / per_token;
-  const int64_t items = n * per_token;
+  constexpr int kPieces = D / kItem<WRITE, T>;
+  const uint64_t magic = ((uint64_t{1} << 40) + kv.heads - 1) / kv.heads;
+  const int64_t items = 2 * n * kv.heads * kPieces;
   // one item per thread until that alone fills the GPU (256 CUs of 2,048 threads)
   const int u = items >= int64_t{256} * 2048 * kInFlight ? kInFlight : 1;
-  const dim3 grid(static_cast<unsigned>((items + kThreads * u - 1) / (kThreads * u)));
+  const int group = u == 1 ? 1 : kTokenGroup;
+  const int64_t half = (n + group - 1) / group * group * kv.heads * kPieces;  // of keys, and of values
+  const dim3 grid(2 * static_cast<unsigned>((half + kThreads * u - 1) / (kThreads * u)));
   auto go = [&](auto write, auto read) {
-    (WRITE ? write : read)<<<grid, kThreads, 0, stream>>>(kv, k, v, chunk, pos, n, per_token, magic);
+    (WRITE ? write : read)<<<grid, kThreads, 0, stream>>>(kv, k, v, chunk, pos, n, magic);
     return hipGetLastError();
   };
   if (u == 1)
