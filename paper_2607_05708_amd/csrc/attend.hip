@@ -22,11 +22,18 @@
 //     loads quarters of a token's row (16 bytes of 4-bit codes of 128
 //     elements: exactly one block, so one scale) straight from the page into
 //     the operand of the first product; values go through the wave's own LDS
-//     rows once, as bf16, to be read back transposed.
+//     rows once, as bf16, to be read back transposed.  Bound by HBM where the
+//     contexts are long (128 x 32,768 tokens in 4 bits 784 us, 5.8 TB/s; a plain
+//     copy reaches 5.1), by the start of a workgroup -- four dependent loads and
+//     the lookups, some 6 us -- where they are short (2,560 tokens 12 us).
 //   attend_tile_kernel  tiles of 128 rows: the workgroup unpacks two units at
 //     a time into LDS for its four waves, into one half of a double buffer
 //     while they work on the other; a wave's matrix products are interleaved
-//     with the exponentials and the unpacking.
+//     with the exponentials and the unpacking.  Bound by the matrix cores and
+//     the vector unit together, at the clock that their power leaves: 4 x 2,048
+//     tokens over 8,192, capped, 1.14 ms (845 TFLOP/s); 8,192 tokens behind
+//     24,576, with a distance bias, 4.76 ms (808 TFLOP/s); a large library
+//     product reaches 1,340.
 #include <type_traits>
 
 #include "kv.h"
@@ -96,7 +103,8 @@ __device__ __forceinline__ int wave_prefix_sum(int x) {
 // floor(q_offsets[i] G / R) + i + t: these starts leave room for every request's tiles and can be searched without a
 // sum, 64 probes at a time; some of the tiles are empty.  (Empty tiles between the others cost more than their start:
 // workgroups go to the XCDs and their shader engines in turn, and with one empty tile for each that is not only half
-// of them got work: 64 requests of 128 rows over 16,384 tokens 1.20 ms, added up 0.66 ms.)
+// of them got work: 64 requests of 128 rows over 16,384 tokens 1.20 ms, added up 0.70 ms; 512 of 128 over 512 tokens
+// 553 and 342 us.  The sum itself shows where there are many short requests: 512 of 2 rows 89 and 98 us.)
 constexpr int kCounted = 512;
 template <int R>
 __device__ __forceinline__ bool find_tile(const AttendArgs& a, uint32_t t, int group, Tile* out) {
@@ -1073,7 +1081,8 @@ __device__ __forceinline__ float wave_sum_f32(float x) {
 
 // A row's partial results, weighed and added by W waves (1: four rows a workgroup): lane s of every wave weighs split
 // s, wave w adds splits w, w + W, ..., whose outputs are on their way before the weights are known; then the waves'
-// sums are added in order.  One wave a row where there are few splits (kJoinSplits).
+// sums are added in order.  One wave a row where there are few splits (kJoinSplits): 32 requests of 96 rows in a few
+// splits 148 us, with four waves a row 162; bound by its two launches' worth of latency (3 to 5 us).
 constexpr int kJoinSplits = 8;
 template <int D, int W>
 __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a, int splits,
@@ -1424,7 +1433,9 @@ int64_t slots_of(int rows, int d) {
   return int64_t{256} * per_cu;
 }
 
-// Rows per request (on average) decide the kernel.  The context is split so that the rounds of workgroups take least,
+// Rows per request (on average) decide the kernel.  4-bit keys, heads of 128, 8 heads, 4,096 tokens a request, us: 128
+// requests of 8 rows over 1,024 tokens in tiles of 16 rows 39, of 32 rows 52; 32 requests of 48 rows in tiles of 32
+// rows 82, of 128 102; of 64 rows 112 and 107, of 96 rows 132 and 148, of 128 rows 185 and 152.  The context is split so that the rounds of workgroups take least,
 // a workgroup being taken to cost its units and kStart more: finding its units, its start and its end.  Tiles of 128
 // rows that fill the GPU are left whole: causal ones are of unequal length, and even out by themselves.
 constexpr int64_t kStart = 16;
