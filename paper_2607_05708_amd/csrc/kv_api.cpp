@@ -137,7 +137,7 @@ mem_status check_sizes(const mem_kv* kv, int64_t m, int32_t k, int64_t total_q, 
   if (heads_q < 1 || heads_q > kMaxHeads || heads_q % kv->heads != 0)
     return fail(MEM_ERR_INVALID_ARG, "heads_q = %d is not a multiple of heads = %d in [1, %d]", heads_q, kv->heads,
                 kMaxHeads);
-  if (m > (1 << 24) || total_q * heads_q > (int64_t{1} << 30))
+  if (m > (1 << 24) || total_q > (int64_t{1} << 30) / heads_q)
     return fail(MEM_ERR_UNSUPPORTED, "more than 2^24 requests or 2^30 query rows");
   return MEM_OK;
 }

@@ -131,6 +131,15 @@ def test_attend_workspace():
     assert size(_kv(), 4, 4096, 4, 32) < 1 << 30
 
 
+@needs_lib
+@pytest.mark.parametrize("total_q", [(1 << 30) // 32 + 1, 1 << 58, (1 << 63) - 1])
+def test_attend_refuses_more_rows_than_it_can_number(total_q):
+    L, kv = pm.lib(), _kv()
+    a = pm.MemAttendArgs(FAKE, FAKE, 1, 8, 32, None, None, 0.1, 0.0, None, 0, 0, None, None, None)
+    assert L.mem_attend(C.byref(kv), C.byref(a), FAKE, total_q, 4096, 128, FAKE, FAKE, FAKE, 1 << 40, None) == -2
+    assert L.mem_attend_workspace_bytes(C.byref(kv), 1, 8, total_q, 32) == 0
+
+
 def test_binding_refuses_host_tensors():
     cpu = torch.zeros((4, 69632), dtype=torch.uint8)
     with pytest.raises(ValueError):
