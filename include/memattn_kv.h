@@ -104,7 +104,7 @@ typedef struct {
   int32_t heads_q;          /* query heads, a multiple of kv->heads, at most 1024: query head h reads
                                key/value head h / (heads_q / heads) */
   const int32_t* q_offsets; /* device [m + 1]: request i's new tokens are rows q_offsets[i] .. q_offsets[i + 1]
-                               of q, non-decreasing from 0 to total_q; NULL: total_q / m each */
+                               of q, non-decreasing within [0, total_q]; NULL: total_q / m each */
   const int32_t* q_pos;     /* device [total_q]: position of each new token in its request's context (any
                                int32; the context's own tokens have positions 0, 1, ...); NULL: the new tokens
                                are the last ones of their context */

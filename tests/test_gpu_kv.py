@@ -332,6 +332,49 @@ def test_row_counts(nq, group):
     p.check("causal", causal=True)
 
 
+@pytest.mark.parametrize("m,hq,most", [(63, 2, 3), (65, 4, 9), (130, 16, 11), (512, 2, 5), (513, 2, 5), (700, 16, 3),
+                                       (600, 16, 11)])
+def test_many_ragged_requests(m, hq, most):
+    # requests of 0 to `most` tokens, in runs of empty ones too: few enough for their tiles to be added up, and more
+    rng = np.random.default_rng(m)
+    nq = rng.integers(0, most + 1, m)
+    nq[m // 3:m // 3 + 20] = 0
+    nq[-3:] = 0
+    lens = [[int(x) for x in rng.integers(0, 33, rng.integers(0, 3))] for _ in range(m)]
+    p = Problem(m + hq, ref.FP8, lens, [int(x) for x in nq], hq, 1, 64, ppc=1)
+    p.check("ragged", causal=True)
+
+
+@pytest.mark.parametrize("nq", [1, 7, 60])
+def test_rows_that_no_request_owns_are_not_written(nq):
+    p = Problem(16, ref.FP4, [[64] * 9, [64] * 3 + [5]], [nq, nq], 4, 2, 128)
+    want = p.gpu(causal=True)
+    total = 2 * nq
+    q = torch.cat([p.q.cuda(), torch.full((9, 4, 128), float("nan"), device="cuda", dtype=torch.bfloat16)])
+    out = (torch.full((total + 9, 4, 128), 7.0, device="cuda", dtype=torch.bfloat16),
+           torch.full((total + 9, 4), 7.0, device="cuda"))
+    got = p.gpu(causal=True, q=q, out=out)
+    assert (got[0][total:] == 7).all() and (got[1][total:] == 7).all()
+    ref.check_attend("owned rows", got[0][:total], got[1][:total], *p.model(causal=True))
+    assert np.allclose(got[1][:total], want[1], rtol=0, atol=1e-4)
+
+
+@pytest.mark.parametrize("nq", [1, 60])
+def test_calls_on_another_stream(nq):
+    p = Problem(17, ref.FP8, [[64] * 12, [64, 5]], [nq, nq], 4, 2, 128)
+    want = p.gpu(causal=True)
+    cache, q, args = p.cache(), p.q.cuda(), [up(p.tok_len), up(p.ids)]
+    off = up(p.off)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(3):                                       # results and workspace are freed and taken again in between
+        got = pm.mem_attend(cache, *args, q, p.scale, q_offsets=off, causal=True, stream=side)
+        side.synchronize()
+        assert np.array_equal(host(got[0]), want[0]) and np.array_equal(host(got[1]), want[1])
+        del got
+        torch.full((1 << 20,), 9.0, device="cuda")
+
+
 @pytest.mark.parametrize("page_tokens,ppc", [(32, 1), (64, 3), (96, 2), (160, 1), (256, 2)])
 @pytest.mark.parametrize("name", list(FMTS))
 def test_page_sizes(name, page_tokens, ppc):
