@@ -109,7 +109,7 @@ typedef struct {
                                int32; the context's own tokens have positions 0, 1, ...); NULL: the new tokens
                                are the last ones of their context */
   float scale;              /* > 0, finite */
-  float softcap;            /* cap of the scores, >= 0, finite; 0 = none */
+  float softcap;            /* cap of the scores, >= 0, finite (large ones change nothing); 0 = none */
   const float* slopes;      /* device [heads_q]: distance bias of each head; NULL = none */
   int32_t causal;           /* != 0: a token sees positions up to its own */
   int32_t window;           /* > 0: a token sees positions above its own minus `window`; 0 = all */
@@ -146,7 +146,8 @@ MEMATTN_API size_t mem_attend_workspace_bytes(const mem_kv* kv, int64_t m, int32
  * heads_q, head_dim] and [total_q, heads_q], contiguous; out is 16-byte
  * aligned.  Products are bf16 with fp32 sums; the softmax weights are rounded
  * to bf16 for the second product (heavy ones to 16 bits) and out is divided by
- * the unrounded weights' sum, which is also lse's.  Rows of q that no request
+ * the unrounded weights' sum, which is also lse's.  A capped score is off by at
+ * most 2^-19 of itself, or with a cap of up to 64 by 2^-21 of the cap.  Rows of q that no request
  * owns are not written.  The context lengths are read on the device: nothing
  * is synchronised, and the call can be captured into a HIP graph.
  */

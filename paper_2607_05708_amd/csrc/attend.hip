@@ -550,11 +550,20 @@ __device__ constexpr int score_token(int j) {
   return WIDTH == 16 ? 16 * (j >> 2) + (j & 3) : 8 * (j >> 2) + (j & 3);
 }
 
-// How raw products become scores in the log2 domain: scaled, capped, biased.  The cap's tanh is
-// 1 - 2 / (1 + e^2x), with two transcendental operations of twice to three times a product's cost each.  Where no score
-// of a wave's unit is above kSmall of the cap, tanh(x) / x as a polynomial of degree 2 in t = x^2 does as well: its
-// series 1 - t / 3 + 2 t^2 / 15 - 17 t^3 / 315 with t^3 replaced by the quadratic that is nearest to it on
-// [0, kSmall^2], off by at most kSmall^6 / 32 (Chebyshev).  With the series' next term that is 1.1e-7 of the score.
+// Caps that a kernel is made for: none, up to kModestCap, above.
+enum Caps { kNoCap, kModestCaps, kLargeCaps };
+constexpr float kModestCap = 64.f;
+
+// How raw products become scores in the log2 domain: scaled, capped, biased.  The cap is softcap * tanh(x), x the
+// scaled product over the cap.  By its definition the tanh is 1 - 2 / (1 + e^2x), with two transcendental operations of
+// twice to three times a product's cost each, and an error of 2^-21 whatever its size.  Where |x| is at most kSmall,
+// tanh(x) / x as a polynomial of degree 2 in t = x^2 does as well: its series 1 - t / 3 + 2 t^2 / 15 - 17 t^3 / 315 with
+// t^3 replaced by the quadratic that is nearest to it on [0, kSmall^2], off by at most kSmall^6 / 32 (Chebyshev).  With
+// the series' next term that is 1.1e-7 of the score.  Units without a larger product take it for all of them.  In the
+// others a modest cap takes the definition for all (off by at most 2^-15, where the weights are rounded by 2^-9 of
+// themselves); of a larger cap that error would be a multiple, so each score goes by its own size, and is off by 2^-19
+// of itself at most.  (The choice for each costs 20 % of a prefill whose scores are of the cap's size, and registers:
+// kernels of their own.)
 struct Scores {
   float c;     // scale * log2(e)
   float k2;    // 2 * log2(e) * scale / softcap
@@ -564,17 +573,20 @@ struct Scores {
   bool bias;
   bool causal;
 
-  static constexpr float kSmall = 0.1875f;
+  static constexpr float kSmall = 0.1875f, kT = kSmall * kSmall, kCubic = 17.f / 315.f;
+  static constexpr float kP0 = 1.f - kCubic * kT * kT * kT / 32.f, kP1 = -1.f / 3.f + kCubic * kT * kT * (9.f / 16.f),
+                         kP2 = 2.f / 15.f - kCubic * kT * 1.5f;
 
   __device__ __forceinline__ explicit Scores(const AttendArgs& a)
       : c(a.scale * kLog2e), cap2(a.softcap * kLog2e), bias(a.slopes != nullptr), causal(a.causal != 0) {
-    const float x = a.softcap > 0.f ? a.scale / a.softcap : 0.f;
+    const float x = a.softcap > 0.f ? fminf(a.scale / a.softcap, 1e38f) : 0.f;  // (finite: 0 * x is 0)
     k2 = 2.f * kLog2e * x;
-    limit = x > 1e-4f ? kSmall / x : -1.f;  // (coefficients of a tiny x would lose bits as denormals)
-    constexpr float kT = kSmall * kSmall, kCubic = 17.f / 315.f;
-    s0 = c * (1.f - kCubic * kT * kT * kT / 32.f);
-    s1 = c * x * x * (-1.f / 3.f + kCubic * kT * kT * (9.f / 16.f));
-    s2 = c * x * x * x * x * (2.f / 15.f - kCubic * kT * 1.5f);
+    // (within these ranges no coefficient and no square of a small product leaves the normal numbers)
+    const bool plain = x >= 0x1p-20f && x <= 0x1p20f && c >= 0x1p-40f && c <= 0x1p40f;
+    limit = plain ? kSmall / x : -1.f;
+    s0 = c * kP0;
+    s1 = c * x * x * kP1;
+    s2 = c * x * x * x * x * kP2;
   }
 
   __device__ __forceinline__ float series(float s) const {  // capped score / s
@@ -583,12 +595,26 @@ struct Scores {
   }
   __device__ __forceinline__ float fraction(float s) const { return __builtin_amdgcn_rcpf(1.f + fast_exp2(s * k2)); }
 
+  // Capped score of any product by its own size: the polynomial in u^2 = (2 log2(e) x)^2, or the definition.
+  __device__ __forceinline__ float capped(float s) const {
+    constexpr float kA = 1.f / (4.f * kLog2e * kLog2e);
+    const float u = s * k2, t = u * u;
+    const float near = s * c * (kP0 + t * (kP1 * kA + t * (kP2 * kA * kA)));
+    const float far = cap2 * fmaf(fraction(s), -2.f, 1.f);
+    return t <= kT / kA ? near : far;
+  }
+
   // Scores of one unit made explicit: what masks and biases need.
-  template <int WIDTH, int N, typename V>
+  template <int WIDTH, int N, Caps CAPS, typename V>
   __device__ __forceinline__ void apply(V& s, const RowRule& rule, const TileRule& tr, int pos, int part) const {
-    if (cap2 != 0.f) {
+    if (CAPS != kNoCap && cap2 != 0.f) {
+      if (CAPS == kModestCaps) {
 #pragma unroll
-      for (int j = 0; j < N; ++j) s[j] = cap2 - 2.f * cap2 * fraction(s[j]);
+        for (int j = 0; j < N; ++j) s[j] = cap2 - 2.f * cap2 * fraction(s[j]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) s[j] = capped(s[j]);
+      }
     }
     const float f = cap2 == 0.f ? c : 1.f;
     if (!bias) {
@@ -677,21 +703,23 @@ struct Rows {
 };
 
 // How a unit's scores become weights 2^(score - ref): from numbers that only want a factor (scores in the log2 domain,
-// or raw products without a cap), or from raw products whose cap (by series or exactly) goes into the exponential's
-// argument.
-enum Mode { kLinear, kSeries, kExact };
+// or raw products without a cap), or from raw products whose cap (by the polynomial, by the definition, or each by its
+// size) goes into the exponential's argument.
+enum Mode { kLinear, kSeries, kExact, kBySize };
 
 template <Mode MODE>
 __device__ __forceinline__ float weigh(float s, float f, const Scores& sc, float ref) {
   if constexpr (MODE == kLinear) return fast_exp2(fmaf(s, f, -ref));
   if constexpr (MODE == kSeries) return fast_exp2(fmaf(s, sc.series(s), -ref));
-  return fast_exp2(fmaf(sc.fraction(s), -2.f * sc.cap2, sc.cap2 - ref));
+  if constexpr (MODE == kExact) return fast_exp2(fmaf(sc.fraction(s), -2.f * sc.cap2, sc.cap2 - ref));
+  return fast_exp2(sc.capped(s) - ref);
 }
 
 // The largest score of a row from the largest number (the cap grows with the product).
 __device__ __forceinline__ float top_score(float top, float f, const Scores& sc, Mode mode) {
   if (mode == kLinear) return top * f;
-  return mode == kSeries ? top * sc.series(top) : sc.cap2 - 2.f * sc.cap2 * sc.fraction(top);
+  if (mode == kSeries) return top * sc.series(top);
+  return mode == kExact ? sc.cap2 - 2.f * sc.cap2 * sc.fraction(top) : sc.capped(top);
 }
 
 // Whether some row of the wave sees something of a unit with this largest score (what weighs little is not left out:
@@ -849,7 +877,8 @@ struct FewShape {
   static constexpr int kArea = kWaves * kWaveBytes > kJoinBytes ? kWaves * kWaveBytes : kJoinBytes;
 };
 
-template <int FMT, int D, int R>
+// CAPS: kModestCaps stands for none too.
+template <int FMT, int D, int R, Caps CAPS>
 __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_few_kernel(AttendArgs a, int splits,
                                                                                 float* __restrict__ part_o,
                                                                                 RowState* __restrict__ part_ml) {
@@ -858,6 +887,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_few_kernel(
   constexpr int kParts = 64 / R;              // lanes that share a row's scores
   constexpr int kScores = kUnit / kParts;     // scores per lane and unit
   constexpr int kQSteps = D / (8 * kParts);   // operands of a row's queries per lane
+  constexpr Mode kLarge = CAPS == kLargeCaps ? kBySize : kExact;  // for units with large products
   extern __shared__ int dyn[];                // the chunk list: cid[k], ub[k + 1], tb[k + 1]
   __shared__ __align__(16) uint8_t area[S::kArea];
   __shared__ Unit list[S::kBatch];
@@ -951,7 +981,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_few_kernel(
       }
       load(pk, next, false);
       const bool ready = u.masked() || scores.bias;
-      if (ready) scores.template apply<R, kScores>(s, rule, tr, u.pos, part);
+      if (ready) scores.template apply<R, kScores, CAPS>(s, rule, tr, u.pos, part);
       if (u.masked()) {
         const int held = u.held();
         const uint32_t seen = visible_tokens(rule, u, prefix);
@@ -976,7 +1006,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_few_kernel(
         for (int j = 0; j < kScores; ++j) most = fmaxf(most, fabsf(s[j]));
         small = !__any(most > scores.limit);
       }
-      const Mode mode = ready || scores.cap2 == 0.f ? kLinear : small ? kSeries : kExact;
+      const Mode mode = ready || scores.cap2 == 0.f ? kLinear : small ? kSeries : kLarge;
       const float f = ready ? 1.f : scores.c;
       const float top = top_score(max_column<R>(max_of(s)), f, scores, mode);
       const bool counts = raise<R, D>(top, st, rows);
@@ -991,7 +1021,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_few_kernel(
         };
         if (mode == kLinear) weigh_all(std::integral_constant<Mode, kLinear>{});
         else if (mode == kSeries) weigh_all(std::integral_constant<Mode, kSeries>{});
-        else weigh_all(std::integral_constant<Mode, kExact>{});
+        else weigh_all(std::integral_constant<Mode, kLarge>{});
       }
       if (counts) {  // values: unpack into the wave's LDS rows, to be read back transposed
 #pragma unroll
@@ -1163,9 +1193,9 @@ struct TileShape {
 // A wave issues in order, so its matrix products only overlap with what stands between them: the second product of a
 // step's first unit is written in groups of one matrix instruction and a share of the second unit's exponentials, the
 // second unit's with a share of the unpacking.  (Two units a step: of one unit's 1.59 us, 0.65 went into the step
-// itself -- barrier, list, maximum -- whatever it did.)  CAPPED: the scores are capped; a kernel has one way to
-// weigh scores in those groups, and takes the rare others apart from them.
-template <int FMT, int D, bool CAPPED>
+// itself -- barrier, list, maximum -- whatever it did.)  A kernel has one way to weigh
+// scores in those groups, and takes the rare others apart from them.
+template <int FMT, int D, Caps CAPS>
 __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 3) void attend_tile_kernel(AttendArgs a, int splits,
                                                                                  int64_t tiles,
                                                                                  float* __restrict__ part_o,
@@ -1174,6 +1204,8 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 3) void att
   using S = TileShape<FMT, D>;
   using Ops = ValueOps<32, D, S::kShift>;
   constexpr int kQSteps = D / 16;
+  constexpr bool kCapped = CAPS != kNoCap;
+  constexpr Mode kLarge = CAPS == kLargeCaps ? kBySize : kExact;  // for units with large products
   extern __shared__ int dyn[];  // the chunk list: cid[k], ub[k + 1], tb[k + 1]
   __shared__ __align__(16) uint16_t key_rows[2][S::kKeys];
   __shared__ __align__(16) uint16_t value_rows[2][S::kValues];
@@ -1312,8 +1344,8 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 3) void att
           __builtin_amdgcn_s_setprio(1);
         }
         if (ready) {
-          scores.template apply<32, 16>(s[0], rule, tr, ua.pos, half);
-          scores.template apply<32, 16>(s[1], rule, tr, ub.pos, half);
+          scores.template apply<32, 16, CAPS>(s[0], rule, tr, ua.pos, half);
+          scores.template apply<32, 16, CAPS>(s[1], rule, tr, ub.pos, half);
           if (masked) {
             const uint32_t seen_a = visible_tokens(rule, ua, prefix), seen_b = visible_tokens(rule, ub, prefix);
             mask_scores<32, 16>(s[0], seen_a, half);
@@ -1324,9 +1356,9 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 3) void att
 #pragma unroll
         for (int j = 0; j < 32; ++j) {
           top = nan_max(top, s[j >> 4][j & 15]);
-          if (CAPPED) most = fmaxf(most, fabsf(s[j >> 4][j & 15]));
+          if (kCapped) most = fmaxf(most, fabsf(s[j >> 4][j & 15]));
         }
-        const Mode mode = !CAPPED || ready ? kLinear : __any(most > scores.limit) ? kExact : kSeries;
+        const Mode mode = !kCapped || ready ? kLinear : __any(most > scores.limit) ? kLarge : kSeries;
         const float f = ready ? 1.f : scores.c;
         const float high = top_score(max_column<32>(top), f, scores, mode);
         const bool counts = raise<32, D>(high, st, rows);
@@ -1356,7 +1388,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 3) void att
         // weight or, where scores are capped, with a mask, a bias or a large score.  (Two flags that the compiler does
         // not know to be one: with an if and an else over the same accumulators it keeps them twice.)
         if (next_masked) check_bad(slot1);
-        constexpr Mode kUsual = CAPPED ? kSeries : kLinear;
+        constexpr Mode kUsual = kCapped ? kSeries : kLinear;
         const bool usual = counts && mode == kUsual && !is_heavy(high, st);
         int usual_too = __builtin_amdgcn_readfirstlane(usual);
         asm volatile("" : "+s"(usual_too));
@@ -1367,7 +1399,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 3) void att
               for (int j = 0; j < 32; ++j) weigh_score(std::integral_constant<Mode, kLinear>{}, j);
             } else {
 #pragma unroll
-              for (int j = 0; j < 32; ++j) weigh_score(std::integral_constant<Mode, kExact>{}, j);
+              for (int j = 0; j < 32; ++j) weigh_score(std::integral_constant<Mode, kLarge>{}, j);
             }
             u32x4_t w[2], rest[2];
 #pragma unroll
@@ -1485,13 +1517,19 @@ hipError_t launch_dim(const AttendArgs& a, const AttendPlan& p, hipStream_t stre
                              : nullptr;
   const dim3 grid(static_cast<unsigned>(p.tiles * a.kv.heads * p.splits));
   const size_t lds = list_bytes(a.k);
+  const bool large = a.softcap > kModestCap;
   if (p.rows == 16)
-    attend_few_kernel<FMT, D, 16><<<grid, kThreads, lds, stream>>>(a, p.splits, po, pml);
+    (large ? attend_few_kernel<FMT, D, 16, kLargeCaps> : attend_few_kernel<FMT, D, 16, kModestCaps>)<<<grid, kThreads,
+                                                                                                     lds, stream>>>(
+        a, p.splits, po, pml);
   else if (p.rows == 32)
-    attend_few_kernel<FMT, D, 32><<<grid, kThreads, lds, stream>>>(a, p.splits, po, pml);
+    (large ? attend_few_kernel<FMT, D, 32, kLargeCaps> : attend_few_kernel<FMT, D, 32, kModestCaps>)<<<grid, kThreads,
+                                                                                                     lds, stream>>>(
+        a, p.splits, po, pml);
   else
-    (a.softcap > 0.f ? attend_tile_kernel<FMT, D, true> : attend_tile_kernel<FMT, D, false>)<<<grid, kThreads, lds,
-                                                                                               stream>>>(
+    (a.softcap == 0.f ? attend_tile_kernel<FMT, D, kNoCap>
+     : large          ? attend_tile_kernel<FMT, D, kLargeCaps>
+                      : attend_tile_kernel<FMT, D, kModestCaps>)<<<grid, kThreads, lds, stream>>>(
         a, p.splits, p.tiles, po, pml);
   if (hipError_t e = hipGetLastError(); e != hipSuccess || p.splits == 1) return e;
   const int64_t out_rows = a.total_q * a.hq;
