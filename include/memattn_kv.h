@@ -139,8 +139,8 @@ MEMATTN_API size_t mem_attend_workspace_bytes(const mem_kv* kv, int64_t m, int32
  * A token that sees nothing gets out = 0 and lse = -inf, and so does every
  * token of an empty context.  Tokens that a query does not see have no
  * influence on it, whatever they hold; a value that is not finite among those
- * that it does see makes its output so, however small its weight (keys that
- * only make a score -inf hide their token).
+ * that it does see makes its output so, however small its weight (also behind a
+ * key that makes the score -inf).
  * q (device bf16, [total_q, heads_q, head_dim] with the strides given) is only
  * read; out (device bf16) and lse (device fp32, nullable) are [total_q,
  * heads_q, head_dim] and [total_q, heads_q], contiguous; out is 16-byte

@@ -722,11 +722,12 @@ __device__ __forceinline__ float top_score(float top, float f, const Scores& sc,
   return mode == kExact ? sc.cap2 - 2.f * sc.cap2 * sc.fraction(top) : sc.capped(top);
 }
 
-// Whether some row of the wave sees something of a unit with this largest score (what weighs little is not left out:
-// its values may be large, or no numbers); raises the running maximum if it has to.
+// Whether a unit with this largest score has to be weighed: if it is masked, and its values that are not finite have
+// been noted and cleared, only where some score of the wave is above -inf; else always (what weighs little or nothing
+// is not left out: its values may be large, or no numbers).  Raises the running maximum if it has to.
 template <int WIDTH, int D>
-__device__ __forceinline__ bool raise(float top, RowState& st, Rows<WIDTH, D>& rows) {
-  if (!__any(top != -INFINITY)) return false;
+__device__ __forceinline__ bool raise(float top, bool masked, RowState& st, Rows<WIDTH, D>& rows) {
+  if (!__any(!masked || top != -INFINITY)) return false;
   if (__any(top > st.m + kLag)) {
     const float mn = fmaxf(st.m, top);
     const float r = mn == -INFINITY ? 1.f : fast_exp2(st.m - mn);
@@ -1009,7 +1010,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_few_kernel(
       const Mode mode = ready || scores.cap2 == 0.f ? kLinear : small ? kSeries : kLarge;
       const float f = ready ? 1.f : scores.c;
       const float top = top_score(max_column<R>(max_of(s)), f, scores, mode);
-      const bool counts = raise<R, D>(top, st, rows);
+      const bool counts = raise<R, D>(top, u.masked(), st, rows);
       if (counts) {
         const float ref = finite_max(st.m);
         auto weigh_all = [&](auto m) {
@@ -1361,7 +1362,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 3) void att
         const Mode mode = !kCapped || ready ? kLinear : __any(most > scores.limit) ? kLarge : kSeries;
         const float f = ready ? 1.f : scores.c;
         const float high = top_score(max_column<32>(top), f, scores, mode);
-        const bool counts = raise<32, D>(high, st, rows);
+        const bool counts = raise<32, D>(high, masked, st, rows);
         const float ref = finite_max(st.m);
         auto weigh_score = [&](auto m, int j) {  // score j of both units' 32
           const float x = weigh<decltype(m)::value>(s[j >> 4][j & 15], f, scores, ref);
