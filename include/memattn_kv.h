@@ -42,7 +42,9 @@ extern "C" {
  * so every step but that rounding is exact and a value has one right code.
  * In MEM_KV_FP8 and MEM_KV_FP4 an infinity counts as the largest finite
  * float, and a block that holds a NaN gets the scale byte 255, which makes
- * all its elements NaN.
+ * all its elements NaN.  Scale bytes that mem_kv_write does not give (below 17,
+ * and above 246 in MEM_KV_FP8 or 252 in MEM_KV_FP4, but for 255) stand for
+ * values that are not specified.
  */
 typedef enum { MEM_KV_BF16 = 0, MEM_KV_FP8 = 1, MEM_KV_FP4 = 2 } mem_kv_format;
 

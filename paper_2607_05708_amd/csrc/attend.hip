@@ -467,11 +467,12 @@ __device__ __forceinline__ u32x4_t piece_step(const Piece<FMT, D>& p, int i) {
   return o;
 }
 
-// Whether a piece holds a value that is not finite.
+// Whether a piece holds a value that is not finite, or may: scales above those that mem_kv_write gives can take a code
+// out of range.
 template <int FMT, int D>
 __device__ __forceinline__ bool piece_bad(const Piece<FMT, D>& p) {
   bool bad = false;
-  if constexpr (FMT != MEM_KV_BF16) bad = (p.sc & 255u) == 255u || (p.sc >> 8) == 255u;
+  if constexpr (FMT != MEM_KV_BF16) bad = max(p.sc & 255u, p.sc >> 8) > kMaxScaleByte<FMT>;
   if constexpr (FMT == MEM_KV_FP8) {
 #pragma unroll
     for (int i = 0; i < Dim<FMT, D>::kWords; ++i)

@@ -81,6 +81,10 @@ typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 typedef short s16x2 __attribute__((ext_vector_type(2)));
 
+// The largest scale byte that mem_kv_write gives a block without a NaN.
+template <int FMT>
+constexpr uint32_t kMaxScaleByte = 127 + (FMT == MEM_KV_FP4 ? 125 : 119);
+
 // Scale byte of a block whose largest magnitude has the bit pattern `amax`
 // (the maximum of the elements' patterns without sign, so that a NaN is above
 // every number): 127 plus the smallest e with amax <= 1.75 * 2^(e + 2) (FP4)
@@ -89,11 +93,10 @@ template <int FMT>
 __device__ __forceinline__ uint32_t kv_scale_byte(uint32_t amax) {
   constexpr int kTop = FMT == MEM_KV_FP4 ? 2 : 8;
   constexpr uint32_t kLimit = FMT == MEM_KV_FP4 ? 0x600000u : 0x680000u;
-  constexpr int kMax = FMT == MEM_KV_FP4 ? 125 : 119;
   if (amax > 0x7F800000u) return 255u;
   const uint32_t a = min(amax, 0x7F7FFFFFu);
   const int e = static_cast<int>(a >> 23) - 127 - kTop + ((a & 0x7FFFFFu) > kLimit ? 1 : 0);
-  return static_cast<uint32_t>(min(max(e, -110), kMax) + 127);
+  return min(static_cast<uint32_t>(max(e, -110) + 127), kMaxScaleByte<FMT>);
 }
 
 // 2^-e of a scale byte that kv_scale_byte returned (a NaN for 255).

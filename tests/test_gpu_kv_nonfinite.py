@@ -60,3 +60,24 @@ def test_a_value_shows_behind_keys_of_minus_infinity(nq, masks, tokens):
     values[page, :, row, 10:12] = (0xC0, 0x7F)
     out, again = p.gpu(**masks)
     assert np.isnan(out[..., 5]).all() and np.array_equal(again, lse)
+
+
+@pytest.mark.parametrize("name,d,byte", [("fp4", 64, 253), ("fp4", 128, 254), ("fp4", 256, 254), ("fp8", 64, 247),
+                                         ("fp8", 128, 250), ("fp8", 256, 254), ("fp8", 256, 255)])
+@pytest.mark.parametrize("nq", NQ)
+def test_bytes_that_no_call_wrote_reach_nobody_who_does_not_see_them(name, d, byte, nq):
+    # places within a chunk's length that hold something else: scales whose products leave the range of fp32
+    fmt = FMTS[name]
+    p = Problem(22 + d, fmt, [[64, 64, 64]], [nq], 4, 2, d)
+    at = 160 if nq == 1 else 192 - nq // 2 - 2                   # (one token sees 162 to 191)
+    masks = dict(causal=True, window=30)
+    clean = p.model(**masks)
+    page, row, _ = p.ctx[0][at]
+    for codes, scales in ref.views(fmt, 32, 2, d, p.pool):
+        codes[page, :, row] = 0x77 if fmt == ref.FP4 else 0x7E      # the largest values
+        scales[page, :, row] = byte
+    out, lse = p.gpu(**masks)
+    qpos = np.arange(nq) + 192 - nq
+    sees = (qpos >= at) & (qpos - 30 < at)
+    assert (~sees).any()
+    ref.check_attend("rows that do not see it", *[x[~sees] for x in (out, lse, *clean)])
