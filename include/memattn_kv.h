@@ -82,7 +82,8 @@ MEMATTN_API size_t mem_kv_page_bytes(int32_t page_tokens, int32_t heads, int32_t
  * MEM_BF16, only read) becomes token pos[i] of chunk chunk[i] (device int32
  * [n] each).  A token whose chunk is outside [0, n_chunks), whose position is
  * outside the chunk or whose page is outside the pool is skipped (-1 marks
- * padding).  No two tokens of a call may name the same place.
+ * padding).  No two tokens of a call may name the same place.  A call is one
+ * launch: some 2^36 elements and more are refused (MEM_ERR_UNSUPPORTED).
  */
 MEMATTN_API mem_status mem_kv_write(const mem_kv* kv, const mem_kv_rows* k, const mem_kv_rows* v, int32_t dtype,
                                     const int32_t* chunk, const int32_t* pos, int64_t n, void* stream);
@@ -151,7 +152,9 @@ MEMATTN_API size_t mem_attend_workspace_bytes(const mem_kv* kv, int64_t m, int32
  * the unrounded weights' sum, which is also lse's.  A capped score is off by at
  * most 2^-19 of itself, or with a cap of up to 64 by 2^-21 of the cap.  Rows of q that no request
  * owns are not written.  The context lengths are read on the device: nothing
- * is synchronised, and the call can be captured into a HIP graph.
+ * is synchronised, and the call can be captured into a HIP graph.  Calls whose
+ * tiles (16, 32 or 128 rows of a key/value head and request) come to 2^24 or
+ * more are refused (MEM_ERR_UNSUPPORTED).
  */
 MEMATTN_API mem_status mem_attend(const mem_kv* kv, const mem_attend_args* args, const void* q, int64_t total_q,
                                   int64_t q_token_stride, int64_t q_head_stride, void* out, float* lse,

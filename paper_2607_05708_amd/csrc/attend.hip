@@ -1485,6 +1485,8 @@ static_assert(2 * sizeof(uint16_t) * (TileShape<MEM_KV_BF16, 256>::kKeys + TileS
                   160 * 1024,
               "a workgroup's LDS");
 
+int64_t join_groups(int64_t rows, int64_t splits) { return splits <= kJoinSplits ? (rows + kWaves - 1) / kWaves : rows; }
+
 AttendPlan make_plan(int d, int64_t m, int k, int64_t units, int64_t total_q, int heads, int heads_q, bool ragged) {
   AttendPlan p;
   const int group = heads_q / heads;
@@ -1496,6 +1498,7 @@ AttendPlan make_plan(int d, int64_t m, int k, int64_t units, int64_t total_q, in
   p.splits = 1;
   const int64_t most = p.rows == kTileRows && work >= slots ? 1 : kMaxSplits;
   for (int64_t s = 1; s <= most && (s == 1 || units / s >= kWaves); ++s) {
+    if (s > 1 && (p.tiles * heads * s > kMaxGroups || join_groups(total_q * heads_q, s) > kMaxGroups)) break;
     const int64_t cost = (work * s + slots - 1) / slots * ((units + s - 1) / s + kStart) + (s > 1 ? s / 4 : 0);
     if (cost < best) {
       best = cost;
@@ -1534,12 +1537,11 @@ hipError_t launch_dim(const AttendArgs& a, const AttendPlan& p, hipStream_t stre
                       : attend_tile_kernel<FMT, D, kModestCaps>)<<<grid, kThreads, lds, stream>>>(
         a, p.splits, p.tiles, po, pml);
   if (hipError_t e = hipGetLastError(); e != hipSuccess || p.splits == 1) return e;
-  const int64_t out_rows = a.total_q * a.hq;
+  const dim3 join(static_cast<unsigned>(join_groups(a.total_q * a.hq, p.splits)));
   if (p.splits <= kJoinSplits)
-    attend_join_kernel<D, 1><<<dim3(static_cast<unsigned>((out_rows + kWaves - 1) / kWaves)), kThreads, 0, stream>>>(
-        a, p.splits, po, pml);
+    attend_join_kernel<D, 1><<<join, kThreads, 0, stream>>>(a, p.splits, po, pml);
   else
-    attend_join_kernel<D, kWaves><<<dim3(static_cast<unsigned>(out_rows)), kThreads, 0, stream>>>(a, p.splits, po, pml);
+    attend_join_kernel<D, kWaves><<<join, kThreads, 0, stream>>>(a, p.splits, po, pml);
   return hipGetLastError();
 }
 
@@ -1570,7 +1572,7 @@ size_t attend_workspace_bytes(int d, int64_t m, int k, int64_t units, int64_t to
 
 bool attend_fits(int d, int64_t m, int k, int64_t units, int64_t total_q, int heads, int heads_q, bool ragged) {
   const AttendPlan p = make_plan(d, m, k, units, total_q, heads, heads_q, ragged);
-  return p.tiles * p.splits <= INT32_MAX / heads;
+  return p.tiles * p.splits * heads <= kMaxGroups;
 }
 
 hipError_t launch_attend(const AttendArgs& a, int fmt, int d, hipStream_t stream) {

@@ -13,6 +13,9 @@ namespace memattn {
 
 constexpr int kKvBlock = 32;  // elements that share a scale
 
+// Workgroups of a launch: all kernels here have 256 threads each, and a launch has fewer than 2^32 threads.
+constexpr int64_t kMaxGroups = (int64_t{1} << 24) - 1;
+
 // Bytes of codes and of scales of a row of d elements.
 __host__ __device__ constexpr int kv_row_bytes(int fmt, int d) {
   return fmt == MEM_KV_BF16 ? 2 * d : fmt == MEM_KV_FP8 ? d : d / 2;
@@ -67,9 +70,11 @@ hipError_t launch_kv_write(const KvView& kv, int fmt, int d, const RowsView& k, 
                            const int32_t* chunk, const int32_t* pos, int64_t n, hipStream_t stream);
 hipError_t launch_kv_read(const KvView& kv, int fmt, int d, const RowsView& k, const RowsView& v, int dtype,
                           const int32_t* chunk, const int32_t* pos, int64_t n, hipStream_t stream);
+// Whether n tokens (of at most 2^40 elements) fit one launch.
+bool kv_move_fits(bool write, int heads, int d, int dtype, int64_t n);
 // `units`: blocks of 32 tokens that a request's chunks can hold.
 size_t attend_workspace_bytes(int d, int64_t m, int k, int64_t units, int64_t total_q, int heads, int heads_q);
-// Whether the call's workgroups fit one launch.
+// Whether the call's workgroups fit its launches.
 bool attend_fits(int d, int64_t m, int k, int64_t units, int64_t total_q, int heads, int heads_q, bool ragged);
 hipError_t launch_attend(const AttendArgs& a, int fmt, int d, hipStream_t stream);
 

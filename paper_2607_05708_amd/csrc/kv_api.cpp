@@ -107,8 +107,7 @@ mem_status move_tokens(bool write, const mem_kv* kv, const mem_kv_rows* k, const
   if (mem_status st = check_rows(v, elem, "v"); st != MEM_OK) return st;
   if (!chunk || !pos) return fail(MEM_ERR_INVALID_ARG, "chunk or pos is NULL");
   if (!aligned(chunk, 4) || !aligned(pos, 4)) return fail(MEM_ERR_INVALID_ARG, "chunk and pos must be 4-byte aligned");
-  const int64_t pieces = 2 * static_cast<int64_t>(kv->heads) * (kv->head_dim / 8);
-  if (n > (static_cast<int64_t>(INT32_MAX) * 256) / pieces - 1)
+  if (n > (int64_t{1} << 40) / (kv->heads * kv->head_dim) || !kv_move_fits(write, kv->heads, kv->head_dim, dtype, n))
     return fail(MEM_ERR_UNSUPPORTED, "n too large for one launch");
   if (!write) {
     for (const mem_kv_rows* r : {k, v})

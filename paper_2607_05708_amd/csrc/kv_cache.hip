@@ -312,23 +312,33 @@ bool rows_aligned(const RowsView& r, int elem) {
   return (a & 15u) == 0;
 }
 
+// Items per thread and workgroups of a call whose rows are moved in `pieces` items each.
+struct MoveGrid {
+  int u;
+  int64_t groups;
+};
+
+MoveGrid move_grid(int heads, int pieces, int64_t n) {
+  const int64_t items = 2 * n * heads * pieces;
+  // one item per thread until that alone fills the GPU (256 CUs of 2,048 threads)
+  const int u = items >= int64_t{256} * 2048 * kInFlight ? kInFlight : 1;
+  const int group = u == 1 ? 1 : kTokenGroup;
+  const int64_t half = (n + group - 1) / group * group * heads * pieces;  // of keys, and of values
+  return {u, 2 * ((half + kThreads * u - 1) / (kThreads * u))};
+}
+
 template <bool WRITE, int FMT, int D, typename T>
 hipError_t launch_typed(const KvView& kv, const RowsView& k, const RowsView& v, const int32_t* chunk,
                         const int32_t* pos, int64_t n, hipStream_t stream) {
   const bool vec = rows_aligned(k, sizeof(T)) && rows_aligned(v, sizeof(T));
-  constexpr int kPieces = D / kItem<WRITE, T>;
   const uint64_t magic = ((uint64_t{1} << 40) + kv.heads - 1) / kv.heads;
-  const int64_t items = 2 * n * kv.heads * kPieces;
-  // one item per thread until that alone fills the GPU (256 CUs of 2,048 threads)
-  const int u = items >= int64_t{256} * 2048 * kInFlight ? kInFlight : 1;
-  const int group = u == 1 ? 1 : kTokenGroup;
-  const int64_t half = (n + group - 1) / group * group * kv.heads * kPieces;  // of keys, and of values
-  const dim3 grid(2 * static_cast<unsigned>((half + kThreads * u - 1) / (kThreads * u)));
+  const MoveGrid g = move_grid(kv.heads, D / kItem<WRITE, T>, n);
+  const dim3 grid(static_cast<unsigned>(g.groups));
   auto go = [&](auto write, auto read) {
     (WRITE ? write : read)<<<grid, kThreads, 0, stream>>>(kv, k, v, chunk, pos, n, magic);
     return hipGetLastError();
   };
-  if (u == 1)
+  if (g.u == 1)
     return vec ? go(kv_write_kernel<FMT, D, T, true, 1>, kv_read_kernel<FMT, D, T, true, 1>)
                : go(kv_write_kernel<FMT, D, T, false, 1>, kv_read_kernel<FMT, D, T, false, 1>);
   return vec ? go(kv_write_kernel<FMT, D, T, true, kInFlight>, kv_read_kernel<FMT, D, T, true, kInFlight>)
@@ -363,6 +373,11 @@ hipError_t launch_any(const KvView& kv, int fmt, int d, const RowsView& k, const
 }
 
 }  // namespace
+
+bool kv_move_fits(bool write, int heads, int d, int dtype, int64_t n) {
+  const int item = write ? kItem<true, float> : dtype == MEM_F32 ? kItem<false, float> : kItem<false, uint16_t>;
+  return move_grid(heads, d / item, n).groups <= kMaxGroups;
+}
 
 hipError_t launch_kv_write(const KvView& kv, int fmt, int d, const RowsView& k, const RowsView& v, int dtype,
                            const int32_t* chunk, const int32_t* pos, int64_t n, hipStream_t stream) {
