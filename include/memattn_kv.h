@@ -92,7 +92,8 @@ MEMATTN_API mem_status mem_kv_write(const mem_kv* kv, const mem_kv_rows* k, cons
  * Read n tokens back: rows i of `k` and `v` (dtype MEM_F32 or MEM_BF16,
  * written) receive the values of token pos[i] of chunk chunk[i], exactly;
  * places that mem_kv_write would skip give zeros.  A place may be named any
- * number of times.  The rows must not overlap each other or the pool.
+ * number of times.  The rows must not overlap each other (those of k may lie
+ * between those of v) or the pool.
  */
 MEMATTN_API mem_status mem_kv_read(const mem_kv* kv, const mem_kv_rows* k, const mem_kv_rows* v, int32_t dtype,
                                    const int32_t* chunk, const int32_t* pos, int64_t n, void* stream);

@@ -3,8 +3,10 @@
 // arguments have been checked.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <cstdlib>
 
 #include "memattn_kv.h"
 #include "error.h"
@@ -79,18 +81,42 @@ KvView view_of(const mem_kv* kv) {
   return v;
 }
 
-mem_status check_rows(const mem_kv_rows* r, int elem, const char* name) {
+mem_status check_rows(const mem_kv* kv, const mem_kv_rows* r, int elem, int64_t n, const char* name) {
   if (!r || !r->data) return fail(MEM_ERR_INVALID_ARG, "%s is NULL", name);
   if (!aligned(r->data, elem)) return fail(MEM_ERR_INVALID_ARG, "%s is not aligned to its elements", name);
   if (r->token_stride < 0 || r->head_stride < 0) return fail(MEM_ERR_INVALID_ARG, "%s has a negative stride", name);
+  constexpr int64_t kReach = int64_t{1} << 56;  // elements; more than any address space
+  int64_t tokens, heads;
+  if (__builtin_mul_overflow(n - 1, r->token_stride, &tokens) || tokens > kReach ||
+      __builtin_mul_overflow(int64_t{kv->heads - 1}, r->head_stride, &heads) || heads > kReach)
+    return fail(MEM_ERR_INVALID_ARG, "the strides of %s lead out of memory", name);
   return MEM_OK;
 }
 
-// First and last byte + 1 that rows cover.
+// First and last byte + 1 that rows cover (their strides have been checked).
 void span_of(const mem_kv* kv, const mem_kv_rows* r, int elem, int64_t n, uintptr_t* lo, uintptr_t* hi) {
   *lo = reinterpret_cast<uintptr_t>(r->data);
   *hi = *lo + static_cast<uintptr_t>(((n - 1) * r->token_stride + (kv->heads - 1) * r->head_stride + kv->head_dim) *
                                      elem);
+}
+
+// Whether some row of n tokens shares an element with a different row, or with any row of the same strides that start
+// `apart` elements later: whether |apart + i token_stride + j head_stride| < head_dim for some |i| < n, |j| < heads
+// (other than both 0 where apart is 0).  For each j only the two i around the zero of that sum can do it.
+bool rows_meet(const mem_kv* kv, const mem_kv_rows* r, int64_t n, int64_t apart) {
+  const int64_t ts = r->token_stride, hs = r->head_stride, d = kv->head_dim, h = kv->heads;
+  if (apart == 0 && ((hs >= d && ts >= (h - 1) * hs + d) || (ts >= d && hs >= (n - 1) * ts + d))) return false;
+  for (int64_t j = apart == 0 ? 0 : 1 - h; j < h; ++j) {
+    const int64_t at = apart + j * hs;
+    int64_t i0 = ts == 0 ? 0 : -at / ts - 1;
+    if (apart == 0 && j == 0) i0 = 1;
+    for (int64_t i = i0; i < i0 + 3; ++i) {
+      const int64_t k = std::min(std::max(i, 1 - n), n - 1);
+      if (apart == 0 && j == 0 && k == 0) continue;
+      if (std::llabs(at + k * ts) < d) return true;
+    }
+  }
+  return false;
 }
 
 mem_status move_tokens(bool write, const mem_kv* kv, const mem_kv_rows* k, const mem_kv_rows* v, int32_t dtype,
@@ -102,17 +128,15 @@ mem_status move_tokens(bool write, const mem_kv* kv, const mem_kv_rows* k, const
   if (n < 0) return fail(MEM_ERR_INVALID_ARG, "n < 0");
   if (n == 0) return MEM_OK;
   if (mem_status st = check_pool(kv); st != MEM_OK) return st;
-  const int elem = dtype == MEM_F32 ? 4 : 2;
-  if (mem_status st = check_rows(k, elem, "k"); st != MEM_OK) return st;
-  if (mem_status st = check_rows(v, elem, "v"); st != MEM_OK) return st;
-  if (!chunk || !pos) return fail(MEM_ERR_INVALID_ARG, "chunk or pos is NULL");
-  if (!aligned(chunk, 4) || !aligned(pos, 4)) return fail(MEM_ERR_INVALID_ARG, "chunk and pos must be 4-byte aligned");
   if (n > (int64_t{1} << 40) / (kv->heads * kv->head_dim) || !kv_move_fits(write, kv->heads, kv->head_dim, dtype, n))
     return fail(MEM_ERR_UNSUPPORTED, "n too large for one launch");
+  const int elem = dtype == MEM_F32 ? 4 : 2;
+  if (mem_status st = check_rows(kv, k, elem, n, "k"); st != MEM_OK) return st;
+  if (mem_status st = check_rows(kv, v, elem, n, "v"); st != MEM_OK) return st;
+  if (!chunk || !pos) return fail(MEM_ERR_INVALID_ARG, "chunk or pos is NULL");
+  if (!aligned(chunk, 4) || !aligned(pos, 4)) return fail(MEM_ERR_INVALID_ARG, "chunk and pos must be 4-byte aligned");
   if (!write) {
-    for (const mem_kv_rows* r : {k, v})
-      if ((n > 1 && r->token_stride < kv->head_dim) || (kv->heads > 1 && r->head_stride < kv->head_dim))
-        return fail(MEM_ERR_INVALID_ARG, "rows of k or v overlap");
+    if (rows_meet(kv, k, n, 0) || rows_meet(kv, v, n, 0)) return fail(MEM_ERR_INVALID_ARG, "rows of k or v overlap");
     uintptr_t k0, k1, v0, v1;
     span_of(kv, k, elem, n, &k0, &k1);
     span_of(kv, v, elem, n, &v0, &v1);
@@ -120,6 +144,13 @@ mem_status move_tokens(bool write, const mem_kv* kv, const mem_kv_rows* k, const
     const uintptr_t p1 = p0 + static_cast<uintptr_t>(kv->pages.n_pages * kv->pages.page_bytes);
     if ((k0 < p1 && p0 < k1) || (v0 < p1 && p0 < v1))
       return fail(MEM_ERR_INVALID_ARG, "k or v overlaps the page pool");
+    if (k0 < v1 && v0 < k1) {  // rows of keys may lie between rows of values, as in a fused array
+      const int64_t apart = (static_cast<int64_t>(v0) - static_cast<int64_t>(k0)) / elem;
+      const bool alike = (n == 1 || k->token_stride == v->token_stride) &&
+                         (kv->heads == 1 || k->head_stride == v->head_stride);
+      if (apart == 0 || (alike && rows_meet(kv, k, n, apart)))
+        return fail(MEM_ERR_INVALID_ARG, "rows of k and v overlap");
+    }
   }
   const RowsView kr{k->data, k->token_stride, k->head_stride}, vr{v->data, v->token_stride, v->head_stride};
   hipStream_t s = static_cast<hipStream_t>(stream);
