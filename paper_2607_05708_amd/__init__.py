@@ -31,6 +31,7 @@ and in ``include/memattn_kv.h``, over the same pages and directory:
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 
@@ -535,12 +536,20 @@ def mem_append_chunks(state: BankState, new_emb: torch.Tensor, stream=None) -> B
     return state
 
 
-def _used_on(stream, *tensors):
-    """Tensors allocated here on the current stream stay theirs until `stream` is done with them."""
+_HERE_TOO = contextlib.nullcontext()
+
+
+def _memory_of(stream):
+    """A context whose allocations are ``stream``'s memory: what held it before is done with when the call's kernels
+    write it.  (Memory of the current stream may still be in use there by work that ``stream`` does not wait for.)"""
+    return _HERE_TOO if stream is None or stream.cuda_stream == _stream(None) else torch.cuda.stream(stream)
+
+
+def _used_here(stream, *tensors):
+    """Results allocated in ``stream``'s memory may be used on the current stream, and freed, without further notice."""
     if stream is not None and stream.cuda_stream != _stream(None):
         for t in tensors:
-            if t is not None:
-                t.record_stream(stream)
+            t.record_stream(torch.cuda.current_stream())
 
 
 def _array(t: torch.Tensor, shape: tuple, name: str, dev: int, dtype=torch.int32) -> int:
@@ -621,9 +630,10 @@ def mem_kv_read(cache: KvCache, chunk: torch.Tensor, pos: torch.Tensor, *, dtype
     places outside the cache give zeros."""
     n, dev = chunk.shape[0], cache._dev
     if out is None:
-        k = torch.empty((n, cache.heads, cache.head_dim), dtype=dtype, device=cache.pool.device)
-        v = torch.empty_like(k)
-        _used_on(stream, k, v)
+        with _memory_of(stream):
+            k = torch.empty((n, cache.heads, cache.head_dim), dtype=dtype, device=cache.pool.device)
+            v = torch.empty_like(k)
+        _used_here(stream, k, v)
     else:
         k, v = out
         dtype = k.dtype
@@ -673,18 +683,19 @@ def mem_attend(cache: KvCache, tok_len: torch.Tensor, ids: torch.Tensor, q: torc
         None if chunk_ns is None else _array(chunk_ns, (n_chunks,), "chunk_ns", dev),
         None if query_ns is None else _array(query_ns, (total_q,), "query_ns", dev))
     if out is None:
-        o = torch.empty((total_q, heads_q, d), dtype=torch.bfloat16, device=q.device)
-        lse = torch.empty((total_q, heads_q), dtype=torch.float32, device=q.device)
-        _used_on(stream, o, lse)
+        with _memory_of(stream):
+            o = torch.empty((total_q, heads_q, d), dtype=torch.bfloat16, device=q.device)
+            lse = torch.empty((total_q, heads_q), dtype=torch.float32, device=q.device)
+        _used_here(stream, o, lse)
         o_ptr, lse_ptr = o.data_ptr(), lse.data_ptr()
     else:
         o, lse = out
         o_ptr = _array(o, (total_q, heads_q, d), "out", dev, torch.bfloat16)
         lse_ptr = None if lse is None else _array(lse, (total_q, heads_q), "out lse", dev, torch.float32)
     if workspace is None:
-        workspace = torch.empty(max(mem_attend_workspace_bytes(cache, m, k, total_q, heads_q), 1), dtype=torch.uint8,
-                                device=q.device)
-        _used_on(stream, workspace)
+        with _memory_of(stream):
+            workspace = torch.empty(max(mem_attend_workspace_bytes(cache, m, k, total_q, heads_q), 1),
+                                    dtype=torch.uint8, device=q.device)
     _dev(workspace, "workspace")
     status = lib().mem_attend(cache._ref, C.byref(a), q.data_ptr(), total_q, token, head, o_ptr, lse_ptr,
                               workspace.data_ptr(), workspace.nbytes, _stream(stream))
