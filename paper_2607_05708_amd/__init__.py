@@ -560,9 +560,17 @@ def _array(t: torch.Tensor, shape: tuple, name: str, dev: int, dtype=torch.int32
     return t.data_ptr()
 
 
+def _i32(x: int, name: str) -> int:
+    """An integer that 32 bits hold (ctypes would cut it to its low bits)."""
+    if not -2 ** 31 <= x < 2 ** 31:
+        raise ValueError(f"{name} = {x} does not fit 32 bits")
+    return x
+
+
 def mem_kv_page_bytes(page_tokens: int, heads: int, head_dim: int, format: int) -> int:
     """Bytes of one page of a key/value cache (0 on invalid sizes)."""
-    return int(lib().mem_kv_page_bytes(page_tokens, heads, head_dim, format))
+    return int(lib().mem_kv_page_bytes(_i32(page_tokens, "page_tokens"), _i32(heads, "heads"),
+                                       _i32(head_dim, "head_dim"), _i32(format, "format")))
 
 
 class KvCache:
@@ -587,7 +595,8 @@ class KvCache:
         self.page_tokens, self.heads, self.head_dim, self.format = page_tokens, heads, head_dim, format
         pages = MemPages(pool.data_ptr(), pool.shape[0], pool.shape[1] * pool.element_size(), ptr, table.shape[0],
                          table.shape[1])
-        self._c = MemKv(pages, page_tokens, heads, head_dim, format)
+        self._c = MemKv(pages, _i32(page_tokens, "page_tokens"), _i32(heads, "heads"), _i32(head_dim, "head_dim"),
+                        _i32(format, "format"))
         self._ref = C.byref(self._c)
 
 
@@ -645,7 +654,7 @@ def mem_kv_read(cache: KvCache, chunk: torch.Tensor, pos: torch.Tensor, *, dtype
 
 
 def mem_attend_workspace_bytes(cache: KvCache, m: int, k: int, total_q: int, heads_q: int) -> int:
-    return int(lib().mem_attend_workspace_bytes(cache._ref, m, k, total_q, heads_q))
+    return int(lib().mem_attend_workspace_bytes(cache._ref, m, _i32(k, "k"), total_q, _i32(heads_q, "heads_q")))
 
 
 def mem_attend(cache: KvCache, tok_len: torch.Tensor, ids: torch.Tensor, q: torch.Tensor, scale: float, *,
@@ -678,7 +687,8 @@ def mem_attend(cache: KvCache, tok_len: torch.Tensor, ids: torch.Tensor, q: torc
         _array(tok_len, (n_chunks,), "tok_len", dev), _array(ids, (m, k), "ids", dev), m, k, heads_q,
         None if q_offsets is None else _array(q_offsets, (m + 1,), "q_offsets", dev),
         None if q_pos is None else _array(q_pos, (total_q,), "q_pos", dev), scale, softcap,
-        None if slopes is None else _array(slopes, (heads_q,), "slopes", dev, torch.float32), 1 if causal else 0, window,
+        None if slopes is None else _array(slopes, (heads_q,), "slopes", dev, torch.float32), 1 if causal else 0,
+        _i32(window, "window"),
         None if prefix_len is None else _array(prefix_len, (m,), "prefix_len", dev),
         None if chunk_ns is None else _array(chunk_ns, (n_chunks,), "chunk_ns", dev),
         None if query_ns is None else _array(query_ns, (total_q,), "query_ns", dev))
