@@ -536,6 +536,15 @@ def mem_append_chunks(state: BankState, new_emb: torch.Tensor, stream=None) -> B
     return state
 
 
+def _stream_for(cache, stream):
+    """_stream(stream) for a call over ``cache``, whose GPU has to be the current one (and the stream's): elsewhere the
+    kernels would run on another GPU than the one that holds its memory."""
+    here = torch.cuda.current_device() if _get_device is None else _get_device()
+    if here != cache._dev or (stream is not None and stream.device.index not in (None, here)):
+        raise ValueError(f"the cache is on GPU {cache._dev}: make it the current one, and use a stream of it")
+    return _stream(stream)
+
+
 _HERE_TOO = contextlib.nullcontext()
 
 
@@ -626,9 +635,10 @@ def mem_kv_write(cache: KvCache, k: torch.Tensor, v: torch.Tensor, chunk: torch.
     token and head strides) become token ``pos[i]`` of chunk ``chunk[i]`` (int32 [n]).  A chunk of -1 skips the
     token; no two tokens may name one place."""
     n, dtype, dev = k.shape[0], k.dtype, cache._dev
+    on = _stream_for(cache, stream)
     status = lib().mem_kv_write(cache._ref, _kv_rows(cache, k, n, dtype, "k"), _kv_rows(cache, v, n, dtype, "v"),
                                 _kv_dtype(dtype), _array(chunk, (n,), "chunk", dev), _array(pos, (n,), "pos", dev), n,
-                                _stream(stream))
+                                on)
     _check("mem_kv_write", status)
 
 
@@ -638,6 +648,7 @@ def mem_kv_read(cache: KvCache, chunk: torch.Tensor, pos: torch.Tensor, *, dtype
     ``dtype`` (or written into ``out``, a pair of such tensors).  Both dtypes hold the cache's values exactly;
     places outside the cache give zeros."""
     n, dev = chunk.shape[0], cache._dev
+    on = _stream_for(cache, stream)
     if out is None:
         with _memory_of(stream):
             k = torch.empty((n, cache.heads, cache.head_dim), dtype=dtype, device=cache.pool.device)
@@ -648,7 +659,7 @@ def mem_kv_read(cache: KvCache, chunk: torch.Tensor, pos: torch.Tensor, *, dtype
         dtype = k.dtype
     status = lib().mem_kv_read(cache._ref, _kv_rows(cache, k, n, dtype, "out k"),
                                _kv_rows(cache, v, n, dtype, "out v"), _kv_dtype(dtype),
-                               _array(chunk, (n,), "chunk", dev), _array(pos, (n,), "pos", dev), n, _stream(stream))
+                               _array(chunk, (n,), "chunk", dev), _array(pos, (n,), "pos", dev), n, on)
     _check("mem_kv_read", status)
     return k, v
 
@@ -679,6 +690,7 @@ def mem_attend(cache: KvCache, tok_len: torch.Tensor, ids: torch.Tensor, q: torc
     m, k = ids.shape
     total_q, heads_q, d = q.shape
     dev, n_chunks = cache._dev, cache.table.shape[0]
+    on = _stream_for(cache, stream)
     token, head, one = q.stride()
     if q.dtype is not torch.bfloat16 or q.get_device() != dev or d != cache.head_dim or (total_q and one != 1):
         raise ValueError(f"q must be bfloat16 [total_q, heads_q, {cache.head_dim}] on the cache's GPU with unit "
@@ -708,6 +720,6 @@ def mem_attend(cache: KvCache, tok_len: torch.Tensor, ids: torch.Tensor, q: torc
                                     dtype=torch.uint8, device=q.device)
     _dev(workspace, "workspace")
     status = lib().mem_attend(cache._ref, C.byref(a), q.data_ptr(), total_q, token, head, o_ptr, lse_ptr,
-                              workspace.data_ptr(), workspace.nbytes, _stream(stream))
+                              workspace.data_ptr(), workspace.nbytes, on)
     _check("mem_attend", status)
     return o, lse

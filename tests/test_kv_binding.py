@@ -53,3 +53,16 @@ def test_integers_of_more_than_32_bits_are_refused(on_host, x):
             pm.mem_attend_workspace_bytes(host_cache(), *args)
     with pytest.raises(pm.MemError, match="launch"):         # without a GPU the same call ends there
         attend(host_cache(), window=7)
+
+
+def test_calls_need_the_caches_gpu_to_be_the_current_one(on_host, monkeypatch):
+    x, at = torch.zeros((2, 1, 64)), torch.zeros(2, dtype=torch.int32)
+    calls = [lambda: attend(host_cache()), lambda: pm.mem_kv_write(host_cache(), x, x.clone(), at, at),
+             lambda: pm.mem_kv_read(host_cache(), at, at, out=(x, x.clone()))]
+    for call in calls:
+        with pytest.raises(pm.MemError, match="launch"):     # without a GPU the call ends there
+            call()
+    monkeypatch.setattr(pm, "_get_device", lambda: 3)
+    for call in calls:
+        with pytest.raises(ValueError, match="current"):
+            call()
