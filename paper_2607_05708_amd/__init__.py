@@ -718,7 +718,8 @@ def mem_attend(cache: KvCache, tok_len: torch.Tensor, ids: torch.Tensor, q: torc
         with _memory_of(stream):
             workspace = torch.empty(max(mem_attend_workspace_bytes(cache, m, k, total_q, heads_q), 1),
                                     dtype=torch.uint8, device=q.device)
-    _dev(workspace, "workspace")
+    if not isinstance(workspace, torch.Tensor) or workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on the cache's GPU")
     status = lib().mem_attend(cache._ref, C.byref(a), q.data_ptr(), total_q, token, head, o_ptr, lse_ptr,
                               workspace.data_ptr(), workspace.nbytes, on)
     _check("mem_attend", status)

@@ -33,8 +33,9 @@ def on_host(monkeypatch):
 def attend(cache, **kw):
     q = torch.zeros((2, 2, 64), dtype=torch.bfloat16)
     out = torch.zeros((2, 2, 64), dtype=torch.bfloat16), None
+    kw = dict(workspace=torch.zeros(1 << 20, dtype=torch.uint8), **kw) if "workspace" not in kw else kw
     return pm.mem_attend(cache, torch.zeros(2, dtype=torch.int32), torch.zeros((2, 2), dtype=torch.int32), q, 1.0,
-                         out=out, workspace=torch.zeros(1 << 20, dtype=torch.uint8), **kw)
+                         out=out, **kw)
 
 
 @pytest.mark.parametrize("x", WIDE)
@@ -66,3 +67,10 @@ def test_calls_need_the_caches_gpu_to_be_the_current_one(on_host, monkeypatch):
     for call in calls:
         with pytest.raises(ValueError, match="current"):
             call()
+
+
+def test_a_workspace_has_the_memory_that_it_counts(on_host):
+    one = torch.zeros(1, dtype=torch.uint8)
+    for bad in (one.expand(1 << 20), torch.zeros((1024, 2048), dtype=torch.uint8)[:, ::2]):
+        with pytest.raises(ValueError, match="workspace"):
+            attend(host_cache(), workspace=bad)
