@@ -151,7 +151,11 @@ MEMATTN_API size_t mem_attend_workspace_bytes(const mem_kv* kv, int64_t m, int32
  * aligned.  Products are bf16 with fp32 sums; the softmax weights are rounded
  * to bf16 for the second product (heavy ones to 16 bits) and out is divided by
  * the unrounded weights' sum, which is also lse's.  A capped score is off by at
- * most 2^-19 of itself, or with a cap of up to 64 by 2^-21 of the cap.  Rows of q that no request
+ * most 2^-19 of itself, or with a cap of up to 64 by 2^-21 of the cap.  Scores,
+ * distances and the sums of weighted values are fp32 before the division by
+ * the weights' sum: weights below some 2^-126 of the largest count as 0, and
+ * weights are relative to a reference that may lag 2^8 behind the largest, so
+ * that values from 2^120 / n on (of n tokens) may overflow.  Rows of q that no request
  * owns are not written.  The context lengths are read on the device: nothing
  * is synchronised, and the call can be captured into a HIP graph.  Calls whose
  * tiles (16, 32 or 128 rows of a key/value head and request) come to 2^24 or

@@ -23,17 +23,24 @@
 //     elements: exactly one block, so one scale) straight from the page into
 //     the operand of the first product; values go through the wave's own LDS
 //     rows once, as bf16, to be read back transposed.  Bound by HBM where the
-//     contexts are long (128 x 32,768 tokens in 4 bits 784 us, 5.8 TB/s; a plain
+//     contexts are long (128 x 32,768 tokens in 4 bits 782 us, 5.8 TB/s; a plain
 //     copy reaches 5.1), by the start of a workgroup -- four dependent loads and
-//     the lookups, some 6 us -- where they are short (2,560 tokens 12 us).
+//     the lookups, some 6 us -- where they are short (2,560 tokens 13 us).
 //   attend_tile_kernel  tiles of 128 rows: the workgroup unpacks two units at
 //     a time into LDS for its four waves, into one half of a double buffer
 //     while they work on the other; a wave's matrix products are interleaved
-//     with the exponentials and the unpacking.  Bound by the matrix cores and
-//     the vector unit together, at the clock that their power leaves: 4 x 2,048
-//     tokens over 8,192, capped, 1.14 ms (845 TFLOP/s); 8,192 tokens behind
-//     24,576, with a distance bias, 4.76 ms (808 TFLOP/s); a large library
-//     product reaches 1,340.
+//     with the exponentials and the unpacking.  4 x 2,048 tokens over 8,192,
+//     capped, 1.13 ms (849 TFLOP/s); 8,192 tokens behind 24,576, with a distance
+//     bias, 4.67 ms (824 TFLOP/s); a large library product reaches 1,360.
+//     Counters of these two: the vector unit issues in 61 and 53 % of the cycles,
+//     the matrix cores are busy in 37 and 33 %, LDS in 40 and 36 % (a quarter of
+//     that bank conflicts); the clock is at 2.3 and 2.4 GHz once the passes
+//     follow each other for some 40 ms, and 1.8 to 2.1 before.  So it is the
+//     vector work between the products, and what does not overlap with it.
+//     Registers are short: heads of 64 (three workgroups a CU) spill 19 to 80 of
+//     them, bf16 with wider heads 20 to 108 (tiles of 32 rows 10 to 12, and 107
+//     at 256), 8 and 4 bits with heads of 256 up to 22, 8 bits with capped scores
+//     and heads of 128 up to 10.
 #include <type_traits>
 
 #include "kv.h"
@@ -556,15 +563,15 @@ enum Caps { kNoCap, kModestCaps, kLargeCaps };
 constexpr float kModestCap = 64.f;
 
 // How raw products become scores in the log2 domain: scaled, capped, biased.  The cap is softcap * tanh(x), x the
-// scaled product over the cap.  By its definition the tanh is 1 - 2 / (1 + e^2x), with two transcendental operations of
-// twice to three times a product's cost each, and an error of 2^-21 whatever its size.  Where |x| is at most kSmall,
-// tanh(x) / x as a polynomial of degree 2 in t = x^2 does as well: its series 1 - t / 3 + 2 t^2 / 15 - 17 t^3 / 315 with
-// t^3 replaced by the quadratic that is nearest to it on [0, kSmall^2], off by at most kSmall^6 / 32 (Chebyshev).  With
-// the series' next term that is 1.1e-7 of the score.  Units without a larger product take it for all of them.  In the
-// others a modest cap takes the definition for all (off by at most 2^-15, where the weights are rounded by 2^-9 of
-// themselves); of a larger cap that error would be a multiple, so each score goes by its own size, and is off by 2^-19
-// of itself at most.  (The choice for each costs 20 % of a prefill whose scores are of the cap's size, and registers:
-// kernels of their own.)
+// scaled product over the cap.  By its definition the tanh is 1 - 2 / (1 + e^2x), with two transcendental operations
+// of twice to three times a product's cost each, and an error of 2^-21 whatever its size.  Where |x| is at most
+// kSmall, tanh(x) / x as a polynomial of degree 2 in t = x^2 does as well: its series 1 - t / 3 + 2 t^2 / 15 - 17 t^3
+// / 315 with t^3 replaced by the quadratic that is nearest to it on [0, kSmall^2], off by at most kSmall^6 / 32
+// (Chebyshev).  With the series' next term that is 1.1e-7 of the score.  Units without a larger product take it for
+// all of them.  In the others a modest cap takes the definition for all (off by at most 2^-15, where the weights are
+// rounded by 2^-9 of themselves); of a larger cap that error would be a multiple, so each score goes by its own size,
+// and is off by 2^-19 of itself at most.  (The choice for each costs 20 % of a prefill whose scores are of the cap's
+// size, and registers: kernels of their own.)
 struct Scores {
   float c;     // scale * log2(e)
   float k2;    // 2 * log2(e) * scale / softcap
@@ -1461,17 +1468,21 @@ int64_t tile_count(bool ragged, int64_t m, int64_t total_q, int group, int R) {
   return m * ((total_q / m * group + R - 1) / R);
 }
 
-// Workgroups that run together on the 256 CUs, by what a kernel's registers and LDS allow.
+// Workgroups that run together on the 256 CUs, by the registers of the 4-bit kernels.  Others differ: with 16 rows
+// heads of 64 in 4 and 8 bits run four a CU, heads of 128 in 8 bits and bf16 two; with 32 rows heads of 64 in 4 and 8
+// bits three, in bf16 two; tiles of 128 rows of heads of 128 one where the list has some 235 entries or more (LDS).
+// Plans for these are right, but their rounds are not those that are counted here.
 int64_t slots_of(int rows, int d) {
   const int per_cu = d == 256 ? 1 : d == 64 ? 3 : rows == 16 ? 3 : 2;
   return int64_t{256} * per_cu;
 }
 
-// Rows per request (on average) decide the kernel.  4-bit keys, heads of 128, 8 heads, 4,096 tokens a request, us: 128
-// requests of 8 rows over 1,024 tokens in tiles of 16 rows 39, of 32 rows 52; 32 requests of 48 rows in tiles of 32
-// rows 82, of 128 102; of 64 rows 112 and 107, of 96 rows 132 and 148, of 128 rows 185 and 152.  The context is split so that the rounds of workgroups take least,
-// a workgroup being taken to cost its units and kStart more: finding its units, its start and its end.  Tiles of 128
-// rows that fill the GPU are left whole: causal ones are of unequal length, and even out by themselves.
+// Rows per request (on average, so that a call of prompts and single tokens has one height for both) decide the
+// kernel.  4-bit keys, heads of 128, 8 heads, 4,096 tokens a request, us: 128 requests of 8 rows over 1,024 tokens in
+// tiles of 16 rows 39, of 32 rows 52; 32 requests of 48 rows in tiles of 32 rows 82, of 128 102; of 64 rows 112 and
+// 107, of 96 rows 132 and 148, of 128 rows 185 and 152.  The context is split so that the rounds of workgroups take
+// least, a workgroup being taken to cost its units and kStart more: finding its units, its start and its end.  Tiles
+// of 128 rows that fill the GPU are left whole: causal ones are of unequal length, and even out by themselves.
 constexpr int64_t kStart = 16;
 
 // Bytes of LDS that a workgroup's chunk list takes.
@@ -1485,7 +1496,9 @@ static_assert(2 * sizeof(uint16_t) * (TileShape<MEM_KV_BF16, 256>::kKeys + TileS
                   160 * 1024,
               "a workgroup's LDS");
 
-int64_t join_groups(int64_t rows, int64_t splits) { return splits <= kJoinSplits ? (rows + kWaves - 1) / kWaves : rows; }
+int64_t join_groups(int64_t rows, int64_t splits) {
+  return splits <= kJoinSplits ? (rows + kWaves - 1) / kWaves : rows;
+}
 
 AttendPlan make_plan(int d, int64_t m, int k, int64_t units, int64_t total_q, int heads, int heads_q, bool ragged) {
   AttendPlan p;

@@ -1,7 +1,7 @@
 // Writing a quantised key/value cache and reading it back.
 //
 // Both move every byte once: a dense row in one direction, its codes and
-// scales in the other, and are bound by HBM (5.4 to 5.9 TB/s in large calls,
+// scales in the other, and are bound by HBM (4.9 to 6.3 TB/s in large calls,
 // where a plain copy reaches 5.1; one token of 64 sessions takes 3.2 us).  An
 // item is eight consecutive elements (four to be read back as fp32); when
 // writing, the four items of a block of 32 are neighbouring lanes, which share
@@ -42,10 +42,11 @@ __device__ __forceinline__ Place kv_place(const KvView& kv, int32_t chunk, int32
 
 // A workgroup's share of the rows, of keys or of values: a call moves all keys, then all values.  (Dense keys and
 // values are arrays of one size, often a power of two apart: written together, both streams meet the same channels and
-// banks.  131,071 tokens read back from 4 bits: token by token with keys and values side by side 192 us, so 125 us,
-// 5.4 TB/s.)  Within them rows go by groups of GROUP consecutive tokens, head by head: consecutive tokens are mostly
+// banks.  131,071 tokens read back from 4 bits: token by token with keys and values side by side 192 us, so 129 us,
+// 5.3 TB/s.)  Within them rows go by groups of GROUP consecutive tokens, head by head: consecutive tokens are mostly
 // neighbours in a page, where heads lie apart, so that a workgroup moves whole stretches of codes and scales (65,536
-// fp32 tokens to 8 bits and back: 244 -> 232 us).  GROUP is 1 in small calls, where a group would be mostly empty.
+// fp32 tokens to 8 bits and back: 5 % less, 138 and 106 us).  GROUP is 1 in small calls, where a group would be mostly
+// empty.
 template <int GROUP>
 struct Share {
   int64_t tok0;      // first token of its first group
