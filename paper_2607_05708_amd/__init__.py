@@ -23,11 +23,21 @@ Names follow the C ABI in ``include/memattn.h``:
 * ``mem_compact_blocks``  -- background block compaction (Eq. 2, Algorithm 2)
 * ``mem_colocate``        -- association-aware relocation (Algorithm 2, online stage)
 
-and in ``include/memattn_kv.h``, over the same pages and directory:
+in ``include/memattn_kv.h``, over the same pages and directory:
 
 * ``KvCache``, ``mem_kv_page_bytes`` -- a paged cache of keys and values in 16, 8 or 4 bits
 * ``mem_kv_write`` / ``mem_kv_read`` -- quantise tokens into it, read them back
 * ``mem_attend``          -- attention of each request's new tokens over its chunks
+
+in ``include/memattn_append.h``:
+
+* ``mem_kv_append``       -- mem_kv_write with the position rotation applied on the way, to keys and queries
+
+and in ``include/memattn_latent.h``:
+
+* ``LatentCache``, ``mem_latent_page_bytes`` -- a paged cache of one latent vector and one rotated key part per token
+* ``mem_latent_append`` / ``mem_latent_read`` -- tokens into it, and back
+* ``mem_latent_attend``   -- attention with keys and values from the latent vectors, expanded or absorbed
 """
 from __future__ import annotations
 
@@ -43,12 +53,16 @@ __all__ = ["MemError", "MEM_F32", "MEM_BF16", "MEM_ORDER_RANK", "MEM_ORDER_TIME"
            "mem_build_relations_scoped", "mem_workspace_bytes_grouped", "mem_retrieve_topk_grouped", "mem_gather_chunks", "mem_gather_budget", "mem_append_chunks",
            "mem_compact_workspace_bytes", "mem_compact_blocks", "mem_colocate_workspace_bytes", "mem_colocate",
            "BankState", "MEM_KV_BF16", "MEM_KV_FP8", "MEM_KV_FP4", "KvCache", "mem_kv_page_bytes", "mem_kv_write",
-           "mem_kv_read", "mem_attend_workspace_bytes", "mem_attend"]
+           "mem_kv_append", "mem_kv_read", "mem_attend_workspace_bytes", "mem_attend", "MEM_LATENT_AUTO",
+           "MEM_LATENT_ABSORBED", "MEM_LATENT_EXPANDED", "LatentCache", "mem_latent_page_bytes", "mem_latent_append",
+           "mem_latent_read", "mem_latent_attend_workspace_bytes", "mem_latent_attend"]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 MEM_F32, MEM_BF16 = 0, 1
 MEM_ORDER_RANK, MEM_ORDER_TIME = 0, 1
 MEM_KV_BF16, MEM_KV_FP8, MEM_KV_FP4 = 0, 1, 2
+MEM_ROTATE_HALVES, MEM_ROTATE_PAIRS = 0, 1
+MEM_LATENT_AUTO, MEM_LATENT_ABSORBED, MEM_LATENT_EXPANDED = 0, 1, 2
 
 
 class MemBank(C.Structure):
@@ -84,6 +98,19 @@ class MemKv(C.Structure):
 
 class MemKvRows(C.Structure):
     _fields_ = [("data", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class MemRotation(C.Structure):
+    _fields_ = [("pos", C.c_void_p), ("freq", C.c_void_p), ("dim", C.c_int32), ("style", C.c_int32)]
+
+
+class MemLatent(C.Structure):
+    _fields_ = [("pages", MemPages), ("page_tokens", C.c_int32), ("latent_dim", C.c_int32), ("rope_dim", C.c_int32),
+                ("format", C.c_int32)]
+
+
+class MemLatentWeights(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("head_stride", C.c_int64), ("row_stride", C.c_int64), ("head_dim", C.c_int32)]
 
 
 class MemAttendArgs(C.Structure):
@@ -160,6 +187,22 @@ def lib():
         L.mem_attend_workspace_bytes.restype = C.c_size_t
         L.mem_attend.argtypes = [C.POINTER(MemKv), C.POINTER(MemAttendArgs), P, i64, i64, i64, P, P, P, C.c_size_t, P]
         L.mem_attend.restype = C.c_int
+        rows = C.POINTER(MemKvRows)
+        L.mem_kv_append.argtypes = [C.POINTER(MemKv), rows, rows, rows, rows, i32, i32, C.POINTER(MemRotation), P, P,
+                                    i64, P]
+        L.mem_kv_append.restype = C.c_int
+        L.mem_latent_page_bytes.argtypes = [i32, i32, i32, i32]
+        L.mem_latent_page_bytes.restype = C.c_size_t
+        L.mem_latent_append.argtypes = [C.POINTER(MemLatent), rows, rows, rows, rows, i32, i32, C.POINTER(MemRotation),
+                                        P, P, i64, P]
+        L.mem_latent_append.restype = C.c_int
+        L.mem_latent_read.argtypes = [C.POINTER(MemLatent), rows, rows, i32, P, P, i64, P]
+        L.mem_latent_read.restype = C.c_int
+        L.mem_latent_attend_workspace_bytes.argtypes = [C.POINTER(MemLatent), i64, i32, i64, i32, i32, i32]
+        L.mem_latent_attend_workspace_bytes.restype = C.c_size_t
+        L.mem_latent_attend.argtypes = [C.POINTER(MemLatent), C.POINTER(MemAttendArgs), rows, rows, i64,
+                                        C.POINTER(MemLatentWeights), i32, P, P, P, C.c_size_t, P]
+        L.mem_latent_attend.restype = C.c_int
         L.mem_status_string.argtypes = [C.c_int]
         L.mem_status_string.restype = C.c_char_p
         L.mem_last_error.argtypes = []
@@ -642,6 +685,63 @@ def mem_kv_write(cache: KvCache, k: torch.Tensor, v: torch.Tensor, chunk: torch.
     _check("mem_kv_write", status)
 
 
+def _head_rows(cache, t: torch.Tensor, shape: tuple, dtype, name: str):
+    """Rows [n, heads, length] of any token and head strides."""
+    if not isinstance(t, torch.Tensor) or t.get_device() != cache._dev or t.dtype is not dtype or t.shape != shape:
+        raise ValueError(f"{name} must be {dtype} {list(shape)} on the cache's GPU")
+    token, head, one = t.stride()
+    if one != 1 and t.numel():
+        raise ValueError(f"{name} must have unit stride along its last dimension")
+    return MemKvRows(t.data_ptr(), token, head)
+
+
+def _rotation(cache, at, freq, n: int, pairs: bool) -> MemRotation:
+    if not isinstance(freq, torch.Tensor) or freq.dim() != 1:
+        raise ValueError("freq must be float32 [pairs]")
+    return MemRotation(_array(at, (n,), "at", cache._dev),
+                       _array(freq, (freq.shape[0],), "freq", cache._dev, torch.float32), 2 * freq.shape[0],
+                       MEM_ROTATE_PAIRS if pairs else MEM_ROTATE_HALVES)
+
+
+def _turned_queries(cache, q, q_out, n: int, length: int, dtype, stream):
+    """(rows of q, rows of q_out, heads, q_out) of an append call; q_out is allocated if it is not given."""
+    if q is None:
+        if q_out is not None:
+            raise ValueError("q_out without q")
+        return None, None, 0, None
+    if not isinstance(q, torch.Tensor) or q.dim() != 3:
+        raise ValueError(f"q must be {dtype} [{n}, heads, {length}]")
+    shape = (n, q.shape[1], length)
+    rows = _head_rows(cache, q, shape, dtype, "q")
+    if q_out is None:
+        with _memory_of(stream):
+            q_out = torch.empty(shape, dtype=torch.bfloat16, device=q.device)
+        _used_here(stream, q_out)
+    return rows, _head_rows(cache, q_out, shape, torch.bfloat16, "q_out"), shape[1], q_out
+
+
+def _ref(x):
+    return None if x is None else C.byref(x)
+
+
+def mem_kv_append(cache: KvCache, k: torch.Tensor, v: torch.Tensor, chunk: torch.Tensor, pos: torch.Tensor,
+                  at: torch.Tensor, freq: torch.Tensor, *, q: torch.Tensor | None = None,
+                  q_out: torch.Tensor | None = None, pairs: bool = False, stream=None):
+    """mem_kv_write with the keys rotated on the way: the first 2 len(freq) elements of token i's rows by the angles
+    ``at[i] * freq`` (``at`` int32 [n], ``freq`` float32; elements j and j + len(freq) are a pair, with ``pairs`` 2 j
+    and 2 j + 1).  With ``q`` ([n, heads_q, head_dim], dtype of ``k``) the queries are rotated too: returns them as
+    bfloat16, written to ``q_out`` if it is given (q itself, or rows apart from q, k and v)."""
+    n, dtype, dev = k.shape[0], k.dtype, cache._dev
+    on = _stream_for(cache, stream)
+    rot = _rotation(cache, at, freq, n, pairs)
+    kr, vr, code = _kv_rows(cache, k, n, dtype, "k"), _kv_rows(cache, v, n, dtype, "v"), _kv_dtype(dtype)
+    c_ptr, p_ptr = _array(chunk, (n,), "chunk", dev), _array(pos, (n,), "pos", dev)
+    qr, qo, heads_q, q_out = _turned_queries(cache, q, q_out, n, cache.head_dim, dtype, stream)
+    _check("mem_kv_append", lib().mem_kv_append(cache._ref, kr, vr, _ref(qr), _ref(qo), heads_q, code, C.byref(rot),
+                                                c_ptr, p_ptr, n, on))
+    return q_out
+
+
 def mem_kv_read(cache: KvCache, chunk: torch.Tensor, pos: torch.Tensor, *, dtype=torch.bfloat16, out=None,
                 stream=None):
     """Tokens ``pos[i]`` of chunks ``chunk[i]`` (int32 [n]) as dense rows: (k, v), each [n, heads, head_dim] of
@@ -724,3 +824,152 @@ def mem_attend(cache: KvCache, tok_len: torch.Tensor, ids: torch.Tensor, q: torc
                               workspace.data_ptr(), workspace.nbytes, on)
     _check("mem_attend", status)
     return o, lse
+
+
+def mem_latent_page_bytes(page_tokens: int, latent_dim: int, rope_dim: int, format: int) -> int:
+    """Bytes of one page of a latent cache (0 on invalid sizes)."""
+    return int(lib().mem_latent_page_bytes(_i32(page_tokens, "page_tokens"), _i32(latent_dim, "latent_dim"),
+                                           _i32(rope_dim, "rope_dim"), _i32(format, "format")))
+
+
+class LatentCache:
+    """One layer's paged cache of a latent vector and a rotated key part per token, over a page pool and its directory.
+
+    ``pool``: uint8 [n_pages, page_bytes] GPU tensor, page_bytes >= mem_latent_page_bytes(...); ``table``: int32
+    [n_chunks, pages_per_chunk] GPU tensor; ``page_tokens`` tokens per page of ``latent_dim`` elements in ``format``
+    (MEM_KV_BF16, MEM_KV_FP8 or MEM_KV_FP4) and ``rope_dim`` in bf16.  The tensors are kept, not copied.
+    """
+
+    def __init__(self, pool: torch.Tensor, table: torch.Tensor, page_tokens: int, latent_dim: int, rope_dim: int,
+                 format: int):
+        _dev(pool, "pool")
+        if pool.dim() != 2 or not pool.is_contiguous():
+            raise ValueError("pool must be contiguous [n_pages, page_bytes]")
+        if table.dim() != 2:
+            raise ValueError("table must be int32 [n_chunks, pages_per_chunk]")
+        self._dev = pool.get_device()
+        ptr = _array(table, tuple(table.shape), "table", self._dev)
+        self.pool, self.table = pool, table
+        self.page_tokens, self.latent_dim, self.rope_dim, self.format = page_tokens, latent_dim, rope_dim, format
+        pages = MemPages(pool.data_ptr(), pool.shape[0], pool.shape[1] * pool.element_size(), ptr, table.shape[0],
+                         table.shape[1])
+        self._c = MemLatent(pages, _i32(page_tokens, "page_tokens"), _i32(latent_dim, "latent_dim"),
+                            _i32(rope_dim, "rope_dim"), _i32(format, "format"))
+        self._ref = C.byref(self._c)
+
+
+def _token_rows(cache: LatentCache, t: torch.Tensor, n: int, length: int, dtype, name: str):
+    """Rows [n, length] of any token stride."""
+    if (not isinstance(t, torch.Tensor) or t.get_device() != cache._dev or t.dtype is not dtype
+            or t.shape != (n, length)):
+        raise ValueError(f"{name} must be {dtype} [{n}, {length}] on the cache's GPU")
+    token, one = t.stride()
+    if one != 1 and n:
+        raise ValueError(f"{name} must have unit stride along its last dimension")
+    return MemKvRows(t.data_ptr(), token, 0)
+
+
+def mem_latent_append(cache: LatentCache, c: torch.Tensor, r: torch.Tensor, chunk: torch.Tensor, pos: torch.Tensor,
+                      at: torch.Tensor | None = None, freq: torch.Tensor | None = None, *,
+                      q: torch.Tensor | None = None, q_out: torch.Tensor | None = None, pairs: bool = False,
+                      stream=None):
+    """Append tokens: rows i of ``c`` [n, latent_dim] and ``r`` [n, rope_dim] (float32 or bfloat16, any token stride)
+    become token ``pos[i]`` of chunk ``chunk[i]`` (int32 [n]; a chunk of -1 skips the token), ``r`` rotated by the
+    angles ``at[i] * freq`` as in mem_kv_append (without ``at`` and ``freq`` it is rotated already).  With ``q``
+    ([n, heads, rope_dim], dtype of ``c``: the rotated part of the queries) these are rotated too: returns them as
+    bfloat16, written to ``q_out`` if it is given."""
+    n, dtype, dev = c.shape[0], c.dtype, cache._dev
+    on = _stream_for(cache, stream)
+    if (at is None) != (freq is None):
+        raise ValueError("at and freq belong together")
+    rot = None if at is None else _rotation(cache, at, freq, n, pairs)
+    cr = _token_rows(cache, c, n, cache.latent_dim, dtype, "c")
+    rr = _token_rows(cache, r, n, cache.rope_dim, dtype, "r")
+    code = _kv_dtype(dtype)
+    c_ptr, p_ptr = _array(chunk, (n,), "chunk", dev), _array(pos, (n,), "pos", dev)
+    qr, qo, heads_q, q_out = _turned_queries(cache, q, q_out, n, cache.rope_dim, dtype, stream)
+    _check("mem_latent_append", lib().mem_latent_append(cache._ref, C.byref(cr), C.byref(rr), _ref(qr), _ref(qo),
+                                                        heads_q, code, _ref(rot), c_ptr, p_ptr, n, on))
+    return q_out
+
+
+def mem_latent_read(cache: LatentCache, chunk: torch.Tensor, pos: torch.Tensor, *, dtype=torch.bfloat16, out=None,
+                    stream=None):
+    """Tokens ``pos[i]`` of chunks ``chunk[i]`` (int32 [n]) as dense rows: (c [n, latent_dim], r [n, rope_dim]) of
+    ``dtype`` (or written into ``out``, a pair of such tensors).  Both dtypes hold the cache's values exactly; places
+    outside the cache give zeros."""
+    n, dev = chunk.shape[0], cache._dev
+    on = _stream_for(cache, stream)
+    if out is None:
+        with _memory_of(stream):
+            c = torch.empty((n, cache.latent_dim), dtype=dtype, device=cache.pool.device)
+            r = torch.empty((n, cache.rope_dim), dtype=dtype, device=cache.pool.device)
+        _used_here(stream, c, r)
+    else:
+        c, r = out
+        dtype = c.dtype
+    cr = _token_rows(cache, c, n, cache.latent_dim, dtype, "out c")
+    rr = _token_rows(cache, r, n, cache.rope_dim, dtype, "out r")
+    _check("mem_latent_read", lib().mem_latent_read(cache._ref, C.byref(cr), C.byref(rr), _kv_dtype(dtype),
+                                                    _array(chunk, (n,), "chunk", dev), _array(pos, (n,), "pos", dev),
+                                                    n, on))
+    return c, r
+
+
+def mem_latent_attend_workspace_bytes(cache: LatentCache, m: int, k: int, total_q: int, heads: int, head_dim: int,
+                                      form: int = MEM_LATENT_AUTO) -> int:
+    return int(lib().mem_latent_attend_workspace_bytes(cache._ref, m, _i32(k, "k"), total_q, _i32(heads, "heads"),
+                                                       _i32(head_dim, "head_dim"), _i32(form, "form")))
+
+
+def mem_latent_attend(cache: LatentCache, tok_len: torch.Tensor, ids: torch.Tensor, q: torch.Tensor, t: torch.Tensor,
+                      w: torch.Tensor, scale: float, *, q_offsets: torch.Tensor | None = None,
+                      q_pos: torch.Tensor | None = None, causal: bool = False, window: int = 0,
+                      prefix_len: torch.Tensor | None = None, chunk_ns: torch.Tensor | None = None,
+                      query_ns: torch.Tensor | None = None, form: int = MEM_LATENT_AUTO,
+                      out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
+                      workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Attention of each request's new tokens over its chunks, keys and values from the latent vectors: out bfloat16
+    [total_q, heads, head_dim].
+
+    ``q`` [total_q, heads, head_dim] and ``t`` [total_q, heads, rope_dim] (bfloat16, any token and head strides): the
+    queries and their rotated part; ``w`` bfloat16 [heads, 2 * head_dim, latent_dim] (any head and row strides): a
+    head's keys are ``[w[h, :head_dim] c, r]``, its values ``w[h, head_dim:] c``.  Scores are ``scale (<q, W c> + <t,
+    r>)``.  Requests, positions and masks as in mem_attend.  ``form``: MEM_LATENT_ABSORBED, MEM_LATENT_EXPANDED, or
+    the one that costs less.  ``lse`` (float32 [total_q, heads]) receives the log sums if it is given.  A token that
+    sees nothing gets zeros and an lse of -inf.
+    """
+    if ids.dim() != 2 or q.dim() != 3 or w.dim() != 3:
+        raise ValueError("ids must be int32 [m, k]; q [total_q, heads, head_dim], w [heads, 2 * head_dim, latent_dim]")
+    m, k = ids.shape
+    total_q, heads, d = q.shape
+    dev, n_chunks = cache._dev, cache.table.shape[0]
+    on = _stream_for(cache, stream)
+    qr = _head_rows(cache, q, (total_q, heads, d), torch.bfloat16, "q")
+    tr = _head_rows(cache, t, (total_q, heads, cache.rope_dim), torch.bfloat16, "t")
+    wr = _head_rows(cache, w, (heads, 2 * d, cache.latent_dim), torch.bfloat16, "w")
+    weights = MemLatentWeights(wr.data, wr.token_stride, wr.head_stride, d)
+    a = MemAttendArgs(
+        _array(tok_len, (n_chunks,), "tok_len", dev), _array(ids, (m, k), "ids", dev), m, k, heads,
+        None if q_offsets is None else _array(q_offsets, (m + 1,), "q_offsets", dev),
+        None if q_pos is None else _array(q_pos, (total_q,), "q_pos", dev), scale, 0.0, None, 1 if causal else 0,
+        _i32(window, "window"),
+        None if prefix_len is None else _array(prefix_len, (m,), "prefix_len", dev),
+        None if chunk_ns is None else _array(chunk_ns, (n_chunks,), "chunk_ns", dev),
+        None if query_ns is None else _array(query_ns, (total_q,), "query_ns", dev))
+    if out is None:
+        with _memory_of(stream):
+            out = torch.empty((total_q, heads, d), dtype=torch.bfloat16, device=q.device)
+        _used_here(stream, out)
+    o_ptr = _array(out, (total_q, heads, d), "out", dev, torch.bfloat16)
+    lse_ptr = None if lse is None else _array(lse, (total_q, heads), "lse", dev, torch.float32)
+    if workspace is None:
+        with _memory_of(stream):
+            workspace = torch.empty(max(mem_latent_attend_workspace_bytes(cache, m, k, total_q, heads, d, form), 1),
+                                    dtype=torch.uint8, device=q.device)
+    if not isinstance(workspace, torch.Tensor) or workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on the cache's GPU")
+    _check("mem_latent_attend", lib().mem_latent_attend(
+        cache._ref, C.byref(a), C.byref(qr), C.byref(tr), total_q, C.byref(weights), form, o_ptr, lse_ptr,
+        workspace.data_ptr(), workspace.nbytes, on))
+    return out

@@ -642,6 +642,82 @@ __device__ __forceinline__ float wave_sum_f32(float x) {
   return (lane_f32(x, 0) + lane_f32(x, 16)) + (lane_f32(x, 32) + lane_f32(x, 48));
 }
 
+// ---------------------------------------------------------------- joining splits
+
+constexpr int kMaxSplits = 64;  // one lane of the join each
+
+// A row's partial results, weighed and added by W waves (1: four rows a workgroup): lane s of every wave weighs split
+// s, wave w adds splits w, w + W, ..., whose outputs are on their way before the weights are known; then the waves'
+// sums are added in order.  One wave a row where there are few splits (kJoinSplits): 32 requests of 96 rows in a few
+// splits 148 us, with four waves a row 162; bound by its two launches' worth of latency (3 to 5 us).
+constexpr int kJoinSplits = 8;
+template <int D, int W>
+__global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a, int splits,
+                                                               const float* __restrict__ part_o,
+                                                               const RowState* __restrict__ part_ml) {
+  constexpr int kPer = D / 64, kBatch = 8;
+  __shared__ float sums[W == 1 ? 1 : W][D];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int first = W == 1 ? 0 : wave;
+  const int64_t rows = a.total_q * a.hq, at = W == 1 ? static_cast<int64_t>(blockIdx.x) * kWaves + wave : blockIdx.x;
+  if (at >= rows) return;
+  if (a.q_offsets) {  // rows that no request owns were not computed
+    const int64_t j = at / a.hq;
+    if (j < a.q_offsets[0] || j >= a.q_offsets[a.m]) return;
+  }
+  RowState st{-INFINITY, 0.f};
+  if (lane < splits) st = part_ml[lane * rows + at];
+  float v[kBatch][kPer];
+  auto load = [&](int s0) {  // (past the last split: the last one again, so that loads stand behind no condition)
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      const float* src = part_o + (min(s0 + W * u, splits - 1) * rows + at) * D + lane * kPer;
+#pragma unroll
+      for (int x = 0; x < kPer; ++x) v[u][x] = src[x];
+    }
+  };
+  load(first);
+  const float m = wave_max_f32(st.m);
+  const float f = fast_exp2(st.m - finite_max(m));
+  const float l = wave_sum_f32(f * st.l);
+  float o[kPer] = {};
+  for (int s0 = first; s0 < splits; s0 += W * kBatch) {
+    if (s0 != first) load(s0);
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      if (s0 + W * u >= splits) continue;
+      const float w = lane_f32(f, s0 + W * u);
+#pragma unroll
+      for (int x = 0; x < kPer; ++x) o[x] += w * v[u][x];
+    }
+  }
+  const float inv = inverse_sum(l);
+  if (W == 1) {
+    __bf16* dst = reinterpret_cast<__bf16*>(a.out + at * D + lane * kPer);
+#pragma unroll
+    for (int x = 0; x < kPer; ++x) dst[x] = static_cast<__bf16>(o[x] * inv);
+    if (a.lse && lane == 0) a.lse[at] = lse_of(m, l);
+    return;
+  }
+#pragma unroll
+  for (int x = 0; x < kPer; ++x) sums[wave][lane * kPer + x] = o[x];
+  __syncthreads();
+  const int d = 2 * threadIdx.x;
+  if (d < D) {
+    float y[2] = {0.f, 0.f};
+    for (int w = 0; w < W; ++w) {
+      y[0] += sums[w][d];
+      y[1] += sums[w][d + 1];
+    }
+    *reinterpret_cast<uint32_t*>(a.out + at * D + d) = pack2(y[0] * inv, y[1] * inv);
+  }
+  if (a.lse && threadIdx.x == 0) a.lse[at] = lse_of(m, l);
+}
+
+inline int64_t join_groups(int64_t rows, int64_t splits) {
+  return splits <= kJoinSplits ? (rows + kWaves - 1) / kWaves : rows;
+}
+
 }  // namespace
 
 }  // namespace memattn

@@ -40,6 +40,22 @@ struct RowsView {
   int64_t hs;
 };
 
+constexpr int kRopeDim = 64;  // elements of a latent cache's rotated key part
+
+// Tokens to append.  Of a latent cache `k` are the latent rows and `v` the key parts.
+struct AppendArgs {
+  KvView kv;
+  RowsView k, v, q, q_out;
+  int32_t hq;  // rows of q per token; 0: none
+  const int32_t* chunk;
+  const int32_t* pos;
+  const int32_t* at;  // positions by which rows are rotated
+  const float* freq;
+  int32_t half;       // pairs of a rotated row
+  bool pairs;         // pair i is (2 i, 2 i + 1), not (i, i + half)
+  int64_t n;
+};
+
 struct AttendArgs {
   KvView kv;
   const int32_t* tok_len;
@@ -72,6 +88,12 @@ hipError_t launch_kv_read(const KvView& kv, int fmt, int d, const RowsView& k, c
                           const int32_t* chunk, const int32_t* pos, int64_t n, hipStream_t stream);
 // Whether n tokens (of at most 2^40 elements) fit one launch.
 bool kv_move_fits(bool write, int heads, int d, int dtype, int64_t n);
+// Whether n tokens fit one launch.
+bool append_fits(bool latent, int half, int64_t n);
+hipError_t launch_kv_append(const AppendArgs& a, int fmt, int d, int dtype, hipStream_t stream);
+hipError_t launch_latent_append(const AppendArgs& a, int fmt, int l, int dtype, hipStream_t stream);
+hipError_t launch_latent_read(const KvView& kv, int fmt, int l, const RowsView& c, const RowsView& r, int dtype,
+                              const int32_t* chunk, const int32_t* pos, int64_t n, hipStream_t stream);
 // `units`: blocks of 32 tokens that a request's chunks can hold.
 size_t attend_workspace_bytes(int d, int64_t m, int k, int64_t units, int64_t total_q, int heads, int heads_q);
 // Whether the call's workgroups fit its launches.
