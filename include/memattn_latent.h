@@ -105,9 +105,10 @@ MEMATTN_API size_t mem_latent_attend_workspace_bytes(const mem_latent* cache, in
  *   lse   = log sum exp(s(p))
  *   out   = sum exp(s(p) - lse) * V_h c_p
  * A token that sees nothing gets out = 0 and lse = -inf.  Tokens that a query does
- * not see have no influence on it, whatever they hold; a value that is not finite
- * among those that it does see makes its outputs so.  q and t (device bf16, strides
- * in `q` and `t`, only read), out (device bf16 [total_q, heads, head_dim],
+ * not see have no influence on it, whatever they hold; an element of a latent vector
+ * that is not finite among those that it does see makes its outputs so, however small
+ * its weight (one of a key part counts as its score says: nothing at -inf).  q and t
+ * (device bf16, strides in `q` and `t`, only read), out (device bf16 [total_q, heads, head_dim],
  * contiguous, 16-byte aligned) and lse (device fp32 [total_q, heads], nullable).
  * Rows that no request owns are not written.
  *

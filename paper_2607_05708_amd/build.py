@@ -27,7 +27,8 @@ DEVICE_FLAGS = [f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-mcode-
 LIBS = {
     "libmemattn.so": ["csrc/api.cpp", "csrc/topk_valu.hip", "csrc/topk_score.hip", "csrc/topk_mfma.hip", "csrc/gather_append.hip",
                       "csrc/compact.hip", "csrc/scope.hip", "csrc/kv_api.cpp", "csrc/kv_cache.hip", "csrc/append.hip",
-                      "csrc/attend.hip", "csrc/latent_api.cpp", "csrc/latent.hip"],
+                      "csrc/attend.hip", "csrc/latent_api.cpp", "csrc/latent.hip",
+                      "csrc/latent_expand.hip"],
     "libmeminputs.so": ["inputs_hip/fill_payload.hip"],
 }
 

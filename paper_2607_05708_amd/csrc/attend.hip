@@ -168,29 +168,6 @@ __device__ __forceinline__ float top_score(float top, float f, const Scores& sc,
   return mode == kExact ? sc.cap2 - 2.f * sc.cap2 * sc.fraction(top) : sc.capped(top);
 }
 
-// Write a row's output, or its part of a split context.
-template <int WIDTH, int D>
-__device__ __forceinline__ void write_rows(const AttendArgs& a, const Rows<WIDTH, D>& rows, RowState st, bool poison,
-                                           int64_t at, int part, int split, int splits, float* part_o,
-                                           RowState* part_ml) {
-  if (splits == 1) {
-    const float inv = poison ? NAN : inverse_sum(st.l);
-    uint16_t* dst = a.out + at * D;
-    rows.each4(part, [&](int d, f32x4 v) {
-      *reinterpret_cast<u32x2_t*>(dst + d) = u32x2_t{pack2(v[0] * inv, v[1] * inv), pack2(v[2] * inv, v[3] * inv)};
-    });
-    if (a.lse && part == 0) a.lse[at] = lse_of(st.m, st.l);
-  } else {
-    const int64_t slot = static_cast<int64_t>(split) * a.total_q * a.hq + at;
-    float* dst = part_o + slot * D;
-    rows.each4(part, [&](int d, f32x4 v) {
-      if (poison) v = f32x4{NAN, NAN, NAN, NAN};
-      *reinterpret_cast<f32x4*>(dst + d) = v;
-    });
-    if (part == 0) part_ml[slot] = st;
-  }
-}
-
 // Values in LDS: bf16 rows whose pitch puts the four (WIDTH 32) or eight (16) rows that a transposing read takes
 // together on different banks; the 16-byte chunks of a row are exchanged within the 64 (32) bytes that such a read
 // takes of it, by the row's number shifted right by SHIFT, so that the writes meet different banks too.

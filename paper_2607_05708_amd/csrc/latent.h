@@ -32,4 +32,9 @@ size_t latent_workspace_bytes(const LatentSizes& s, mem_latent_form form);
 bool latent_fits(const LatentSizes& s, mem_latent_form form, bool ragged);
 hipError_t launch_latent_attend(const LatentArgs& x, const LatentSizes& s, mem_latent_form form, hipStream_t stream);
 
+// The expanded form's.
+size_t expanded_workspace_bytes(const LatentSizes& s, bool ragged);
+bool expanded_fits(const LatentSizes& s, bool ragged);
+hipError_t launch_expanded(const LatentArgs& x, const LatentSizes& s, hipStream_t stream);
+
 }  // namespace memattn

@@ -92,12 +92,10 @@ struct Part {
     }
     *reinterpret_cast<u32x4_t*>(dst + L + 8 * (part ^ f)) = rope;
   }
-  // Whether it holds a value that is not finite, or may (scales that no write gives).
+  // Whether it holds a latent value that is not finite, or may (scales that no write gives).  The key part only goes into
+  // scores.
   __device__ __forceinline__ bool bad() const {
     u16x2 most = {0, 0};
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, rope[j] & 0x7FFF7FFFu));
     bool x = false;
 #pragma unroll
     for (int y = 0; y < kLoads; ++y)
@@ -498,40 +496,49 @@ hipError_t launch_absorbed(const LatentArgs& x, const LatentSizes& s, hipStream_
 }
 
 template <int FMT, int L>
-hipError_t launch_head(const LatentArgs& x, const LatentSizes& s, mem_latent_form, hipStream_t stream) {
+hipError_t launch_head(const LatentArgs& x, const LatentSizes& s, hipStream_t stream) {
   return s.head_dim == 64 ? launch_absorbed<FMT, L, 64>(x, s, stream) : launch_absorbed<FMT, L, 128>(x, s, stream);
 }
 
 template <int FMT>
-hipError_t launch_fmt(const LatentArgs& x, const LatentSizes& s, mem_latent_form form, hipStream_t stream) {
-  return s.latent == 256 ? launch_head<FMT, 256>(x, s, form, stream) : launch_head<FMT, 512>(x, s, form, stream);
+hipError_t launch_fmt(const LatentArgs& x, const LatentSizes& s, hipStream_t stream) {
+  return s.latent == 256 ? launch_head<FMT, 256>(x, s, stream) : launch_head<FMT, 512>(x, s, stream);
 }
 
 }  // namespace
 
-mem_latent_form choose_latent_form(const LatentSizes&, int32_t) { return MEM_LATENT_ABSORBED; }
+mem_latent_form choose_latent_form(const LatentSizes& s, int32_t asked) {
+  if (asked != MEM_LATENT_AUTO) return static_cast<mem_latent_form>(asked);
+  // products of a head, in units of a pair's 2 elements each: rows (2 L + R) absorbed, rows (2 d + R) and 2 d L for
+  // each token of the context expanded
+  const int64_t rows = s.total_q / s.m, d = s.head_dim, l = s.latent;
+  return rows * (l - d) > d * l ? MEM_LATENT_EXPANDED : MEM_LATENT_ABSORBED;
+}
 
-// The larger of the two forms of a call (ragged or not), so that one size serves both.
-size_t latent_workspace_bytes(const LatentSizes& s, mem_latent_form) {
+// The larger of the two cases of a call (ragged or not), so that one size serves both.
+size_t latent_workspace_bytes(const LatentSizes& s, mem_latent_form form) {
   size_t need = 0;
   for (int ragged = 0; ragged < 2; ++ragged) {
     if (!ragged && s.total_q % s.m != 0) continue;
-    const size_t b = absorbed_space(s, absorbed_plan(s, ragged != 0).splits).end;
+    const size_t b = form == MEM_LATENT_EXPANDED ? expanded_workspace_bytes(s, ragged != 0)
+                                                 : absorbed_space(s, absorbed_plan(s, ragged != 0).splits).end;
     need = b > need ? b : need;
   }
   return need;
 }
 
-bool latent_fits(const LatentSizes& s, mem_latent_form, bool ragged) {
+bool latent_fits(const LatentSizes& s, mem_latent_form form, bool ragged) {
+  if (form == MEM_LATENT_EXPANDED) return expanded_fits(s, ragged);
   const AbsorbedPlan p = absorbed_plan(s, ragged);
   return p.tiles * p.splits <= kMaxGroups && query_groups(s.total_q) < 65536 && out_groups(s.total_q, s.head_dim) < 65536;
 }
 
 hipError_t launch_latent_attend(const LatentArgs& x, const LatentSizes& s, mem_latent_form form, hipStream_t stream) {
+  if (form == MEM_LATENT_EXPANDED) return launch_expanded(x, s, stream);
   switch (s.fmt) {
-    case MEM_KV_BF16: return launch_fmt<MEM_KV_BF16>(x, s, form, stream);
-    case MEM_KV_FP8: return launch_fmt<MEM_KV_FP8>(x, s, form, stream);
-    default: return launch_fmt<MEM_KV_FP4>(x, s, form, stream);
+    case MEM_KV_BF16: return launch_fmt<MEM_KV_BF16>(x, s, stream);
+    case MEM_KV_FP8: return launch_fmt<MEM_KV_FP8>(x, s, stream);
+    default: return launch_fmt<MEM_KV_FP4>(x, s, stream);
   }
 }
 
