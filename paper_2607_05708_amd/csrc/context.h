@@ -148,11 +148,13 @@ struct ChunkList {
   int k;
 };
 
-template <int THREADS = kThreads>
+// (with KEEP false the chunks stay where they are in memory, and only the sums take LDS)
+template <int THREADS = kThreads, bool KEEP = true>
 __device__ __forceinline__ ChunkList scan_list(const AttendArgs& a, int req, int* lds, int* tmp) {
   const int k = a.k;
-  const ChunkList L{lds, lds + k, lds + 2 * k + 1, k};
   const int32_t* ids = a.ids + static_cast<int64_t>(req) * k;
+  const ChunkList L = KEEP ? ChunkList{lds, lds + k, lds + 2 * k + 1, k}
+                           : ChunkList{const_cast<int32_t*>(ids), lds, lds + k + 1, k};
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int cap = a.kv.ppc * a.kv.page_tokens;
   const int per = (k + THREADS - 1) / THREADS;
@@ -161,7 +163,7 @@ __device__ __forceinline__ ChunkList scan_list(const AttendArgs& a, int req, int
   for (int c = c0; c < c1; ++c) {
     const int32_t id = ids[c];
     const int len = id >= 0 && id < a.kv.n_chunks ? min(max(a.tok_len[id], 0), cap) : 0;
-    L.cid[c] = id;
+    if (KEEP) L.cid[c] = id;
     L.ub[c] = u;
     L.tb[c] = t;
     u += (len + kUnit - 1) / kUnit;

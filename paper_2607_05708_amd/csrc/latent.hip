@@ -35,19 +35,6 @@ struct Part {
   u32x4_t rope;
   uint32_t sc[kScaleWords];
 
-  __device__ __forceinline__ void load(const uint8_t* row, const uint8_t* rope_row, const uint8_t* scales, int part) {
-#pragma unroll
-    for (int y = 0; y < kLoads; ++y) codes[y] = *reinterpret_cast<const u32x4_t*>(row + 16 * (part + 8 * y));
-    rope = *reinterpret_cast<const u32x4_t*>(rope_row + 16 * part);
-    if constexpr (FMT != MEM_KV_BF16) {
-#pragma unroll
-      for (int i = 0; i < kScaleWords / 2; ++i) {
-        const u32x2_t v = reinterpret_cast<const u32x2_t*>(scales)[i];
-        sc[2 * i] = v[0];
-        sc[2 * i + 1] = v[1];
-      }
-    }
-  }
   __device__ __forceinline__ void clear() {
 #pragma unroll
     for (int y = 0; y < kLoads; ++y) codes[y] = u32x4_t{0, 0, 0, 0};
@@ -80,17 +67,16 @@ struct Part {
     }
     return o;
   }
-  // Into its LDS row.
-  __device__ __forceinline__ void store(uint16_t* dst, int row, int part) const {
-    const int f = exchange(row);
-#pragma unroll
-    for (int y = 0; y < kLoads; ++y) {
+  // Piece z of unpacking it into its LDS row: chunks, then the key part.
+  static constexpr int kPieces = kLoads * kChunks + 1;
+  __device__ __forceinline__ void store(uint16_t* dst, int exchanged, int part, int z) const {
+    if (z == kPieces - 1) {
+      *reinterpret_cast<u32x4_t*>(dst + L + 8 * (part ^ exchanged)) = rope;
+    } else {
+      const int y = z / kChunks, c = z % kChunks;
       const float s = FMT == MEM_KV_BF16 ? 1.f : kv_scale(scale_byte(y, part));
-#pragma unroll
-      for (int c = 0; c < kChunks; ++c)
-        *reinterpret_cast<u32x4_t*>(dst + 8 * ((kChunks * (part + 8 * y) + c) ^ f)) = chunk(y, c, s);
+      *reinterpret_cast<u32x4_t*>(dst + 8 * ((kChunks * (part + 8 * y) + c) ^ exchanged)) = chunk(y, c, s);
     }
-    *reinterpret_cast<u32x4_t*>(dst + L + 8 * (part ^ f)) = rope;
   }
   // Whether it holds a latent value that is not finite, or may (scales that no write gives).  The key part only goes into
   // scores.
@@ -200,6 +186,27 @@ struct LatentShape {
   static constexpr int kUnitElems = kUnit * kLatentPitch<L>;  // a unit's rows in LDS
 };
 
+// x + both halves of a pair of bf16.
+__device__ __forceinline__ float add_pair(uint32_t pair, float x) {
+  constexpr uint32_t kOnes = 0x3F803F80u;
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(s16x2, pair), __builtin_bit_cast(s16x2, kOnes), x, false);
+}
+
+// Scales rows whose registers are accumulators.  (The compiler would otherwise keep them, for the multiplications' sake,
+// where the matrix products cannot: of 32 x 512 it spills most.)
+template <int D>
+__device__ __forceinline__ void scale_rows(Rows<32, D>& rows, float f) {
+#pragma unroll
+  for (int n = 0; n < D / 32; ++n) {
+    f32x16 x = rows.o[n];
+    asm volatile("" : "+a"(x));
+    f32x16 y = x * f;
+    asm volatile("" : "+a"(y));
+    rows.o[n] = y;
+    issue_first();
+  }
+}
+
 // Tiles of 32 RG rows: wave w has the 32 rows w / (4 / RG) of the tile and, of the second product, a share of the
 // columns; waves with the same rows make their scores each for itself.
 template <int FMT, int L, int RG>
@@ -213,8 +220,8 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attend_kernel(LatentArgs x
   constexpr int kPitch = kLatentPitch<L>, kShare = 4 / RG, kColumns = L / kShare;
   constexpr int kSteps = (L + kRopeDim) / 16;
   constexpr int kBlocks = kColumns / 32;
-  extern __shared__ int dyn[];  // the chunk list: cid[k], ub[k + 1], tb[k + 1]
-  __shared__ __align__(16) uint16_t unit_rows[2][S::kUnitElems];
+  extern __shared__ int dyn[];  // of the chunk list: ub[k + 1], tb[k + 1]
+  __shared__ __align__(16) uint16_t unit_rows[3][S::kUnitElems];
   __shared__ Unit list[S::kBatch];
   __shared__ int tmp[2 * kWaves];
   // Tokens of a masked unit whose values are not finite: of the unit at hand, of the next, and of the one after that,
@@ -229,7 +236,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attend_kernel(LatentArgs x
   const int split = static_cast<int>(blockIdx.x - tile * splits);
   Tile t;
   if (!find_tile<32 * RG>(a, static_cast<uint32_t>(tiles) - 1 - tile, a.hq, &t)) return;
-  const ChunkList list_of = scan_list(a, t.req, dyn, tmp);
+  const ChunkList list_of = scan_list<kThreads, false>(a, t.req, dyn, tmp);
   const int ctx = list_of.tb[a.k];
   const int prefix = a.prefix_len ? __builtin_amdgcn_readfirstlane(min(max(a.prefix_len[t.req], 0), kFar)) : 0;
   const int my_row = t.r0 + min(32 * rg + col, t.rows - 1);
@@ -251,9 +258,10 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attend_kernel(LatentArgs x
   Rows<32, kColumns> rows;
   rows.clear();
   RowState st{-INFINITY, 0.f};
+  float rounded = 0.f;  // sum of the weights as the second product takes them, which the outputs are divided by
   bool poison = false;
 
-  const int tok = tid >> 3, part = tid & 7;  // the part of a row that this thread unpacks
+  const int tok = tid >> 3, part = tid & 7, exchanged = exchange(tok);  // the part of a row that this thread unpacks
   const int key_at = col * kPitch, f = exchange(col);
   const int even = key_at + 8 * (half ^ f), odd = key_at + 8 * ((2 + half) ^ f);  // chunks 0 and 2 (+ half) of a row
   int value_at;  // transposed operands: rows 4 half + .. of the unit, 16 columns
@@ -270,95 +278,200 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attend_kernel(LatentArgs x
     if (n == 0) continue;
     if (tid < 2) bad_tok[tid] = 0;
     __syncthreads();
-    auto load = [&](const Unit& u) {
-      if (tok < u.held()) {
-        const int row = u.row() + tok;
-        const uint8_t* page = a.kv.pool + (u.at - u.row() * P::kRow);
-        p.load(page + row * P::kRow, page + T * P::kRow + row * (2 * kRopeDim),
-               page + T * (P::kRow + 2 * kRopeDim) + row * P::kSc, part);
-      } else {
-        p.clear();
+    // this thread's row of a unit (of those that it holds): the unit's page, and its bytes there
+    struct Place {
+      const uint8_t *page, *parts, *scales;  // the same in every lane
+      uint32_t row;
+    };
+    auto place = [&](const Unit& u) {
+      const uint8_t* page = a.kv.pool + (u.at - u.row() * P::kRow);
+      return Place{page, page + T * P::kRow, page + T * (P::kRow + 2 * kRopeDim),
+                   static_cast<uint32_t>(u.row() + min(tok, u.held() - 1))};
+    };
+    auto load_codes = [&](const Place& from, int y) {
+      p.codes[y] = *reinterpret_cast<const u32x4_t*>(from.page + (from.row * P::kRow + 16 * part + 128 * y));
+    };
+    auto load_rope = [&](const Place& from) {
+      p.rope = *reinterpret_cast<const u32x4_t*>(from.parts + (from.row * (2 * kRopeDim) + 16 * part));
+    };
+    auto load_scales = [&](const Place& from) {
+      if constexpr (FMT != MEM_KV_BF16) {
+#pragma unroll
+        for (int i = 0; i < P::kScaleWords / 2; ++i) {
+          const u32x2_t v = reinterpret_cast<const u32x2_t*>(from.scales + from.row * P::kSc)[i];
+          p.sc[2 * i] = v[0];
+          p.sc[2 * i + 1] = v[1];
+        }
       }
     };
-    auto check_bad = [&](int to) {  // values of a masked unit that are not finite are noted and left out
+    // tokens that a masked unit does not hold are cleared, values that are not finite are noted and left out
+    auto check = [&](const Unit& u, int to) {
+      if (tok >= u.held()) p.clear();
       const bool bad = p.bad();
       const uint64_t vote = __ballot(bad);
       if (bad) atomicOr(&bad_tok[to], 1u << tok);
       if ((vote >> (lane & 56)) & 255u) p.clear();
     };
-    Unit u = uniform_unit(list[0]);
-    load(u);
-    if (u.masked()) check_bad(0);
-    p.store(unit_rows[0] + tok * kPitch, tok, part);
-    Unit next = uniform_unit(list[min(1, n - 1)]);
-    load(next);
+    // Piece z of the next unit, and the load of the same piece of the one after it.
+    auto advance = [&](uint16_t* to, const Place& from, int z) {
+      p.store(to, exchanged, part, z);
+      if (z == P::kPieces - 1) load_rope(from);
+      else if (z % P::kChunks == P::kChunks - 1) load_codes(from, z / P::kChunks);
+    };
+    Unit u = uniform_unit(list[0]), next = uniform_unit(list[min(1, n - 1)]);
+    {
+      const Place from = place(u);
+#pragma unroll
+      for (int y = 0; y < P::kLoads; ++y) load_codes(from, y);
+      load_rope(from);
+      load_scales(from);
+    }
+    if (u.masked()) check(u, 0);
+    {
+      uint16_t* to = unit_rows[0] + tok * kPitch;
+      const Place from = place(next);
+#pragma unroll
+      for (int z = 0; z < P::kPieces; ++z) advance(to, from, z);
+      load_scales(from);
+    }
     __syncthreads();
-    int slot = 0;  // i mod 3
-    for (int i = 0; i < n; ++i) {
-      const Unit after = list[min(i + 2, n - 1)];
-      const int slot1 = slot == 2 ? 0 : slot + 1;
-      if (tid == 0) bad_tok[slot == 0 ? 2 : slot - 1] = 0;
+    // Weights of the unit before: its second product is made beside the exponentials of the unit at hand.
+    u32x4_t w[2];
+    bool pending = false;
+    int slot = 0;  // i mod 3: the unit's buffer, and its word of bad_tok
+    for (int i = 0; i <= n; ++i) {
+      const Unit after = uniform_unit(list[min(i + 2, n - 1)]);
+      const int slot1 = slot == 2 ? 0 : slot + 1, slot2 = slot == 0 ? 2 : slot - 1;
+      const bool has = i < n;
+      if (tid == 0) bad_tok[slot2] = 0;
+      if (i + 1 < n && next.masked()) check(next, slot1);
+      uint16_t* to = unit_rows[slot1] + tok * kPitch;
+      const Place from = place(after);
       if (works) {
-        const uint16_t* keys = unit_rows[i & 1];
+        const uint16_t* keys = unit_rows[slot];
+        const uint16_t* values = unit_rows[slot2] + value_at;
         f32x16 s;
 #pragma unroll
         for (int j = 0; j < 16; ++j) s[j] = 0.f;
-#pragma unroll
-        for (int y = 0; y < kSteps; ++y) {
-          const u32x4_t k = *reinterpret_cast<const u32x4_t*>(keys + (y & 1 ? odd : even) + 32 * (y >> 1));
-          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(k), q[y], s, 0, 0, 0);
-        }
-        if (u.masked()) {
-          const uint32_t seen = visible_tokens(rule, u, prefix);
-          mask_scores<32, 16>(s, seen, half);
-          poison |= (seen & bad_tok[slot]) != 0;
-        }
-        float top = s[0];
-#pragma unroll
-        for (int j = 1; j < 16; ++j) top = nan_max(top, s[j]);
-        const float high = max_column<32>(top) * c;
-        if (raise<32, kColumns>(high, u.masked(), st, rows)) {
-          const float ref = finite_max(st.m);
-#pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            s[j] = fast_exp2(fmaf(s[j], c, -ref));
-            st.l += s[j];
-          }
-          u32x4_t w[2], rest[2];
-          pack_weights<16>(s, w);
-          auto add = [&](const u32x4_t (&v)[2]) {
-#pragma unroll
-            for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-              for (int y = 0; y < 2; ++y) {
-                const uint16_t* src = keys + value_at + 16 * y * kPitch + 32 * b;
-                const u32x2_t v0 = lds_transpose4(src), v1 = lds_transpose4(src + 8 * kPitch);
-                rows.o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(u32x4_t{v0[0], v0[1], v1[0], v1[1]}),
-                                                                    as_bf16x8(v[y]), rows.o[b], 0, 0, 0);
-              }
+        constexpr int kFirst = (P::kPieces + 1) / 2;  // pieces beside the first product
+        if (has) {
+          constexpr int kAhead = 3;
+          auto key = [&](int y) {
+            return *reinterpret_cast<const u32x4_t*>(keys + (y & 1 ? odd : even) + 32 * (y >> 1));
           };
-          add(w);
-          if (is_heavy(high, st)) {
-            pack_rests<16>(s, w, rest);
-            add(rest);
+          u32x4_t k[kSteps];
+#pragma unroll
+          for (int y = 0; y < kAhead; ++y) k[y] = key(y);
+          issue_first();
+#pragma unroll
+          for (int y = 0; y < kSteps; ++y) {
+            if (y + kAhead < kSteps) k[y + kAhead] = key(y + kAhead);
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(k[y]), q[y], s, 0, 0, 0);
+            if (y * kFirst / kSteps != (y + 1) * kFirst / kSteps) advance(to, from, y * kFirst / kSteps);
+            issue_first();
           }
         }
+        bool counts = false;
+        float high = -INFINITY;
+        if (has) {
+          if (u.masked()) {
+            const uint32_t seen = visible_tokens(rule, u, prefix);
+            mask_scores<32, 16>(s, seen, half);
+            poison |= (seen & bad_tok[slot]) != 0;
+          }
+          float top = s[0];
+#pragma unroll
+          for (int j = 1; j < 16; ++j) top = nan_max(top, s[j]);
+          high = max_column<32>(top) * c;
+          counts = __any(!u.masked() || high != -INFINITY);
+        }
+        auto value = [&](int x) {  // operand x: columns 32 (x / 2), tokens 16 (x % 2)
+          const uint16_t* src = values + 16 * (x & 1) * kPitch + 32 * (x >> 1);
+          const u32x2_t v0 = lds_transpose4(src), v1 = lds_transpose4(src + 8 * kPitch);
+          return as_bf16x8(u32x4_t{v0[0], v0[1], v1[0], v1[1]});
+        };
+        constexpr int kOps = 2 * kBlocks;
+        auto add = [&](const u32x4_t (&by)[2], auto share) {
+          constexpr int kAhead = 2;
+          bf16x8 v[kOps];
+#pragma unroll
+          for (int x = 0; x < kAhead; ++x) v[x] = value(x);
+          issue_first();
+#pragma unroll
+          for (int x = 0; x < kOps; ++x) {
+            if (x + kAhead < kOps) v[x + kAhead] = value(x + kAhead);
+            rows.o[x >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[x], as_bf16x8(by[x & 1]), rows.o[x >> 1], 0, 0, 0);
+            share(x);
+            issue_first();
+          }
+        };
+        const bool up = counts && __any(high > st.m + kLag);
+        u32x4_t now[2];
+        auto weigh_score = [&](float ref, int j) {
+          s[j] = fast_exp2(fmaf(s[j], c, -ref));
+          st.l += s[j];
+          if (j & 1) {
+            const uint32_t pair = pack2(s[j - 1], s[j]);
+            now[j >> 3][(j >> 1) & 3] = pair;
+            rounded = add_pair(pair, rounded);
+          }
+        };
+        // The usual way: both in one.  (Two flags that the compiler does not know to be one: with an if and an else
+        // over the same accumulators it keeps them twice.)
+        const bool usual = pending && counts && !up;
+        int usual_too = __builtin_amdgcn_readfirstlane(usual);
+        asm volatile("" : "+s"(usual_too));
+        if (!usual) {
+          if (pending) add(w, [](int) {});
+          if (up) {
+            const float mn = fmaxf(st.m, high);
+            const float r = mn == -INFINITY ? 1.f : fast_exp2(st.m - mn);
+            st.l *= r;
+            rounded *= r;
+            scale_rows(rows, r);
+            st.m = mn;
+          }
+          if (counts) {
+            const float ref = finite_max(st.m);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) weigh_score(ref, j);
+          }
+#pragma unroll
+          for (int z = kFirst; z < P::kPieces; ++z) advance(to, from, z);
+        }
+        if (usual_too) {
+          const float ref = finite_max(st.m);
+          add(w, [&](int x) {
+            constexpr int kSecond = P::kPieces - kFirst;
+#pragma unroll
+            for (int j = 16 * x / kOps; j < 16 * (x + 1) / kOps; ++j) weigh_score(ref, j);
+#pragma unroll
+            for (int z = kSecond * x / kOps; z < kSecond * (x + 1) / kOps; ++z) advance(to, from, kFirst + z);
+          });
+        }
+        if (!has) break;
+        pending = counts;
+        w[0] = now[0];
+        w[1] = now[1];
+      } else {
+        if (!has) break;
+#pragma unroll
+        for (int z = 0; z < P::kPieces; ++z) advance(to, from, z);
       }
-      if (i + 1 < n && next.masked()) check_bad(slot1);
-      p.store(unit_rows[(i + 1) & 1] + tok * kPitch, tok, part);
+      load_scales(from);
       u = next;
-      next = uniform_unit(after);
-      load(next);
+      next = after;
       slot = slot1;
       __syncthreads();
     }
   }
 
   st.l = sum_column<32>(st.l);
+  rounded = sum_column<32>(rounded);
   poison = any_column<32>(poison, col);
   if (32 * rg + col >= t.rows) return;
   if (splits == 1) {
-    const float inv = poison ? NAN : inverse_sum(st.l);
+    const float inv = poison ? NAN : inverse_sum(rounded);
     uint16_t* dst = sums + row_at * L + cg * kColumns;
     rows.each4(half, [&](int d, f32x4 v) {
       *reinterpret_cast<u32x2_t*>(dst + d) = u32x2_t{pack2(v[0] * inv, v[1] * inv), pack2(v[2] * inv, v[3] * inv)};
@@ -367,9 +480,9 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attend_kernel(LatentArgs x
   } else {
     const int64_t at = static_cast<int64_t>(split) * a.total_q * a.hq + row_at;
     float* dst = part_o + at * L + cg * kColumns;
+    const float even_out = poison ? NAN : st.l == 0.f ? 0.f : st.l * inverse_sum(rounded);  // the join divides by l
     rows.each4(half, [&](int d, f32x4 v) {
-      if (poison) v = f32x4{NAN, NAN, NAN, NAN};
-      *reinterpret_cast<f32x4*>(dst + d) = v;
+      *reinterpret_cast<f32x4*>(dst + d) = v * even_out;
     });
     if (half == 0 && cg == 0) part_ml[at] = poison ? RowState{st.m, NAN} : st;
   }
@@ -407,7 +520,7 @@ __global__ __launch_bounds__(kThreads) void latent_out_kernel(LatentArgs x, cons
 // ---------------------------------------------------------------- launches
 
 size_t align256(size_t b) { return (b + 255) & ~static_cast<size_t>(255); }
-size_t list_bytes(int k) { return (3 * static_cast<size_t>(k) + 2) * sizeof(int); }
+size_t list_bytes(int k) { return (2 * static_cast<size_t>(k) + 2) * sizeof(int); }
 
 struct AbsorbedPlan {
   int rg;  // tiles of 32 rg rows
