@@ -168,59 +168,6 @@ __device__ __forceinline__ float top_score(float top, float f, const Scores& sc,
   return mode == kExact ? sc.cap2 - 2.f * sc.cap2 * sc.fraction(top) : sc.capped(top);
 }
 
-// Values in LDS: bf16 rows whose pitch puts the four (WIDTH 32) or eight (16) rows that a transposing read takes
-// together on different banks; the 16-byte chunks of a row are exchanged within the 64 (32) bytes that such a read
-// takes of it, by the row's number shifted right by SHIFT, so that the writes meet different banks too.
-template <int WIDTH, int D>
-constexpr int kValuePitch = D + WIDTH;
-template <int WIDTH, int SHIFT>
-__device__ __forceinline__ int value_chunk(int row, int chunk) {
-  return chunk ^ ((row >> SHIFT) & (WIDTH == 32 ? 3 : 1));
-}
-
-// Transposed operands of the values of 32 tokens in LDS rows at `rows`: operand n of WIDTH 16 is for the output columns
-// 16 n .. + 15, of 32 for the columns 32 (n / 2) .. + 31 and every second 16 tokens.
-template <int WIDTH, int D, int SHIFT>
-struct ValueOps {
-  static constexpr int kOps = D / WIDTH * (WIDTH == 16 ? 1 : 2);
-  static constexpr int P = kValuePitch<WIDTH, D>;
-  const uint16_t* src[WIDTH == 16 ? 1 : 4];
-
-  __device__ __forceinline__ ValueOps(const uint16_t* rows, int lane) {
-    static_assert(WIDTH != 16 || SHIFT <= 3, "rows 16 apart have the same exchange");
-    const int i = lane & 15;
-    if constexpr (WIDTH == 16) {
-      const int r = 4 * (lane >> 4) + (i >> 2);  // rows r and r + 16, columns 16 n + 4 (i & 3)
-      src[0] = rows + r * P + 8 * value_chunk<16, SHIFT>(r, (i & 3) >> 1) + 4 * (i & 1);
-    } else {
-      // rows r + 8 y, columns 32 n + 16 (lane >> 4 & 1) + 4 (i & 3)
-      const int r = 4 * (lane >> 5) + (i >> 2), c = 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
-#pragma unroll
-      for (int y = 0; y < 4; ++y)
-        src[y] = rows + (r + 8 * y) * P + 8 * value_chunk<32, SHIFT>(r + 8 * y, c) + 4 * (i & 1);
-    }
-  }
-  __device__ __forceinline__ bf16x8 operator[](int n) const {
-    if constexpr (WIDTH == 16) return pair(src[0] + 16 * n, src[0] + 16 * P + 16 * n);
-    else return pair(src[2 * (n & 1)] + 32 * (n >> 1), src[2 * (n & 1) + 1] + 32 * (n >> 1));
-  }
-  // O^T += V^T P^T for operand n, with the weights of the lane's row.
-  static __device__ __forceinline__ void multiply(Rows<WIDTH, D>& out, int n, bf16x8 v, const u32x4_t* w) {
-    if constexpr (WIDTH == 16) {
-      out.o[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, as_bf16x8(w[0]), out.o[n], 0, 0, 0);
-    } else {
-      auto& o = out.o[n >> 1];
-      o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, as_bf16x8(w[n & 1]), o, 0, 0, 0);
-    }
-  }
-
- private:
-  static __device__ __forceinline__ bf16x8 pair(const uint16_t* p0, const uint16_t* p1) {
-    const u32x2_t v0 = lds_transpose4(p0), v1 = lds_transpose4(p1);
-    return as_bf16x8(u32x4_t{v0[0], v0[1], v1[0], v1[1]});
-  }
-};
-
 // Unpack a quarter row of values into its LDS row.
 template <int WIDTH, int SHIFT, int FMT, int D>
 __device__ __forceinline__ void store_values(const Piece<FMT, D>& p, uint16_t* v, int row, int quarter) {

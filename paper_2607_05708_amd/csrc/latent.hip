@@ -180,31 +180,59 @@ __global__ __launch_bounds__(kThreads) void latent_query_kernel(LatentArgs x, in
 
 // ---------------------------------------------------------------- attention over latent vectors
 
-template <int L>
+template <int L, int RG>
 struct LatentShape {
-  static constexpr int kBatch = 128;                          // units resolved at a time
+  static constexpr int kBatch = 64;                           // units resolved at a time
   static constexpr int kUnitElems = kUnit * kLatentPitch<L>;  // a unit's rows in LDS
+  // Operands of a row's query that LDS holds: with 512 columns of 32 rows a wave's outputs take all 256 accumulation
+  // registers, and what else it needs is more than the others with all 36 operands.  (Registers spilled to memory would
+  // wait, at each reload, for the loads of the units ahead: 986 us for LAST.)
+  static constexpr int kParked = L == 512 && RG == 4 ? 10 : 0;
 };
+
+// Scales rows whose registers are accumulation registers.  (The compiler would otherwise keep them, for the
+// multiplications' sake, where the matrix products cannot: of 32 x 512 it spills most.)
+template <int WIDTH, int D>
+__device__ __forceinline__ void scale_rows(Rows<WIDTH, D>& rows, float f) {
+#pragma unroll
+  for (int n = 0; n < D / WIDTH; ++n) {
+    auto x = rows.o[n];
+    asm volatile("" : "+a"(x));
+    auto y = x * f;
+    asm volatile("" : "+a"(y));
+    rows.o[n] = y;
+    if (WIDTH == 32 || n % 4 == 3) issue_first();
+  }
+}
+
+// Write columns first .. + N - 1 of a row's weighted sum of latent vectors, or of its part of a split context.  `rounded`
+// is the sum of the weights as the product took them, and what it is divided by, so that their roundings cancel where a
+// few weigh most; the join divides by l.
+template <int WIDTH, int N, int L>
+__device__ __forceinline__ void write_sums(const AttendArgs& a, const Rows<WIDTH, N>& rows, RowState st, float rounded,
+                                           bool poison, int64_t row_at, int part, int split, int splits, int first,
+                                           uint16_t* sums, float* part_o, RowState* part_ml) {
+  if (poison) st.l = NAN;
+  if (splits == 1) {
+    const float inv = poison ? NAN : inverse_sum(rounded);
+    uint16_t* dst = sums + row_at * L + first;
+    rows.each4(part, [&](int d, f32x4 v) {
+      *reinterpret_cast<u32x2_t*>(dst + d) = u32x2_t{pack2(v[0] * inv, v[1] * inv), pack2(v[2] * inv, v[3] * inv)};
+    });
+    if (a.lse && part == 0 && first == 0) a.lse[row_at] = lse_of(st.m, st.l);
+  } else {
+    const int64_t at = static_cast<int64_t>(split) * a.total_q * a.hq + row_at;
+    const float even = st.l == 0.f ? 0.f : st.l * inverse_sum(rounded);
+    float* dst = part_o + at * L + first;
+    rows.each4(part, [&](int d, f32x4 v) { *reinterpret_cast<f32x4*>(dst + d) = v * even; });
+    if (part == 0 && first == 0) part_ml[at] = st;
+  }
+}
 
 // x + both halves of a pair of bf16.
 __device__ __forceinline__ float add_pair(uint32_t pair, float x) {
   constexpr uint32_t kOnes = 0x3F803F80u;
   return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(s16x2, pair), __builtin_bit_cast(s16x2, kOnes), x, false);
-}
-
-// Scales rows whose registers are accumulators.  (The compiler would otherwise keep them, for the multiplications' sake,
-// where the matrix products cannot: of 32 x 512 it spills most.)
-template <int D>
-__device__ __forceinline__ void scale_rows(Rows<32, D>& rows, float f) {
-#pragma unroll
-  for (int n = 0; n < D / 32; ++n) {
-    f32x16 x = rows.o[n];
-    asm volatile("" : "+a"(x));
-    f32x16 y = x * f;
-    asm volatile("" : "+a"(y));
-    rows.o[n] = y;
-    issue_first();
-  }
 }
 
 // Tiles of 32 RG rows: wave w has the 32 rows w / (4 / RG) of the tile and, of the second product, a share of the
@@ -216,12 +244,13 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attend_kernel(LatentArgs x
                                                                  float* __restrict__ part_o,
                                                                  RowState* __restrict__ part_ml) {
   using P = Part<FMT, L>;
-  using S = LatentShape<L>;
+  using S = LatentShape<L, RG>;
   constexpr int kPitch = kLatentPitch<L>, kShare = 4 / RG, kColumns = L / kShare;
   constexpr int kSteps = (L + kRopeDim) / 16;
   constexpr int kBlocks = kColumns / 32;
   extern __shared__ int dyn[];  // of the chunk list: ub[k + 1], tb[k + 1]
   __shared__ __align__(16) uint16_t unit_rows[3][S::kUnitElems];
+  __shared__ __align__(16) uint16_t parked[S::kParked > 0 ? kWaves * S::kParked * 64 * 8 : 8];
   __shared__ Unit list[S::kBatch];
   __shared__ int tmp[2 * kWaves];
   // Tokens of a masked unit whose values are not finite: of the unit at hand, of the next, and of the one after that,
@@ -240,7 +269,6 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attend_kernel(LatentArgs x
   const int ctx = list_of.tb[a.k];
   const int prefix = a.prefix_len ? __builtin_amdgcn_readfirstlane(min(max(a.prefix_len[t.req], 0), kFar)) : 0;
   const int my_row = t.r0 + min(32 * rg + col, t.rows - 1);
-  const bool works = 32 * rg < t.rows;
   const RowRule rule = row_rule(a, t, ctx, 0, a.hq, my_row);
   const TileRule tr = tile_rule<32 * RG>(a, t, ctx, 0, a.hq);
   const Span span = visible_units(list_of, prefix, tr.lo, tr.hi);
@@ -249,9 +277,18 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attend_kernel(LatentArgs x
   const int u1 = static_cast<int>(static_cast<int64_t>(n_units) * (split + 1) / splits);
 
   // lane (col, half) holds elements 16 s + 8 half .. + 7 of row `col` of the wave
-  bf16x8 q[kSteps];
+  constexpr int kKept = kSteps - S::kParked;
+  bf16x8 q[kKept];
   const int64_t row_at = static_cast<int64_t>(t.q0) * a.hq + my_row;
   load_queries(query_rows + row_at * kQueryRow<L> + 8 * half, 16, q);
+  const uint16_t* my_parked = parked + (wave * S::kParked * 64 + lane) * 8;
+  if constexpr (S::kParked > 0) {
+    bf16x8 more[S::kParked];
+    load_queries(query_rows + row_at * kQueryRow<L> + 16 * kKept + 8 * half, 16, more);
+#pragma unroll
+    for (int y = 0; y < S::kParked; ++y)
+      *reinterpret_cast<bf16x8*>(parked + ((wave * S::kParked + y) * 64 + lane) * 8) = more[y];
+  }
 
   const float c = a.scale * kLog2e;
   const int64_t T = a.kv.page_tokens;
@@ -294,14 +331,16 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attend_kernel(LatentArgs x
     auto load_rope = [&](const Place& from) {
       p.rope = *reinterpret_cast<const u32x4_t*>(from.parts + (from.row * (2 * kRopeDim) + 16 * part));
     };
-    auto load_scales = [&](const Place& from) {
+    auto load_scales = [&](const Place& from, uint32_t (&to)[P::kScaleWords]) {
       if constexpr (FMT != MEM_KV_BF16) {
 #pragma unroll
         for (int i = 0; i < P::kScaleWords / 2; ++i) {
           const u32x2_t v = reinterpret_cast<const u32x2_t*>(from.scales + from.row * P::kSc)[i];
-          p.sc[2 * i] = v[0];
-          p.sc[2 * i + 1] = v[1];
+          to[2 * i] = v[0];
+          to[2 * i + 1] = v[1];
         }
+      } else {
+        to[0] = 0;
       }
     };
     // tokens that a masked unit does not hold are cleared, values that are not finite are noted and left out
@@ -324,87 +363,102 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attend_kernel(LatentArgs x
 #pragma unroll
       for (int y = 0; y < P::kLoads; ++y) load_codes(from, y);
       load_rope(from);
-      load_scales(from);
+      load_scales(from, p.sc);
     }
     if (u.masked()) check(u, 0);
     {
       uint16_t* to = unit_rows[0] + tok * kPitch;
       const Place from = place(next);
+      // (in the order of the steps, so that the compiler can count what is in flight behind a load)
+      uint32_t scales[P::kScaleWords];
+      load_scales(from, scales);
+      issue_first();
 #pragma unroll
-      for (int z = 0; z < P::kPieces; ++z) advance(to, from, z);
-      load_scales(from);
+      for (int z = 0; z < P::kPieces; ++z) {
+        advance(to, from, z);
+        issue_first();
+      }
+#pragma unroll
+      for (int j = 0; j < P::kScaleWords; ++j) p.sc[j] = scales[j];
     }
     __syncthreads();
     // Weights of the unit before: its second product is made beside the exponentials of the unit at hand.
     u32x4_t w[2];
     bool pending = false;
+    const uint16_t* values = nullptr;  // its rows
+    auto value = [&](int x) {          // operand x: columns 32 (x / 2), tokens 16 (x % 2)
+      const uint16_t* src = values + 16 * (x & 1) * kPitch + 32 * (x >> 1);
+      const u32x2_t v0 = lds_transpose4(src), v1 = lds_transpose4(src + 8 * kPitch);
+      return as_bf16x8(u32x4_t{v0[0], v0[1], v1[0], v1[1]});
+    };
+    constexpr int kOps = 2 * kBlocks;
+    auto add_values = [&](auto share) {
+      constexpr int kAhead = 2;
+      bf16x8 v[kOps];
+#pragma unroll
+      for (int x = 0; x < kAhead; ++x) v[x] = value(x);
+      issue_first();
+#pragma unroll
+      for (int x = 0; x < kOps; ++x) {
+        if (x + kAhead < kOps) v[x + kAhead] = value(x + kAhead);
+        rows.o[x >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[x], as_bf16x8(w[x & 1]), rows.o[x >> 1], 0, 0, 0);
+        share(x);
+        issue_first();
+      }
+    };
     int slot = 0;  // i mod 3: the unit's buffer, and its word of bad_tok
-    for (int i = 0; i <= n; ++i) {
+    for (int i = 0; i < n; ++i) {
       const Unit after = uniform_unit(list[min(i + 2, n - 1)]);
       const int slot1 = slot == 2 ? 0 : slot + 1, slot2 = slot == 0 ? 2 : slot - 1;
-      const bool has = i < n;
       if (tid == 0) bad_tok[slot2] = 0;
       if (i + 1 < n && next.masked()) check(next, slot1);
       uint16_t* to = unit_rows[slot1] + tok * kPitch;
       const Place from = place(after);
-      if (works) {
+      // (the scale bytes of the unit after the next are the first loads of a step, and wait in registers of their own:
+      // what unpacking begins with would otherwise be the youngest load, and wait for all)
+      uint32_t scales[P::kScaleWords];
+      load_scales(from, scales);
+      issue_first();
+      // (a wave without rows goes along with its tile's last row: with a path of its own the compiler copies the loads
+      // of the units ahead from register to register, which waits for them)
+      {
         const uint16_t* keys = unit_rows[slot];
-        const uint16_t* values = unit_rows[slot2] + value_at;
+        values = unit_rows[slot2] + value_at;
         f32x16 s;
 #pragma unroll
         for (int j = 0; j < 16; ++j) s[j] = 0.f;
-        constexpr int kFirst = (P::kPieces + 1) / 2;  // pieces beside the first product
-        if (has) {
+        {
           constexpr int kAhead = 3;
           auto key = [&](int y) {
             return *reinterpret_cast<const u32x4_t*>(keys + (y & 1 ? odd : even) + 32 * (y >> 1));
           };
+          auto query = [&](int y) { return *reinterpret_cast<const bf16x8*>(my_parked + (y - kKept) * 512); };
           u32x4_t k[kSteps];
+          bf16x8 pq[S::kParked + 1];
 #pragma unroll
           for (int y = 0; y < kAhead; ++y) k[y] = key(y);
           issue_first();
 #pragma unroll
           for (int y = 0; y < kSteps; ++y) {
             if (y + kAhead < kSteps) k[y + kAhead] = key(y + kAhead);
-            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(k[y]), q[y], s, 0, 0, 0);
-            if (y * kFirst / kSteps != (y + 1) * kFirst / kSteps) advance(to, from, y * kFirst / kSteps);
+            if (y + kAhead < kSteps && y + kAhead >= kKept) pq[y + kAhead - kKept] = query(y + kAhead);
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(k[y]),
+                                                        y < kKept ? q[y < kKept ? y : 0] : pq[y < kKept ? 0 : y - kKept],
+                                                        s, 0, 0, 0);
+            if (y * P::kPieces / kSteps != (y + 1) * P::kPieces / kSteps) advance(to, from, y * P::kPieces / kSteps);
             issue_first();
           }
         }
-        bool counts = false;
-        float high = -INFINITY;
-        if (has) {
-          if (u.masked()) {
-            const uint32_t seen = visible_tokens(rule, u, prefix);
-            mask_scores<32, 16>(s, seen, half);
-            poison |= (seen & bad_tok[slot]) != 0;
-          }
-          float top = s[0];
-#pragma unroll
-          for (int j = 1; j < 16; ++j) top = nan_max(top, s[j]);
-          high = max_column<32>(top) * c;
-          counts = __any(!u.masked() || high != -INFINITY);
+        if (u.masked()) {
+          const uint32_t seen = visible_tokens(rule, u, prefix);
+          mask_scores<32, 16>(s, seen, half);
+          poison |= (seen & bad_tok[slot]) != 0;
         }
-        auto value = [&](int x) {  // operand x: columns 32 (x / 2), tokens 16 (x % 2)
-          const uint16_t* src = values + 16 * (x & 1) * kPitch + 32 * (x >> 1);
-          const u32x2_t v0 = lds_transpose4(src), v1 = lds_transpose4(src + 8 * kPitch);
-          return as_bf16x8(u32x4_t{v0[0], v0[1], v1[0], v1[1]});
-        };
-        constexpr int kOps = 2 * kBlocks;
-        auto add = [&](const u32x4_t (&by)[2], auto share) {
-          constexpr int kAhead = 2;
-          bf16x8 v[kOps];
+        float top = s[0];
 #pragma unroll
-          for (int x = 0; x < kAhead; ++x) v[x] = value(x);
-          issue_first();
-#pragma unroll
-          for (int x = 0; x < kOps; ++x) {
-            if (x + kAhead < kOps) v[x + kAhead] = value(x + kAhead);
-            rows.o[x >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[x], as_bf16x8(by[x & 1]), rows.o[x >> 1], 0, 0, 0);
-            share(x);
-            issue_first();
-          }
-        };
+        for (int j = 1; j < 16; ++j) top = nan_max(top, s[j]);
+        const float high = max_column<32>(top) * c;
+        const bool counts = __any(!u.masked() || high != -INFINITY);
         const bool up = counts && __any(high > st.m + kLag);
         u32x4_t now[2];
         auto weigh_score = [&](float ref, int j) {
@@ -422,7 +476,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attend_kernel(LatentArgs x
         int usual_too = __builtin_amdgcn_readfirstlane(usual);
         asm volatile("" : "+s"(usual_too));
         if (!usual) {
-          if (pending) add(w, [](int) {});
+          if (pending) add_values([](int) {});
           if (up) {
             const float mn = fmaxf(st.m, high);
             const float r = mn == -INFINITY ? 1.f : fast_exp2(st.m - mn);
@@ -436,33 +490,28 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attend_kernel(LatentArgs x
 #pragma unroll
             for (int j = 0; j < 16; ++j) weigh_score(ref, j);
           }
-#pragma unroll
-          for (int z = kFirst; z < P::kPieces; ++z) advance(to, from, z);
         }
         if (usual_too) {
           const float ref = finite_max(st.m);
-          add(w, [&](int x) {
-            constexpr int kSecond = P::kPieces - kFirst;
+          add_values([&](int x) {
 #pragma unroll
             for (int j = 16 * x / kOps; j < 16 * (x + 1) / kOps; ++j) weigh_score(ref, j);
-#pragma unroll
-            for (int z = kSecond * x / kOps; z < kSecond * (x + 1) / kOps; ++z) advance(to, from, kFirst + z);
           });
         }
-        if (!has) break;
         pending = counts;
         w[0] = now[0];
         w[1] = now[1];
-      } else {
-        if (!has) break;
-#pragma unroll
-        for (int z = 0; z < P::kPieces; ++z) advance(to, from, z);
       }
-      load_scales(from);
+#pragma unroll
+      for (int j = 0; j < P::kScaleWords; ++j) p.sc[j] = scales[j];
       u = next;
       next = after;
       slot = slot1;
       __syncthreads();
+    }
+    if (pending) {
+      values = unit_rows[slot == 0 ? 2 : slot - 1] + value_at;
+      add_values([](int) {});
     }
   }
 
@@ -470,22 +519,333 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attend_kernel(LatentArgs x
   rounded = sum_column<32>(rounded);
   poison = any_column<32>(poison, col);
   if (32 * rg + col >= t.rows) return;
-  if (splits == 1) {
-    const float inv = poison ? NAN : inverse_sum(rounded);
-    uint16_t* dst = sums + row_at * L + cg * kColumns;
-    rows.each4(half, [&](int d, f32x4 v) {
-      *reinterpret_cast<u32x2_t*>(dst + d) = u32x2_t{pack2(v[0] * inv, v[1] * inv), pack2(v[2] * inv, v[3] * inv)};
-    });
-    if (a.lse && half == 0 && cg == 0) a.lse[row_at] = poison ? NAN : lse_of(st.m, st.l);
-  } else {
-    const int64_t at = static_cast<int64_t>(split) * a.total_q * a.hq + row_at;
-    float* dst = part_o + at * L + cg * kColumns;
-    const float even_out = poison ? NAN : st.l == 0.f ? 0.f : st.l * inverse_sum(rounded);  // the join divides by l
-    rows.each4(half, [&](int d, f32x4 v) {
-      *reinterpret_cast<f32x4*>(dst + d) = v * even_out;
-    });
-    if (half == 0 && cg == 0) part_ml[at] = poison ? RowState{st.m, NAN} : st;
+  write_sums<32, kColumns, L>(a, rows, st, rounded, poison, row_at, half, split, splits, cg * kColumns, sums, part_o,
+                              part_ml);
+}
+
+// ---------------------------------------------------------------- few rows
+
+// A lane's parts of two tokens' rows (16 apart): 16-byte loads 4 parts apart, the key part's two, and the scale bytes.
+template <int FMT, int L>
+struct Quarter {
+  static constexpr int kRow = kv_row_bytes(FMT, L);
+  static constexpr int kSc = kv_scale_bytes(FMT, L);
+  static constexpr int kElems = 16 * L / kRow;   // elements of a load
+  static constexpr int kLoads = L / (4 * kElems);
+  static constexpr int kChunks = kElems / 8;     // operands of eight elements that a load becomes
+  static constexpr int kScaleWords = FMT == MEM_KV_BF16 ? 1 : kSc / 4;
+  u32x4_t codes[kLoads], rope[2];
+  uint32_t sc[kScaleWords];
+
+  __device__ __forceinline__ uint32_t scale_byte(int y, int part) const {
+    if constexpr (FMT == MEM_KV_FP8) return sc[y >> 1] >> (16 * (y & 1) + 8 * (part >> 1)) & 255u;  // block 2 y + part / 2
+    return sc[y] >> (8 * part) & 255u;                                                             // block 4 y + part
   }
+  __device__ __forceinline__ u32x4_t chunk(int y, int c, float s) const {
+    if constexpr (FMT == MEM_KV_BF16) return codes[y];
+    u32x4_t o;
+    if constexpr (FMT == MEM_KV_FP4) {
+      const uint32_t x = codes[y][c];
+      o[0] = bits_of(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, s, 0));
+      o[1] = bits_of(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, s, 1));
+      o[2] = bits_of(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, s, 2));
+      o[3] = bits_of(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, s, 3));
+    } else if constexpr (FMT == MEM_KV_FP8) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        o[2 * j] = bits_of(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[y][2 * c + j], s, false));
+        o[2 * j + 1] = bits_of(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[y][2 * c + j], s, true));
+      }
+    }
+    return o;
+  }
+  // Whether it holds a latent value that is not finite, or may.
+  __device__ __forceinline__ bool bad() const {
+    u16x2 most = {0, 0};
+    bool x = false;
+#pragma unroll
+    for (int y = 0; y < kLoads; ++y)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if constexpr (FMT == MEM_KV_BF16)
+          most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, codes[y][j] & 0x7FFF7FFFu));
+        if constexpr (FMT == MEM_KV_FP8) x |= (((codes[y][j] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) != 0;
+      }
+    if constexpr (FMT != MEM_KV_BF16) {
+#pragma unroll
+      for (int i = 0; i < kScaleWords; ++i)
+#pragma unroll
+        for (int b = 0; b < 4; ++b) x |= (sc[i] >> (8 * b) & 255u) > kMaxScaleByte<FMT>;
+    }
+    return x || most[0] >= 0x7F80u || most[1] >= 0x7F80u;
+  }
+  __device__ __forceinline__ void clear(bool parts) {
+#pragma unroll
+    for (int y = 0; y < kLoads; ++y) codes[y] = u32x4_t{0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < kScaleWords; ++i) sc[i] = 0x7F7F7F7Fu;
+    if (parts) rope[0] = rope[1] = u32x4_t{0, 0, 0, 0};
+  }
+};
+
+template <int L>
+struct FewShape {
+  static constexpr int kRows = 16;
+  static constexpr int kBatch = 128;                                    // units resolved at a time
+  static constexpr int kWaveBytes = kUnit * kValuePitch<16, L> * 2;     // a wave's unit as bf16
+  static constexpr int kJoinBytes = 2 * kRows * L * 4;                  // two waves' outputs at the end
+  static constexpr int kArea = kWaves * kWaveBytes > kJoinBytes ? kWaves * kWaveBytes : kJoinBytes;
+  static constexpr int kShift = 3;
+};
+
+// Workgroups that share a CU.
+constexpr int few_per_cu(int fmt, int latent) { return latent == 256 && fmt != MEM_KV_BF16 ? 2 : 1; }
+
+// Tiles of 16 rows: each wave streams its own units with no barrier.  A lane loads parts of two tokens' rows straight
+// from the page; unpacked, they are operands of the first product, and go through the wave's own LDS rows once to be
+// read back transposed for the second.  Each load is made again, for the wave's next unit, as soon as it has been used.
+template <int FMT, int L>
+__global__ __launch_bounds__(kThreads, few_per_cu(FMT, L)) void latent_few_kernel(LatentArgs x, int splits,
+                                                                             const uint16_t* __restrict__ query_rows,
+                                                                             uint16_t* __restrict__ sums,
+                                                                             float* __restrict__ part_o,
+                                                                             RowState* __restrict__ part_ml) {
+  using P = Quarter<FMT, L>;
+  using S = FewShape<L>;
+  constexpr int R = S::kRows, kSteps = L / 32, kOps = L / 16;
+  extern __shared__ int dyn[];  // of the chunk list: ub[k + 1], tb[k + 1]
+  __shared__ __align__(16) uint8_t area[S::kArea];
+  __shared__ Unit list[S::kBatch];
+  __shared__ int tmp[2 * kWaves];
+  __shared__ RowState joint[2][64];
+  __shared__ float joint_rounded[2][64];
+  __shared__ int joint_poison[2][64];
+
+  const AttendArgs& a = x.a;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int col = lane & 15, part = lane >> 4;
+  const uint32_t tile = blockIdx.x / static_cast<uint32_t>(splits);
+  const int split = static_cast<int>(blockIdx.x - tile * splits);
+  Tile t;
+  if (!find_tile<R>(a, tile, a.hq, &t)) return;
+  const ChunkList list_of = scan_list<kThreads, false>(a, t.req, dyn, tmp);
+  const int ctx = list_of.tb[a.k];
+  const int prefix = a.prefix_len ? __builtin_amdgcn_readfirstlane(min(max(a.prefix_len[t.req], 0), kFar)) : 0;
+  const int my_row = t.r0 + min(col, t.rows - 1);
+  const RowRule rule = row_rule(a, t, ctx, 0, a.hq, my_row);
+  const TileRule tr = tile_rule<R>(a, t, ctx, 0, a.hq);
+  const Span span = visible_units(list_of, prefix, tr.lo, tr.hi);
+  const int n_units = __builtin_amdgcn_readfirstlane(span.count());
+  const int u0 = static_cast<int>(static_cast<int64_t>(n_units) * split / splits);
+  const int u1 = static_cast<int>(static_cast<int64_t>(n_units) * (split + 1) / splits);
+
+  // queries in the order of the loads: operand (y, c) of a lane holds elements E (4 y + part) + 8 c .. + 7
+  bf16x8 q[kSteps], qr[2];
+  const int64_t row_at = static_cast<int64_t>(t.q0) * a.hq + my_row;
+  {
+    const uint16_t* src = query_rows + row_at * kQueryRow<L>;
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+      const int y = i / P::kChunks, cc = i % P::kChunks;
+      q[i] = as_bf16x8(*reinterpret_cast<const u32x4_t*>(src + P::kElems * (4 * y + part) + 8 * cc));
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) qr[i] = as_bf16x8(*reinterpret_cast<const u32x4_t*>(src + L + 32 * i + 8 * part));
+  }
+
+  const float c = a.scale * kLog2e;
+  const int64_t T = a.kv.page_tokens;
+  uint16_t* rows_of = reinterpret_cast<uint16_t*>(area + wave * S::kWaveBytes);
+  const ValueOps<16, L, S::kShift> ops(rows_of, lane);
+  Rows<16, L> rows;
+  rows.clear();
+  RowState st{-INFINITY, 0.f};
+  float rounded = 0.f;
+  bool poison = false;
+  P p[2];
+
+  struct Place {
+    const uint8_t *page, *parts, *scales;  // the same in every lane
+    uint32_t row[2];
+  };
+  auto place = [&](const Unit& u) {
+    const uint8_t* page = a.kv.pool + (u.at - u.row() * P::kRow);
+    Place w{page, page + T * P::kRow, page + T * (P::kRow + 2 * kRopeDim), {}};
+#pragma unroll
+    for (int h = 0; h < 2; ++h) w.row[h] = static_cast<uint32_t>(u.row() + min(16 * h + col, u.held() - 1));
+    return w;
+  };
+  auto load_codes = [&](const Place& from, int h, int y) {
+    p[h].codes[y] = *reinterpret_cast<const u32x4_t*>(from.page + (from.row[h] * P::kRow + 16 * part + 64 * y));
+  };
+  auto load_rope = [&](const Place& from, int h, int y) {
+    p[h].rope[y] =
+        *reinterpret_cast<const u32x4_t*>(from.parts + (from.row[h] * (2 * kRopeDim) + 16 * part + 64 * y));
+  };
+  auto load_scales = [&](const Place& from, int h, uint32_t (&to)[P::kScaleWords]) {
+    if constexpr (FMT != MEM_KV_BF16) {
+#pragma unroll
+      for (int i = 0; i < P::kScaleWords / 2; ++i) {
+        const u32x2_t v = reinterpret_cast<const u32x2_t*>(from.scales + from.row[h] * P::kSc)[i];
+        to[2 * i] = v[0];
+        to[2 * i + 1] = v[1];
+      }
+    } else {
+      to[0] = 0;
+    }
+  };
+
+  for (int last = u1 - 1; last >= u0; last -= S::kBatch) {
+    __syncthreads();
+    const int n = resolve_units<S::kBatch>(a, list_of, span, tr, prefix, 0, P::kRow, last, min(S::kBatch, last - u0 + 1),
+                                           list, tmp);
+    if (wave >= n) continue;
+    Unit u = uniform_unit(list[wave]);
+    {
+      const Place from = place(u);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) load_scales(from, h, p[h].sc);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int y = 0; y < P::kLoads; ++y) load_codes(from, h, y);
+#pragma unroll
+        for (int y = 0; y < 2; ++y) load_rope(from, h, y);
+      }
+    }
+    for (int i = wave; i < n; i += kWaves) {
+      const Unit next = uniform_unit(list[i + kWaves < n ? i + kWaves : i]);
+      const Place from = place(next);
+      uint32_t bad = 0;
+      if (u.masked()) {  // tokens that are not held are cleared, values that are not finite are noted and left out
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int tok = 16 * h + col;
+          if (tok >= u.held()) p[h].clear(true);
+          uint64_t vote = __ballot(p[h].bad());
+          vote |= vote >> 32;
+          vote |= vote >> 16;
+          if ((vote >> col) & 1u) p[h].clear(false);
+          bad |= static_cast<uint32_t>(vote & 0xFFFFu) << (16 * h);
+        }
+      }
+      uint32_t scales[2][P::kScaleWords];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) load_scales(from, h, scales[h]);
+      issue_first();
+      f32x4 sum[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        sum[h] = f32x4{0.f, 0.f, 0.f, 0.f};
+        uint16_t* dst = rows_of + (16 * h + col) * kValuePitch<16, L>;
+#pragma unroll
+        for (int y = 0; y < P::kLoads; ++y) {
+          const float s = FMT == MEM_KV_BF16 ? 1.f : kv_scale(p[h].scale_byte(y, part));
+#pragma unroll
+          for (int cc = 0; cc < P::kChunks; ++cc) {
+            const u32x4_t k = p[h].chunk(y, cc, s);
+            sum[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(k), q[y * P::kChunks + cc], sum[h], 0, 0, 0);
+            *reinterpret_cast<u32x4_t*>(
+                dst + 8 * value_chunk<16, S::kShift>(16 * h + col, P::kChunks * (part + 4 * y) + cc)) = k;
+          }
+          load_codes(from, h, y);
+          issue_first();
+        }
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          sum[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(p[h].rope[y]), qr[y], sum[h], 0, 0, 0);
+          load_rope(from, h, y);
+          issue_first();
+        }
+      }
+      float s[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s[j] = sum[j >> 2][j & 3];
+      if (u.masked()) {
+        const uint32_t seen = visible_tokens(rule, u, prefix);
+        mask_scores<16, 8>(s, seen, part);
+        poison |= (seen & bad) != 0;
+      }
+      const float high = max_column<16>(max_of(s)) * c;
+      const bool counts = __any(!u.masked() || high != -INFINITY);
+      if (counts) {
+        if (__any(high > st.m + kLag)) {
+          const float mn = fmaxf(st.m, high);
+          const float r = mn == -INFINITY ? 1.f : fast_exp2(st.m - mn);
+          st.l *= r;
+          rounded *= r;
+          if constexpr (L == 512) scale_rows(rows, r);
+          else rows.scale(r);
+          st.m = mn;
+        }
+        const float ref = finite_max(st.m);
+        u32x4_t w;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          s[j] = fast_exp2(fmaf(s[j], c, -ref));
+          st.l += s[j];
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          w[j] = pack2(s[2 * j], s[2 * j + 1]);
+          rounded = add_pair(w[j], rounded);
+        }
+        __builtin_amdgcn_wave_barrier();
+        constexpr int kTogether = 8;  // operands loaded ahead of their products
+#pragma unroll
+        for (int n0 = 0; n0 < kOps; n0 += kTogether) {
+          bf16x8 v[kTogether];
+#pragma unroll
+          for (int y = 0; y < kTogether; ++y) v[y] = ops[n0 + y];
+          issue_first();
+#pragma unroll
+          for (int y = 0; y < kTogether; ++y) ops.multiply(rows, n0 + y, v[y], &w);
+        }
+        __builtin_amdgcn_wave_barrier();
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int j = 0; j < P::kScaleWords; ++j) p[h].sc[j] = scales[h][j];
+      u = next;
+    }
+  }
+
+  // join the waves: 2 and 3 into 0 and 1, then 1 into 0 (a lane holds the same outputs in every wave)
+  st.l = sum_column<16>(st.l);
+  rounded = sum_column<16>(rounded);
+  poison = any_column<16>(poison, col);
+  float* store = reinterpret_cast<float*>(area);
+#pragma unroll
+  for (int from = 2; from >= 1; --from) {
+    __syncthreads();  // what `area` held is done with
+    if (wave >= from && wave < 2 * from) {
+      float* dst = store + (wave - from) * R * L + lane * 4;
+      int i = 0;
+      rows.each4(part, [&](int, f32x4 v) { *reinterpret_cast<f32x4*>(dst + 256 * i++) = v; });
+      joint[wave - from][lane] = st;
+      joint_rounded[wave - from][lane] = rounded;
+      joint_poison[wave - from][lane] = poison;
+    }
+    __syncthreads();
+    if (wave < from) {
+      const RowState other = joint[wave][lane];
+      poison |= joint_poison[wave][lane] != 0;
+      const float mn = fmaxf(st.m, other.m), ref = finite_max(mn);
+      const float f0 = fast_exp2(st.m - ref), f1 = fast_exp2(other.m - ref);
+      st.l = st.l * f0 + other.l * f1;
+      rounded = rounded * f0 + joint_rounded[wave][lane] * f1;
+      st.m = mn;
+      const float* src = store + wave * R * L + lane * 4;
+#pragma unroll
+      for (int i = 0; i < kOps; ++i) {
+        const f32x4 v = *reinterpret_cast<const f32x4*>(src + 256 * i);
+        rows.o[i] = rows.o[i] * f0 + v * f1;
+      }
+    }
+  }
+  if (wave > 0 || col >= t.rows) return;
+  write_sums<16, L, L>(a, rows, st, rounded, poison, row_at, part, split, splits, 0, sums, part_o, part_ml);
 }
 
 // ---------------------------------------------------------------- outputs
@@ -523,20 +883,33 @@ size_t align256(size_t b) { return (b + 255) & ~static_cast<size_t>(255); }
 size_t list_bytes(int k) { return (2 * static_cast<size_t>(k) + 2) * sizeof(int); }
 
 struct AbsorbedPlan {
-  int rg;  // tiles of 32 rg rows
+  int rows;  // of a tile: 16 (few-rows kernel), 64 or 128
   int64_t tiles;
   int splits;
 };
 
 constexpr int64_t kStart = 16;  // a workgroup's start and end, in units
 
+// Tiles of 128 rows of 512 elements leave 4 KB of a CU's 160 KB for the chunk list, tiles of 16 rows 20 KB: calls with
+// longer lists (more than 511 and 2,559 chunks) take tiles of 64, which leave 40.
+bool list_fits_tiles(int latent, int k) { return latent < 512 || list_bytes(k) <= 4096; }
+bool list_fits_few(int latent, int k) { return latent < 512 || list_bytes(k) <= 20 * 1024; }
+static_assert(FewShape<512>::kArea + FewShape<512>::kBatch * sizeof(Unit) + 2048 + 20 * 1024 <= 160 * 1024,
+              "a workgroup's LDS");
+static_assert(2 * 3 * LatentShape<512, 2>::kUnitElems + LatentShape<512, 2>::kBatch * sizeof(Unit) + 128 + 8 * 4097 <=
+                  160 * 1024,
+              "a workgroup's LDS");
+static_assert(2 * (3 * LatentShape<512, 4>::kUnitElems + 4 * 64 * 8 * LatentShape<512, 4>::kParked) +
+                      LatentShape<512, 4>::kBatch * sizeof(Unit) + 128 + 4096 <= 160 * 1024,
+              "a workgroup's LDS");
+
 AbsorbedPlan absorbed_plan(const LatentSizes& s, bool ragged) {
   AbsorbedPlan p;
   const int64_t rows = s.total_q * s.heads;
-  p.rg = rows <= 32 * s.m ? 1 : rows <= 64 * s.m ? 2 : 4;
-  const int R = 32 * p.rg;
+  p.rows = rows <= 32 * s.m && list_fits_few(s.latent, s.k) ? 16 : rows <= 64 * s.m || !list_fits_tiles(s.latent, s.k) ? 64 : 128;
+  const int R = p.rows;
   p.tiles = ragged ? rows / R + s.m : s.m * ((s.total_q / s.m * s.heads + R - 1) / R);
-  const int64_t work = ragged ? (rows + R - 1) / R + s.m / 2 : p.tiles, slots = 256;
+  const int64_t work = ragged ? (rows + R - 1) / R + s.m / 2 : p.tiles, slots = 256 * (R == 16 ? few_per_cu(s.fmt, s.latent) : 1);
   int64_t best = INT64_MAX;
   p.splits = 1;
   for (int64_t n = 1; n <= kMaxSplits && (n == 1 || s.units / n >= 4); ++n) {
@@ -588,10 +961,11 @@ hipError_t launch_absorbed(const LatentArgs& x, const LatentSizes& s, hipStream_
                               stream>>>(x, kQueryBlocks, queries);
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   const unsigned grid = static_cast<unsigned>(p.tiles * p.splits);
-  (p.rg == 1   ? latent_attend_kernel<FMT, L, 1>
-   : p.rg == 2 ? latent_attend_kernel<FMT, L, 2>
-               : latent_attend_kernel<FMT, L, 4>)<<<grid, kThreads, list_bytes(s.k), stream>>>(
-      x, p.splits, p.tiles, queries, sums, part_o, part_ml);
+  if (p.rows == 16)
+    latent_few_kernel<FMT, L><<<grid, kThreads, list_bytes(s.k), stream>>>(x, p.splits, queries, sums, part_o, part_ml);
+  else
+    (p.rows == 64 ? latent_attend_kernel<FMT, L, 2> : latent_attend_kernel<FMT, L, 4>)<<<
+        grid, kThreads, list_bytes(s.k), stream>>>(x, p.splits, p.tiles, queries, sums, part_o, part_ml);
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   if (p.splits > 1) {
     AttendArgs j = x.a;

@@ -249,6 +249,16 @@ def test_split_contexts(form, m, nq, k):
 
 
 @pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("h,nq,k", [(2, 1, 2600), (1, 5, 4096), (16, 9, 520), (16, 9, 4096)])
+@pytest.mark.parametrize("latent", [256, 512])
+def test_long_lists(form, h, nq, k, latent):
+    # lists that leave a tile's other memory too little: other tiles
+    rng = np.random.default_rng(k)
+    p = Problem(k, FMTS["fp8"], [list(rng.integers(0, 3, 300)), [5]], [nq, nq], h, 64, latent, k=k, holes=True)
+    p.check("long", forms=[form], causal=True)
+
+
+@pytest.mark.parametrize("form", FORMS)
 def test_many_ragged_requests(form):
     rng = np.random.default_rng(17)
     m = 600
