@@ -5,6 +5,8 @@
 //   latent_attend_kernel  attention of those rows over the cache
 //   attend_join_kernel    joins the parts of split contexts
 //   latent_out_kernel     V_h times the weighted sum of latent vectors
+#include <algorithm>
+
 #include "context.h"
 #include "kv.h"
 #include "latent.h"
@@ -180,6 +182,22 @@ __global__ __launch_bounds__(kThreads) void latent_query_kernel(LatentArgs x, in
 
 // ---------------------------------------------------------------- attention over latent vectors
 
+constexpr int kXcds = 8;
+
+// Which tile and split a workgroup has.  Workgroups go to the XCDs in turn, and each XCD has an L2 of its own: the `side`
+// tiles that read one context (the rows of a request are consecutive tiles) follow each other on one XCD.
+struct Job {
+  int64_t tile;  // may be past the last one
+  int split;
+};
+__device__ __forceinline__ Job job_of(uint32_t block, int side, int splits) {
+  const uint32_t xcd = block % kXcds, at = block / kXcds, group = at / side * kXcds + xcd;
+  return {static_cast<int64_t>(group / splits) * side + at % side, static_cast<int>(group % splits)};
+}
+inline int64_t job_blocks(int64_t tiles, int side, int splits) {
+  return ((tiles + side - 1) / side * splits + kXcds - 1) / kXcds * kXcds * side;
+}
+
 template <int L, int RG>
 struct LatentShape {
   static constexpr int kBatch = 64;                           // units resolved at a time
@@ -238,7 +256,7 @@ __device__ __forceinline__ float add_pair(uint32_t pair, float x) {
 // Tiles of 32 RG rows: wave w has the 32 rows w / (4 / RG) of the tile and, of the second product, a share of the
 // columns; waves with the same rows make their scores each for itself.
 template <int FMT, int L, int RG>
-__global__ __launch_bounds__(kThreads, 1) void latent_attend_kernel(LatentArgs x, int splits, int64_t tiles,
+__global__ __launch_bounds__(kThreads, 1) void latent_attend_kernel(LatentArgs x, int splits, int64_t tiles, int side,
                                                                  const uint16_t* __restrict__ query_rows,
                                                                  uint16_t* __restrict__ sums,
                                                                  float* __restrict__ part_o,
@@ -261,10 +279,10 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attend_kernel(LatentArgs x
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 31, half = lane >> 5;
   const int rg = wave / kShare, cg = wave % kShare;
-  const uint32_t tile = blockIdx.x / static_cast<uint32_t>(splits);
-  const int split = static_cast<int>(blockIdx.x - tile * splits);
+  const Job job = job_of(blockIdx.x, side, splits);
+  const int split = job.split;
   Tile t;
-  if (!find_tile<32 * RG>(a, static_cast<uint32_t>(tiles) - 1 - tile, a.hq, &t)) return;
+  if (job.tile >= tiles || !find_tile<32 * RG>(a, static_cast<uint32_t>(tiles - 1 - job.tile), a.hq, &t)) return;
   const ChunkList list_of = scan_list<kThreads, false>(a, t.req, dyn, tmp);
   const int ctx = list_of.tb[a.k];
   const int prefix = a.prefix_len ? __builtin_amdgcn_readfirstlane(min(max(a.prefix_len[t.req], 0), kFar)) : 0;
@@ -605,7 +623,7 @@ constexpr int few_per_cu(int fmt, int latent) { return latent == 256 && fmt != M
 // from the page; unpacked, they are operands of the first product, and go through the wave's own LDS rows once to be
 // read back transposed for the second.  Each load is made again, for the wave's next unit, as soon as it has been used.
 template <int FMT, int L>
-__global__ __launch_bounds__(kThreads, few_per_cu(FMT, L)) void latent_few_kernel(LatentArgs x, int splits,
+__global__ __launch_bounds__(kThreads, few_per_cu(FMT, L)) void latent_few_kernel(LatentArgs x, int splits, int64_t tiles, int side,
                                                                              const uint16_t* __restrict__ query_rows,
                                                                              uint16_t* __restrict__ sums,
                                                                              float* __restrict__ part_o,
@@ -624,10 +642,10 @@ __global__ __launch_bounds__(kThreads, few_per_cu(FMT, L)) void latent_few_kerne
   const AttendArgs& a = x.a;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 15, part = lane >> 4;
-  const uint32_t tile = blockIdx.x / static_cast<uint32_t>(splits);
-  const int split = static_cast<int>(blockIdx.x - tile * splits);
+  const Job job = job_of(blockIdx.x, side, splits);
+  const int split = job.split;
   Tile t;
-  if (!find_tile<R>(a, tile, a.hq, &t)) return;
+  if (job.tile >= tiles || !find_tile<R>(a, static_cast<uint32_t>(job.tile), a.hq, &t)) return;
   const ChunkList list_of = scan_list<kThreads, false>(a, t.req, dyn, tmp);
   const int ctx = list_of.tb[a.k];
   const int prefix = a.prefix_len ? __builtin_amdgcn_readfirstlane(min(max(a.prefix_len[t.req], 0), kFar)) : 0;
@@ -886,6 +904,7 @@ struct AbsorbedPlan {
   int rows;  // of a tile: 16 (few-rows kernel), 64 or 128
   int64_t tiles;
   int splits;
+  int side;  // tiles of a request, on average
 };
 
 constexpr int64_t kStart = 16;  // a workgroup's start and end, in units
@@ -910,10 +929,11 @@ AbsorbedPlan absorbed_plan(const LatentSizes& s, bool ragged) {
   const int R = p.rows;
   p.tiles = ragged ? rows / R + s.m : s.m * ((s.total_q / s.m * s.heads + R - 1) / R);
   const int64_t work = ragged ? (rows + R - 1) / R + s.m / 2 : p.tiles, slots = 256 * (R == 16 ? few_per_cu(s.fmt, s.latent) : 1);
+  p.side = static_cast<int>(std::min<int64_t>(std::max<int64_t>((rows / s.m + R - 1) / R, 1), 64));
   int64_t best = INT64_MAX;
   p.splits = 1;
   for (int64_t n = 1; n <= kMaxSplits && (n == 1 || s.units / n >= 4); ++n) {
-    if (n > 1 && (p.tiles * n > kMaxGroups || join_groups(rows, n) > kMaxGroups)) break;
+    if (n > 1 && (job_blocks(p.tiles, p.side, n) > kMaxGroups || join_groups(rows, n) > kMaxGroups)) break;
     const int64_t cost = (work * n + slots - 1) / slots * ((s.units + n - 1) / n + kStart) + (n > 1 ? n / 4 : 0);
     if (cost < best) {
       best = cost;
@@ -960,12 +980,13 @@ hipError_t launch_absorbed(const LatentArgs& x, const LatentSizes& s, hipStream_
   latent_query_kernel<L, D><<<dim3(s.heads, L / 128, static_cast<unsigned>(query_groups(s.total_q))), kThreads, 0,
                               stream>>>(x, kQueryBlocks, queries);
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  const unsigned grid = static_cast<unsigned>(p.tiles * p.splits);
+  const unsigned grid = static_cast<unsigned>(job_blocks(p.tiles, p.side, p.splits));
   if (p.rows == 16)
-    latent_few_kernel<FMT, L><<<grid, kThreads, list_bytes(s.k), stream>>>(x, p.splits, queries, sums, part_o, part_ml);
+    latent_few_kernel<FMT, L><<<grid, kThreads, list_bytes(s.k), stream>>>(x, p.splits, p.tiles, p.side, queries, sums,
+                                                                          part_o, part_ml);
   else
     (p.rows == 64 ? latent_attend_kernel<FMT, L, 2> : latent_attend_kernel<FMT, L, 4>)<<<
-        grid, kThreads, list_bytes(s.k), stream>>>(x, p.splits, p.tiles, queries, sums, part_o, part_ml);
+        grid, kThreads, list_bytes(s.k), stream>>>(x, p.splits, p.tiles, p.side, queries, sums, part_o, part_ml);
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   if (p.splits > 1) {
     AttendArgs j = x.a;
@@ -1017,7 +1038,7 @@ size_t latent_workspace_bytes(const LatentSizes& s, mem_latent_form form) {
 bool latent_fits(const LatentSizes& s, mem_latent_form form, bool ragged) {
   if (form == MEM_LATENT_EXPANDED) return expanded_fits(s, ragged);
   const AbsorbedPlan p = absorbed_plan(s, ragged);
-  return p.tiles * p.splits <= kMaxGroups && query_groups(s.total_q) < 65536 && out_groups(s.total_q, s.head_dim) < 65536;
+  return job_blocks(p.tiles, p.side, p.splits) <= kMaxGroups && query_groups(s.total_q) < 65536 && out_groups(s.total_q, s.head_dim) < 65536;
 }
 
 hipError_t launch_latent_attend(const LatentArgs& x, const LatentSizes& s, mem_latent_form form, hipStream_t stream) {
