@@ -10,19 +10,12 @@
 #include "context.h"
 #include "kv.h"
 #include "latent.h"
+#include "latent_rows.h"
 #include "device_common.h"
 
 namespace memattn {
 
 namespace {
-
-// Rows of L latent elements and the key part in LDS, bf16.  The pitch is an odd multiple of 64 bytes, and the 16-byte
-// chunks of a row are exchanged within 64 bytes by bits 1 and 2 of the row's number: eight rows' chunks of one column
-// (the first product reads them along a row) lie in different banks, and so do the pieces of four rows that a
-// transposing read takes (the second product).
-template <int L>
-constexpr int kLatentPitch = L + kRopeDim + 32;
-__device__ __forceinline__ int exchange(int row) { return (row & 2) | ((row >> 2) & 1); }
 
 // A thread's part of a token's row, 1/8 of it: 16-byte loads 8 parts apart, the key part, and the row's scale bytes.
 template <int FMT, int L>
@@ -221,36 +214,6 @@ __device__ __forceinline__ void scale_rows(Rows<WIDTH, D>& rows, float f) {
     rows.o[n] = y;
     if (WIDTH == 32 || n % 4 == 3) issue_first();
   }
-}
-
-// Write columns first .. + N - 1 of a row's weighted sum of latent vectors, or of its part of a split context.  `rounded`
-// is the sum of the weights as the product took them, and what it is divided by, so that their roundings cancel where a
-// few weigh most; the join divides by l.
-template <int WIDTH, int N, int L>
-__device__ __forceinline__ void write_sums(const AttendArgs& a, const Rows<WIDTH, N>& rows, RowState st, float rounded,
-                                           bool poison, int64_t row_at, int part, int split, int splits, int first,
-                                           uint16_t* sums, float* part_o, RowState* part_ml) {
-  if (poison) st.l = NAN;
-  if (splits == 1) {
-    const float inv = poison ? NAN : inverse_sum(rounded);
-    uint16_t* dst = sums + row_at * L + first;
-    rows.each4(part, [&](int d, f32x4 v) {
-      *reinterpret_cast<u32x2_t*>(dst + d) = u32x2_t{pack2(v[0] * inv, v[1] * inv), pack2(v[2] * inv, v[3] * inv)};
-    });
-    if (a.lse && part == 0 && first == 0) a.lse[row_at] = lse_of(st.m, st.l);
-  } else {
-    const int64_t at = static_cast<int64_t>(split) * a.total_q * a.hq + row_at;
-    const float even = st.l == 0.f ? 0.f : st.l * inverse_sum(rounded);
-    float* dst = part_o + at * L + first;
-    rows.each4(part, [&](int d, f32x4 v) { *reinterpret_cast<f32x4*>(dst + d) = v * even; });
-    if (part == 0 && first == 0) part_ml[at] = st;
-  }
-}
-
-// x + both halves of a pair of bf16.
-__device__ __forceinline__ float add_pair(uint32_t pair, float x) {
-  constexpr uint32_t kOnes = 0x3F803F80u;
-  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(s16x2, pair), __builtin_bit_cast(s16x2, kOnes), x, false);
 }
 
 // Tiles of 32 RG rows: wave w has the 32 rows w / (4 / RG) of the tile and, of the second product, a share of the

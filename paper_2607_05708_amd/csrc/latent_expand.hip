@@ -12,6 +12,7 @@
 #include "context.h"
 #include "kv.h"
 #include "latent.h"
+#include "latent_rows.h"
 #include "device_common.h"
 
 namespace memattn {
@@ -26,10 +27,9 @@ struct Source {
   int32_t held;
 };
 
-// Rows of L elements in LDS as in latent.hip, without the key part.
+// Rows of L elements in LDS: see kLatentPitch.
 template <int L>
 constexpr int kPitchOf = L + 32;
-__device__ __forceinline__ int exchange(int row) { return (row & 2) | ((row >> 2) & 1); }
 
 // ---------------------------------------------------------------- units
 
@@ -38,7 +38,7 @@ __global__ __launch_bounds__(kThreads) void latent_units_kernel(AttendArgs a, in
   extern __shared__ int dyn[];
   __shared__ int tmp[2 * kWaves];
   const int req = blockIdx.x;
-  const ChunkList L = scan_list(a, req, dyn, tmp);
+  const ChunkList L = scan_list<kThreads, false>(a, req, dyn, tmp);
   const int n = L.ub[a.k];
   if (threadIdx.x == 0) counts[req] = n;
   for (int u = threadIdx.x; u < n; u += kThreads) {
@@ -200,21 +200,24 @@ struct ExpandedShape {
   static constexpr int kKeyPitch = kKey + 32, kValuePitch = D + 32;
 };
 
-// Tiles of 32 WAVES rows (new tokens) of a head: as attend_tile_kernel, a unit a step, keys and values through
-// registers into one half of a double buffer while the waves work on the other.
+// Tiles of 32 WAVES rows (new tokens) of a head.  Units go through a ring of three in LDS: while the waves make the
+// scores of unit i, they unpack unit i + 1 and load unit i + 2; the second product of unit i - 1 is written in groups of
+// one matrix instruction and a share of unit i's exponentials (a wave issues in order, so that only what stands between
+// its matrix products overlaps with them).
 template <int D, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 2) void expanded_attend_kernel(
     LatentArgs x, int splits, int64_t tiles, int64_t units, int h0, int heads, const uint16_t* __restrict__ key_rows,
     const uint16_t* __restrict__ value_rows, float* __restrict__ part_o, RowState* __restrict__ part_ml) {
   using S = ExpandedShape<D>;
   constexpr int kThreadsHere = 64 * WAVES, kR = 32 * WAVES;
-  constexpr int kSteps = S::kKey / 16, kBlocks = D / 32;
+  constexpr int kSteps = S::kKey / 16, kBlocks = D / 32, kOps = 2 * kBlocks;
   constexpr int kKeyChunks = S::kKey / 8, kValueChunks = D / 8;              // 16-byte chunks of a row
   constexpr int kKeyLoads = kUnit * kKeyChunks / kThreadsHere, kValueLoads = kUnit * kValueChunks / kThreadsHere;
+  constexpr int kPieces = kKeyLoads + kValueLoads;
   static_assert(kUnit * kKeyChunks % kThreadsHere == 0 && kUnit * kValueChunks % kThreadsHere == 0, "whole loads");
-  extern __shared__ int dyn[];  // the chunk list: cid[k], ub[k + 1], tb[k + 1]
-  __shared__ __align__(16) uint16_t keys[2][kUnit * S::kKeyPitch];
-  __shared__ __align__(16) uint16_t values[2][kUnit * S::kValuePitch];
+  extern __shared__ int dyn[];  // of the chunk list: ub[k + 1], tb[k + 1]
+  __shared__ __align__(16) uint16_t keys[3][kUnit * S::kKeyPitch];
+  __shared__ __align__(16) uint16_t values[3][kUnit * S::kValuePitch];
   __shared__ Unit list[S::kBatch];
   __shared__ int tmp[2 * WAVES];
   __shared__ uint32_t bad_tok[3];  // tokens of a masked unit whose values are not finite: at hand, next, cleared
@@ -226,11 +229,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void expanded_attend_kernel(
   const int g = static_cast<int>(blockIdx.x - b * heads), split = static_cast<int>(b - tile * splits);
   Tile t;
   if (!find_tile<kR>(a, static_cast<uint32_t>(tiles) - 1 - tile, 1, &t)) return;  // the latest rows see most: first
-  const ChunkList list_of = scan_list<kThreadsHere>(a, t.req, dyn, tmp);
+  const ChunkList list_of = scan_list<kThreadsHere, false>(a, t.req, dyn, tmp);
   const int ctx = list_of.tb[a.k];
   const int prefix = a.prefix_len ? __builtin_amdgcn_readfirstlane(min(max(a.prefix_len[t.req], 0), kFar)) : 0;
   const int my_row = t.r0 + min(32 * wave + col, t.rows - 1);
-  const bool works = 32 * wave < t.rows;
   const RowRule rule = row_rule(a, t, ctx, g, 1, my_row);
   const TileRule tr = tile_rule<kR>(a, t, ctx, g, 1);
   const Span span = visible_units(list_of, prefix, tr.lo, tr.hi);
@@ -254,6 +256,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void expanded_attend_kernel(
   Rows<32, D> rows;
   rows.clear();
   RowState st{-INFINITY, 0.f};
+  float rounded = 0.f;  // sum of the weights as the second product takes them
   bool poison = false;
 
   const int f = exchange(col);
@@ -263,7 +266,16 @@ __global__ __launch_bounds__(64 * WAVES, 2) void expanded_attend_kernel(
     const int i = lane & 15, r = 4 * half + (i >> 2), cc = 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
     value_at = r * S::kValuePitch + 8 * (cc ^ exchange(r)) + 4 * (i & 1);
   }
-  u32x4_t pk[kKeyLoads], pv[kValueLoads];
+  // a thread's 16-byte pieces of a unit: of the key rows, then of the value rows
+  u32x4_t p[kPieces];
+  int row_of[kPieces], place_of[kPieces];  // the piece's token, and where it goes in LDS
+#pragma unroll
+  for (int z = 0; z < kPieces; ++z) {
+    const bool is_v = z >= kKeyLoads;
+    const int at = tid + (is_v ? z - kKeyLoads : z) * kThreadsHere, chunks = is_v ? kValueChunks : kKeyChunks;
+    row_of[z] = at / chunks;
+    place_of[z] = row_of[z] * (is_v ? S::kValuePitch : S::kKeyPitch) + 8 * ((at % chunks) ^ exchange(row_of[z]));
+  }
 
   for (int last = u1 - 1; last >= u0; last -= S::kBatch) {
     __syncthreads();
@@ -272,129 +284,168 @@ __global__ __launch_bounds__(64 * WAVES, 2) void expanded_attend_kernel(
     if (n == 0) continue;
     if (tid < 2) bad_tok[tid] = 0;
     __syncthreads();
-    auto load = [&](const Unit& u) {  // (rows behind the last held token are the workspace's, and are not used)
-      const uint16_t* ks = my_keys + u.at * (kUnit * S::kKey);
-      const uint16_t* vs = my_values + u.at * (kUnit * D);
-#pragma unroll
-      for (int i = 0; i < kKeyLoads; ++i) {
-        const int at = tid + i * kThreadsHere;
-        pk[i] = *reinterpret_cast<const u32x4_t*>(ks + 8 * at);
-        if (at / kKeyChunks >= u.held()) pk[i] = u32x4_t{0, 0, 0, 0};
-      }
-#pragma unroll
-      for (int i = 0; i < kValueLoads; ++i) {
-        const int at = tid + i * kThreadsHere;
-        pv[i] = *reinterpret_cast<const u32x4_t*>(vs + 8 * at);
-        if (at / kValueChunks >= u.held()) pv[i] = u32x4_t{0, 0, 0, 0};
-      }
+    auto load = [&](const Unit& u, int z) {  // (what lies behind the last held token is cleared before it is used)
+      p[z] = z < kKeyLoads
+                 ? *reinterpret_cast<const u32x4_t*>(my_keys + u.at * (kUnit * S::kKey) + 8 * (tid + z * kThreadsHere))
+                 : *reinterpret_cast<const u32x4_t*>(my_values + u.at * (kUnit * D) +
+                                                     8 * (tid + (z - kKeyLoads) * kThreadsHere));
     };
-    auto check_bad = [&](int to) {  // values of a masked unit that are not finite are noted and left out
+    // tokens that a masked unit does not hold are cleared, values that are not finite are noted and left out
+    auto check = [&](const Unit& u, int to) {
 #pragma unroll
-      for (int i = 0; i < kValueLoads; ++i) {
+      for (int z = 0; z < kPieces; ++z) {
+        if (row_of[z] >= u.held()) p[z] = u32x4_t{0, 0, 0, 0};
+        if (z < kKeyLoads) continue;
         u16x2 most = {0, 0};
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, pv[i][j] & 0x7FFF7FFFu));
+          most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, p[z][j] & 0x7FFF7FFFu));
         if (most[0] >= 0x7F80u || most[1] >= 0x7F80u) {
-          atomicOr(&bad_tok[to], 1u << ((tid + i * kThreadsHere) / kValueChunks));
-          pv[i] = u32x4_t{0, 0, 0, 0};
+          atomicOr(&bad_tok[to], 1u << row_of[z]);
+          p[z] = u32x4_t{0, 0, 0, 0};
         }
       }
     };
-    auto store = [&](int buffer) {
+    // Piece z of the next unit, and the load of the same piece of the one after it.
+    auto advance = [&](int to, const Unit& from, int z) {
+      *reinterpret_cast<u32x4_t*>((z < kKeyLoads ? keys[to] : values[to]) + place_of[z]) = p[z];
+      load(from, z);
+    };
+    Unit u = uniform_unit(list[0]), next = uniform_unit(list[min(1, n - 1)]);
 #pragma unroll
-      for (int i = 0; i < kKeyLoads; ++i) {
-        const int at = tid + i * kThreadsHere, r = at / kKeyChunks, cc = at % kKeyChunks;
-        *reinterpret_cast<u32x4_t*>(keys[buffer] + r * S::kKeyPitch + 8 * (cc ^ exchange(r))) = pk[i];
-      }
+    for (int z = 0; z < kPieces; ++z) load(u, z);
+    if (u.masked()) check(u, 0);
 #pragma unroll
-      for (int i = 0; i < kValueLoads; ++i) {
-        const int at = tid + i * kThreadsHere, r = at / kValueChunks, cc = at % kValueChunks;
-        *reinterpret_cast<u32x4_t*>(values[buffer] + r * S::kValuePitch + 8 * (cc ^ exchange(r))) = pv[i];
+    for (int z = 0; z < kPieces; ++z) {
+      advance(0, next, z);
+      issue_first();
+    }
+    __syncthreads();
+    u32x4_t w[2];  // weights of the unit before
+    bool pending = false;
+    const uint16_t* value_src = nullptr;
+    auto value = [&](int o) {  // operand o: columns 32 (o / 2), tokens 16 (o % 2)
+      const uint16_t* src = value_src + 16 * (o & 1) * S::kValuePitch + 32 * (o >> 1);
+      const u32x2_t v0 = lds_transpose4(src), v1 = lds_transpose4(src + 8 * S::kValuePitch);
+      return as_bf16x8(u32x4_t{v0[0], v0[1], v1[0], v1[1]});
+    };
+    auto add_values = [&](auto share) {
+      constexpr int kAhead = 3;
+      bf16x8 v[kOps];
+#pragma unroll
+      for (int o = 0; o < kAhead; ++o) v[o] = value(o);
+      issue_first();
+#pragma unroll
+      for (int o = 0; o < kOps; ++o) {
+        if (o + kAhead < kOps) v[o + kAhead] = value(o + kAhead);
+        rows.o[o >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[o], as_bf16x8(w[o & 1]), rows.o[o >> 1], 0, 0, 0);
+        share(o);
+        issue_first();
       }
     };
-    Unit u = uniform_unit(list[0]);
-    load(u);
-    if (u.masked()) check_bad(0);
-    store(0);
-    Unit next = uniform_unit(list[min(1, n - 1)]);
-    load(next);
-    __syncthreads();
-    int slot = 0;  // i mod 3
+    int slot = 0;  // i mod 3: the unit's buffer, and its word of bad_tok
     for (int i = 0; i < n; ++i) {
-      const Unit after = list[min(i + 2, n - 1)];
-      const int slot1 = slot == 2 ? 0 : slot + 1;
-      if (tid == 0) bad_tok[slot == 0 ? 2 : slot - 1] = 0;
-      if (works) {
-        const uint16_t* kp = keys[i & 1];
-        const uint16_t* vp = values[i & 1];
-        f32x16 s;
+      const Unit after = uniform_unit(list[min(i + 2, n - 1)]);
+      const int slot1 = slot == 2 ? 0 : slot + 1, slot2 = slot == 0 ? 2 : slot - 1;
+      if (tid == 0) bad_tok[slot2] = 0;
+      if (i + 1 < n && next.masked()) check(next, slot1);
+      const uint16_t* kp = keys[slot];
+      value_src = values[slot2] + value_at;
+      f32x16 s;
 #pragma unroll
-        for (int j = 0; j < 16; ++j) s[j] = 0.f;
+      for (int j = 0; j < 16; ++j) s[j] = 0.f;
+      {
+        constexpr int kAhead = 3;
+        auto key = [&](int y) {
+          return *reinterpret_cast<const u32x4_t*>(kp + (y & 1 ? odd : even) + 32 * (y >> 1));
+        };
+        u32x4_t k[kSteps];
+#pragma unroll
+        for (int y = 0; y < kAhead; ++y) k[y] = key(y);
+        issue_first();
 #pragma unroll
         for (int y = 0; y < kSteps; ++y) {
-          const u32x4_t k = *reinterpret_cast<const u32x4_t*>(kp + (y & 1 ? odd : even) + 32 * (y >> 1));
-          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(k), q[y], s, 0, 0, 0);
-        }
-        if (u.masked()) {
-          const uint32_t seen = visible_tokens(rule, u, prefix);
-          mask_scores<32, 16>(s, seen, half);
-          poison |= (seen & bad_tok[slot]) != 0;
-        }
-        float top = s[0];
-#pragma unroll
-        for (int j = 1; j < 16; ++j) top = nan_max(top, s[j]);
-        const float high = max_column<32>(top) * c;
-        if (raise<32, D>(high, u.masked(), st, rows)) {
-          const float ref = finite_max(st.m);
-#pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            s[j] = fast_exp2(fmaf(s[j], c, -ref));
-            st.l += s[j];
-          }
-          u32x4_t w[2], rest[2];
-          pack_weights<16>(s, w);
-          auto add = [&](const u32x4_t (&v)[2]) {
-#pragma unroll
-            for (int n0 = 0; n0 < kBlocks; ++n0)
-#pragma unroll
-              for (int y = 0; y < 2; ++y) {
-                const uint16_t* src = vp + value_at + 16 * y * S::kValuePitch + 32 * n0;
-                const u32x2_t v0 = lds_transpose4(src), v1 = lds_transpose4(src + 8 * S::kValuePitch);
-                rows.o[n0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(u32x4_t{v0[0], v0[1], v1[0], v1[1]}),
-                                                                     as_bf16x8(v[y]), rows.o[n0], 0, 0, 0);
-              }
-          };
-          add(w);
-          if (is_heavy(high, st)) {
-            pack_rests<16>(s, w, rest);
-            add(rest);
-          }
+          if (y + kAhead < kSteps) k[y + kAhead] = key(y + kAhead);
+          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(k[y]), q[y], s, 0, 0, 0);
+          if (y * kPieces / kSteps != (y + 1) * kPieces / kSteps) advance(slot1, after, y * kPieces / kSteps);
+          issue_first();
         }
       }
-      if (i + 1 < n && next.masked()) check_bad(slot1);
-      store((i + 1) & 1);
+      if (u.masked()) {
+        const uint32_t seen = visible_tokens(rule, u, prefix);
+        mask_scores<32, 16>(s, seen, half);
+        poison |= (seen & bad_tok[slot]) != 0;
+      }
+      float top = s[0];
+#pragma unroll
+      for (int j = 1; j < 16; ++j) top = nan_max(top, s[j]);
+      const float high = max_column<32>(top) * c;
+      const bool counts = __any(!u.masked() || high != -INFINITY);
+      const bool up = counts && __any(high > st.m + kLag);
+      u32x4_t now[2];
+      auto weigh_score = [&](float ref, int j) {
+        s[j] = fast_exp2(fmaf(s[j], c, -ref));
+        st.l += s[j];
+        if (j & 1) {
+          const uint32_t pair = pack2(s[j - 1], s[j]);
+          now[j >> 3][(j >> 1) & 3] = pair;
+          rounded = add_pair(pair, rounded);
+        }
+      };
+      // The usual way: both in one.  (Two flags that the compiler does not know to be one: with an if and an else over
+      // the same accumulators it keeps them twice.)
+      const bool usual = pending && counts && !up;
+      int usual_too = __builtin_amdgcn_readfirstlane(usual);
+      asm volatile("" : "+s"(usual_too));
+      if (!usual) {
+        if (pending) add_values([](int) {});
+        if (up) {
+          const float mn = fmaxf(st.m, high);
+          const float r = mn == -INFINITY ? 1.f : fast_exp2(st.m - mn);
+          st.l *= r;
+          rounded *= r;
+          rows.scale(r);
+          st.m = mn;
+        }
+        if (counts) {
+          const float ref = finite_max(st.m);
+#pragma unroll
+          for (int j = 0; j < 16; ++j) weigh_score(ref, j);
+        }
+      }
+      if (usual_too) {
+        const float ref = finite_max(st.m);
+        add_values([&](int o) {
+#pragma unroll
+          for (int j = 16 * o / kOps; j < 16 * (o + 1) / kOps; ++j) weigh_score(ref, j);
+        });
+      }
+      pending = counts;
+      w[0] = now[0];
+      w[1] = now[1];
       u = next;
-      next = uniform_unit(after);
-      load(next);
+      next = after;
       slot = slot1;
       __syncthreads();
+    }
+    if (pending) {
+      value_src = values[slot == 0 ? 2 : slot - 1] + value_at;
+      add_values([](int) {});
     }
   }
 
   st.l = sum_column<32>(st.l);
+  rounded = sum_column<32>(rounded);
   poison = any_column<32>(poison, col);
   if (32 * wave + col >= t.rows) return;
-  AttendArgs to = a;
-  to.out = x.out;
-  if (poison) st.l = NAN;
-  write_rows<32, D>(to, rows, st, poison, tok_at * a.hq + h0 + g, half, split, splits, part_o, part_ml);
+  write_sums<32, D, D>(a, rows, st, rounded, poison, tok_at * a.hq + h0 + g, half, split, splits, 0, x.out, part_o,
+                       part_ml);
 }
 
 // ---------------------------------------------------------------- launches
 
 size_t align256(size_t b) { return (b + 255) & ~static_cast<size_t>(255); }
-size_t list_bytes(int k) { return (3 * static_cast<size_t>(k) + 2) * sizeof(int); }
+size_t list_bytes(int k) { return (2 * static_cast<size_t>(k) + 2) * sizeof(int); }
 
 struct ExpandedPlan {
   int waves;
