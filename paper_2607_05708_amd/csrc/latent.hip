@@ -201,21 +201,6 @@ struct LatentShape {
   static constexpr int kParked = L == 512 && RG == 4 ? 10 : 0;
 };
 
-// Scales rows whose registers are accumulation registers.  (The compiler would otherwise keep them, for the
-// multiplications' sake, where the matrix products cannot: of 32 x 512 it spills most.)
-template <int WIDTH, int D>
-__device__ __forceinline__ void scale_rows(Rows<WIDTH, D>& rows, float f) {
-#pragma unroll
-  for (int n = 0; n < D / WIDTH; ++n) {
-    auto x = rows.o[n];
-    asm volatile("" : "+a"(x));
-    auto y = x * f;
-    asm volatile("" : "+a"(y));
-    rows.o[n] = y;
-    if (WIDTH == 32 || n % 4 == 3) issue_first();
-  }
-}
-
 // Tiles of 32 RG rows: wave w has the 32 rows w / (4 / RG) of the tile and, of the second product, a share of the
 // columns; waves with the same rows make their scores each for itself.
 template <int FMT, int L, int RG>

@@ -8,6 +8,7 @@
 //
 // Row 32 u + j of a head's keys and values is token j of the request's unit u.
 #include <algorithm>
+#include <type_traits>
 
 #include "context.h"
 #include "kv.h"
@@ -193,6 +194,8 @@ __global__ __launch_bounds__(kThreads, 1) void latent_expand_kernel(LatentArgs x
 
 // ---------------------------------------------------------------- attention
 
+constexpr int kTileRows = 128;
+
 template <int D>
 struct ExpandedShape {
   static constexpr int kKey = D + kRopeDim;
@@ -200,27 +203,30 @@ struct ExpandedShape {
   static constexpr int kKeyPitch = kKey + 32, kValuePitch = D + 32;
 };
 
-// Tiles of 32 WAVES rows (new tokens) of a head.  Units go through a ring of three in LDS: while the waves make the
-// scores of unit i, they unpack unit i + 1 and load unit i + 2; the second product of unit i - 1 is written in groups of
-// one matrix instruction and a share of unit i's exponentials (a wave issues in order, so that only what stands between
-// its matrix products overlaps with them).
-template <int D, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, 2) void expanded_attend_kernel(
-    LatentArgs x, int splits, int64_t tiles, int64_t units, int h0, int heads, const uint16_t* __restrict__ key_rows,
-    const uint16_t* __restrict__ value_rows, float* __restrict__ part_o, RowState* __restrict__ part_ml) {
+// Tiles of 128 rows (new tokens) of a head, 32 a wave.  A step t makes the scores of unit t, the weights of unit t - 1
+// and the second product of unit t - 2, and unpacks unit t + 1: a wave issues in order, so that only what stands between
+// its matrix products overlaps with them, and the exponentials are shared out over all of a step's.  They go by the
+// running maximum as it is; where a score turns out to be above it by more than the lag (rare: the largest score of a
+// unit is known at the end of its step), that unit's are made again.
+template <int D>
+__global__ __launch_bounds__(kThreads, 2) void expanded_attend_kernel(LatentArgs x, int splits, int64_t tiles,
+                                                                   int64_t units, int h0, int heads,
+                                                                   const uint16_t* __restrict__ key_rows,
+                                                                   const uint16_t* __restrict__ value_rows,
+                                                                   float* __restrict__ part_o,
+                                                                   RowState* __restrict__ part_ml) {
   using S = ExpandedShape<D>;
-  constexpr int kThreadsHere = 64 * WAVES, kR = 32 * WAVES;
   constexpr int kSteps = S::kKey / 16, kBlocks = D / 32, kOps = 2 * kBlocks;
   constexpr int kKeyChunks = S::kKey / 8, kValueChunks = D / 8;              // 16-byte chunks of a row
-  constexpr int kKeyLoads = kUnit * kKeyChunks / kThreadsHere, kValueLoads = kUnit * kValueChunks / kThreadsHere;
+  constexpr int kKeyLoads = kUnit * kKeyChunks / kThreads, kValueLoads = kUnit * kValueChunks / kThreads;
   constexpr int kPieces = kKeyLoads + kValueLoads;
-  static_assert(kUnit * kKeyChunks % kThreadsHere == 0 && kUnit * kValueChunks % kThreadsHere == 0, "whole loads");
+  static_assert(kUnit * kKeyChunks % kThreads == 0 && kUnit * kValueChunks % kThreads == 0, "whole loads");
   extern __shared__ int dyn[];  // of the chunk list: ub[k + 1], tb[k + 1]
-  __shared__ __align__(16) uint16_t keys[3][kUnit * S::kKeyPitch];
-  __shared__ __align__(16) uint16_t values[3][kUnit * S::kValuePitch];
+  __shared__ __align__(16) uint16_t keys[2][kUnit * S::kKeyPitch];
+  __shared__ __align__(16) uint16_t values[4][kUnit * S::kValuePitch];
   __shared__ Unit list[S::kBatch];
-  __shared__ int tmp[2 * WAVES];
-  __shared__ uint32_t bad_tok[3];  // tokens of a masked unit whose values are not finite: at hand, next, cleared
+  __shared__ int tmp[2 * kWaves];
+  __shared__ uint32_t bad_tok[4];  // tokens of a masked unit whose values are not finite
 
   const AttendArgs& a = x.a;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -228,13 +234,13 @@ __global__ __launch_bounds__(64 * WAVES, 2) void expanded_attend_kernel(
   const uint32_t b = blockIdx.x / static_cast<uint32_t>(heads), tile = b / static_cast<uint32_t>(splits);
   const int g = static_cast<int>(blockIdx.x - b * heads), split = static_cast<int>(b - tile * splits);
   Tile t;
-  if (!find_tile<kR>(a, static_cast<uint32_t>(tiles) - 1 - tile, 1, &t)) return;  // the latest rows see most: first
-  const ChunkList list_of = scan_list<kThreadsHere, false>(a, t.req, dyn, tmp);
+  if (!find_tile<kTileRows>(a, static_cast<uint32_t>(tiles) - 1 - tile, 1, &t)) return;  // the latest rows see most: first
+  const ChunkList list_of = scan_list<kThreads, false>(a, t.req, dyn, tmp);
   const int ctx = list_of.tb[a.k];
   const int prefix = a.prefix_len ? __builtin_amdgcn_readfirstlane(min(max(a.prefix_len[t.req], 0), kFar)) : 0;
   const int my_row = t.r0 + min(32 * wave + col, t.rows - 1);
   const RowRule rule = row_rule(a, t, ctx, g, 1, my_row);
-  const TileRule tr = tile_rule<kR>(a, t, ctx, g, 1);
+  const TileRule tr = tile_rule<kTileRows>(a, t, ctx, g, 1);
   const Span span = visible_units(list_of, prefix, tr.lo, tr.hi);
   const int n_units = __builtin_amdgcn_readfirstlane(span.count());
   const int u0 = static_cast<int>(static_cast<int64_t>(n_units) * split / splits);
@@ -250,9 +256,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void expanded_attend_kernel(
     for (int i = 0; i < kSteps; ++i) q[i] = i < D / 16 ? own[i < D / 16 ? i : 0] : turned[i < D / 16 ? 0 : i - D / 16];
   }
   const float c = a.scale * kLog2e;
-  const int64_t slots = a.m * units * kUnit;
-  const uint16_t* my_keys = key_rows + (g * slots + t.req * units * kUnit) * S::kKey;
-  const uint16_t* my_values = value_rows + (g * slots + t.req * units * kUnit) * D;
+  const int64_t row0 = (g * a.m + __builtin_amdgcn_readfirstlane(t.req)) * units * kUnit;
+  const uint8_t* my_keys = reinterpret_cast<const uint8_t*>(key_rows + row0 * S::kKey);
+  const uint8_t* my_values = reinterpret_cast<const uint8_t*>(value_rows + row0 * D);
   Rows<32, D> rows;
   rows.clear();
   RowState st{-INFINITY, 0.f};
@@ -272,23 +278,26 @@ __global__ __launch_bounds__(64 * WAVES, 2) void expanded_attend_kernel(
 #pragma unroll
   for (int z = 0; z < kPieces; ++z) {
     const bool is_v = z >= kKeyLoads;
-    const int at = tid + (is_v ? z - kKeyLoads : z) * kThreadsHere, chunks = is_v ? kValueChunks : kKeyChunks;
+    const int at = tid + (is_v ? z - kKeyLoads : z) * kThreads, chunks = is_v ? kValueChunks : kKeyChunks;
     row_of[z] = at / chunks;
     place_of[z] = row_of[z] * (is_v ? S::kValuePitch : S::kKeyPitch) + 8 * ((at % chunks) ^ exchange(row_of[z]));
   }
 
   for (int last = u1 - 1; last >= u0; last -= S::kBatch) {
     __syncthreads();
-    const int n = resolve_units<S::kBatch, kThreadsHere, true>(a, list_of, span, tr, prefix, 0, 0, last,
-                                                             min(S::kBatch, last - u0 + 1), list, tmp);
+    const int n = resolve_units<S::kBatch, kThreads, true>(a, list_of, span, tr, prefix, 0, 0, last,
+                                                         min(S::kBatch, last - u0 + 1), list, tmp);
     if (n == 0) continue;
-    if (tid < 2) bad_tok[tid] = 0;
+    if (tid < 4) bad_tok[tid] = 0;
+    // the first two steps' second products are of weights 0: their values have to be numbers
+    for (int z = tid; z < 2 * kUnit * S::kValuePitch / 8; z += kThreads)
+      reinterpret_cast<u32x4_t*>(values[2])[z] = u32x4_t{0, 0, 0, 0};
     __syncthreads();
+    const uint32_t mine = 16u * tid;
     auto load = [&](const Unit& u, int z) {  // (what lies behind the last held token is cleared before it is used)
-      p[z] = z < kKeyLoads
-                 ? *reinterpret_cast<const u32x4_t*>(my_keys + u.at * (kUnit * S::kKey) + 8 * (tid + z * kThreadsHere))
-                 : *reinterpret_cast<const u32x4_t*>(my_values + u.at * (kUnit * D) +
-                                                     8 * (tid + (z - kKeyLoads) * kThreadsHere));
+      const uint8_t* src = z < kKeyLoads ? my_keys + u.at * (kUnit * S::kKey * 2) + z * (16 * kThreads)
+                                         : my_values + u.at * (kUnit * D * 2) + (z - kKeyLoads) * (16 * kThreads);
+      p[z] = *reinterpret_cast<const u32x4_t*>(src + mine);
     };
     // tokens that a masked unit does not hold are cleared, values that are not finite are noted and left out
     auto check = [&](const Unit& u, int to) {
@@ -308,10 +317,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void expanded_attend_kernel(
     };
     // Piece z of the next unit, and the load of the same piece of the one after it.
     auto advance = [&](int to, const Unit& from, int z) {
-      *reinterpret_cast<u32x4_t*>((z < kKeyLoads ? keys[to] : values[to]) + place_of[z]) = p[z];
+      *reinterpret_cast<u32x4_t*>((z < kKeyLoads ? keys[to & 1] : values[to & 3]) + place_of[z]) = p[z];
       load(from, z);
     };
-    Unit u = uniform_unit(list[0]), next = uniform_unit(list[min(1, n - 1)]);
+    Unit u = uniform_unit(list[0]), next = uniform_unit(list[min(1, n - 1)]), old = u;
 #pragma unroll
     for (int z = 0; z < kPieces; ++z) load(u, z);
     if (u.masked()) check(u, 0);
@@ -321,39 +330,46 @@ __global__ __launch_bounds__(64 * WAVES, 2) void expanded_attend_kernel(
       issue_first();
     }
     __syncthreads();
-    u32x4_t w[2];  // weights of the unit before
-    bool pending = false;
-    const uint16_t* value_src = nullptr;
-    auto value = [&](int o) {  // operand o: columns 32 (o / 2), tokens 16 (o % 2)
-      const uint16_t* src = value_src + 16 * (o & 1) * S::kValuePitch + 32 * (o >> 1);
-      const u32x2_t v0 = lds_transpose4(src), v1 = lds_transpose4(src + 8 * S::kValuePitch);
-      return as_bf16x8(u32x4_t{v0[0], v0[1], v1[0], v1[1]});
-    };
-    auto add_values = [&](auto share) {
-      constexpr int kAhead = 3;
-      bf16x8 v[kOps];
+    // Scores of units t and t - 1, weights of units t - 1 and t - 2: [t & 1] is made in step t.
+    f32x16 s[2];
+    u32x4_t w[2][2];
 #pragma unroll
-      for (int o = 0; o < kAhead; ++o) v[o] = value(o);
-      issue_first();
-#pragma unroll
-      for (int o = 0; o < kOps; ++o) {
-        if (o + kAhead < kOps) v[o + kAhead] = value(o + kAhead);
-        rows.o[o >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[o], as_bf16x8(w[o & 1]), rows.o[o >> 1], 0, 0, 0);
-        share(o);
-        issue_first();
-      }
-    };
-    int slot = 0;  // i mod 3: the unit's buffer, and its word of bad_tok
-    for (int i = 0; i < n; ++i) {
+    for (int j = 0; j < 16; ++j) s[1][j] = -INFINITY;
+    w[1][0] = w[1][1] = u32x4_t{0, 0, 0, 0};
+
+    auto step = [&](auto parity, int i) {
+      constexpr int kNew = decltype(parity)::value, kOld = 1 - kNew;
+      f32x16 &sn = s[kNew], &so = s[kOld];
+      const u32x4_t(&wo)[2] = w[kOld];
+      u32x4_t(&wn)[2] = w[kNew];
       const Unit after = uniform_unit(list[min(i + 2, n - 1)]);
-      const int slot1 = slot == 2 ? 0 : slot + 1, slot2 = slot == 0 ? 2 : slot - 1;
-      if (tid == 0) bad_tok[slot2] = 0;
-      if (i + 1 < n && next.masked()) check(next, slot1);
-      const uint16_t* kp = keys[slot];
-      value_src = values[slot2] + value_at;
-      f32x16 s;
+      if (tid == 0) bad_tok[(i + 2) & 3] = 0;
+      if (i + 1 < n && next.masked()) check(next, (i + 1) & 3);
+      if (i > 0 && i <= n && old.masked()) {
+        const uint32_t seen = visible_tokens(rule, old, prefix);
+        mask_scores<32, 16>(so, seen, half);
+        poison |= (seen & bad_tok[(i + 3) & 3]) != 0;
+      }
+      const uint16_t* kp = keys[i & 1];
+      const uint16_t* vp = values[(i + 2) & 3] + value_at;
+      float ref = finite_max(st.m), l = 0.f, lr = 0.f, top = so[0], e[2];
+      auto weigh = [&](int j) {  // scores 2 j and 2 j + 1 of unit t - 1
 #pragma unroll
-      for (int j = 0; j < 16; ++j) s[j] = 0.f;
+        for (int y = 0; y < 2; ++y) {
+          e[y] = fast_exp2(fmaf(so[2 * j + y], c, -ref));
+          l += e[y];
+        }
+        const uint32_t pair = pack2(e[0], e[1]);
+        wn[j >> 2][j & 3] = pair;
+        lr = add_pair(pair, lr);
+      };
+      constexpr int kSlots = kSteps + kOps;
+      auto share = [&](int slot) {
+#pragma unroll
+        for (int j = 8 * slot / kSlots; j < 8 * (slot + 1) / kSlots; ++j) weigh(j);
+      };
+#pragma unroll
+      for (int j = 0; j < 16; ++j) sn[j] = 0.f;
       {
         constexpr int kAhead = 3;
         auto key = [&](int y) {
@@ -366,71 +382,61 @@ __global__ __launch_bounds__(64 * WAVES, 2) void expanded_attend_kernel(
 #pragma unroll
         for (int y = 0; y < kSteps; ++y) {
           if (y + kAhead < kSteps) k[y + kAhead] = key(y + kAhead);
-          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(k[y]), q[y], s, 0, 0, 0);
-          if (y * kPieces / kSteps != (y + 1) * kPieces / kSteps) advance(slot1, after, y * kPieces / kSteps);
+          sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(k[y]), q[y], sn, 0, 0, 0);
+          if (y * kPieces / kSteps != (y + 1) * kPieces / kSteps) advance(i + 1, after, y * kPieces / kSteps);
+#pragma unroll
+          for (int j = 16 * y / kSteps; j < 16 * (y + 1) / kSteps; ++j) top = nan_max(top, so[j]);
+          share(y);
           issue_first();
         }
       }
-      if (u.masked()) {
-        const uint32_t seen = visible_tokens(rule, u, prefix);
-        mask_scores<32, 16>(s, seen, half);
-        poison |= (seen & bad_tok[slot]) != 0;
-      }
-      float top = s[0];
+      {  // the second product of unit t - 2: operand o has columns 32 (o / 2), tokens 16 (o % 2)
+        constexpr int kAhead = 3;
+        auto value = [&](int o) {
+          const uint16_t* src = vp + 16 * (o & 1) * S::kValuePitch + 32 * (o >> 1);
+          const u32x2_t v0 = lds_transpose4(src), v1 = lds_transpose4(src + 8 * S::kValuePitch);
+          return as_bf16x8(u32x4_t{v0[0], v0[1], v1[0], v1[1]});
+        };
+        bf16x8 v[kOps];
 #pragma unroll
-      for (int j = 1; j < 16; ++j) top = nan_max(top, s[j]);
+        for (int o = 0; o < kAhead; ++o) v[o] = value(o);
+        issue_first();
+#pragma unroll
+        for (int o = 0; o < kOps; ++o) {
+          if (o + kAhead < kOps) v[o + kAhead] = value(o + kAhead);
+          rows.o[o >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[o], as_bf16x8(wo[o & 1]), rows.o[o >> 1], 0, 0, 0);
+          share(kSteps + o);
+          issue_first();
+        }
+      }
       const float high = max_column<32>(top) * c;
-      const bool counts = __any(!u.masked() || high != -INFINITY);
-      const bool up = counts && __any(high > st.m + kLag);
-      u32x4_t now[2];
-      auto weigh_score = [&](float ref, int j) {
-        s[j] = fast_exp2(fmaf(s[j], c, -ref));
-        st.l += s[j];
-        if (j & 1) {
-          const uint32_t pair = pack2(s[j - 1], s[j]);
-          now[j >> 3][(j >> 1) & 3] = pair;
-          rounded = add_pair(pair, rounded);
-        }
-      };
-      // The usual way: both in one.  (Two flags that the compiler does not know to be one: with an if and an else over
-      // the same accumulators it keeps them twice.)
-      const bool usual = pending && counts && !up;
-      int usual_too = __builtin_amdgcn_readfirstlane(usual);
-      asm volatile("" : "+s"(usual_too));
-      if (!usual) {
-        if (pending) add_values([](int) {});
-        if (up) {
-          const float mn = fmaxf(st.m, high);
-          const float r = mn == -INFINITY ? 1.f : fast_exp2(st.m - mn);
-          st.l *= r;
-          rounded *= r;
-          rows.scale(r);
-          st.m = mn;
-        }
-        if (counts) {
-          const float ref = finite_max(st.m);
+      if (__any(high > st.m + kLag)) {
+        const float mn = fmaxf(st.m, high);
+        const float by = mn == -INFINITY ? 1.f : fast_exp2(st.m - mn);
+        st.l *= by;
+        rounded *= by;
+        rows.scale(by);
+        st.m = mn;
+        ref = finite_max(mn);
+        l = lr = 0.f;
 #pragma unroll
-          for (int j = 0; j < 16; ++j) weigh_score(ref, j);
-        }
+        for (int j = 0; j < 8; ++j) weigh(j);
       }
-      if (usual_too) {
-        const float ref = finite_max(st.m);
-        add_values([&](int o) {
+      st.l += l;
+      rounded += lr;
+      if (i >= n) {  // what follows the last unit weighs nothing
 #pragma unroll
-          for (int j = 16 * o / kOps; j < 16 * (o + 1) / kOps; ++j) weigh_score(ref, j);
-        });
+        for (int j = 0; j < 16; ++j) sn[j] = -INFINITY;
       }
-      pending = counts;
-      w[0] = now[0];
-      w[1] = now[1];
+      old = u;
       u = next;
       next = after;
-      slot = slot1;
       __syncthreads();
-    }
-    if (pending) {
-      value_src = values[slot == 0 ? 2 : slot - 1] + value_at;
-      add_values([](int) {});
+    };
+    // Steps n and n + 1 only finish the last units.
+    for (int i = 0; i < n + 2; i += 2) {
+      step(std::integral_constant<int, 0>{}, i);
+      if (i + 1 < n + 2) step(std::integral_constant<int, 1>{}, i + 1);
     }
   }
 
@@ -448,7 +454,6 @@ size_t align256(size_t b) { return (b + 255) & ~static_cast<size_t>(255); }
 size_t list_bytes(int k) { return (2 * static_cast<size_t>(k) + 2) * sizeof(int); }
 
 struct ExpandedPlan {
-  int waves;
   int64_t tiles;
   int splits;
   int heads;  // at a time
@@ -463,8 +468,7 @@ size_t head_bytes(const LatentSizes& s) {
 
 ExpandedPlan expanded_plan(const LatentSizes& s, bool ragged) {
   ExpandedPlan p;
-  p.waves = 4;
-  const int R = 32 * p.waves;
+  const int R = kTileRows;
   p.tiles = ragged ? s.total_q / R + s.m : s.m * ((s.total_q / s.m + R - 1) / R);
   p.heads = static_cast<int>(std::min<size_t>(std::max<size_t>(kExpandBytes / head_bytes(s), 1), s.heads));
   const int64_t filled = ragged ? (s.total_q + R - 1) / R + s.m / 2 : p.tiles, work = filled * p.heads, slots = 512;
@@ -524,8 +528,8 @@ hipError_t launch(const LatentArgs& x, const LatentSizes& s, hipStream_t stream)
     latent_expand_kernel<FMT, L, D><<<dim3(static_cast<unsigned>(groups), (heads + per - 1) / per), kThreads, 0,
                                       stream>>>(x, s.units, sources, counts, h0, heads, per, keys, values);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    expanded_attend_kernel<D, 4><<<static_cast<unsigned>(p.tiles * heads * p.splits), 256, list_bytes(s.k), stream>>>(
-        x, p.splits, p.tiles, s.units, h0, heads, keys, values, part_o, part_ml);
+    expanded_attend_kernel<D><<<static_cast<unsigned>(p.tiles * heads * p.splits), kThreads, list_bytes(s.k),
+                                stream>>>(x, p.splits, p.tiles, s.units, h0, heads, keys, values, part_o, part_ml);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   }
   if (p.splits > 1) {

@@ -24,6 +24,21 @@ __device__ __forceinline__ float add_pair(uint32_t pair, float x) {
   return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(s16x2, pair), __builtin_bit_cast(s16x2, kOnes), x, false);
 }
 
+// Scales rows whose registers are accumulation registers.  (The compiler would otherwise keep them, for the
+// multiplications' sake, where the matrix products cannot: of 32 x 512 it spills most.)
+template <int WIDTH, int D>
+__device__ __forceinline__ void scale_rows(Rows<WIDTH, D>& rows, float f) {
+#pragma unroll
+  for (int n = 0; n < D / WIDTH; ++n) {
+    auto x = rows.o[n];
+    asm volatile("" : "+a"(x));
+    auto y = x * f;
+    asm volatile("" : "+a"(y));
+    rows.o[n] = y;
+    if (WIDTH == 32 || n % 4 == 3) issue_first();
+  }
+}
+
 // Write elements first .. + N - 1 of a row's weighted sum (of L), or of its part of a split context.  `rounded`
 // is the sum of the weights as the product took them, and what it is divided by, so that their roundings cancel where a
 // few weigh most; the join divides by l.
