@@ -137,13 +137,9 @@ __global__ __launch_bounds__(kThreads) void latent_query_kernel(LatentArgs x, in
   // transposed operands: columns 32 wave .. of W_h, rows 16 y + 4 half + 0..3 and + 8
   bf16x8 a[D / 16];
   {
-    const int i = lane & 15, r = 4 * half + (i >> 2), c = 4 * wave + 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
-    const uint16_t* src = wk + r * kPitch + 8 * (c ^ exchange(r)) + 4 * (i & 1);
+    const Transposed<kPitch> columns(lane);
 #pragma unroll
-    for (int y = 0; y < D / 16; ++y) {
-      const u32x2_t v0 = lds_transpose4(src + 16 * y * kPitch), v1 = lds_transpose4(src + (16 * y + 8) * kPitch);
-      a[y] = as_bf16x8(u32x4_t{v0[0], v0[1], v1[0], v1[1]});
-    }
+    for (int y = 0; y < D / 16; ++y) a[y] = columns(wk + 16 * y * kPitch + 32 * wave);
   }
   for (int b = 0; b < blocks; ++b) {
     const int64_t tok = tok0 + b * kTokenBlock + col;
@@ -267,11 +263,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attend_kernel(LatentArgs x
   const int tok = tid >> 3, part = tid & 7, exchanged = exchange(tok);  // the part of a row that this thread unpacks
   const int key_at = col * kPitch, f = exchange(col);
   const int even = key_at + 8 * (half ^ f), odd = key_at + 8 * ((2 + half) ^ f);  // chunks 0 and 2 (+ half) of a row
-  int value_at;  // transposed operands: rows 4 half + .. of the unit, 16 columns
-  {
-    const int i = lane & 15, r = 4 * half + (i >> 2), cc = 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
-    value_at = r * kPitch + 8 * (cc ^ exchange(r)) + 4 * (i & 1) + cg * kColumns;
-  }
+  const Transposed<kPitch> columns(lane);
   P p;
 
   for (int last = u1 - 1; last >= u0; last -= S::kBatch) {
@@ -353,9 +345,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attend_kernel(LatentArgs x
     bool pending = false;
     const uint16_t* values = nullptr;  // its rows
     auto value = [&](int x) {          // operand x: columns 32 (x / 2), tokens 16 (x % 2)
-      const uint16_t* src = values + 16 * (x & 1) * kPitch + 32 * (x >> 1);
-      const u32x2_t v0 = lds_transpose4(src), v1 = lds_transpose4(src + 8 * kPitch);
-      return as_bf16x8(u32x4_t{v0[0], v0[1], v1[0], v1[1]});
+      return columns(values + 16 * (x & 1) * kPitch + 32 * (x >> 1));
     };
     constexpr int kOps = 2 * kBlocks;
     auto add_values = [&](auto share) {
@@ -389,7 +379,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attend_kernel(LatentArgs x
       // of the units ahead from register to register, which waits for them)
       {
         const uint16_t* keys = unit_rows[slot];
-        values = unit_rows[slot2] + value_at;
+        values = unit_rows[slot2] + cg * kColumns;
         f32x16 s;
 #pragma unroll
         for (int j = 0; j < 16; ++j) s[j] = 0.f;
@@ -476,7 +466,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attend_kernel(LatentArgs x
       __syncthreads();
     }
     if (pending) {
-      values = unit_rows[slot == 0 ? 2 : slot - 1] + value_at;
+      values = unit_rows[slot == 0 ? 2 : slot - 1] + cg * kColumns;
       add_values([](int) {});
     }
   }

@@ -6,7 +6,8 @@
 //   expanded_attend_kernel  attention over them, head by head
 //   attend_join_kernel      joins the parts of split contexts
 //
-// Row 32 u + j of a head's keys and values is token j of the request's unit u.
+// Of a head, a unit's keys (or values) are one block [element / 8][token][element % 8]: the 16 bytes that a lane of a
+// matrix product has of a token lie next to its neighbours', so that blocks are written and read in whole lines.
 #include <algorithm>
 #include <type_traits>
 
@@ -125,21 +126,32 @@ __global__ __launch_bounds__(kThreads, 1) void latent_expand_kernel(LatentArgs x
     *reinterpret_cast<u32x4_t*>(rows + t * kPitch + 8 * (c ^ exchange(t))) = v;
   }
   for (int i = tid; i < kGroupTokens * 8; i += kThreads) {
-    const int t = i / 8, c = i % 8, u = u0 + t / kUnit;
+    const int t = i % kUnit, c = i / kUnit % 8, k = i / (8 * kUnit), u = u0 + k;
     if (u >= n) break;
     const Source s = sources[req * units + u];
-    if (s.at < 0 || t % kUnit >= s.held) continue;
-    const int row = s.row + t % kUnit;
+    if (s.at < 0 || t >= s.held) continue;
+    const int row = s.row + t;
     const u32x4_t v = *reinterpret_cast<const u32x4_t*>(a.kv.pool + (s.at - static_cast<int64_t>(s.row) * kRow) +
                                                         T * kRow + static_cast<int64_t>(row) * 2 * kRopeDim + 16 * c);
     for (int h = hb; h < he; ++h)
-      *reinterpret_cast<u32x4_t*>(keys + (h * slots + slot0 + t) * kKeyRow + D + 8 * c) = v;
+      *reinterpret_cast<u32x4_t*>(keys + (h * slots + slot0 + k * kUnit) * kKeyRow + ((D / 8 + c) * kUnit + t) * 8) = v;
   }
   __syncthreads();
 
   const int f = exchange(col);
+  // W and V: a wave's rows, 128 elements a step, each loaded again for the next step (maybe of the next head) as soon as
+  // it has been used.
+  constexpr int kStep = 128, kHeadSteps = L / kStep;
+  u32x4_t w[kBlocks][8];
+  auto load = [&](int h, int s, int b, int y) {
+    const uint16_t* src = x.w + (h0 + h) * x.w_hs + (wave * kMine + 32 * b + col) * x.w_rs + 32 * half + kStep * s;
+    w[b][y] = *reinterpret_cast<const u32x4_t*>(src + 64 * (y >> 2) + 8 * (y & 3));
+  };
+#pragma unroll
+  for (int y = 0; y < 8; ++y)
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b) load(hb, 0, b, y);
   for (int h = hb; h < he; ++h) {
-    const uint16_t* w = x.w + (h0 + h) * x.w_hs + (wave * kMine + col) * x.w_rs + 32 * half;
     f32x16 o[kBlocks][kGroupUnits];
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b)
@@ -147,38 +159,38 @@ __global__ __launch_bounds__(kThreads, 1) void latent_expand_kernel(LatentArgs x
       for (int u = 0; u < kGroupUnits; ++u)
 #pragma unroll
         for (int j = 0; j < 16; ++j) o[b][u][j] = 0.f;
-    u32x4_t next[kBlocks][4];
+#pragma unroll 1
+    for (int s = 0; s < kHeadSteps; ++s) {
+      const bool last = s + 1 == kHeadSteps;
+      const int next_h = last ? min(h + 1, he - 1) : h, next_s = last ? 0 : s + 1;
+      const uint16_t* src = rows + col * kPitch + kStep * s + 32 * half;
+      auto token = [&](int i) {  // operand of y = i / 4 and unit i % 4
+        const int y = i / kGroupUnits, u = i % kGroupUnits;
+        return as_bf16x8(*reinterpret_cast<const u32x4_t*>(src + 32 * u * kPitch + 64 * (y >> 2) + 8 * ((y & 3) ^ f)));
+      };
+      constexpr int kAhead = 4, kAll = 8 * kGroupUnits;
+      bf16x8 k[kAll];
 #pragma unroll
-    for (int b = 0; b < kBlocks; ++b)
+      for (int i = 0; i < kAhead; ++i) k[i] = token(i);
+      issue_first();
 #pragma unroll
-      for (int y = 0; y < 4; ++y) next[b][y] = *reinterpret_cast<const u32x4_t*>(w + 32 * b * x.w_rs + 8 * y);
-#pragma unroll 2
-    for (int s = 0; s < L / 64; ++s) {
-      u32x4_t cur[kBlocks][4];
+      for (int i = 0; i < kAll; ++i) {
+        const int y = i / kGroupUnits, u = i % kGroupUnits;
+        if (i + kAhead < kAll) k[i + kAhead] = token(i + kAhead);
 #pragma unroll
-      for (int b = 0; b < kBlocks; ++b)
+        for (int b = 0; b < kBlocks; ++b)
+          o[b][u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(w[b][y]), k[i], o[b][u], 0, 0, 0);
+        if (u + 1 == kGroupUnits) {
 #pragma unroll
-        for (int y = 0; y < 4; ++y) {
-          cur[b][y] = next[b][y];
-          if (s + 1 < L / 64)
-            next[b][y] = *reinterpret_cast<const u32x4_t*>(w + 32 * b * x.w_rs + 64 * (s + 1) + 8 * y);
+          for (int b = 0; b < kBlocks; ++b) load(next_h, next_s, b, y);
         }
-#pragma unroll
-      for (int y = 0; y < 4; ++y) {
-#pragma unroll
-        for (int u = 0; u < kGroupUnits; ++u) {
-          const bf16x8 k = as_bf16x8(*reinterpret_cast<const u32x4_t*>(
-              rows + (32 * u + col) * kPitch + 64 * s + 32 * half + 8 * (y ^ f)));
-#pragma unroll
-          for (int b = 0; b < kBlocks; ++b)
-            o[b][u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(cur[b][y]), k, o[b][u], 0, 0, 0);
-        }
+        issue_first();
       }
     }
     const bool is_v = wave * kMine >= D;
-    uint16_t* dst = is_v ? values + (h * slots + slot0 + col) * D + wave * kMine - D
-                         : keys + (h * slots + slot0 + col) * kKeyRow + wave * kMine;
-    const int pitch = is_v ? D : kKeyRow;
+    uint16_t* dst = is_v ? values + (h * slots + slot0) * D + (wave * kMine - D) * kUnit
+                         : keys + (h * slots + slot0) * kKeyRow + wave * kMine * kUnit;
+    const int block = (is_v ? D : kKeyRow) * kUnit;
 #pragma unroll
     for (int u = 0; u < kGroupUnits; ++u) {
       if (u0 + u >= n) break;
@@ -186,7 +198,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_expand_kernel(LatentArgs x
       for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
         for (int y = 0; y < 4; ++y)
-          *reinterpret_cast<u32x2_t*>(dst + 32 * u * pitch + 32 * b + 8 * y + 4 * half) =
+          *reinterpret_cast<u32x2_t*>(dst + u * block + ((4 * b + y) * kUnit + col) * 8 + 4 * half) =
               u32x2_t{pack2(o[b][u][4 * y], o[b][u][4 * y + 1]), pack2(o[b][u][4 * y + 2], o[b][u][4 * y + 3])};
     }
   }
@@ -267,20 +279,16 @@ __global__ __launch_bounds__(kThreads, 2) void expanded_attend_kernel(LatentArgs
 
   const int f = exchange(col);
   const int even = col * S::kKeyPitch + 8 * (half ^ f), odd = col * S::kKeyPitch + 8 * ((2 + half) ^ f);
-  int value_at;
-  {
-    const int i = lane & 15, r = 4 * half + (i >> 2), cc = 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
-    value_at = r * S::kValuePitch + 8 * (cc ^ exchange(r)) + 4 * (i & 1);
-  }
+  const Transposed<S::kValuePitch> columns(lane);
   // a thread's 16-byte pieces of a unit: of the key rows, then of the value rows
   u32x4_t p[kPieces];
   int row_of[kPieces], place_of[kPieces];  // the piece's token, and where it goes in LDS
 #pragma unroll
   for (int z = 0; z < kPieces; ++z) {
     const bool is_v = z >= kKeyLoads;
-    const int at = tid + (is_v ? z - kKeyLoads : z) * kThreads, chunks = is_v ? kValueChunks : kKeyChunks;
-    row_of[z] = at / chunks;
-    place_of[z] = row_of[z] * (is_v ? S::kValuePitch : S::kKeyPitch) + 8 * ((at % chunks) ^ exchange(row_of[z]));
+    const int at = tid + (is_v ? z - kKeyLoads : z) * kThreads;
+    row_of[z] = at % kUnit;
+    place_of[z] = row_of[z] * (is_v ? S::kValuePitch : S::kKeyPitch) + 8 * ((at / kUnit) ^ exchange(row_of[z]));
   }
 
   for (int last = u1 - 1; last >= u0; last -= S::kBatch) {
@@ -351,7 +359,7 @@ __global__ __launch_bounds__(kThreads, 2) void expanded_attend_kernel(LatentArgs
         poison |= (seen & bad_tok[(i + 3) & 3]) != 0;
       }
       const uint16_t* kp = keys[i & 1];
-      const uint16_t* vp = values[(i + 2) & 3] + value_at;
+      const uint16_t* vp = values[(i + 2) & 3];
       float ref = finite_max(st.m), l = 0.f, lr = 0.f, top = so[0], e[2];
       auto weigh = [&](int j) {  // scores 2 j and 2 j + 1 of unit t - 1
 #pragma unroll
@@ -392,11 +400,7 @@ __global__ __launch_bounds__(kThreads, 2) void expanded_attend_kernel(LatentArgs
       }
       {  // the second product of unit t - 2: operand o has columns 32 (o / 2), tokens 16 (o % 2)
         constexpr int kAhead = 3;
-        auto value = [&](int o) {
-          const uint16_t* src = vp + 16 * (o & 1) * S::kValuePitch + 32 * (o >> 1);
-          const u32x2_t v0 = lds_transpose4(src), v1 = lds_transpose4(src + 8 * S::kValuePitch);
-          return as_bf16x8(u32x4_t{v0[0], v0[1], v1[0], v1[1]});
-        };
+        auto value = [&](int o) { return columns(vp + 16 * (o & 1) * S::kValuePitch + 32 * (o >> 1)); };
         bf16x8 v[kOps];
 #pragma unroll
         for (int o = 0; o < kAhead; ++o) v[o] = value(o);

@@ -10,13 +10,33 @@ namespace memattn {
 
 namespace {
 
-// Rows of L latent elements and the key part in LDS, bf16.  The pitch is an odd multiple of 64 bytes, and the 16-byte
-// chunks of a row are exchanged within 64 bytes by bits 1 and 2 of the row's number: eight rows' chunks of one column
-// (the first product reads them along a row) lie in different banks, and so do the pieces of four rows that a
-// transposing read takes (the second product).
+// Rows of L latent elements and the key part in LDS, bf16.  The pitch is an odd multiple of 64 bytes, so that four rows
+// lie in different banks, and the 16-byte chunks of a row are exchanged within 64 bytes by bits 2 and 3 of the row's
+// number: neither reads along a row (the first product's operands: one column of 32 rows) nor transposing reads (the
+// second product's) conflict.  (By bits 1 and 2 36 % of the cycles of these reads were conflicts.)
 template <int L>
 constexpr int kLatentPitch = L + kRopeDim + 32;
-__device__ __forceinline__ int exchange(int row) { return (row & 2) | ((row >> 2) & 1); }
+__device__ __forceinline__ int exchange(int row) { return (row >> 2) & 3; }
+
+// Where a lane reads transposed operands of 16 rows (of 32 columns from a multiple of 32 on): rows 0 .. 7 at [0], 8 .. 15
+// at [1], elements from the first row's.  Both are the same again 16 rows on.
+template <int PITCH>
+struct Transposed {
+  int at[2];
+
+  __device__ __forceinline__ explicit Transposed(int lane) {
+    const int i = lane & 15, c = 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      const int r = 4 * (lane >> 5) + (i >> 2) + 8 * y;
+      at[y] = r * PITCH + 8 * (c ^ exchange(r)) + 4 * (i & 1);
+    }
+  }
+  __device__ __forceinline__ bf16x8 operator()(const uint16_t* rows) const {
+    const u32x2_t v0 = lds_transpose4(rows + at[0]), v1 = lds_transpose4(rows + at[1]);
+    return as_bf16x8(u32x4_t{v0[0], v0[1], v1[0], v1[1]});
+  }
+};
 
 // x + both halves of a pair of bf16.
 __device__ __forceinline__ float add_pair(uint32_t pair, float x) {
