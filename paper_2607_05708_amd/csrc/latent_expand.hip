@@ -59,32 +59,6 @@ __global__ __launch_bounds__(kThreads) void latent_units_kernel(AttendArgs a, in
 constexpr int kGroupUnits = 4;                     // units of a workgroup
 constexpr int kGroupTokens = kGroupUnits * kUnit;  // 128
 
-// 16 bytes of a row's elements 8 i .. 8 i + 7 as bf16.
-template <int FMT, int L>
-__device__ __forceinline__ u32x4_t latent_chunk(const uint8_t* codes, const uint8_t* scales, int i) {
-  if constexpr (FMT == MEM_KV_BF16) {
-    return *reinterpret_cast<const u32x4_t*>(codes + 16 * i);
-  } else {
-    const float s = kv_scale(scales[i / 4]);
-    u32x4_t o;
-    if constexpr (FMT == MEM_KV_FP4) {
-      const uint32_t c = *reinterpret_cast<const uint32_t*>(codes + 4 * i);
-      o[0] = bits_of(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 0));
-      o[1] = bits_of(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 1));
-      o[2] = bits_of(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 2));
-      o[3] = bits_of(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 3));
-    } else {
-      const u32x2_t c = *reinterpret_cast<const u32x2_t*>(codes + 8 * i);
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        o[2 * j] = bits_of(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[j], s, false));
-        o[2 * j + 1] = bits_of(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[j], s, true));
-      }
-    }
-    return o;
-  }
-}
-
 // Workgroup (four units of a request, a share of the heads): the tokens' latent vectors stay in LDS as bf16; for each
 // head a wave makes a quarter of its keys' and values' elements for all 128 tokens, its rows of W and V straight from
 // memory.  The order of a product's k is free as long as both operands have it: lane (row, half) takes 64 consecutive
@@ -95,8 +69,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_expand_kernel(LatentArgs x
                                                                  const int* __restrict__ counts, int h0, int heads,
                                                                  int per, uint16_t* __restrict__ keys,
                                                                  uint16_t* __restrict__ values) {
-  constexpr int kRow = kv_row_bytes(FMT, L), kSc = kv_scale_bytes(FMT, L), kPitch = kPitchOf<L>;
-  constexpr int kKeyRow = D + kRopeDim, kMine = 2 * D / kWaves, kBlocks = kMine / 32;  // rows of W and V of a wave
+  constexpr int kPitch = kPitchOf<L>, kKeyRow = D + kRopeDim, kMine = 2 * D / kWaves, kBlocks = kMine / 32;  // rows of W and V of a wave
   __shared__ __align__(16) uint16_t rows[kGroupTokens * kPitch];
   const AttendArgs& a = x.a;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -111,36 +84,34 @@ __global__ __launch_bounds__(kThreads, 1) void latent_expand_kernel(LatentArgs x
 
   // latent vectors into LDS, and the key parts into the heads' keys
   const int hb = blockIdx.y * per, he = min(hb + per, heads);
-  for (int i = tid; i < kGroupTokens * (L / 8); i += kThreads) {
-    const int t = i / (L / 8), c = i % (L / 8), u = u0 + t / kUnit;
-    u32x4_t v = {0, 0, 0, 0};
-    if (u < n) {
-      const Source s = sources[req * units + u];
-      if (s.at >= 0 && t % kUnit < s.held) {
-        const int row = s.row + t % kUnit;
-        const uint8_t* page = a.kv.pool + (s.at - static_cast<int64_t>(s.row) * kRow);
-        v = latent_chunk<FMT, L>(page + static_cast<int64_t>(row) * kRow,
-                                 page + T * (kRow + 2 * kRopeDim) + static_cast<int64_t>(row) * kSc, c);
-      }
+  {
+    const int tok = tid >> 3, part = tid & 7;
+    Part<FMT, L> p[kGroupUnits];
+    bool held[kGroupUnits];
+#pragma unroll
+    for (int k = 0; k < kGroupUnits; ++k) {
+      const Source s = sources[req * units + min(u0 + k, n - 1)];
+      held[k] = u0 + k < n && s.at >= 0 && tok < s.held;
+      const int64_t at = max(s.at, int64_t{0}) - (s.at >= 0 ? static_cast<int64_t>(s.row) * Part<FMT, L>::kRow : 0);
+      p[k].clear();
+      if (held[k]) p[k].load(a.kv.pool + at, T, s.row + tok, part);
     }
-    *reinterpret_cast<u32x4_t*>(rows + t * kPitch + 8 * (c ^ exchange(t))) = v;
-  }
-  for (int i = tid; i < kGroupTokens * 8; i += kThreads) {
-    const int t = i % kUnit, c = i / kUnit % 8, k = i / (8 * kUnit), u = u0 + k;
-    if (u >= n) break;
-    const Source s = sources[req * units + u];
-    if (s.at < 0 || t >= s.held) continue;
-    const int row = s.row + t;
-    const u32x4_t v = *reinterpret_cast<const u32x4_t*>(a.kv.pool + (s.at - static_cast<int64_t>(s.row) * kRow) +
-                                                        T * kRow + static_cast<int64_t>(row) * 2 * kRopeDim + 16 * c);
-    for (int h = hb; h < he; ++h)
-      *reinterpret_cast<u32x4_t*>(keys + (h * slots + slot0 + k * kUnit) * kKeyRow + ((D / 8 + c) * kUnit + t) * 8) = v;
+#pragma unroll
+    for (int k = 0; k < kGroupUnits; ++k) {
+      const int t = kUnit * k + tok;
+#pragma unroll
+      for (int z = 0; z < Part<FMT, L>::kPieces - 1; ++z) p[k].store(rows + t * kPitch, exchange(t), part, z);
+      if (held[k])
+        for (int h = hb; h < he; ++h)
+          *reinterpret_cast<u32x4_t*>(keys + (h * slots + slot0 + kUnit * k) * kKeyRow +
+                                      ((D / 8 + part) * kUnit + tok) * 8) = p[k].rope;
+    }
   }
   __syncthreads();
 
   const int f = exchange(col);
-  // W and V: a wave's rows, 128 elements a step, each loaded again for the next step (maybe of the next head) as soon as
-  // it has been used.
+  // W and V: a wave's rows, 128 elements a step, loaded again for the next step (maybe of the next head) as soon as a
+  // line has been used.
   constexpr int kStep = 128, kHeadSteps = L / kStep;
   u32x4_t w[kBlocks][8];
   auto load = [&](int h, int s, int b, int y) {
@@ -180,9 +151,11 @@ __global__ __launch_bounds__(kThreads, 1) void latent_expand_kernel(LatentArgs x
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b)
           o[b][u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(w[b][y]), k[i], o[b][u], 0, 0, 0);
-        if (u + 1 == kGroupUnits) {
+        if (u + 1 == kGroupUnits && y % 4 == 3) {  // the four loads of a line together, while it is in the cache
 #pragma unroll
-          for (int b = 0; b < kBlocks; ++b) load(next_h, next_s, b, y);
+          for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+            for (int z = y - 3; z <= y; ++z) load(next_h, next_s, b, z);
         }
         issue_first();
       }

@@ -44,6 +44,100 @@ __device__ __forceinline__ float add_pair(uint32_t pair, float x) {
   return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(s16x2, pair), __builtin_bit_cast(s16x2, kOnes), x, false);
 }
 
+// A thread's part of a token's row, 1/8 of it: 16-byte loads 8 parts apart, the key part, and the row's scale bytes.
+template <int FMT, int L>
+struct Part {
+  static constexpr int kRow = kv_row_bytes(FMT, L);
+  static constexpr int kSc = kv_scale_bytes(FMT, L);
+  static constexpr int kElems = 16 * L / kRow;          // elements of a load: 8, 16 or 32
+  static constexpr int kLoads = L / (8 * kElems);
+  static constexpr int kChunks = kElems / 8;            // 16-byte chunks of bf16 that a load becomes
+  static constexpr int kScaleWords = FMT == MEM_KV_BF16 ? 1 : kSc / 4;
+  u32x4_t codes[kLoads];
+  u32x4_t rope;
+  uint32_t sc[kScaleWords];
+
+  // All of it, from row `row` of a page of T tokens.
+  __device__ __forceinline__ void load(const uint8_t* page, int64_t T, uint32_t row, int part) {
+#pragma unroll
+    for (int y = 0; y < kLoads; ++y)
+      codes[y] = *reinterpret_cast<const u32x4_t*>(page + (row * kRow + 16 * part + 128 * y));
+    rope = *reinterpret_cast<const u32x4_t*>(page + T * kRow + (row * (2 * kRopeDim) + 16 * part));
+    if constexpr (FMT != MEM_KV_BF16) {
+#pragma unroll
+      for (int i = 0; i < kScaleWords / 2; ++i) {
+        const u32x2_t v = reinterpret_cast<const u32x2_t*>(page + T * (kRow + 2 * kRopeDim) + row * kSc)[i];
+        sc[2 * i] = v[0];
+        sc[2 * i + 1] = v[1];
+      }
+    }
+  }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int y = 0; y < kLoads; ++y) codes[y] = u32x4_t{0, 0, 0, 0};
+    rope = u32x4_t{0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < kScaleWords; ++i) sc[i] = 0x7F7F7F7Fu;
+  }
+  // Scale byte of load y.
+  __device__ __forceinline__ uint32_t scale_byte(int y, int part) const {
+    if constexpr (FMT == MEM_KV_FP8) return sc[y] >> (8 * (part >> 1)) & 255u;  // block part / 2 + 4 y
+    const uint32_t w = part & 4 ? sc[2 * y + 1] : sc[2 * y];                    // block part + 8 y
+    return w >> (8 * (part & 3)) & 255u;
+  }
+  // Chunk c of load y as bf16.
+  __device__ __forceinline__ u32x4_t chunk(int y, int c, float s) const {
+    if constexpr (FMT == MEM_KV_BF16) return codes[y];
+    u32x4_t o;
+    if constexpr (FMT == MEM_KV_FP4) {
+      const uint32_t x = codes[y][c];
+      o[0] = bits_of(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, s, 0));
+      o[1] = bits_of(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, s, 1));
+      o[2] = bits_of(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, s, 2));
+      o[3] = bits_of(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, s, 3));
+    } else if constexpr (FMT == MEM_KV_FP8) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        o[2 * j] = bits_of(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[y][2 * c + j], s, false));
+        o[2 * j + 1] = bits_of(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[y][2 * c + j], s, true));
+      }
+    }
+    return o;
+  }
+  // Piece z of unpacking it into its LDS row: chunks, then the key part.
+  static constexpr int kPieces = kLoads * kChunks + 1;
+  __device__ __forceinline__ void store(uint16_t* dst, int exchanged, int part, int z) const {
+    if (z == kPieces - 1) {
+      *reinterpret_cast<u32x4_t*>(dst + L + 8 * (part ^ exchanged)) = rope;
+    } else {
+      const int y = z / kChunks, c = z % kChunks;
+      const float s = FMT == MEM_KV_BF16 ? 1.f : kv_scale(scale_byte(y, part));
+      *reinterpret_cast<u32x4_t*>(dst + 8 * ((kChunks * (part + 8 * y) + c) ^ exchanged)) = chunk(y, c, s);
+    }
+  }
+  // Whether it holds a latent value that is not finite, or may (scales that no write gives).  The key part only goes into
+  // scores.
+  __device__ __forceinline__ bool bad() const {
+    u16x2 most = {0, 0};
+    bool x = false;
+#pragma unroll
+    for (int y = 0; y < kLoads; ++y)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if constexpr (FMT == MEM_KV_BF16)
+          most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, codes[y][j] & 0x7FFF7FFFu));
+        if constexpr (FMT == MEM_KV_FP8) x |= (((codes[y][j] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) != 0;
+      }
+    if constexpr (FMT != MEM_KV_BF16) {
+#pragma unroll
+      for (int i = 0; i < kScaleWords; ++i)
+#pragma unroll
+        for (int b = 0; b < 4; ++b) x |= (sc[i] >> (8 * b) & 255u) > kMaxScaleByte<FMT>;
+    }
+    return x || most[0] >= 0x7F80u || most[1] >= 0x7F80u;
+  }
+};
+
 // Scales rows whose registers are accumulation registers.  (The compiler would otherwise keep them, for the
 // multiplications' sake, where the matrix products cannot: of 32 x 512 it spills most.)
 template <int WIDTH, int D>
