@@ -40,6 +40,25 @@ __device__ __forceinline__ float to_odd(double x) {
   return __uint_as_float(u | 1u);
 }
 
+// N numbers rounded so.  Those that are normal in fp32 are cut off, with what that leaves as the last bit (a fifth of the
+// operations, and no 64-bit ones); if some are not, all go the long way.
+template <int N>
+__device__ __forceinline__ void all_to_odd(const double (&x)[N], float* y) {
+  bool other = false;
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    const uint64_t bits = __builtin_bit_cast(uint64_t, x[j]);
+    const uint32_t hi = static_cast<uint32_t>(bits >> 32), lo = static_cast<uint32_t>(bits);
+    other |= (hi >> 20 & 0x7FFu) - 897u >= 254u;
+    const uint32_t cut = static_cast<uint32_t>(bits >> 29) - (896u << 23) & 0x7FFFFFFFu;
+    y[j] = __uint_as_float((hi & 0x80000000u) | cut | min(lo << 3, 1u));
+  }
+  if (other) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) y[j] = to_odd(x[j]);
+  }
+}
+
 // The places of the workgroup's tokens tok0 .. tok0 + group - 1 and the turns of their pairs; ends with a barrier.
 __device__ __forceinline__ void open_tokens(const AppendArgs& a, int64_t tok0, int group, Place* places, Turn* turns) {
   const int tid = threadIdx.x;
@@ -65,13 +84,15 @@ __device__ __forceinline__ void turn_item(float* x, int i, int half, bool pairs,
   const bool inside = turned && 8 * i < 2 * half;
   if (pairs) {
     if (!inside) return;
+    double z[8];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const Turn t = turns[4 * i + j];
       const double p = x[2 * j], q = x[2 * j + 1];
-      x[2 * j] = to_odd(p * t.cos - q * t.sin);
-      x[2 * j + 1] = to_odd(p * t.sin + q * t.cos);
+      z[2 * j] = p * t.cos - q * t.sin;
+      z[2 * j + 1] = p * t.sin + q * t.cos;
     }
+    all_to_odd(z, x);
     return;
   }
   const bool low = 8 * i < half;
@@ -81,12 +102,14 @@ __device__ __forceinline__ void turn_item(float* x, int i, int half, bool pairs,
   for (int j = 0; j < 8; ++j)
     y[j] = __uint_as_float(static_cast<uint32_t>(__builtin_amdgcn_ds_bpermute(4 * other, __float_as_int(x[j]))));
   if (!inside) return;
+  double z[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     const Turn t = turns[8 * i + j - (low ? 0 : half)];
-    const double p = x[j], q = y[j];
-    x[j] = to_odd(low ? p * t.cos - q * t.sin : q * t.sin + p * t.cos);
+    const double p = x[j], q = low ? -static_cast<double>(y[j]) : y[j];
+    z[j] = p * t.cos + q * t.sin;
   }
+  all_to_odd(z, x);
 }
 
 // A workgroup's rows are numbered head by head (keys, values, queries), 1 << shift tokens each.
@@ -97,7 +120,6 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(AppendArgs a, int s
   __shared__ Turn turns[kMaxAngles];
   const int group = 1 << shift;
   const int64_t tok0 = static_cast<int64_t>(blockIdx.x) << shift;
-  open_tokens(a, tok0, group, places, turns);
   const int hk = a.kv.heads, items = ((2 * hk + a.hq) << shift) * kPieces;
   for (int at0 = 0; at0 < items; at0 += kThreads * U) {
     float x[U][8];
@@ -110,9 +132,10 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(AppendArgs a, int s
       const RowsView& src = is_q ? a.q : is_v ? a.v : a.k;
       const int h = is_q ? head - 2 * hk : is_v ? head - hk : head;
       for (int j = 0; j < 8; ++j) x[u][j] = 0.f;
-      if (at < items && tok < a.n && (is_q || places[t].page >= 0))
+      if (at < items && tok < a.n)
         load8<T, VEC, NT>(static_cast<const T*>(src.data) + tok * src.ts + h * src.hs + 8 * i, x[u]);
     }
+    if (at0 == 0) open_tokens(a, tok0, group, places, turns);  // (beside the first loads)
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int at = at0 + u * kThreads + static_cast<int>(threadIdx.x);
@@ -143,7 +166,6 @@ __global__ __launch_bounds__(kThreads) void latent_append_kernel(AppendArgs a, i
   __shared__ Turn turns[kMaxAngles];
   const int group = 1 << shift;
   const int64_t tok0 = static_cast<int64_t>(blockIdx.x) << shift, tokens = a.kv.page_tokens;
-  open_tokens(a, tok0, group, places, turns);
   const int latent = kPieces << shift, items = latent + ((1 + a.hq) << shift) * kParts;
   struct Item {
     int i, t, head;  // piece of its row, token, and row: -1 latent, 0 key part, 1 + query head
@@ -162,10 +184,11 @@ __global__ __launch_bounds__(kThreads) void latent_append_kernel(AppendArgs a, i
       const int64_t tok = tok0 + m.t;
       const RowsView& src = m.head < 0 ? a.k : m.head == 0 ? a.v : a.q;
       for (int j = 0; j < 8; ++j) x[u][j] = 0.f;
-      if (at < items && tok < a.n && (m.head > 0 || places[m.t].page >= 0))
+      if (at < items && tok < a.n)
         load8<T, VEC, NT>(
             static_cast<const T*>(src.data) + tok * src.ts + (m.head > 0 ? m.head - 1 : 0) * src.hs + 8 * m.i, x[u]);
     }
+    if (at0 == 0) open_tokens(a, tok0, group, places, turns);  // (beside the first loads)
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int at = at0 + u * kThreads + static_cast<int>(threadIdx.x);

@@ -2,9 +2,10 @@
 // all heads share a token's latent vector as key and value.
 //
 //   latent_query_kernel   W_h^T q and the query's rotated part as one row, bf16
-//   latent_attend_kernel  attention of those rows over the cache
-//   attend_join_kernel    joins the parts of split contexts
-//   latent_out_kernel     V_h times the weighted sum of latent vectors
+//   latent_few_kernel,    attention of those rows over the cache: tiles of 16
+//   latent_attend_kernel  rows, of 64 or 128
+//   latent_out_kernel     joins the parts of split contexts, and takes V_h to the
+//                         weighted sums of latent vectors
 #include <algorithm>
 
 #include "context.h"
@@ -123,7 +124,6 @@ struct LatentShape {
 template <int FMT, int L, int RG>
 __global__ __launch_bounds__(kThreads, 1) void latent_attend_kernel(LatentArgs x, int splits, int64_t tiles, int side,
                                                                  const uint16_t* __restrict__ query_rows,
-                                                                 uint16_t* __restrict__ sums,
                                                                  float* __restrict__ part_o,
                                                                  RowState* __restrict__ part_ml) {
   using P = Part<FMT, L>;
@@ -192,7 +192,10 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attend_kernel(LatentArgs x
     const int n = resolve_units<S::kBatch>(a, list_of, span, tr, prefix, 0, P::kRow, last, min(S::kBatch, last - u0 + 1),
                                            list, tmp);
     if (n == 0) continue;
-    if (tid < 2) bad_tok[tid] = 0;
+    if (tid < 3) bad_tok[tid] = 0;
+    // the first step's second product is of weights 0: its values have to be numbers
+    for (int z = tid; z < S::kUnitElems / 8; z += kThreads)
+      reinterpret_cast<u32x4_t*>(unit_rows[2])[z] = u32x4_t{0, 0, 0, 0};
     __syncthreads();
     // this thread's row of a unit (of those that it holds): the unit's page, and its bytes there
     struct Place {
@@ -261,30 +264,12 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attend_kernel(LatentArgs x
       for (int j = 0; j < P::kScaleWords; ++j) p.sc[j] = scales[j];
     }
     __syncthreads();
-    // Weights of the unit before: its second product is made beside the exponentials of the unit at hand.
-    u32x4_t w[2];
-    bool pending = false;
-    const uint16_t* values = nullptr;  // its rows
-    auto value = [&](int x) {          // operand x: columns 32 (x / 2), tokens 16 (x % 2)
-      return columns(values + 16 * (x & 1) * kPitch + 32 * (x >> 1));
-    };
+    // A step makes the scores of unit i, then its weights beside the second product of unit i - 1.  They go by the
+    // running maximum as it is; where a score turns out to be above it by more than the lag (rare), they are made again.
     constexpr int kOps = 2 * kBlocks;
-    auto add_values = [&](auto share) {
-      constexpr int kAhead = 2;
-      bf16x8 v[kOps];
-#pragma unroll
-      for (int x = 0; x < kAhead; ++x) v[x] = value(x);
-      issue_first();
-#pragma unroll
-      for (int x = 0; x < kOps; ++x) {
-        if (x + kAhead < kOps) v[x + kAhead] = value(x + kAhead);
-        rows.o[x >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[x], as_bf16x8(w[x & 1]), rows.o[x >> 1], 0, 0, 0);
-        share(x);
-        issue_first();
-      }
-    };
+    u32x4_t w[2] = {u32x4_t{0, 0, 0, 0}, u32x4_t{0, 0, 0, 0}};
     int slot = 0;  // i mod 3: the unit's buffer, and its word of bad_tok
-    for (int i = 0; i < n; ++i) {
+    for (int i = 0; i <= n; ++i) {  // (step n only finishes the last unit)
       const Unit after = uniform_unit(list[min(i + 2, n - 1)]);
       const int slot1 = slot == 2 ? 0 : slot + 1, slot2 = slot == 0 ? 2 : slot - 1;
       if (tid == 0) bad_tok[slot2] = 0;
@@ -298,87 +283,89 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attend_kernel(LatentArgs x
       issue_first();
       // (a wave without rows goes along with its tile's last row: with a path of its own the compiler copies the loads
       // of the units ahead from register to register, which waits for them)
+      const uint16_t* keys = unit_rows[slot];
+      const uint16_t* values = unit_rows[slot2] + cg * kColumns;
+      f32x16 s;
+#pragma unroll
+      for (int j = 0; j < 16; ++j) s[j] = 0.f;
       {
-        const uint16_t* keys = unit_rows[slot];
-        values = unit_rows[slot2] + cg * kColumns;
-        f32x16 s;
-#pragma unroll
-        for (int j = 0; j < 16; ++j) s[j] = 0.f;
-        {
-          constexpr int kAhead = 3;
-          auto key = [&](int y) {
-            return *reinterpret_cast<const u32x4_t*>(keys + (y & 1 ? odd : even) + 32 * (y >> 1));
-          };
-          auto query = [&](int y) { return *reinterpret_cast<const bf16x8*>(my_parked + (y - kKept) * 512); };
-          u32x4_t k[kSteps];
-          bf16x8 pq[S::kParked + 1];
-#pragma unroll
-          for (int y = 0; y < kAhead; ++y) k[y] = key(y);
-          issue_first();
-#pragma unroll
-          for (int y = 0; y < kSteps; ++y) {
-            if (y + kAhead < kSteps) k[y + kAhead] = key(y + kAhead);
-            if (y + kAhead < kSteps && y + kAhead >= kKept) pq[y + kAhead - kKept] = query(y + kAhead);
-            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(k[y]),
-                                                        y < kKept ? q[y < kKept ? y : 0] : pq[y < kKept ? 0 : y - kKept],
-                                                        s, 0, 0, 0);
-            if (y * P::kPieces / kSteps != (y + 1) * P::kPieces / kSteps) advance(to, from, y * P::kPieces / kSteps);
-            issue_first();
-          }
-        }
-        if (u.masked()) {
-          const uint32_t seen = visible_tokens(rule, u, prefix);
-          mask_scores<32, 16>(s, seen, half);
-          poison |= (seen & bad_tok[slot]) != 0;
-        }
-        float top = s[0];
-#pragma unroll
-        for (int j = 1; j < 16; ++j) top = nan_max(top, s[j]);
-        const float high = max_column<32>(top) * c;
-        const bool counts = __any(!u.masked() || high != -INFINITY);
-        const bool up = counts && __any(high > st.m + kLag);
-        u32x4_t now[2];
-        auto weigh_score = [&](float ref, int j) {
-          s[j] = fast_exp2(fmaf(s[j], c, -ref));
-          st.l += s[j];
-          if (j & 1) {
-            const uint32_t pair = pack2(s[j - 1], s[j]);
-            now[j >> 3][(j >> 1) & 3] = pair;
-            rounded = add_pair(pair, rounded);
-          }
+        constexpr int kAhead = 3;
+        auto key = [&](int y) {
+          return *reinterpret_cast<const u32x4_t*>(keys + (y & 1 ? odd : even) + 32 * (y >> 1));
         };
-        // The usual way: both in one.  (Two flags that the compiler does not know to be one: with an if and an else
-        // over the same accumulators it keeps them twice.)
-        const bool usual = pending && counts && !up;
-        int usual_too = __builtin_amdgcn_readfirstlane(usual);
-        asm volatile("" : "+s"(usual_too));
-        if (!usual) {
-          if (pending) add_values([](int) {});
-          if (up) {
-            const float mn = fmaxf(st.m, high);
-            const float r = mn == -INFINITY ? 1.f : fast_exp2(st.m - mn);
-            st.l *= r;
-            rounded *= r;
-            scale_rows(rows, r);
-            st.m = mn;
-          }
-          if (counts) {
-            const float ref = finite_max(st.m);
+        auto query = [&](int y) { return *reinterpret_cast<const bf16x8*>(my_parked + (y - kKept) * 512); };
+        u32x4_t k[kSteps];
+        bf16x8 pq[S::kParked + 1];
 #pragma unroll
-            for (int j = 0; j < 16; ++j) weigh_score(ref, j);
-          }
-        }
-        if (usual_too) {
-          const float ref = finite_max(st.m);
-          add_values([&](int x) {
+        for (int y = 0; y < kAhead; ++y) k[y] = key(y);
+        issue_first();
 #pragma unroll
-            for (int j = 16 * x / kOps; j < 16 * (x + 1) / kOps; ++j) weigh_score(ref, j);
-          });
+        for (int y = 0; y < kSteps; ++y) {
+          if (y + kAhead < kSteps) k[y + kAhead] = key(y + kAhead);
+          if (y + kAhead < kSteps && y + kAhead >= kKept) pq[y + kAhead - kKept] = query(y + kAhead);
+          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(k[y]),
+                                                      y < kKept ? q[y < kKept ? y : 0] : pq[y < kKept ? 0 : y - kKept],
+                                                      s, 0, 0, 0);
+          if (y * P::kPieces / kSteps != (y + 1) * P::kPieces / kSteps) advance(to, from, y * P::kPieces / kSteps);
+          issue_first();
         }
-        pending = counts;
-        w[0] = now[0];
-        w[1] = now[1];
       }
+      if (i == n) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) s[j] = -INFINITY;
+      } else if (u.masked()) {
+        const uint32_t seen = visible_tokens(rule, u, prefix);
+        mask_scores<32, 16>(s, seen, half);
+        poison |= (seen & bad_tok[slot]) != 0;
+      }
+      u32x4_t now[2];
+      float ref = finite_max(st.m), l = 0.f, lr = 0.f, top = s[0], e[2];
+      auto weigh = [&](int j) {  // scores 2 j and 2 j + 1
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          e[y] = fast_exp2(fmaf(s[2 * j + y], c, -ref));
+          l += e[y];
+        }
+        const uint32_t pair = pack2(e[0], e[1]);
+        now[j >> 2][j & 3] = pair;
+        lr = add_pair(pair, lr);
+      };
+      {  // operand x: columns 32 (x / 2), tokens 16 (x % 2)
+        constexpr int kAhead = 2;
+        auto value = [&](int x) { return columns(values + 16 * (x & 1) * kPitch + 32 * (x >> 1)); };
+        bf16x8 v[kOps];
+#pragma unroll
+        for (int x = 0; x < kAhead; ++x) v[x] = value(x);
+        issue_first();
+#pragma unroll
+        for (int x = 0; x < kOps; ++x) {
+          if (x + kAhead < kOps) v[x + kAhead] = value(x + kAhead);
+          rows.o[x >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[x], as_bf16x8(w[x & 1]), rows.o[x >> 1], 0, 0, 0);
+#pragma unroll
+          for (int j = 8 * x / kOps; j < 8 * (x + 1) / kOps; ++j) {
+            top = nan_max(top, nan_max(s[2 * j], s[2 * j + 1]));
+            weigh(j);
+          }
+          issue_first();
+        }
+      }
+      const float high = max_column<32>(top) * c;
+      if (__any(high > st.m + kLag)) {
+        const float mn = fmaxf(st.m, high);
+        const float by = mn == -INFINITY ? 1.f : fast_exp2(st.m - mn);
+        st.l *= by;
+        rounded *= by;
+        scale_rows(rows, by);
+        st.m = mn;
+        ref = finite_max(mn);
+        l = lr = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) weigh(j);
+      }
+      st.l += l;
+      rounded += lr;
+      w[0] = now[0];
+      w[1] = now[1];
 #pragma unroll
       for (int j = 0; j < P::kScaleWords; ++j) p.sc[j] = scales[j];
       u = next;
@@ -386,18 +373,13 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attend_kernel(LatentArgs x
       slot = slot1;
       __syncthreads();
     }
-    if (pending) {
-      values = unit_rows[slot == 0 ? 2 : slot - 1] + cg * kColumns;
-      add_values([](int) {});
-    }
   }
 
   st.l = sum_column<32>(st.l);
   rounded = sum_column<32>(rounded);
   poison = any_column<32>(poison, col);
   if (32 * rg + col >= t.rows) return;
-  write_sums<32, kColumns, L>(a, rows, st, rounded, poison, row_at, half, split, splits, cg * kColumns, sums, part_o,
-                              part_ml);
+  write_part<32, kColumns, L>(a, rows, st, rounded, poison, row_at, half, split, cg * kColumns, part_o, part_ml);
 }
 
 // ---------------------------------------------------------------- few rows
@@ -484,8 +466,7 @@ constexpr int few_per_cu(int fmt, int latent) { return latent == 256 && fmt != M
 template <int FMT, int L>
 __global__ __launch_bounds__(kThreads, few_per_cu(FMT, L)) void latent_few_kernel(LatentArgs x, int splits, int64_t tiles, int side,
                                                                              const uint16_t* __restrict__ query_rows,
-                                                                             uint16_t* __restrict__ sums,
-                                                                             float* __restrict__ part_o,
+                                                                                         float* __restrict__ part_o,
                                                                              RowState* __restrict__ part_ml) {
   using P = Quarter<FMT, L>;
   using S = FewShape<L>;
@@ -495,7 +476,6 @@ __global__ __launch_bounds__(kThreads, few_per_cu(FMT, L)) void latent_few_kerne
   __shared__ Unit list[S::kBatch];
   __shared__ int tmp[2 * kWaves];
   __shared__ RowState joint[2][64];
-  __shared__ float joint_rounded[2][64];
   __shared__ int joint_poison[2][64];
 
   const AttendArgs& a = x.a;
@@ -537,7 +517,6 @@ __global__ __launch_bounds__(kThreads, few_per_cu(FMT, L)) void latent_few_kerne
   Rows<16, L> rows;
   rows.clear();
   RowState st{-INFINITY, 0.f};
-  float rounded = 0.f;
   bool poison = false;
   P p[2];
 
@@ -650,13 +629,13 @@ __global__ __launch_bounds__(kThreads, few_per_cu(FMT, L)) void latent_few_kerne
           const float mn = fmaxf(st.m, high);
           const float r = mn == -INFINITY ? 1.f : fast_exp2(st.m - mn);
           st.l *= r;
-          rounded *= r;
           if constexpr (L == 512) scale_rows(rows, r);
           else rows.scale(r);
           st.m = mn;
         }
         const float ref = finite_max(st.m);
-        u32x4_t w;
+        // weights as two bf16 numbers each: the product is a small part of what a unit costs here
+        u32x4_t w, rest;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           s[j] = fast_exp2(fmaf(s[j], c, -ref));
@@ -665,7 +644,7 @@ __global__ __launch_bounds__(kThreads, few_per_cu(FMT, L)) void latent_few_kerne
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           w[j] = pack2(s[2 * j], s[2 * j + 1]);
-          rounded = add_pair(w[j], rounded);
+          rest[j] = rest2(s[2 * j], s[2 * j + 1], w[j]);
         }
         __builtin_amdgcn_wave_barrier();
         constexpr int kTogether = 8;  // operands loaded ahead of their products
@@ -677,6 +656,8 @@ __global__ __launch_bounds__(kThreads, few_per_cu(FMT, L)) void latent_few_kerne
           issue_first();
 #pragma unroll
           for (int y = 0; y < kTogether; ++y) ops.multiply(rows, n0 + y, v[y], &w);
+#pragma unroll
+          for (int y = 0; y < kTogether; ++y) ops.multiply(rows, n0 + y, v[y], &rest);
         }
         __builtin_amdgcn_wave_barrier();
       }
@@ -690,7 +671,6 @@ __global__ __launch_bounds__(kThreads, few_per_cu(FMT, L)) void latent_few_kerne
 
   // join the waves: 2 and 3 into 0 and 1, then 1 into 0 (a lane holds the same outputs in every wave)
   st.l = sum_column<16>(st.l);
-  rounded = sum_column<16>(rounded);
   poison = any_column<16>(poison, col);
   float* store = reinterpret_cast<float*>(area);
 #pragma unroll
@@ -701,7 +681,6 @@ __global__ __launch_bounds__(kThreads, few_per_cu(FMT, L)) void latent_few_kerne
       int i = 0;
       rows.each4(part, [&](int, f32x4 v) { *reinterpret_cast<f32x4*>(dst + 256 * i++) = v; });
       joint[wave - from][lane] = st;
-      joint_rounded[wave - from][lane] = rounded;
       joint_poison[wave - from][lane] = poison;
     }
     __syncthreads();
@@ -711,7 +690,6 @@ __global__ __launch_bounds__(kThreads, few_per_cu(FMT, L)) void latent_few_kerne
       const float mn = fmaxf(st.m, other.m), ref = finite_max(mn);
       const float f0 = fast_exp2(st.m - ref), f1 = fast_exp2(other.m - ref);
       st.l = st.l * f0 + other.l * f1;
-      rounded = rounded * f0 + joint_rounded[wave][lane] * f1;
       st.m = mn;
       const float* src = store + wave * R * L + lane * 4;
 #pragma unroll
@@ -722,31 +700,96 @@ __global__ __launch_bounds__(kThreads, few_per_cu(FMT, L)) void latent_few_kerne
     }
   }
   if (wave > 0 || col >= t.rows) return;
-  write_sums<16, L, L>(a, rows, st, rounded, poison, row_at, part, split, splits, 0, sums, part_o, part_ml);
+  write_part<16, L, L>(a, rows, st, st.l, poison, row_at, part, split, 0, part_o, part_ml);
 }
 
 // ---------------------------------------------------------------- outputs
 
-// Workgroup (head, 32 or 64 tokens): a wave has 32 of the output's elements for 32 tokens.
+// Workgroup (head, 32 tokens): joins the parts of its rows' sums (in a fixed order; a context that is not split has one
+// part), and multiplies them by V_h.  The sums go into the product as two bf16 numbers each, so that only the output is
+// rounded; V_h is on its way meanwhile.  A wave has 32 of the output's elements, with heads of 64 half of the sum's.
 template <int L, int D>
-__global__ __launch_bounds__(kThreads) void latent_out_kernel(LatentArgs x, const uint16_t* __restrict__ sums) {
-  constexpr int kAcross = D / 32, kBlocks = kWaves / kAcross;
+__global__ __launch_bounds__(kThreads) void latent_out_kernel(LatentArgs x, int splits,
+                                                           const float* __restrict__ part_o,
+                                                           const RowState* __restrict__ part_ml) {
+  constexpr int kAcross = D / 32, kShares = kWaves / kAcross, kSteps = L / 16 / kShares;
+  constexpr int kPitch = L + 32, kPer = L / 64, kTogether = 4;
+  __shared__ __align__(16) uint16_t high[kTokenBlock * kPitch], low[kTokenBlock * kPitch];
+  __shared__ float halves[kShares == 2 ? kAcross * 64 * 16 : 1];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int col = lane & 31, half = lane >> 5, j0 = 32 * (wave % kAcross);
+  const int col = lane & 31, half = lane >> 5, j0 = 32 * (wave % kAcross), k0 = wave / kAcross * (L / kShares);
   const int h = blockIdx.x;
-  const int64_t tok0 = (static_cast<int64_t>(blockIdx.y) * kBlocks + wave / kAcross) * kTokenBlock, tok = tok0 + col;
-  if (tok0 >= x.a.total_q) return;
-  const uint16_t* w = x.w + h * x.w_hs + (D + j0 + col) * x.w_rs + 8 * half;
-  const uint16_t* s = sums + (min(tok, x.a.total_q - 1) * x.a.hq + h) * L + 8 * half;
+  const int64_t tok0 = static_cast<int64_t>(blockIdx.y) * kTokenBlock, total = x.a.total_q, rows = total * x.a.hq;
+  const int64_t first = x.a.q_offsets ? max(x.a.q_offsets[0], 0) : 0;
+  const int64_t last = x.a.q_offsets ? min(static_cast<int64_t>(x.a.q_offsets[x.a.m]), total) : total;
+  const uint16_t* src = x.w + h * x.w_hs + (D + j0 + col) * x.w_rs + k0 + 8 * half;
+  u32x4_t w[kSteps];
+#pragma unroll
+  for (int y = 0; y < kSteps; ++y) w[y] = *reinterpret_cast<const u32x4_t*>(src + 16 * y);
+
+  for (int r = wave; r < kTokenBlock; r += kWaves) {
+    const int64_t tok = tok0 + r, at = tok * x.a.hq + h;
+    float o[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) o[i] = 0.f;
+    if (tok >= first && tok < last) {  // (rows that no request owns were not computed)
+      RowState st{-INFINITY, 0.f};
+      if (lane < splits) st = part_ml[lane * rows + at];
+      const float m = wave_max_f32(st.m), f = fast_exp2(st.m - finite_max(m)), l = wave_sum_f32(f * st.l);
+      for (int s0 = 0; s0 < splits; s0 += kTogether) {
+        float v[kTogether][kPer];
+#pragma unroll
+        for (int u = 0; u < kTogether; ++u) {  // (past the last split: the last one again, so that nothing is conditional)
+          const float* from = part_o + (min(s0 + u, splits - 1) * rows + at) * L + lane * kPer;
+#pragma unroll
+          for (int i = 0; i < kPer; ++i) v[u][i] = from[i];
+        }
+#pragma unroll
+        for (int u = 0; u < kTogether; ++u) {
+          if (s0 + u >= splits) continue;
+          const float g = lane_f32(f, s0 + u);
+#pragma unroll
+          for (int i = 0; i < kPer; ++i) o[i] += g * v[u][i];
+        }
+      }
+      const float inv = inverse_sum(l);
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) o[i] *= inv;
+      if (x.a.lse && lane == 0) x.a.lse[at] = lse_of(m, l);
+    }
+    const int place = r * kPitch + 8 * ((lane * kPer / 8) ^ exchange(r)) + lane * kPer % 8;
+#pragma unroll
+    for (int i = 0; i < kPer; i += 2) {
+      const uint32_t pair = pack2(o[i], o[i + 1]);
+      *reinterpret_cast<uint32_t*>(high + place + i) = pair;
+      *reinterpret_cast<uint32_t*>(low + place + i) = rest2(o[i], o[i + 1], pair);
+    }
+  }
+  __syncthreads();
   f32x16 o;
 #pragma unroll
   for (int j = 0; j < 16; ++j) o[j] = 0.f;
-#pragma unroll 8
-  for (int y = 0; y < L / 16; ++y)
-    o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*reinterpret_cast<const u32x4_t*>(w + 16 * y)),
-                                                as_bf16x8(*reinterpret_cast<const u32x4_t*>(s + 16 * y)), o, 0, 0, 0);
-  if (tok >= x.a.total_q) return;
-  if (x.a.q_offsets && (tok < x.a.q_offsets[0] || tok >= x.a.q_offsets[x.a.m])) return;  // no request's
+#pragma unroll
+  for (int y = 0; y < kSteps; ++y) {
+    const int place = col * kPitch + 8 * ((k0 / 8 + 2 * y + half) ^ exchange(col));
+    o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(w[y]),
+                                                as_bf16x8(*reinterpret_cast<const u32x4_t*>(low + place)), o, 0, 0, 0);
+    o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(w[y]),
+                                                as_bf16x8(*reinterpret_cast<const u32x4_t*>(high + place)), o, 0, 0, 0);
+  }
+  if constexpr (kShares == 2) {
+    float* mine = halves + (wave % kAcross) * 64 * 16 + lane;
+    if (wave >= kAcross) {
+#pragma unroll
+      for (int j = 0; j < 16; ++j) mine[64 * j] = o[j];
+    }
+    __syncthreads();
+    if (wave >= kAcross) return;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) o[j] += mine[64 * j];
+  }
+  const int64_t tok = tok0 + col;
+  if (tok < first || tok >= last) return;
   uint16_t* dst = x.out + (tok * x.a.hq + h) * D + j0 + 4 * half;
 #pragma unroll
   for (int y = 0; y < 4; ++y)
@@ -792,7 +835,7 @@ AbsorbedPlan absorbed_plan(const LatentSizes& s, bool ragged) {
   int64_t best = INT64_MAX;
   p.splits = 1;
   for (int64_t n = 1; n <= kMaxSplits && (n == 1 || s.units / n >= 4); ++n) {
-    if (n > 1 && (job_blocks(p.tiles, p.side, n) > kMaxGroups || join_groups(rows, n) > kMaxGroups)) break;
+    if (n > 1 && (job_blocks(p.tiles, p.side, n) > kMaxGroups)) break;
     const int64_t cost = (work * n + slots - 1) / slots * ((s.units + n - 1) / n + kStart) + (n > 1 ? n / 4 : 0);
     if (cost < best) {
       best = cost;
@@ -802,19 +845,18 @@ AbsorbedPlan absorbed_plan(const LatentSizes& s, bool ragged) {
   return p;
 }
 
-// Workspace of the absorbed form: query rows, sums, and the parts of split contexts.
+// Workspace of the absorbed form: query rows, and the parts of their sums.
 struct AbsorbedSpace {
-  size_t queries, sums, part_o, part_ml, end;
+  size_t queries, part_o, part_ml, end;
 };
 
 AbsorbedSpace absorbed_space(const LatentSizes& s, int splits) {
   const size_t rows = static_cast<size_t>(s.total_q) * s.heads;
   AbsorbedSpace w;
   w.queries = 0;
-  w.sums = align256(rows * (s.latent + kRopeDim) * 2);
-  w.part_o = w.sums + align256(rows * s.latent * 2);
-  w.part_ml = w.part_o + (splits > 1 ? align256(splits * rows * s.latent * sizeof(float)) : 0);
-  w.end = w.part_ml + (splits > 1 ? align256(splits * rows * sizeof(RowState)) : 0);
+  w.part_o = align256(rows * (s.latent + kRopeDim) * 2);
+  w.part_ml = w.part_o + align256(splits * rows * s.latent * sizeof(float));
+  w.end = w.part_ml + align256(splits * rows * sizeof(RowState));
   return w;
 }
 
@@ -822,10 +864,7 @@ constexpr int kQueryBlocks = 8;  // blocks of tokens of a workgroup of latent_qu
 int64_t query_groups(int64_t total_q) {
   return (total_q + kQueryBlocks * kTokenBlock - 1) / (kQueryBlocks * kTokenBlock);
 }
-int64_t out_groups(int64_t total_q, int d) {
-  const int tokens = kTokenBlock * kWaves / (d / 32);
-  return (total_q + tokens - 1) / tokens;
-}
+int64_t out_groups(int64_t total_q) { return (total_q + kTokenBlock - 1) / kTokenBlock; }
 
 template <int FMT, int L, int D>
 hipError_t launch_absorbed(const LatentArgs& x, const LatentSizes& s, hipStream_t stream) {
@@ -833,7 +872,6 @@ hipError_t launch_absorbed(const LatentArgs& x, const LatentSizes& s, hipStream_
   const AbsorbedSpace at = absorbed_space(s, p.splits);
   uint8_t* ws = static_cast<uint8_t*>(x.ws);
   uint16_t* queries = reinterpret_cast<uint16_t*>(ws + at.queries);
-  uint16_t* sums = reinterpret_cast<uint16_t*>(ws + at.sums);
   float* part_o = reinterpret_cast<float*>(ws + at.part_o);
   RowState* part_ml = reinterpret_cast<RowState*>(ws + at.part_ml);
   latent_query_kernel<L, D><<<dim3(s.heads, L / 128, static_cast<unsigned>(query_groups(s.total_q))), kThreads, 0,
@@ -841,24 +879,14 @@ hipError_t launch_absorbed(const LatentArgs& x, const LatentSizes& s, hipStream_
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   const unsigned grid = static_cast<unsigned>(job_blocks(p.tiles, p.side, p.splits));
   if (p.rows == 16)
-    latent_few_kernel<FMT, L><<<grid, kThreads, list_bytes(s.k), stream>>>(x, p.splits, p.tiles, p.side, queries, sums,
-                                                                          part_o, part_ml);
+    latent_few_kernel<FMT, L><<<grid, kThreads, list_bytes(s.k), stream>>>(x, p.splits, p.tiles, p.side, queries, part_o,
+                                                                          part_ml);
   else
     (p.rows == 64 ? latent_attend_kernel<FMT, L, 2> : latent_attend_kernel<FMT, L, 4>)<<<
-        grid, kThreads, list_bytes(s.k), stream>>>(x, p.splits, p.tiles, p.side, queries, sums, part_o, part_ml);
+        grid, kThreads, list_bytes(s.k), stream>>>(x, p.splits, p.tiles, p.side, queries, part_o, part_ml);
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  if (p.splits > 1) {
-    AttendArgs j = x.a;
-    j.out = sums;
-    const dim3 join(static_cast<unsigned>(join_groups(s.total_q * s.heads, p.splits)));
-    if (p.splits <= kJoinSplits)
-      attend_join_kernel<L, 1><<<join, kThreads, 0, stream>>>(j, p.splits, part_o, part_ml);
-    else
-      attend_join_kernel<L, kWaves><<<join, kThreads, 0, stream>>>(j, p.splits, part_o, part_ml);
-    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  }
-  latent_out_kernel<L, D><<<dim3(s.heads, static_cast<unsigned>(out_groups(s.total_q, D))), kThreads, 0, stream>>>(x,
-                                                                                                                sums);
+  latent_out_kernel<L, D><<<dim3(s.heads, static_cast<unsigned>(out_groups(s.total_q))), kThreads, 0, stream>>>(
+      x, p.splits, part_o, part_ml);
   return hipGetLastError();
 }
 
@@ -897,7 +925,7 @@ size_t latent_workspace_bytes(const LatentSizes& s, mem_latent_form form) {
 bool latent_fits(const LatentSizes& s, mem_latent_form form, bool ragged) {
   if (form == MEM_LATENT_EXPANDED) return expanded_fits(s, ragged);
   const AbsorbedPlan p = absorbed_plan(s, ragged);
-  return job_blocks(p.tiles, p.side, p.splits) <= kMaxGroups && query_groups(s.total_q) < 65536 && out_groups(s.total_q, s.head_dim) < 65536;
+  return job_blocks(p.tiles, p.side, p.splits) <= kMaxGroups && query_groups(s.total_q) < 65536 && out_groups(s.total_q) < 65536;
 }
 
 hipError_t launch_latent_attend(const LatentArgs& x, const LatentSizes& s, mem_latent_form form, hipStream_t stream) {

@@ -421,8 +421,7 @@ __global__ __launch_bounds__(kThreads, 2) void expanded_attend_kernel(LatentArgs
   rounded = sum_column<32>(rounded);
   poison = any_column<32>(poison, col);
   if (32 * wave + col >= t.rows) return;
-  write_sums<32, D, D>(a, rows, st, rounded, poison, tok_at * a.hq + h0 + g, half, split, splits, 0, x.out, part_o,
-                       part_ml);
+  write_sums<32, D>(a, rows, st, rounded, poison, tok_at * a.hq + h0 + g, half, split, splits, x.out, part_o, part_ml);
 }
 
 // ---------------------------------------------------------------- launches

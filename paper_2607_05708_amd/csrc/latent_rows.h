@@ -153,28 +153,36 @@ __device__ __forceinline__ void scale_rows(Rows<WIDTH, D>& rows, float f) {
   }
 }
 
-// Write elements first .. + N - 1 of a row's weighted sum (of L), or of its part of a split context.  `rounded`
-// is the sum of the weights as the product took them, and what it is divided by, so that their roundings cancel where a
-// few weigh most; the join divides by l.
+// Write elements first .. + N - 1 of a row's weighted sum (of L) as part `split` of it.  `rounded` is the sum of the
+// weights as the product took them: dividing by it lets their roundings cancel where a few weigh most; what joins the
+// parts divides by l.
 template <int WIDTH, int N, int L>
-__device__ __forceinline__ void write_sums(const AttendArgs& a, const Rows<WIDTH, N>& rows, RowState st, float rounded,
-                                           bool poison, int64_t row_at, int part, int split, int splits, int first,
-                                           uint16_t* sums, float* part_o, RowState* part_ml) {
+__device__ __forceinline__ void write_part(const AttendArgs& a, const Rows<WIDTH, N>& rows, RowState st, float rounded,
+                                           bool poison, int64_t row_at, int part, int split, int first, float* part_o,
+                                           RowState* part_ml) {
   if (poison) st.l = NAN;
-  if (splits == 1) {
-    const float inv = poison ? NAN : inverse_sum(rounded);
-    uint16_t* dst = sums + row_at * L + first;
-    rows.each4(part, [&](int d, f32x4 v) {
-      *reinterpret_cast<u32x2_t*>(dst + d) = u32x2_t{pack2(v[0] * inv, v[1] * inv), pack2(v[2] * inv, v[3] * inv)};
-    });
-    if (a.lse && part == 0 && first == 0) a.lse[row_at] = lse_of(st.m, st.l);
-  } else {
-    const int64_t at = static_cast<int64_t>(split) * a.total_q * a.hq + row_at;
-    const float even = st.l == 0.f ? 0.f : st.l * inverse_sum(rounded);
-    float* dst = part_o + at * L + first;
-    rows.each4(part, [&](int d, f32x4 v) { *reinterpret_cast<f32x4*>(dst + d) = v * even; });
-    if (part == 0 && first == 0) part_ml[at] = st;
+  const int64_t at = static_cast<int64_t>(split) * a.total_q * a.hq + row_at;
+  const float even = st.l == 0.f ? 0.f : st.l * inverse_sum(rounded);
+  float* dst = part_o + at * L + first;
+  rows.each4(part, [&](int d, f32x4 v) { *reinterpret_cast<f32x4*>(dst + d) = v * even; });
+  if (part == 0 && first == 0) part_ml[at] = st;
+}
+
+// The same, but where the context is not split the row itself, as bf16.
+template <int WIDTH, int L>
+__device__ __forceinline__ void write_sums(const AttendArgs& a, const Rows<WIDTH, L>& rows, RowState st, float rounded,
+                                           bool poison, int64_t row_at, int part, int split, int splits, uint16_t* out,
+                                           float* part_o, RowState* part_ml) {
+  if (splits > 1) {
+    write_part<WIDTH, L, L>(a, rows, st, rounded, poison, row_at, part, split, 0, part_o, part_ml);
+    return;
   }
+  const float inv = poison ? NAN : inverse_sum(rounded);
+  uint16_t* dst = out + row_at * L;
+  rows.each4(part, [&](int d, f32x4 v) {
+    *reinterpret_cast<u32x2_t*>(dst + d) = u32x2_t{pack2(v[0] * inv, v[1] * inv), pack2(v[2] * inv, v[3] * inv)};
+  });
+  if (a.lse && part == 0) a.lse[row_at] = poison ? NAN : lse_of(st.m, st.l);
 }
 
 }  // namespace
