@@ -116,7 +116,8 @@ MEMATTN_API size_t mem_latent_attend_workspace_bytes(const mem_latent* cache, in
  * softmax weights and the sum of weighted latent vectors in the absorbed form, keys,
  * values and weights in the expanded form: a score is off by at most 2^-8 of the sum
  * of its products' magnitudes, an output by some 2^-7 of the largest value's
- * magnitude.  Nothing is synchronised; the call can be captured into a HIP graph.
+ * magnitude.  The workspace is rewritten by each call, and calls that share one must
+ * not overlap.  Nothing is synchronised; the call can be captured into a HIP graph.
  * Calls whose tiles come to 2^24 or more are refused (MEM_ERR_UNSUPPORTED).
  */
 MEMATTN_API mem_status mem_latent_attend(const mem_latent* cache, const mem_attend_args* args, const mem_kv_rows* q,

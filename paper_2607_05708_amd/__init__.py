@@ -970,6 +970,6 @@ def mem_latent_attend(cache: LatentCache, tok_len: torch.Tensor, ids: torch.Tens
     if not isinstance(workspace, torch.Tensor) or workspace.get_device() != dev or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous tensor on the cache's GPU")
     _check("mem_latent_attend", lib().mem_latent_attend(
-        cache._ref, C.byref(a), C.byref(qr), C.byref(tr), total_q, C.byref(weights), form, o_ptr, lse_ptr,
+        cache._ref, C.byref(a), C.byref(qr), C.byref(tr), total_q, C.byref(weights), _i32(form, "form"), o_ptr, lse_ptr,
         workspace.data_ptr(), workspace.nbytes, on))
     return out

@@ -22,7 +22,6 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMaxGroup = 16;    // tokens of a workgroup
-constexpr int U = 4;             // items in flight per thread
 constexpr int kMaxAngles = 512;  // pairs of a workgroup's tokens
 
 struct Turn {
@@ -120,39 +119,44 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(AppendArgs a, int s
   __shared__ Turn turns[kMaxAngles];
   const int group = 1 << shift;
   const int64_t tok0 = static_cast<int64_t>(blockIdx.x) << shift;
+  open_tokens(a, tok0, group, places, turns);
   const int hk = a.kv.heads, items = ((2 * hk + a.hq) << shift) * kPieces;
-  for (int at0 = 0; at0 < items; at0 += kThreads * U) {
-    float x[U][8];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int at = at0 + u * kThreads + static_cast<int>(threadIdx.x);
-      const int row = at / kPieces, i = at % kPieces, t = row & (group - 1), head = row >> shift;
-      const int64_t tok = tok0 + t;
-      const bool is_q = head >= 2 * hk, is_v = !is_q && head >= hk;
-      const RowsView& src = is_q ? a.q : is_v ? a.v : a.k;
-      const int h = is_q ? head - 2 * hk : is_v ? head - hk : head;
-      for (int j = 0; j < 8; ++j) x[u][j] = 0.f;
-      if (at < items && tok < a.n)
-        load8<T, VEC, NT>(static_cast<const T*>(src.data) + tok * src.ts + h * src.hs + 8 * i, x[u]);
-    }
-    if (at0 == 0) open_tokens(a, tok0, group, places, turns);  // (beside the first loads)
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int at = at0 + u * kThreads + static_cast<int>(threadIdx.x);
-      const int row = at / kPieces, i = at % kPieces, t = row & (group - 1), head = row >> shift;
-      const int64_t tok = tok0 + t;
-      const bool is_q = head >= 2 * hk, is_v = !is_q && head >= hk, live = at < items && tok < a.n;
-      turn_item(x[u], i, a.half, a.pairs, turns + t * a.half, live && !is_v);
-      if (live && is_q)
-        store_item<uint16_t, VEC, NT>(
-            static_cast<uint16_t*>(a.q_out.data) + tok * a.q_out.ts + (head - 2 * hk) * a.q_out.hs + 8 * i, x[u]);
-      const Place p = places[t];
-      const bool kept = live && !is_q && p.page >= 0;
-      int64_t co, so;
-      kv_offsets<FMT, D, 8>(a.kv, is_v ? head - hk : head, is_v, p.row, i, &co, &so);
-      uint8_t* base = a.kv.pool + p.page * a.kv.page_bytes;
-      encode_item<FMT>(x[u], kept ? base + co : nullptr, kept ? base + so : nullptr, threadIdx.x % 4 == 0, kept);
-    }
+  // (one item a thread: many waves keep more in flight than many items a wave; 32,768 tokens 194 us, with the next item
+  // on its way 203, with four 227)
+  struct Item {
+    int i, t, head;  // piece of its row, token, and row: keys, values, queries
+    bool is_q, is_v;
+  };
+  auto item = [&](int at) {
+    const int row = at / kPieces, head = row >> shift;
+    const bool is_q = head >= 2 * hk, is_v = !is_q && head >= hk;
+    return Item{at % kPieces, row & (group - 1), is_q ? head - 2 * hk : is_v ? head - hk : head, is_q, is_v};
+  };
+  auto fetch = [&](int at, float (&x)[8]) {
+    const Item m = item(at);
+    const int64_t tok = tok0 + m.t;
+    const RowsView& src = m.is_q ? a.q : m.is_v ? a.v : a.k;
+    for (int j = 0; j < 8; ++j) x[j] = 0.f;
+    if (at < items && tok < a.n && (m.is_q || places[m.t].page >= 0))
+      load8<T, VEC, NT>(static_cast<const T*>(src.data) + tok * src.ts + m.head * src.hs + 8 * m.i, x);
+  };
+  for (int at0 = 0; at0 < items; at0 += kThreads) {
+    const int at = at0 + static_cast<int>(threadIdx.x);
+    float x[8];
+    fetch(at, x);
+    const Item m = item(at);
+    const int64_t tok = tok0 + m.t;
+    const bool live = at < items && tok < a.n;
+    turn_item(x, m.i, a.half, a.pairs, turns + m.t * a.half, live && !m.is_v);
+    if (live && m.is_q)
+      store_item<uint16_t, VEC, NT>(
+          static_cast<uint16_t*>(a.q_out.data) + tok * a.q_out.ts + m.head * a.q_out.hs + 8 * m.i, x);
+    const Place p = places[m.t];
+    const bool kept = live && !m.is_q && p.page >= 0;
+    int64_t co, so;
+    kv_offsets<FMT, D, 8>(a.kv, m.head, m.is_v, p.row, m.i, &co, &so);
+    uint8_t* base = a.kv.pool + p.page * a.kv.page_bytes;
+    encode_item<FMT>(x, kept ? base + co : nullptr, kept ? base + so : nullptr, threadIdx.x % 4 == 0, kept);
   }
 }
 
@@ -166,6 +170,7 @@ __global__ __launch_bounds__(kThreads) void latent_append_kernel(AppendArgs a, i
   __shared__ Turn turns[kMaxAngles];
   const int group = 1 << shift;
   const int64_t tok0 = static_cast<int64_t>(blockIdx.x) << shift, tokens = a.kv.page_tokens;
+  open_tokens(a, tok0, group, places, turns);
   const int latent = kPieces << shift, items = latent + ((1 + a.hq) << shift) * kParts;
   struct Item {
     int i, t, head;  // piece of its row, token, and row: -1 latent, 0 key part, 1 + query head
@@ -175,43 +180,37 @@ __global__ __launch_bounds__(kThreads) void latent_append_kernel(AppendArgs a, i
     const int row = (at - latent) / kParts;
     return Item{at % kParts, row & (group - 1), row >> shift};
   };
-  for (int at0 = 0; at0 < items; at0 += kThreads * U) {
-    float x[U][8];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int at = at0 + u * kThreads + static_cast<int>(threadIdx.x);
-      const Item m = item(at);
-      const int64_t tok = tok0 + m.t;
-      const RowsView& src = m.head < 0 ? a.k : m.head == 0 ? a.v : a.q;
-      for (int j = 0; j < 8; ++j) x[u][j] = 0.f;
-      if (at < items && tok < a.n)
-        load8<T, VEC, NT>(
-            static_cast<const T*>(src.data) + tok * src.ts + (m.head > 0 ? m.head - 1 : 0) * src.hs + 8 * m.i, x[u]);
-    }
-    if (at0 == 0) open_tokens(a, tok0, group, places, turns);  // (beside the first loads)
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int at = at0 + u * kThreads + static_cast<int>(threadIdx.x);
-      const Item m = item(at);
-      const int64_t tok = tok0 + m.t;
-      const bool live = at < items && tok < a.n;
-      turn_item(x[u], m.i, a.half, a.pairs, turns + m.t * a.half, live && m.head >= 0);
-      if (live && m.head > 0)
-        store_item<uint16_t, VEC, NT>(
-            static_cast<uint16_t*>(a.q_out.data) + tok * a.q_out.ts + (m.head - 1) * a.q_out.hs + 8 * m.i, x[u]);
-      const Place p = places[m.t];
-      const bool kept = live && p.page >= 0;
-      uint8_t* base = a.kv.pool + p.page * a.kv.page_bytes;
-      if (kept && m.head == 0)
-        store_item<uint16_t, true, false>(
-            reinterpret_cast<uint16_t*>(base + tokens * kRow + static_cast<int64_t>(p.row) * 2 * kRopeDim) + 8 * m.i,
-            x[u]);
-      const bool is_latent = kept && m.head < 0;
-      encode_item<FMT>(x[u], is_latent ? base + static_cast<int64_t>(p.row) * kRow + m.i * (kRow / kPieces) : nullptr,
-                       is_latent ? base + tokens * (kRow + 2 * kRopeDim) + static_cast<int64_t>(p.row) * kSc + m.i / 4
-                                 : nullptr,
-                       threadIdx.x % 4 == 0, is_latent);
-    }
+  auto fetch = [&](int at, float (&x)[8]) {
+    const Item m = item(at);
+    const int64_t tok = tok0 + m.t;
+    const RowsView& src = m.head < 0 ? a.k : m.head == 0 ? a.v : a.q;
+    for (int j = 0; j < 8; ++j) x[j] = 0.f;
+    if (at < items && tok < a.n && (m.head > 0 || places[m.t].page >= 0))
+      load8<T, VEC, NT>(static_cast<const T*>(src.data) + tok * src.ts + (m.head > 0 ? m.head - 1 : 0) * src.hs + 8 * m.i,
+                        x);
+  };
+  for (int at0 = 0; at0 < items; at0 += kThreads) {
+    const int at = at0 + static_cast<int>(threadIdx.x);
+    float x[8];
+    fetch(at, x);
+    const Item m = item(at);
+    const int64_t tok = tok0 + m.t;
+    const bool live = at < items && tok < a.n;
+    turn_item(x, m.i, a.half, a.pairs, turns + m.t * a.half, live && m.head >= 0);
+    if (live && m.head > 0)
+      store_item<uint16_t, VEC, NT>(
+          static_cast<uint16_t*>(a.q_out.data) + tok * a.q_out.ts + (m.head - 1) * a.q_out.hs + 8 * m.i, x);
+    const Place p = places[m.t];
+    const bool kept = live && p.page >= 0;
+    uint8_t* base = a.kv.pool + p.page * a.kv.page_bytes;
+    if (kept && m.head == 0)
+      store_item<uint16_t, true, false>(
+          reinterpret_cast<uint16_t*>(base + tokens * kRow + static_cast<int64_t>(p.row) * 2 * kRopeDim) + 8 * m.i, x);
+    const bool is_latent = kept && m.head < 0;
+    encode_item<FMT>(x, is_latent ? base + static_cast<int64_t>(p.row) * kRow + m.i * (kRow / kPieces) : nullptr,
+                     is_latent ? base + tokens * (kRow + 2 * kRopeDim) + static_cast<int64_t>(p.row) * kSc + m.i / 4
+                               : nullptr,
+                     threadIdx.x % 4 == 0, is_latent);
   }
 }
 
@@ -222,6 +221,7 @@ __global__ __launch_bounds__(kThreads) void latent_read_kernel(KvView kv, RowsVi
                                                                const int32_t* __restrict__ pos, int64_t n, int shift) {
   constexpr int kN = 16 / static_cast<int>(sizeof(T)), kPieces = L / kN, kParts = kRopeDim / kN;
   constexpr int kRow = kv_row_bytes(FMT, L), kSc = kv_scale_bytes(FMT, L);
+  constexpr int U = 4;  // items in flight per thread
   constexpr int kBytes = kN * kRow / L;  // of an item's codes
   __shared__ Place places[kMaxGroup];
   const int group = 1 << shift;
@@ -305,7 +305,7 @@ int group_shift(int64_t n, int half, int most) {
 
 // Tokens of a workgroup of a cache of keys and values: stretches of a page's rows of a head; of a latent cache, whose
 // tokens are smaller.
-constexpr int kKvGroup = 4, kLatentGroup = kMaxGroup;
+constexpr int kKvGroup = 8, kLatentGroup = kMaxGroup;
 
 template <int FMT, int D, bool LATENT>
 hipError_t launch_append(const AppendArgs& a, int dtype, hipStream_t stream) {

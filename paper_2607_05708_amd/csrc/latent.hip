@@ -705,21 +705,23 @@ __global__ __launch_bounds__(kThreads, few_per_cu(FMT, L)) void latent_few_kerne
 
 // ---------------------------------------------------------------- outputs
 
-// Workgroup (head, 32 tokens): joins the parts of its rows' sums (in a fixed order; a context that is not split has one
-// part), and multiplies them by V_h.  The sums go into the product as two bf16 numbers each, so that only the output is
+// Workgroup (head, up to 32 tokens): joins the parts of its rows' sums (in a fixed order; a context that is not split has
+// one part), and multiplies them by V_h.  The sums go into the product as two bf16 numbers each, so that only the output is
 // rounded; V_h is on its way meanwhile.  A wave has 32 of the output's elements, with heads of 64 half of the sum's.
-template <int L, int D>
-__global__ __launch_bounds__(kThreads) void latent_out_kernel(LatentArgs x, int splits,
+// T: parts that are loaded together, the first ones before their weights are known.
+template <int L, int D, int T>
+__global__ __launch_bounds__(kThreads) void latent_out_kernel(LatentArgs x, int splits, int tokens,
                                                            const float* __restrict__ part_o,
                                                            const RowState* __restrict__ part_ml) {
   constexpr int kAcross = D / 32, kShares = kWaves / kAcross, kSteps = L / 16 / kShares;
-  constexpr int kPitch = L + 32, kPer = L / 64, kTogether = 4;
+  constexpr int kPitch = L + 32, kPer = L / 64;
   __shared__ __align__(16) uint16_t high[kTokenBlock * kPitch], low[kTokenBlock * kPitch];
   __shared__ float halves[kShares == 2 ? kAcross * 64 * 16 : 1];
+  __shared__ bool sees[kTokenBlock];  // rows that see something: the others are 0 whatever V_h holds
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 31, half = lane >> 5, j0 = 32 * (wave % kAcross), k0 = wave / kAcross * (L / kShares);
   const int h = blockIdx.x;
-  const int64_t tok0 = static_cast<int64_t>(blockIdx.y) * kTokenBlock, total = x.a.total_q, rows = total * x.a.hq;
+  const int64_t tok0 = static_cast<int64_t>(blockIdx.y) * tokens, total = x.a.total_q, rows = total * x.a.hq;
   const int64_t first = x.a.q_offsets ? max(x.a.q_offsets[0], 0) : 0;
   const int64_t last = x.a.q_offsets ? min(static_cast<int64_t>(x.a.q_offsets[x.a.m]), total) : total;
   const uint16_t* src = x.w + h * x.w_hs + (D + j0 + col) * x.w_rs + k0 + 8 * half;
@@ -730,22 +732,27 @@ __global__ __launch_bounds__(kThreads) void latent_out_kernel(LatentArgs x, int 
   for (int r = wave; r < kTokenBlock; r += kWaves) {
     const int64_t tok = tok0 + r, at = tok * x.a.hq + h;
     float o[kPer];
+    bool seen = false;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) o[i] = 0.f;
-    if (tok >= first && tok < last) {  // (rows that no request owns were not computed)
+    if (r < tokens && tok >= first && tok < last) {  // (rows that no request owns were not computed)
       RowState st{-INFINITY, 0.f};
       if (lane < splits) st = part_ml[lane * rows + at];
-      const float m = wave_max_f32(st.m), f = fast_exp2(st.m - finite_max(m)), l = wave_sum_f32(f * st.l);
-      for (int s0 = 0; s0 < splits; s0 += kTogether) {
-        float v[kTogether][kPer];
+      float v[T][kPer];
+      auto load = [&](int s0) {  // (past the last part: the last one again, so that nothing is conditional)
 #pragma unroll
-        for (int u = 0; u < kTogether; ++u) {  // (past the last split: the last one again, so that nothing is conditional)
+        for (int u = 0; u < T; ++u) {
           const float* from = part_o + (min(s0 + u, splits - 1) * rows + at) * L + lane * kPer;
 #pragma unroll
           for (int i = 0; i < kPer; ++i) v[u][i] = from[i];
         }
+      };
+      load(0);
+      const float m = wave_max_f32(st.m), f = fast_exp2(st.m - finite_max(m)), l = wave_sum_f32(f * st.l);
+      for (int s0 = 0; s0 < splits; s0 += T) {
+        if (s0 > 0) load(s0);
 #pragma unroll
-        for (int u = 0; u < kTogether; ++u) {
+        for (int u = 0; u < T; ++u) {
           if (s0 + u >= splits) continue;
           const float g = lane_f32(f, s0 + u);
 #pragma unroll
@@ -753,10 +760,12 @@ __global__ __launch_bounds__(kThreads) void latent_out_kernel(LatentArgs x, int 
         }
       }
       const float inv = inverse_sum(l);
+      seen = l != 0.f;
 #pragma unroll
       for (int i = 0; i < kPer; ++i) o[i] *= inv;
       if (x.a.lse && lane == 0) x.a.lse[at] = lse_of(m, l);
     }
+    if (lane == 0) sees[r] = seen;
     const int place = r * kPitch + 8 * ((lane * kPer / 8) ^ exchange(r)) + lane * kPer % 8;
 #pragma unroll
     for (int i = 0; i < kPer; i += 2) {
@@ -789,8 +798,12 @@ __global__ __launch_bounds__(kThreads) void latent_out_kernel(LatentArgs x, int 
     for (int j = 0; j < 16; ++j) o[j] += mine[64 * j];
   }
   const int64_t tok = tok0 + col;
-  if (tok < first || tok >= last) return;
+  if (col >= tokens || tok < first || tok >= last) return;
   uint16_t* dst = x.out + (tok * x.a.hq + h) * D + j0 + 4 * half;
+  if (!sees[col]) {
+#pragma unroll
+    for (int j = 0; j < 16; ++j) o[j] = 0.f;
+  }
 #pragma unroll
   for (int y = 0; y < 4; ++y)
     *reinterpret_cast<u32x2_t*>(dst + 8 * y) =
@@ -864,7 +877,17 @@ constexpr int kQueryBlocks = 8;  // blocks of tokens of a workgroup of latent_qu
 int64_t query_groups(int64_t total_q) {
   return (total_q + kQueryBlocks * kTokenBlock - 1) / (kQueryBlocks * kTokenBlock);
 }
-int64_t out_groups(int64_t total_q) { return (total_q + kTokenBlock - 1) / kTokenBlock; }
+// Tokens of a workgroup of latent_out_kernel: fewer where that lets more CUs join (64 tokens of 32 heads in 4 parts: 17 us
+// with 32, LAST with 4).
+int out_tokens(int64_t total_q, int heads) {
+  int t = kTokenBlock;
+  while (t > 4 && (total_q + t - 1) / t * heads < 256) t /= 2;
+  return t;
+}
+int64_t out_groups(int64_t total_q, int heads) {
+  const int t = out_tokens(total_q, heads);
+  return (total_q + t - 1) / t;
+}
 
 template <int FMT, int L, int D>
 hipError_t launch_absorbed(const LatentArgs& x, const LatentSizes& s, hipStream_t stream) {
@@ -885,8 +908,9 @@ hipError_t launch_absorbed(const LatentArgs& x, const LatentSizes& s, hipStream_
     (p.rows == 64 ? latent_attend_kernel<FMT, L, 2> : latent_attend_kernel<FMT, L, 4>)<<<
         grid, kThreads, list_bytes(s.k), stream>>>(x, p.splits, p.tiles, p.side, queries, part_o, part_ml);
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  latent_out_kernel<L, D><<<dim3(s.heads, static_cast<unsigned>(out_groups(s.total_q))), kThreads, 0, stream>>>(
-      x, p.splits, part_o, part_ml);
+  (p.splits <= 4 ? latent_out_kernel<L, D, 4> : latent_out_kernel<L, D, 16>)<<<
+      dim3(s.heads, static_cast<unsigned>(out_groups(s.total_q, s.heads))), kThreads, 0, stream>>>(
+      x, p.splits, out_tokens(s.total_q, s.heads), part_o, part_ml);
   return hipGetLastError();
 }
 
@@ -925,7 +949,9 @@ size_t latent_workspace_bytes(const LatentSizes& s, mem_latent_form form) {
 bool latent_fits(const LatentSizes& s, mem_latent_form form, bool ragged) {
   if (form == MEM_LATENT_EXPANDED) return expanded_fits(s, ragged);
   const AbsorbedPlan p = absorbed_plan(s, ragged);
-  return job_blocks(p.tiles, p.side, p.splits) <= kMaxGroups && query_groups(s.total_q) < 65536 && out_groups(s.total_q) < 65536;
+  const int64_t q = query_groups(s.total_q), o = out_groups(s.total_q, s.heads);
+  return job_blocks(p.tiles, p.side, p.splits) <= kMaxGroups && q < 65536 && o < 65536 &&
+         q * (s.latent / 128) * s.heads <= kMaxGroups && o * s.heads <= kMaxGroups;
 }
 
 hipError_t launch_latent_attend(const LatentArgs& x, const LatentSizes& s, mem_latent_form form, hipStream_t stream) {

@@ -535,7 +535,7 @@ size_t expanded_workspace_bytes(const LatentSizes& s, bool ragged) {
 
 bool expanded_fits(const LatentSizes& s, bool ragged) {
   const ExpandedPlan p = expanded_plan(s, ragged);
-  return p.tiles * p.splits * p.heads <= kMaxGroups && expand_groups(s) <= kMaxGroups / s.heads;
+  return p.tiles * p.splits * p.heads <= kMaxGroups && expand_groups(s) <= kMaxGroups / s.heads && s.m <= kMaxGroups;
 }
 
 hipError_t launch_expanded(const LatentArgs& x, const LatentSizes& s, hipStream_t stream) {
