@@ -107,7 +107,9 @@ MEMATTN_API size_t mem_latent_attend_workspace_bytes(const mem_latent* cache, in
  * A token that sees nothing gets out = 0 and lse = -inf.  Tokens that a query does
  * not see have no influence on it, whatever they hold; an element of a latent vector
  * that is not finite among those that it does see makes its outputs so, however small
- * its weight (one of a key part counts as its score says: nothing at -inf).  q and t
+ * its weight (one of a key part counts as its score says: nothing at -inf).  An
+ * element of w that is not finite makes the outputs that take it so, of rows that see
+ * something, and may make the others of its head so.  q and t
  * (device bf16, strides in `q` and `t`, only read), out (device bf16 [total_q, heads, head_dim],
  * contiguous, 16-byte aligned) and lse (device fp32 [total_q, heads], nullable).
  * Rows that no request owns are not written.
