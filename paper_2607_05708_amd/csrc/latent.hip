@@ -95,8 +95,10 @@ __global__ __launch_bounds__(kThreads) void latent_query_kernel(LatentArgs x, in
 
 constexpr int kXcds = 8;
 
-// Which tile and split a workgroup has.  Workgroups go to the XCDs in turn, and each XCD has an L2 of its own: the `side`
-// tiles that read one context (the rows of a request are consecutive tiles) follow each other on one XCD.
+// Which tile and split a workgroup has.  Workgroups go to the XCDs in turn, and each XCD has an L2 of its own: `side` tiles
+// that read one context (the rows of a request are consecutive tiles) follow each other on one XCD.  Tiles that ragged
+// requests leave empty come last: started first, they leave the others unevenly spread (one request of 128 tokens, 16 heads,
+// in 16 parts: 122 us, now 75).
 struct Job {
   int64_t tile;  // may be past the last one
   int split;
@@ -115,7 +117,7 @@ struct LatentShape {
   static constexpr int kUnitElems = kUnit * kLatentPitch<L>;  // a unit's rows in LDS
   // Operands of a row's query that LDS holds: with 512 columns of 32 rows a wave's outputs take all 256 accumulation
   // registers, and what else it needs is more than the others with all 36 operands.  (Registers spilled to memory would
-  // wait, at each reload, for the loads of the units ahead: 986 us for LAST.)
+  // wait, at each reload, for the loads of the units ahead: 64 x 32,768 fp8 tokens, 128 heads, 991 us without, 764 with 10.)
   static constexpr int kParked = L == 512 && RG == 4 ? 10 : 0;
 };
 
@@ -147,7 +149,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attend_kernel(LatentArgs x
   const Job job = job_of(blockIdx.x, side, splits);
   const int split = job.split;
   Tile t;
-  if (job.tile >= tiles || !find_tile<32 * RG>(a, static_cast<uint32_t>(tiles - 1 - job.tile), a.hq, &t)) return;
+  if (job.tile >= tiles || !find_tile<32 * RG>(a, static_cast<uint32_t>(job.tile), a.hq, &t)) return;
   const ChunkList list_of = scan_list<kThreads, false>(a, t.req, dyn, tmp);
   const int ctx = list_of.tb[a.k];
   const int prefix = a.prefix_len ? __builtin_amdgcn_readfirstlane(min(max(a.prefix_len[t.req], 0), kFar)) : 0;
@@ -736,8 +738,9 @@ __global__ __launch_bounds__(kThreads) void latent_out_kernel(LatentArgs x, int 
 #pragma unroll
     for (int i = 0; i < kPer; ++i) o[i] = 0.f;
     if (r < tokens && tok >= first && tok < last) {  // (rows that no request owns were not computed)
-      RowState st{-INFINITY, 0.f};
-      if (lane < splits) st = part_ml[lane * rows + at];
+      RowState st[2] = {{-INFINITY, 0.f}, {-INFINITY, 0.f}};  // of parts `lane` and 64 + `lane`
+      if (lane < splits) st[0] = part_ml[lane * rows + at];
+      if (64 + lane < splits) st[1] = part_ml[(64 + lane) * rows + at];
       float v[T][kPer];
       auto load = [&](int s0) {  // (past the last part: the last one again, so that nothing is conditional)
 #pragma unroll
@@ -748,13 +751,15 @@ __global__ __launch_bounds__(kThreads) void latent_out_kernel(LatentArgs x, int 
         }
       };
       load(0);
-      const float m = wave_max_f32(st.m), f = fast_exp2(st.m - finite_max(m)), l = wave_sum_f32(f * st.l);
+      const float m = wave_max_f32(fmaxf(st[0].m, st[1].m));
+      const float f[2] = {fast_exp2(st[0].m - finite_max(m)), fast_exp2(st[1].m - finite_max(m))};
+      const float l = wave_sum_f32(f[0] * st[0].l + f[1] * st[1].l);
       for (int s0 = 0; s0 < splits; s0 += T) {
         if (s0 > 0) load(s0);
 #pragma unroll
         for (int u = 0; u < T; ++u) {
           if (s0 + u >= splits) continue;
-          const float g = lane_f32(f, s0 + u);
+          const float g = lane_f32(s0 < 64 ? f[0] : f[1], (s0 + u) & 63);
 #pragma unroll
           for (int i = 0; i < kPer; ++i) o[i] += g * v[u][i];
         }
@@ -819,10 +824,20 @@ struct AbsorbedPlan {
   int rows;  // of a tile: 16 (few-rows kernel), 64 or 128
   int64_t tiles;
   int splits;
-  int side;  // tiles of a request, on average
+  int side;  // tiles that follow each other on an XCD
 };
 
-constexpr int64_t kStart = 16;  // a workgroup's start and end, in units
+// Parts of a context, by what a call would take in units of a tile: the passes of the busiest XCD's CUs, each with its
+// units and its start and end; then the join, of whose rows kJoinRows are written and read while a tile works on a unit.
+// (Both from timings of 14 shapes with 1 to 128 parts: one request of 48 tokens and 16 heads over 8,192, us: 1 part 555,
+// 8 111, 16 84, 32 72, 40, which need a second pass, 104.)  Up to 128 parts, two states a lane of latent_out_kernel: one
+// token over 131,072, 16 heads, 64 us, with 64 parts 74; of 4 tokens 103 and 137.
+constexpr int64_t kStart = 16;
+constexpr int64_t kJoinRows = 10'000;
+constexpr int kMostParts = 128;
+// Tiles that stay on one XCD: with all of a request's, an XCD has whole requests or none (4 requests of 96 tokens, 16 heads:
+// 12 tiles each 317 us, 4 of them 209); to 16 of them no case was faster than with 4.
+constexpr int kMaxSide = 4;
 
 // Tiles of 128 rows of 512 elements leave 4 KB of a CU's 160 KB for the chunk list, tiles of 16 rows 20 KB: calls with
 // longer lists (more than 511 and 2,559 chunks) take tiles of 64, which leave 40.
@@ -843,13 +858,21 @@ AbsorbedPlan absorbed_plan(const LatentSizes& s, bool ragged) {
   p.rows = rows <= 32 * s.m && list_fits_few(s.latent, s.k) ? 16 : rows <= 64 * s.m || !list_fits_tiles(s.latent, s.k) ? 64 : 128;
   const int R = p.rows;
   p.tiles = ragged ? rows / R + s.m : s.m * ((s.total_q / s.m * s.heads + R - 1) / R);
-  const int64_t work = ragged ? (rows + R - 1) / R + s.m / 2 : p.tiles, slots = 256 * (R == 16 ? few_per_cu(s.fmt, s.latent) : 1);
-  p.side = static_cast<int>(std::min<int64_t>(std::max<int64_t>((rows / s.m + R - 1) / R, 1), 64));
+  // How many tiles ragged requests have is for the kernel to find.  They are taken to be alike; where that means one tile
+  // each, of several tokens, some may have two, and a count of parts that suits both is sought.
+  const int64_t each = (std::max<int64_t>(rows / s.m, 1) + R - 1) / R, alike = s.m * each;
+  const int64_t uneven = ragged && each == 1 && s.total_q > s.m ? std::max(alike, (rows + R - 1) / R + s.m / 2) : alike;
+  const int64_t slots = 256 / kXcds * (R == 16 ? few_per_cu(s.fmt, s.latent) : 1);  // workgroups that run on an XCD
+  p.side = static_cast<int>(std::min<int64_t>(each, kMaxSide));
   int64_t best = INT64_MAX;
   p.splits = 1;
-  for (int64_t n = 1; n <= kMaxSplits && (n == 1 || s.units / n >= 4); ++n) {
-    if (n > 1 && (job_blocks(p.tiles, p.side, n) > kMaxGroups)) break;
-    const int64_t cost = (work * n + slots - 1) / slots * ((s.units + n - 1) / n + kStart) + (n > 1 ? n / 4 : 0);
+  for (int64_t n = 1; n <= kMostParts && (n == 1 || s.units / n >= 4); ++n) {
+    if (n > 1 && job_blocks(p.tiles, p.side, n) > kMaxGroups) break;
+    auto passes = [&](int64_t work) {
+      return (((work + p.side - 1) / p.side * n + kXcds - 1) / kXcds * p.side + slots - 1) / slots;
+    };
+    const int64_t cost = (2 * passes(alike) + passes(uneven)) * ((s.units + n - 1) / n + kStart) +
+                         3 * (n / 16 + rows * (n - 1) / kJoinRows);
     if (cost < best) {
       best = cost;
       p.splits = static_cast<int>(n);
@@ -878,7 +901,7 @@ int64_t query_groups(int64_t total_q) {
   return (total_q + kQueryBlocks * kTokenBlock - 1) / (kQueryBlocks * kTokenBlock);
 }
 // Tokens of a workgroup of latent_out_kernel: fewer where that lets more CUs join (64 tokens of 32 heads in 4 parts: 17 us
-// with 32, LAST with 4).
+// with 32, 11.7 with 8; with 4, whose V_h is read twice as often, 14.4).
 int out_tokens(int64_t total_q, int heads) {
   int t = kTokenBlock;
   while (t > 4 && (total_q + t - 1) / t * heads < 256) t /= 2;
@@ -928,8 +951,12 @@ hipError_t launch_fmt(const LatentArgs& x, const LatentSizes& s, hipStream_t str
 
 mem_latent_form choose_latent_form(const LatentSizes& s, int32_t asked) {
   if (asked != MEM_LATENT_AUTO) return static_cast<mem_latent_form>(asked);
-  // products of a head, in units of a pair's 2 elements each: rows (2 L + R) absorbed, rows (2 d + R) and 2 d L for
-  // each token of the context expanded
+  // Products of a head, in units of a pair's 2 elements each: rows (2 L + R) absorbed, rows (2 d + R) and 2 d L for each
+  // token of the context expanded.  Measured, us, absorbed and expanded, 512 elements and heads of 128 (the rule changes
+  // at 171 tokens): 8 requests over 8,192 tokens, 16 heads, 128 tokens 455 and 548, 256 764 and 584; one over 4,096, 128
+  // heads, 128 tokens 218 and 286, 160 303 and 319; 256 elements, heads of 64 (86 tokens): 4 over 8,192, 64 tokens 100 and
+  // 106, 128 156 and 126.  Single requests of few heads change over earlier (16 heads over 8,192: 64 tokens 79 and 89, 128
+  // 103 and 95) and short contexts at once (1,024: 16 tokens 50 and 40), by less than 30 us.
   const int64_t rows = s.total_q / s.m, d = s.head_dim, l = s.latent;
   return rows * (l - d) > d * l ? MEM_LATENT_EXPANDED : MEM_LATENT_ABSORBED;
 }
