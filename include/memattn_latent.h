@@ -109,17 +109,19 @@ MEMATTN_API size_t mem_latent_attend_workspace_bytes(const mem_latent* cache, in
  * that is not finite among those that it does see makes its outputs so, however small
  * its weight (one of a key part counts as its score says: nothing at -inf).  An
  * element of w that is not finite makes the outputs that take it so, of rows that see
- * something, and may make the others of its head so.  q and t
- * (device bf16, strides in `q` and `t`, only read), out (device bf16 [total_q, heads, head_dim],
- * contiguous, 16-byte aligned) and lse (device fp32 [total_q, heads], nullable).
- * Rows that no request owns are not written.
+ * something, and may make the others of its head so.  q and t (device bf16, strides
+ * in `q` and `t`, only read), out (device bf16 [total_q, heads, head_dim], contiguous,
+ * 16-byte aligned) and lse (device fp32 [total_q, heads], nullable).  Rows that no
+ * request owns are not written.  out, lse and the workspace must not overlap each
+ * other, q, t, w or the pool.
  *
- * Products are bf16 with fp32 sums.  Rounded to bf16 on the way are W_h^T q, the
- * softmax weights and the sum of weighted latent vectors in the absorbed form, keys,
- * values and weights in the expanded form: a score is off by at most 2^-8 of the sum
- * of its products' magnitudes, an output by some 2^-7 of the largest value's
- * magnitude.  The workspace is rewritten by each call, and calls that share one must
- * not overlap.  Nothing is synchronised; the call can be captured into a HIP graph.
+ * Products are bf16 with fp32 sums.  Rounded to bf16 on the way are W_h^T q and the
+ * softmax weights in the absorbed form (the weighted sums of latent vectors are taken
+ * through V_h as two bf16 numbers each), keys, values and weights in the expanded
+ * form: a score is off by at most 2^-8 of the sum of its products' magnitudes, an
+ * output by some 2^-7 of the largest value's magnitude.  The workspace is rewritten
+ * by each call, and calls that share one must not overlap.  Nothing is synchronised;
+ * the call can be captured into a HIP graph.
  * Calls whose tiles come to 2^24 or more are refused (MEM_ERR_UNSUPPORTED).
  */
 MEMATTN_API mem_status mem_latent_attend(const mem_latent* cache, const mem_attend_args* args, const mem_kv_rows* q,

@@ -12,6 +12,8 @@ namespace memattn {
 
 namespace {
 
+constexpr int64_t kMaxStride = int64_t{1} << 44;  // elements: of heads and rows together, within a 64-bit address
+
 bool known_latent(int32_t l) { return l == 256 || l == 512; }
 bool known_head(int32_t d) { return d == 64 || d == 128; }
 
@@ -44,6 +46,33 @@ mem_status check_sizes(const mem_latent* c, int64_t m, int32_t k, int64_t total_
     return fail(MEM_ERR_INVALID_ARG, "form %d is no mem_latent_form", form);
   if (m > (1 << 24) || total_q > (int64_t{1} << 30) / heads)
     return fail(MEM_ERR_UNSUPPORTED, "more than 2^24 requests or 2^30 query rows");
+  return MEM_OK;
+}
+
+// What a call writes lies apart from the rest of it and from what it reads: tiles write their outputs while others read.
+mem_status check_apart(const mem_latent* c, const mem_kv_rows* q, const mem_kv_rows* t, const mem_latent_weights* w,
+                       const LatentSizes& s, const void* out, const float* lse, const void* workspace, size_t need) {
+  struct {
+    const char* name;
+    uintptr_t lo, hi;
+  } x[7] = {{"out"}, {"lse"}, {"workspace"}, {"q"}, {"t"}, {"w"}, {"the page pool"}};
+  const uintptr_t rows = static_cast<uintptr_t>(s.total_q) * s.heads;
+  auto set = [&](int i, const void* from, uintptr_t bytes) {
+    x[i].lo = reinterpret_cast<uintptr_t>(from);
+    x[i].hi = x[i].lo + bytes;
+  };
+  set(0, out, rows * s.head_dim * 2);
+  set(1, lse, lse ? rows * sizeof(float) : 0);
+  set(2, workspace, need);
+  span_of(q, s.heads, s.head_dim, 2, s.total_q, &x[3].lo, &x[3].hi);
+  span_of(t, s.heads, kRopeDim, 2, s.total_q, &x[4].lo, &x[4].hi);
+  set(5, w->data, 2 * static_cast<uintptr_t>((s.heads - 1) * w->head_stride + (2 * s.head_dim - 1) * w->row_stride +
+                                             s.latent));
+  set(6, c->pages.pool, static_cast<uintptr_t>(c->pages.n_pages * c->pages.page_bytes));
+  for (int i = 0; i < 3; ++i)
+    for (int j = i + 1; j < 7; ++j)
+      if (x[i].lo < x[j].hi && x[j].lo < x[i].hi)
+        return fail(MEM_ERR_INVALID_ARG, "%s overlaps %s", x[i].name, x[j].name);
   return MEM_OK;
 }
 
@@ -146,6 +175,8 @@ mem_status mem_latent_attend(const mem_latent* cache, const mem_attend_args* a, 
   if (!aligned(w->data, 16)) return fail(MEM_ERR_INVALID_ARG, "w's data must be 16-byte aligned");
   if (w->head_stride < 0 || w->row_stride < 0 || w->head_stride % 8 != 0 || w->row_stride % 8 != 0)
     return fail(MEM_ERR_INVALID_ARG, "w's strides must be multiples of 8, and not negative");
+  if (w->head_stride > kMaxStride || w->row_stride > kMaxStride)
+    return fail(MEM_ERR_INVALID_ARG, "the strides of w lead out of memory");
   if (!aligned(out, 16)) return fail(MEM_ERR_INVALID_ARG, "out must be 16-byte aligned");
   if (mem_status st = check_alignment(a, lse); st != MEM_OK) return st;
   const LatentSizes s = sizes_of(cache, a->m, a->k, total_q, a->heads_q, w->head_dim);
@@ -156,6 +187,7 @@ mem_status mem_latent_attend(const mem_latent* cache, const mem_attend_args* a, 
   if (!workspace) return fail(MEM_ERR_WORKSPACE, "workspace is NULL");
   if (!aligned(workspace, 16)) return fail(MEM_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
   if (ws_bytes < need) return fail(MEM_ERR_WORKSPACE, "workspace of %zu bytes < %zu needed", ws_bytes, need);
+  if (mem_status st = check_apart(cache, q, t, w, s, out, lse, workspace, need); st != MEM_OK) return st;
   LatentArgs x{};
   x.a = attend_args(a, view_of(cache), total_q);
   x.a.lse = lse;

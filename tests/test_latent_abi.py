@@ -204,6 +204,15 @@ def test_latent_attend_refusals():
         need = L.mem_latent_attend_workspace_bytes(C.byref(_latent()), 4, 8, 4, 32, 128, form)
         assert need > 0 and need % 16 == 0
         assert go(form=form, ws=None) == -3 and go(form=form, ws_bytes=need - 1) == -3
+        # what is written, on itself or on what is read: q and w at FAR and FAKE, the pool and the workspace further on
+        far = dict(q=_rows(), t=_rows(2 * FAR), data=3 * FAR, out=4 * FAR, lse=5 * FAR, ws=6 * FAR, form=form)
+        for kw, names in ((dict(out=FAR), b"out overlaps q"), (dict(out=2 * FAR), b"out overlaps t"),
+                          (dict(out=3 * FAR), b"out overlaps w"), (dict(lse=FAR), b"lse overlaps q"),
+                          (dict(lse=4 * FAR), b"out overlaps lse"), (dict(ws=4 * FAR - 16), b"out overlaps workspace"),
+                          (dict(ws=2 * FAR), b"workspace overlaps t"), (dict(out=FAKE), b"out overlaps the page pool")):
+            assert go(**{**far, **kw}) == -1 and L.mem_last_error() == names, (kw, L.mem_last_error())
+    for kw in (dict(head_stride=1 << 45), dict(row_stride=1 << 45)):
+        assert go(**kw) == -1 and b"out of memory" in L.mem_last_error()
     assert go(total_q=1 << 26, m=1 << 26) == -2 and go(total_q=(1 << 30) // 32 + 1, m=1) == -2
     assert go(total_q=0) == 0 and go(total_q=0, m=0) == 0
     for total, m, heads, form in ((1 << 24, 1 << 24, 1, 2), (1 << 30, 1, 1, 1), (1 << 24, 1 << 24, 1, 1)):
