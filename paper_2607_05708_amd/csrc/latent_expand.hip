@@ -6,8 +6,10 @@
 //   expanded_attend_kernel  attention over them, head by head
 //   attend_join_kernel      joins the parts of split contexts
 //
-// Of a head, a unit's keys (or values) are one block [element / 8][token][element % 8]: the 16 bytes that a lane of a
-// matrix product has of a token lie next to its neighbours', so that blocks are written and read in whole lines.
+// Of a head, a unit's keys are one block [element / 8][token][element % 8], its values one of [token / 16][token / 4 % 2]
+// [element][token / 8 % 2][token % 4]: in both, the 16 bytes that a lane of a matrix product has lie next to its
+// neighbours'.  Blocks are written, copied into LDS and read there in whole lines, without bank conflicts, and the values
+// come transposed as the second product takes them.
 #include <algorithm>
 #include <type_traits>
 
@@ -113,68 +115,85 @@ __global__ __launch_bounds__(kThreads, 1) void latent_expand_kernel(LatentArgs x
   // W and V: a wave's rows, 128 elements a step, loaded again for the next step (maybe of the next head) as soon as a
   // line has been used.
   constexpr int kStep = 128, kHeadSteps = L / kStep;
-  u32x4_t w[kBlocks][8];
-  auto load = [&](int h, int s, int b, int y) {
-    const uint16_t* src = x.w + (h0 + h) * x.w_hs + (wave * kMine + 32 * b + col) * x.w_rs + 32 * half + kStep * s;
-    w[b][y] = *reinterpret_cast<const u32x4_t*>(src + 64 * (y >> 2) + 8 * (y & 3));
-  };
+  // Waves that make values have the product's other order, so that a lane gets tokens of an element.
+  auto make = [&](auto which) {
+    constexpr bool kValues = decltype(which)::value;
+    u32x4_t w[kBlocks][8];
+    auto load = [&](int h, int s, int b, int y) {
+      const uint16_t* src = x.w + (h0 + h) * x.w_hs + (wave * kMine + 32 * b + col) * x.w_rs + 32 * half + kStep * s;
+      w[b][y] = *reinterpret_cast<const u32x4_t*>(src + 64 * (y >> 2) + 8 * (y & 3));
+    };
 #pragma unroll
-  for (int y = 0; y < 8; ++y)
+    for (int y = 0; y < 8; ++y)
 #pragma unroll
-    for (int b = 0; b < kBlocks; ++b) load(hb, 0, b, y);
-  for (int h = hb; h < he; ++h) {
-    f32x16 o[kBlocks][kGroupUnits];
-#pragma unroll
-    for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-      for (int u = 0; u < kGroupUnits; ++u)
-#pragma unroll
-        for (int j = 0; j < 16; ++j) o[b][u][j] = 0.f;
-#pragma unroll 1
-    for (int s = 0; s < kHeadSteps; ++s) {
-      const bool last = s + 1 == kHeadSteps;
-      const int next_h = last ? min(h + 1, he - 1) : h, next_s = last ? 0 : s + 1;
-      const uint16_t* src = rows + col * kPitch + kStep * s + 32 * half;
-      auto token = [&](int i) {  // operand of y = i / 4 and unit i % 4
-        const int y = i / kGroupUnits, u = i % kGroupUnits;
-        return as_bf16x8(*reinterpret_cast<const u32x4_t*>(src + 32 * u * kPitch + 64 * (y >> 2) + 8 * ((y & 3) ^ f)));
-      };
-      constexpr int kAhead = 4, kAll = 8 * kGroupUnits;
-      bf16x8 k[kAll];
-#pragma unroll
-      for (int i = 0; i < kAhead; ++i) k[i] = token(i);
-      issue_first();
-#pragma unroll
-      for (int i = 0; i < kAll; ++i) {
-        const int y = i / kGroupUnits, u = i % kGroupUnits;
-        if (i + kAhead < kAll) k[i + kAhead] = token(i + kAhead);
-#pragma unroll
-        for (int b = 0; b < kBlocks; ++b)
-          o[b][u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(w[b][y]), k[i], o[b][u], 0, 0, 0);
-        if (u + 1 == kGroupUnits && y % 4 == 3) {  // the four loads of a line together, while it is in the cache
-#pragma unroll
-          for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-            for (int z = y - 3; z <= y; ++z) load(next_h, next_s, b, z);
-        }
-        issue_first();
-      }
-    }
-    const bool is_v = wave * kMine >= D;
-    uint16_t* dst = is_v ? values + (h * slots + slot0) * D + (wave * kMine - D) * kUnit
-                         : keys + (h * slots + slot0) * kKeyRow + wave * kMine * kUnit;
-    const int block = (is_v ? D : kKeyRow) * kUnit;
-#pragma unroll
-    for (int u = 0; u < kGroupUnits; ++u) {
-      if (u0 + u >= n) break;
+      for (int b = 0; b < kBlocks; ++b) load(hb, 0, b, y);
+    for (int h = hb; h < he; ++h) {
+      f32x16 o[kBlocks][kGroupUnits];
 #pragma unroll
       for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-        for (int y = 0; y < 4; ++y)
-          *reinterpret_cast<u32x2_t*>(dst + u * block + ((4 * b + y) * kUnit + col) * 8 + 4 * half) =
-              u32x2_t{pack2(o[b][u][4 * y], o[b][u][4 * y + 1]), pack2(o[b][u][4 * y + 2], o[b][u][4 * y + 3])};
+        for (int u = 0; u < kGroupUnits; ++u)
+#pragma unroll
+          for (int j = 0; j < 16; ++j) o[b][u][j] = 0.f;
+#pragma unroll 1
+      for (int s = 0; s < kHeadSteps; ++s) {
+        const bool last = s + 1 == kHeadSteps;
+        const int next_h = last ? min(h + 1, he - 1) : h, next_s = last ? 0 : s + 1;
+        const uint16_t* src = rows + col * kPitch + kStep * s + 32 * half;
+        auto token = [&](int i) {  // operand of y = i / 4 and unit i % 4
+          const int y = i / kGroupUnits, u = i % kGroupUnits;
+          return as_bf16x8(*reinterpret_cast<const u32x4_t*>(src + 32 * u * kPitch + 64 * (y >> 2) + 8 * ((y & 3) ^ f)));
+        };
+        constexpr int kAhead = 4, kAll = 8 * kGroupUnits;
+        bf16x8 k[kAll];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) k[i] = token(i);
+        issue_first();
+#pragma unroll
+        for (int i = 0; i < kAll; ++i) {
+          const int y = i / kGroupUnits, u = i % kGroupUnits;
+          if (i + kAhead < kAll) k[i + kAhead] = token(i + kAhead);
+#pragma unroll
+          for (int b = 0; b < kBlocks; ++b)
+            o[b][u] = kValues ? __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[i], as_bf16x8(w[b][y]), o[b][u], 0, 0, 0)
+                              : __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(w[b][y]), k[i], o[b][u], 0, 0, 0);
+          if (u + 1 == kGroupUnits && y % 4 == 3) {  // the four loads of a line together, while it is in the cache
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+              for (int z = y - 3; z <= y; ++z) load(next_h, next_s, b, z);
+          }
+          issue_first();
+        }
+      }
+      uint16_t* dst = kValues ? values + (h * slots + slot0) * D + (wave * kMine - D + col + half * D) * 8
+                              : keys + (h * slots + slot0) * kKeyRow + wave * kMine * kUnit + col * 8 + 4 * half;
+#pragma unroll
+      for (int u = 0; u < kGroupUnits; ++u) {
+        if (u0 + u >= n) break;
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b) {
+          u32x4_t v[2];
+#pragma unroll
+          for (int y = 0; y < 8; ++y) v[y >> 2][y & 3] = pack2(o[b][u][2 * y], o[b][u][2 * y + 1]);
+          if constexpr (kValues) {  // a lane has an element's tokens
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+              *reinterpret_cast<u32x4_t*>(dst + u * kUnit * D + (2 * y * D + 32 * b) * 8) = v[y];
+          } else {                  // a token's elements
+#pragma unroll
+            for (int y = 0; y < 4; ++y)
+              *reinterpret_cast<u32x2_t*>(dst + u * kUnit * kKeyRow + (4 * b + y) * kUnit * 8) =
+                  u32x2_t{v[y >> 1][2 * (y & 1)], v[y >> 1][2 * (y & 1) + 1]};
+          }
+        }
+      }
     }
-  }
+  };
+  if (wave * kMine >= D)
+    make(std::true_type{});
+  else
+    make(std::false_type{});
 }
 
 // ---------------------------------------------------------------- attention
@@ -184,8 +203,7 @@ constexpr int kTileRows = 128;
 template <int D>
 struct ExpandedShape {
   static constexpr int kKey = D + kRopeDim;
-  static constexpr int kBatch = 128;         // units resolved at a time
-  static constexpr int kKeyPitch = kKey + 32, kValuePitch = D + 32;
+  static constexpr int kBatch = 128;  // units resolved at a time
 };
 
 // Tiles of 128 rows (new tokens) of a head, 32 a wave.  A step t makes the scores of unit t, the weights of unit t - 1
@@ -207,8 +225,8 @@ __global__ __launch_bounds__(kThreads, 2) void expanded_attend_kernel(LatentArgs
   constexpr int kPieces = kKeyLoads + kValueLoads;
   static_assert(kUnit * kKeyChunks % kThreads == 0 && kUnit * kValueChunks % kThreads == 0, "whole loads");
   extern __shared__ int dyn[];  // of the chunk list: ub[k + 1], tb[k + 1]
-  __shared__ __align__(16) uint16_t keys[2][kUnit * S::kKeyPitch];
-  __shared__ __align__(16) uint16_t values[4][kUnit * S::kValuePitch];
+  __shared__ __align__(16) uint16_t keys[2][kUnit * S::kKey];
+  __shared__ __align__(16) uint16_t values[4][kUnit * D];
   __shared__ Unit list[S::kBatch];
   __shared__ int tmp[2 * kWaves];
   __shared__ uint32_t bad_tok[4];  // tokens of a masked unit whose values are not finite
@@ -250,19 +268,8 @@ __global__ __launch_bounds__(kThreads, 2) void expanded_attend_kernel(LatentArgs
   float rounded = 0.f;  // sum of the weights as the second product takes them
   bool poison = false;
 
-  const int f = exchange(col);
-  const int even = col * S::kKeyPitch + 8 * (half ^ f), odd = col * S::kKeyPitch + 8 * ((2 + half) ^ f);
-  const Transposed<S::kValuePitch> columns(lane);
-  // a thread's 16-byte pieces of a unit: of the key rows, then of the value rows
-  u32x4_t p[kPieces];
-  int row_of[kPieces], place_of[kPieces];  // the piece's token, and where it goes in LDS
-#pragma unroll
-  for (int z = 0; z < kPieces; ++z) {
-    const bool is_v = z >= kKeyLoads;
-    const int at = tid + (is_v ? z - kKeyLoads : z) * kThreads;
-    row_of[z] = at % kUnit;
-    place_of[z] = row_of[z] * (is_v ? S::kValuePitch : S::kKeyPitch) + 8 * ((at / kUnit) ^ exchange(row_of[z]));
-  }
+  const int key_at = 8 * (half * kUnit + col), value_at = 8 * (half * D + col);
+  u32x4_t p[kPieces];  // a thread's 16-byte pieces of a unit: of its keys (of token tid % 32), then of its values
 
   for (int last = u1 - 1; last >= u0; last -= S::kBatch) {
     __syncthreads();
@@ -271,7 +278,7 @@ __global__ __launch_bounds__(kThreads, 2) void expanded_attend_kernel(LatentArgs
     if (n == 0) continue;
     if (tid < 4) bad_tok[tid] = 0;
     // the first two steps' second products are of weights 0: their values have to be numbers
-    for (int z = tid; z < 2 * kUnit * S::kValuePitch / 8; z += kThreads)
+    for (int z = tid; z < 2 * kUnit * D / 8; z += kThreads)
       reinterpret_cast<u32x4_t*>(values[2])[z] = u32x4_t{0, 0, 0, 0};
     __syncthreads();
     const uint32_t mine = 16u * tid;
@@ -282,23 +289,34 @@ __global__ __launch_bounds__(kThreads, 2) void expanded_attend_kernel(LatentArgs
     };
     // tokens that a masked unit does not hold are cleared, values that are not finite are noted and left out
     auto check = [&](const Unit& u, int to) {
+      if (u.held() < kUnit) {
 #pragma unroll
-      for (int z = 0; z < kPieces; ++z) {
-        if (row_of[z] >= u.held()) p[z] = u32x4_t{0, 0, 0, 0};
-        if (z < kKeyLoads) continue;
+        for (int z = 0; z < kKeyLoads; ++z)
+          if (tid % kUnit >= u.held()) p[z] = u32x4_t{0, 0, 0, 0};
+      }
+#pragma unroll
+      for (int z = kKeyLoads; z < kPieces; ++z) {
         u16x2 most = {0, 0};
 #pragma unroll
         for (int j = 0; j < 4; ++j)
           most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, p[z][j] & 0x7FFF7FFFu));
-        if (most[0] >= 0x7F80u || most[1] >= 0x7F80u) {
-          atomicOr(&bad_tok[to], 1u << row_of[z]);
-          p[z] = u32x4_t{0, 0, 0, 0};
+        if (u.held() == kUnit && most[0] < 0x7F80u && most[1] < 0x7F80u) continue;
+        const int block = ((z - kKeyLoads) * kThreads + tid) / D;
+        uint32_t bad = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int t = 16 * (block >> 1) + 4 * (block & 1) + 8 * (j >> 2) + (j & 3);
+          const bool wrong = (p[z][j >> 1] >> 16 * (j & 1) & 0x7FFFu) >= 0x7F80u;
+          if (t >= u.held() || wrong) p[z][j >> 1] &= 0xFFFFu << 16 * (1 - (j & 1));
+          if (t < u.held() && wrong) bad |= 1u << t;
         }
+        if (bad) atomicOr(&bad_tok[to], bad);
       }
     };
     // Piece z of the next unit, and the load of the same piece of the one after it.
     auto advance = [&](int to, const Unit& from, int z) {
-      *reinterpret_cast<u32x4_t*>((z < kKeyLoads ? keys[to & 1] : values[to & 3]) + place_of[z]) = p[z];
+      uint16_t* dst = z < kKeyLoads ? keys[to & 1] + 8 * z * kThreads : values[to & 3] + 8 * (z - kKeyLoads) * kThreads;
+      *reinterpret_cast<u32x4_t*>(dst + 8 * tid) = p[z];
       load(from, z);
     };
     Unit u = uniform_unit(list[0]), next = uniform_unit(list[min(1, n - 1)]), old = u;
@@ -354,7 +372,7 @@ __global__ __launch_bounds__(kThreads, 2) void expanded_attend_kernel(LatentArgs
       {
         constexpr int kAhead = 3;
         auto key = [&](int y) {
-          return *reinterpret_cast<const u32x4_t*>(kp + (y & 1 ? odd : even) + 32 * (y >> 1));
+          return *reinterpret_cast<const u32x4_t*>(kp + key_at + 16 * kUnit * y);
         };
         u32x4_t k[kSteps];
 #pragma unroll
@@ -373,7 +391,9 @@ __global__ __launch_bounds__(kThreads, 2) void expanded_attend_kernel(LatentArgs
       }
       {  // the second product of unit t - 2: operand o has columns 32 (o / 2), tokens 16 (o % 2)
         constexpr int kAhead = 3;
-        auto value = [&](int o) { return columns(vp + 16 * (o & 1) * S::kValuePitch + 32 * (o >> 1)); };
+        auto value = [&](int o) {
+          return as_bf16x8(*reinterpret_cast<const u32x4_t*>(vp + value_at + 8 * (2 * (o & 1) * D + 32 * (o >> 1))));
+        };
         bf16x8 v[kOps];
 #pragma unroll
         for (int o = 0; o < kAhead; ++o) v[o] = value(o);
