@@ -44,7 +44,10 @@ __global__ __launch_bounds__(kThreads) void latent_units_kernel(AttendArgs a, in
   const int req = blockIdx.x;
   const ChunkList L = scan_list<kThreads, false>(a, req, dyn, tmp);
   const int n = L.ub[a.k];
-  if (threadIdx.x == 0) counts[req] = n;
+  if (threadIdx.x == 0) {
+    counts[req] = n;
+    counts[a.m + req] = 0;  // whether some value made of the context is not finite
+  }
   for (int u = threadIdx.x; u < n; u += kThreads) {
     const int c = find_entry(L.ub, L.k, u);
     const int t = (u - L.ub[c]) * kUnit;
@@ -68,7 +71,7 @@ constexpr int kGroupTokens = kGroupUnits * kUnit;  // 128
 template <int FMT, int L, int D>
 __global__ __launch_bounds__(kThreads, 1) void latent_expand_kernel(LatentArgs x, int64_t units,
                                                                  const Source* __restrict__ sources,
-                                                                 const int* __restrict__ counts, int h0, int heads,
+                                                                 int* __restrict__ counts, int h0, int heads,
                                                                  int per, uint16_t* __restrict__ keys,
                                                                  uint16_t* __restrict__ values) {
   constexpr int kPitch = kPitchOf<L>, kKeyRow = D + kRopeDim, kMine = 2 * D / kWaves, kBlocks = kMine / 32;  // rows of W and V of a wave
@@ -166,6 +169,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_expand_kernel(LatentArgs x
           issue_first();
         }
       }
+      u16x2 most = {0, 0};
       uint16_t* dst = kValues ? values + (h * slots + slot0) * D + (wave * kMine - D + col + half * D) * 8
                               : keys + (h * slots + slot0) * kKeyRow + wave * kMine * kUnit + col * 8 + 4 * half;
 #pragma unroll
@@ -178,8 +182,12 @@ __global__ __launch_bounds__(kThreads, 1) void latent_expand_kernel(LatentArgs x
           for (int y = 0; y < 8; ++y) v[y >> 2][y & 3] = pack2(o[b][u][2 * y], o[b][u][2 * y + 1]);
           if constexpr (kValues) {  // a lane has an element's tokens
 #pragma unroll
-            for (int y = 0; y < 2; ++y)
+            for (int y = 0; y < 2; ++y) {
               *reinterpret_cast<u32x4_t*>(dst + u * kUnit * D + (2 * y * D + 32 * b) * 8) = v[y];
+#pragma unroll
+              for (int j = 0; j < 4; ++j)
+                most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, v[y][j] & 0x7FFF7FFFu));
+            }
           } else {                  // a token's elements
 #pragma unroll
             for (int y = 0; y < 4; ++y)
@@ -188,6 +196,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_expand_kernel(LatentArgs x
           }
         }
       }
+      if (kValues && (most[0] >= 0x7F80u || most[1] >= 0x7F80u)) counts[a.m + req] = 1;
     }
   };
   if (wave * kMine >= D)
@@ -206,6 +215,19 @@ struct ExpandedShape {
   static constexpr int kBatch = 128;  // units resolved at a time
 };
 
+// 16 bytes from `base` + `from` of each lane to LDS, lane after lane from `to` on.  In assembly, as the compiler would wait
+// for it at the next read of any LDS: wait_for_lds() and a barrier stand between it and what reads it.  (M0 is the
+// compiler's to save; its code here does not use it.)
+__device__ __forceinline__ void load_to_lds(const uint8_t* base, uint32_t from, const uint16_t* to) {
+  const uint32_t at = static_cast<uint32_t>(
+      reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) uint16_t*)to));
+  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1"
+               :
+               : "v"(from), "s"(base), "s"(__builtin_amdgcn_readfirstlane(at))
+               : "memory");
+}
+__device__ __forceinline__ void wait_for_lds() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
 // Tiles of 128 rows (new tokens) of a head, 32 a wave.  A step t makes the scores of unit t, the weights of unit t - 1
 // and the second product of unit t - 2, and unpacks unit t + 1: a wave issues in order, so that only what stands between
 // its matrix products overlaps with them, and the exponentials are shared out over all of a step's.  They go by the
@@ -216,6 +238,7 @@ __global__ __launch_bounds__(kThreads, 2) void expanded_attend_kernel(LatentArgs
                                                                    int64_t units, int h0, int heads,
                                                                    const uint16_t* __restrict__ key_rows,
                                                                    const uint16_t* __restrict__ value_rows,
+                                                                   const int* __restrict__ counts,
                                                                    float* __restrict__ part_o,
                                                                    RowState* __restrict__ part_ml) {
   using S = ExpandedShape<D>;
@@ -258,6 +281,7 @@ __global__ __launch_bounds__(kThreads, 2) void expanded_attend_kernel(LatentArgs
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) q[i] = i < D / 16 ? own[i < D / 16 ? i : 0] : turned[i < D / 16 ? 0 : i - D / 16];
   }
+  const bool odd = counts[a.m + __builtin_amdgcn_readfirstlane(t.req)] != 0;
   const float c = a.scale * kLog2e;
   const int64_t row0 = (g * a.m + __builtin_amdgcn_readfirstlane(t.req)) * units * kUnit;
   const uint8_t* my_keys = reinterpret_cast<const uint8_t*>(key_rows + row0 * S::kKey);
@@ -269,7 +293,6 @@ __global__ __launch_bounds__(kThreads, 2) void expanded_attend_kernel(LatentArgs
   bool poison = false;
 
   const int key_at = 8 * (half * kUnit + col), value_at = 8 * (half * D + col);
-  u32x4_t p[kPieces];  // a thread's 16-byte pieces of a unit: of its keys (of token tid % 32), then of its values
 
   for (int last = u1 - 1; last >= u0; last -= S::kBatch) {
     __syncthreads();
@@ -281,53 +304,42 @@ __global__ __launch_bounds__(kThreads, 2) void expanded_attend_kernel(LatentArgs
     for (int z = tid; z < 2 * kUnit * D / 8; z += kThreads)
       reinterpret_cast<u32x4_t*>(values[2])[z] = u32x4_t{0, 0, 0, 0};
     __syncthreads();
-    const uint32_t mine = 16u * tid;
-    auto load = [&](const Unit& u, int z) {  // (what lies behind the last held token is cleared before it is used)
+    // Piece z of a unit straight into LDS, 16 bytes a thread: of its keys (of token tid % 32), then of its values.
+    auto load = [&](const Unit& u, int to, int z) {
       const uint8_t* src = z < kKeyLoads ? my_keys + u.at * (kUnit * S::kKey * 2) + z * (16 * kThreads)
                                          : my_values + u.at * (kUnit * D * 2) + (z - kKeyLoads) * (16 * kThreads);
-      p[z] = *reinterpret_cast<const u32x4_t*>(src + mine);
+      const uint16_t* dst = z < kKeyLoads ? keys[to & 1] + 8 * z * kThreads : values[to & 3] + 8 * (z - kKeyLoads) * kThreads;
+      load_to_lds(src, 16 * tid, dst + 8 * 64 * wave);
     };
-    // tokens that a masked unit does not hold are cleared, values that are not finite are noted and left out
+    // Where some value of the request is not finite: those of a masked unit are noted and left out.  (A unit's values
+    // behind its tokens are 0, or not finite; its scores there are masked.)
     auto check = [&](const Unit& u, int to) {
-      if (u.held() < kUnit) {
+      u32x4_t* value = reinterpret_cast<u32x4_t*>(values[to & 3]) + tid;
 #pragma unroll
-        for (int z = 0; z < kKeyLoads; ++z)
-          if (tid % kUnit >= u.held()) p[z] = u32x4_t{0, 0, 0, 0};
-      }
-#pragma unroll
-      for (int z = kKeyLoads; z < kPieces; ++z) {
+      for (int z = 0; z < kValueLoads; ++z) {
+        u32x4_t p = value[z * kThreads];
         u16x2 most = {0, 0};
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, p[z][j] & 0x7FFF7FFFu));
-        if (u.held() == kUnit && most[0] < 0x7F80u && most[1] < 0x7F80u) continue;
-        const int block = ((z - kKeyLoads) * kThreads + tid) / D;
+        for (int j = 0; j < 4; ++j) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, p[j] & 0x7FFF7FFFu));
+        if (most[0] < 0x7F80u && most[1] < 0x7F80u) continue;
+        const int block = (z * kThreads + tid) / D;
         uint32_t bad = 0;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const int t = 16 * (block >> 1) + 4 * (block & 1) + 8 * (j >> 2) + (j & 3);
-          const bool wrong = (p[z][j >> 1] >> 16 * (j & 1) & 0x7FFFu) >= 0x7F80u;
-          if (t >= u.held() || wrong) p[z][j >> 1] &= 0xFFFFu << 16 * (1 - (j & 1));
+          const bool wrong = (p[j >> 1] >> 16 * (j & 1) & 0x7FFFu) >= 0x7F80u;
+          if (wrong) p[j >> 1] &= 0xFFFFu << 16 * (1 - (j & 1));
           if (t < u.held() && wrong) bad |= 1u << t;
         }
-        if (bad) atomicOr(&bad_tok[to], bad);
+        value[z * kThreads] = p;
+        if (bad) atomicOr(&bad_tok[to & 3], bad);
       }
-    };
-    // Piece z of the next unit, and the load of the same piece of the one after it.
-    auto advance = [&](int to, const Unit& from, int z) {
-      uint16_t* dst = z < kKeyLoads ? keys[to & 1] + 8 * z * kThreads : values[to & 3] + 8 * (z - kKeyLoads) * kThreads;
-      *reinterpret_cast<u32x4_t*>(dst + 8 * tid) = p[z];
-      load(from, z);
     };
     Unit u = uniform_unit(list[0]), next = uniform_unit(list[min(1, n - 1)]), old = u;
 #pragma unroll
-    for (int z = 0; z < kPieces; ++z) load(u, z);
-    if (u.masked()) check(u, 0);
-#pragma unroll
-    for (int z = 0; z < kPieces; ++z) {
-      advance(0, next, z);
-      issue_first();
-    }
+    for (int z = 0; z < kPieces; ++z) load(u, 0, z);
+    wait_for_lds();
+    if (odd && u.masked()) check(u, 0);
     __syncthreads();
     // Scores of units t and t - 1, weights of units t - 1 and t - 2: [t & 1] is made in step t.
     f32x16 s[2];
@@ -343,7 +355,8 @@ __global__ __launch_bounds__(kThreads, 2) void expanded_attend_kernel(LatentArgs
       u32x4_t(&wn)[2] = w[kNew];
       const Unit after = uniform_unit(list[min(i + 2, n - 1)]);
       if (tid == 0) bad_tok[(i + 2) & 3] = 0;
-      if (i + 1 < n && next.masked()) check(next, (i + 1) & 3);
+#pragma unroll
+      for (int z = 0; z < kPieces; ++z) load(next, i + 1, z);
       if (i > 0 && i <= n && old.masked()) {
         const uint32_t seen = visible_tokens(rule, old, prefix);
         mask_scores<32, 16>(so, seen, half);
@@ -382,7 +395,6 @@ __global__ __launch_bounds__(kThreads, 2) void expanded_attend_kernel(LatentArgs
         for (int y = 0; y < kSteps; ++y) {
           if (y + kAhead < kSteps) k[y + kAhead] = key(y + kAhead);
           sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(k[y]), q[y], sn, 0, 0, 0);
-          if (y * kPieces / kSteps != (y + 1) * kPieces / kSteps) advance(i + 1, after, y * kPieces / kSteps);
 #pragma unroll
           for (int j = 16 * y / kSteps; j < 16 * (y + 1) / kSteps; ++j) top = nan_max(top, so[j]);
           share(y);
@@ -425,6 +437,8 @@ __global__ __launch_bounds__(kThreads, 2) void expanded_attend_kernel(LatentArgs
 #pragma unroll
         for (int j = 0; j < 16; ++j) sn[j] = -INFINITY;
       }
+      wait_for_lds();
+      if (odd && i + 1 < n && next.masked()) check(next, i + 1);
       old = u;
       u = next;
       next = after;
@@ -491,7 +505,7 @@ ExpandedSpace expanded_space(const LatentSizes& s, const ExpandedPlan& p) {
   ExpandedSpace w;
   w.sources = 0;
   w.counts = align256(static_cast<size_t>(s.m) * s.units * sizeof(Source));
-  w.keys = w.counts + align256(s.m * sizeof(int));
+  w.keys = w.counts + align256(2 * s.m * sizeof(int));
   w.values = w.keys + align256(p.heads * slots * (s.head_dim + kRopeDim) * 2);
   w.part_o = w.values + align256(p.heads * slots * s.head_dim * 2);
   w.part_ml = w.part_o + (p.splits > 1 ? align256(p.splits * rows * s.head_dim * sizeof(float)) : 0);
@@ -525,7 +539,8 @@ hipError_t launch(const LatentArgs& x, const LatentSizes& s, hipStream_t stream)
                                       stream>>>(x, s.units, sources, counts, h0, heads, per, keys, values);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     expanded_attend_kernel<D><<<static_cast<unsigned>(p.tiles * heads * p.splits), kThreads, list_bytes(s.k),
-                                stream>>>(x, p.splits, p.tiles, s.units, h0, heads, keys, values, part_o, part_ml);
+                                stream>>>(x, p.splits, p.tiles, s.units, h0, heads, keys, values, counts, part_o,
+                                part_ml);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   }
   if (p.splits > 1) {
