@@ -67,7 +67,9 @@ constexpr int kGroupTokens = kGroupUnits * kUnit;  // 128
 // Workgroup (four units of a request, a share of the heads): the tokens' latent vectors stay in LDS as bf16; for each
 // head a wave makes a quarter of its keys' and values' elements for all 128 tokens, its rows of W and V straight from
 // memory.  The order of a product's k is free as long as both operands have it: lane (row, half) takes 64 consecutive
-// bytes of each 128 of its row.
+// bytes of each 128 of its row.  Bound by the waits for its loads and stores, which leave in order (matrix cores busy
+// 34 %): 4 x 8,192 tokens of 8 bits, 16 heads, 253 us with the latent vectors of a group loaded one after the other, 175
+// with all at once and W's and V's rows for the next head on their way.
 template <int FMT, int L, int D>
 __global__ __launch_bounds__(kThreads, 1) void latent_expand_kernel(LatentArgs x, int64_t units,
                                                                  const Source* __restrict__ sources,
@@ -216,12 +218,12 @@ struct ExpandedShape {
 };
 
 // 16 bytes from `base` + `from` of each lane to LDS, lane after lane from `to` on.  In assembly, as the compiler would wait
-// for it at the next read of any LDS: wait_for_lds() and a barrier stand between it and what reads it.  (M0 is the
-// compiler's to save; its code here does not use it.)
+// for it at the next read of any LDS: wait_for_lds() and a barrier stand between it and what reads it.  M0 is the
+// compiler's to save, whose code here does not use it (a host test looks); a wait state has to follow its write.
 __device__ __forceinline__ void load_to_lds(const uint8_t* base, uint32_t from, const uint16_t* to) {
   const uint32_t at = static_cast<uint32_t>(
       reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) uint16_t*)to));
-  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1"
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
                :
                : "v"(from), "s"(base), "s"(__builtin_amdgcn_readfirstlane(at))
                : "memory");
@@ -229,10 +231,14 @@ __device__ __forceinline__ void load_to_lds(const uint8_t* base, uint32_t from, 
 __device__ __forceinline__ void wait_for_lds() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 // Tiles of 128 rows (new tokens) of a head, 32 a wave.  A step t makes the scores of unit t, the weights of unit t - 1
-// and the second product of unit t - 2, and unpacks unit t + 1: a wave issues in order, so that only what stands between
-// its matrix products overlaps with them, and the exponentials are shared out over all of a step's.  They go by the
+// and the second product of unit t - 2, while unit t + 1 goes straight into LDS: a wave issues in order, so that only what
+// stands between its matrix products overlaps with them, and the exponentials are shared out over all of a step's.  They go by the
 // running maximum as it is; where a score turns out to be above it by more than the lag (rare: the largest score of a
 // unit is known at the end of its step), that unit's are made again.
+// Bound by issue: 8,192 tokens behind 24,576, 32 heads of 128, matrix cores busy 48 % and the vector unit issuing 47 % of
+// the cycles.  5,780 us with rows in a pitch and values transposed on their way out of LDS (a quarter of whose cycles were
+// bank conflicts); 5,680 with blocks as they lie in the workspace; 5,530 without the way through registers, 13 of which
+// were spilled.  Units loaded two steps ahead change nothing.
 template <int D>
 __global__ __launch_bounds__(kThreads, 2) void expanded_attend_kernel(LatentArgs x, int splits, int64_t tiles,
                                                                    int64_t units, int h0, int heads,
