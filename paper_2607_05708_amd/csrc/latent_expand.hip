@@ -235,10 +235,10 @@ __device__ __forceinline__ void wait_for_lds() { asm volatile("s_waitcnt vmcnt(0
 // stands between its matrix products overlaps with them, and the exponentials are shared out over all of a step's.  They go by the
 // running maximum as it is; where a score turns out to be above it by more than the lag (rare: the largest score of a
 // unit is known at the end of its step), that unit's are made again.
-// Bound by issue: 8,192 tokens behind 24,576, 32 heads of 128, matrix cores busy 48 % and the vector unit issuing 47 % of
-// the cycles.  5,780 us with rows in a pitch and values transposed on their way out of LDS (a quarter of whose cycles were
-// bank conflicts); 5,680 with blocks as they lie in the workspace; 5,530 without the way through registers, 13 of which
-// were spilled.  Units loaded two steps ahead change nothing.
+// Bound by issue and the waits at a step's end: 8,192 tokens behind 24,576, 32 heads of 128, 4,830 us, the matrix cores busy
+// in 45 % and the vector unit issuing in 42 % of the cycles.  5,320 with rows in a pitch and values transposed on their way
+// out of LDS (a quarter of whose cycles were bank conflicts); 5,170 with blocks as they lie in the workspace, through
+// registers, 13 of which were spilled.  Units loaded two steps ahead change nothing with heads of 64.
 template <int D>
 __global__ __launch_bounds__(kThreads, 2) void expanded_attend_kernel(LatentArgs x, int splits, int64_t tiles,
                                                                    int64_t units, int h0, int heads,
