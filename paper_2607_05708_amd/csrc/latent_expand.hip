@@ -574,9 +574,10 @@ size_t expanded_workspace_bytes(const LatentSizes& s, bool ragged) {
   return expanded_space(s, expanded_plan(s, ragged)).end;
 }
 
+// (heads add workgroups to latent_expand_kernel only up to 512 of them: see launch())
 bool expanded_fits(const LatentSizes& s, bool ragged) {
   const ExpandedPlan p = expanded_plan(s, ragged);
-  return p.tiles * p.splits * p.heads <= kMaxGroups && expand_groups(s) <= kMaxGroups / s.heads && s.m <= kMaxGroups;
+  return p.tiles * p.splits * p.heads <= kMaxGroups && expand_groups(s) <= kMaxGroups && s.m <= kMaxGroups;
 }
 
 hipError_t launch_expanded(const LatentArgs& x, const LatentSizes& s, hipStream_t stream) {
