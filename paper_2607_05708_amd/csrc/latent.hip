@@ -727,7 +727,7 @@ __global__ __launch_bounds__(kThreads) void latent_out_kernel(LatentArgs x, int 
   constexpr int kPitch = L + 32, kPer = L / 64;
   __shared__ __align__(16) uint16_t high[kTokenBlock * kPitch], low[kTokenBlock * kPitch];
   __shared__ float halves[kShares == 2 ? kAcross * 64 * 16 : 1];
-  __shared__ bool sees[kTokenBlock];  // rows that see something: the others are 0 whatever V_h holds
+  __shared__ bool sees[kTokenBlock];  // rows that something counts for: the others are 0 whatever V_h holds
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 31, half = lane >> 5, j0 = 32 * (wave % kAcross), k0 = wave / kAcross * (L / kShares);
   const int h = blockIdx.x;
@@ -773,9 +773,14 @@ __global__ __launch_bounds__(kThreads) void latent_out_kernel(LatentArgs x, int 
         }
       }
       const float inv = inverse_sum(l);
-      seen = l != 0.f;
+      bool odd = false;
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) o[i] *= inv;
+      for (int i = 0; i < kPer; ++i) {
+        o[i] *= inv;
+        odd |= o[i] != o[i];
+      }
+      // (values that are not finite count behind weights of 0 too: scores of minus infinity)
+      seen = l != 0.f || __any(odd);
       if (x.a.lse && lane == 0) x.a.lse[at] = lse_of(m, l);
     }
     if (lane == 0) sees[r] = seen;
