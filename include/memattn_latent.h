@@ -86,12 +86,21 @@ typedef struct {
  *   MEM_LATENT_ABSORBED  takes W_h to the query (W_h^T q) and V_h behind the sum:
  *                        all heads share the latent vectors as keys and values, and
  *                        nothing is made of the context: for few new tokens.
- * MEM_LATENT_AUTO takes the one that costs less, by the sizes on the host.
+ * MEM_LATENT_AUTO chooses by the sizes on the host alone: expanded where total_q / m,
+ * rounded down, is above head_dim * latent_dim / (latent_dim - head_dim), as costs less
+ * where the requests have about as many new tokens each and see most of their contexts.
+ * It does not know masks, lengths, or how new tokens are spread, and both forms are
+ * planned for contexts at their capacity: with a short window, documents of which little
+ * is seen, one long turn beside single tokens, or lists with room for much more than
+ * they hold, the other form may cost many times less, and the caller names it.
  */
 typedef enum { MEM_LATENT_AUTO = 0, MEM_LATENT_ABSORBED = 1, MEM_LATENT_EXPANDED = 2 } mem_latent_form;
 
 /* Workspace for mem_latent_attend with these sizes, whatever its masks and
- * q_offsets (0 on invalid sizes). */
+ * q_offsets (0 on invalid sizes).  The expanded form's holds keys and values of all m
+ * contexts at their capacity, m * k * pages_per_chunk * page_tokens * (2 head_dim +
+ * rope_dim) * 2 bytes a head, of as many heads as 1 GiB holds and of one at least; the
+ * absorbed form's goes by total_q * heads. */
 MEMATTN_API size_t mem_latent_attend_workspace_bytes(const mem_latent* cache, int64_t m, int32_t k, int64_t total_q,
                                                      int32_t heads, int32_t head_dim, int32_t form);
 
@@ -108,21 +117,27 @@ MEMATTN_API size_t mem_latent_attend_workspace_bytes(const mem_latent* cache, in
  * not see have no influence on it, whatever they hold; an element of a latent vector
  * that is not finite among those that it does see makes its outputs so, however small
  * its weight (one of a key part counts as its score says: nothing at -inf).  An
- * element of w that is not finite makes the outputs that take it so, of rows that see
- * something, and may make the others of its head so.  q and t (device bf16, strides
+ * element of V_h that is not finite makes the outputs that take it so, of rows that see
+ * something, and may make the others of its head so; one of W_h counts as the scores
+ * that it makes say.  q and t (device bf16, strides
  * in `q` and `t`, only read), out (device bf16 [total_q, heads, head_dim], contiguous,
  * 16-byte aligned) and lse (device fp32 [total_q, heads], nullable).  Rows that no
  * request owns are not written.  out, lse and the workspace must not overlap each
  * other, q, t, w or the pool.
  *
- * Products are bf16 with fp32 sums.  Rounded to bf16 on the way are W_h^T q and the
- * softmax weights in the absorbed form (the weighted sums of latent vectors are taken
- * through V_h as two bf16 numbers each), keys, values and weights in the expanded
- * form: a score is off by at most 2^-8 of the sum of its products' magnitudes, an
- * output by some 2^-7 of the largest value's magnitude.  The workspace is rewritten
- * by each call, and calls that share one must not overlap.  Nothing is synchronised;
- * the call can be captured into a HIP graph.
- * Calls whose tiles come to 2^24 or more are refused (MEM_ERR_UNSUPPORTED).
+ * Products are bf16 with fp32 sums.  Rounded to bf16 on the way are, in the absorbed
+ * form, W_h^T q and the softmax weights, in the expanded form keys, values and weights.
+ * (The absorbed form takes the weighted sums of latent vectors through V_h as two bf16
+ * numbers each, and so it takes the weights where a request has at most 32 rows on
+ * average, new tokens times heads, and a list of at most 2,559 chunks.)  A score is off
+ * by at most e = 2^-8 * scale * the sum of its products' magnitudes, besides fp32 sums;
+ * an output by at most exp(2 e) - 1 times sum exp(s(p) - lse) |V_h c_p|, with the largest
+ * e, and by 2^-7 times that sum for rounded weights, 2^-8 times it for rounded values, and
+ * 2^-8 of itself.  The workspace is rewritten by each call, and calls that share one must
+ * not overlap.  Nothing is synchronised; the call can be captured into a HIP graph.
+ * Refused (MEM_ERR_UNSUPPORTED) are calls whose tiles come to 2^24 or more; expanded
+ * ones whose contexts have room for 2^24 groups of 128 tokens; absorbed ones of more
+ * than 2^21 - 32 new tokens, or of 2^29 rows.
  */
 MEMATTN_API mem_status mem_latent_attend(const mem_latent* cache, const mem_attend_args* args, const mem_kv_rows* q,
                                          const mem_kv_rows* t, int64_t total_q, const mem_latent_weights* w,

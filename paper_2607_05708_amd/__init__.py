@@ -936,7 +936,9 @@ def mem_latent_attend(cache: LatentCache, tok_len: torch.Tensor, ids: torch.Tens
     queries and their rotated part; ``w`` bfloat16 [heads, 2 * head_dim, latent_dim] (any head and row strides): a
     head's keys are ``[w[h, :head_dim] c, r]``, its values ``w[h, head_dim:] c``.  Scores are ``scale (<q, W c> + <t,
     r>)``.  Requests, positions and masks as in mem_attend.  ``form``: MEM_LATENT_ABSORBED, MEM_LATENT_EXPANDED, or
-    the one that costs less.  ``lse`` (float32 [total_q, heads]) receives the log sums if it is given.  A token that
+    MEM_LATENT_AUTO, which goes by the mean of the requests' new tokens alone: with a short window, turns of unlike
+    length, or lists with room for much more than they hold (the expanded form's workspace grows with it), name the
+    form.  ``lse`` (float32 [total_q, heads]) receives the log sums if it is given.  A token that
     sees nothing gets zeros and an lse of -inf.
     """
     if ids.dim() != 2 or q.dim() != 3 or w.dim() != 3:

@@ -40,7 +40,8 @@ __device__ __forceinline__ u32x2_t load4(const uint16_t* p, bool vec) {
 
 // Workgroup (head, 128 of the L columns, tokens): W_h's part goes to LDS once, then products of 32 columns a wave with
 // blocks of 32 tokens.  (W is read once for eight blocks; 64 tokens of 32 heads of 128 by 512 take 8.4 us, 128 heads 16: half
-// of it the start, and 32 MB.)
+// of it the start, and 32 MB.)  They are rounded to bf16 as the operands of the scores' products: as two bf16 numbers
+// each, the attention would take 1.5 times the products.
 template <int L, int D>
 __global__ __launch_bounds__(kThreads) void latent_query_kernel(LatentArgs x, int blocks, uint16_t* __restrict__ rows) {
   constexpr int kCols = 128, kPitch = kCols + 32;
@@ -840,9 +841,9 @@ struct AbsorbedPlan {
   int side;  // tiles that follow each other on an XCD
 };
 
-// Parts of a context, by what a call would take in units of a tile: the passes of the busiest XCD's CUs, each with its
-// units and its start and end; then the join, of whose rows kJoinRows are written and read while a tile works on a unit.
-// (Both from timings of 14 shapes with 1 to 128 parts: one request of 48 tokens and 16 heads over 8,192, us: 1 part 555,
+// Parts of a context, taken at its capacity (the units of shorter ones, or that a window leaves, go to as many), by what a
+// call would take in units of a tile: the passes of the busiest XCD's CUs, each with its units and its start and end;
+// then the join, of whose rows kJoinRows are written and read while a tile works on a unit.  (Both from timings of 14 shapes with 1 to 128 parts: one request of 48 tokens and 16 heads over 8,192, us: 1 part 555,
 // 8 111, 16 84, 32 72, 40, which need a second pass, 104.)  Up to 128 parts, two states a lane of latent_out_kernel: one
 // token over 131,072, 16 heads, 64 us, with 64 parts 74; of 4 tokens 103 and 137.
 constexpr int64_t kStart = 16;
@@ -969,7 +970,8 @@ mem_latent_form choose_latent_form(const LatentSizes& s, int32_t asked) {
   // at 171 tokens): 8 requests over 8,192 tokens, 16 heads, 128 tokens 455 and 548, 256 764 and 584; one over 4,096, 128
   // heads, 128 tokens 218 and 286, 160 303 and 319; 256 elements, heads of 64 (86 tokens): 4 over 8,192, 64 tokens 100 and
   // 106, 128 156 and 126.  Single requests of few heads change over earlier (16 heads over 8,192: 64 tokens 79 and 89, 128
-  // 103 and 95) and short contexts at once (1,024: 16 tokens 50 and 40), by less than 30 us.
+  // 103 and 95) and short contexts at once (1,024: 16 tokens 50 and 40), by less than 30 us.  Masks, lengths and how new
+  // tokens are spread over the requests are not known here: the workspace is asked for without them.
   const int64_t rows = s.total_q / s.m, d = s.head_dim, l = s.latent;
   return rows * (l - d) > d * l ? MEM_LATENT_EXPANDED : MEM_LATENT_ABSORBED;
 }

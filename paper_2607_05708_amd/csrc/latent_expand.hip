@@ -67,8 +67,9 @@ constexpr int kGroupTokens = kGroupUnits * kUnit;  // 128
 // Workgroup (four units of a request, a share of the heads): the tokens' latent vectors stay in LDS as bf16; for each
 // head a wave makes a quarter of its keys' and values' elements for all 128 tokens, its rows of W and V straight from
 // memory.  The order of a product's k is free as long as both operands have it: lane (row, half) takes 64 consecutive
-// bytes of each 128 of its row.  Bound by the waits for its loads and stores, which leave in order (matrix cores busy
-// 34 %): 4 x 8,192 tokens of 8 bits, 16 heads, 253 us with the latent vectors of a group loaded one after the other, 175
+// bytes of each 128 of its row.  Keys and values are rounded to bf16 as the attention's operands: as two numbers each they
+// would take twice the memory and 1.7 to 1.8 times the attention's products.  Units that no row sees are made too.
+// Bound by the waits for its loads and stores, which leave in order (matrix cores busy 34 %): 4 x 8,192 tokens of 8 bits, 16 heads, 253 us with the latent vectors of a group loaded one after the other, 175
 // with all at once and W's and V's rows for the next head on their way.
 template <int FMT, int L, int D>
 __global__ __launch_bounds__(kThreads, 1) void latent_expand_kernel(LatentArgs x, int64_t units,
@@ -574,7 +575,7 @@ size_t expanded_workspace_bytes(const LatentSizes& s, bool ragged) {
   return expanded_space(s, expanded_plan(s, ragged)).end;
 }
 
-// (heads add workgroups to latent_expand_kernel only up to 512 of them: see launch())
+// (heads are shared out over more workgroups of latent_expand_kernel only where there are fewer than 512)
 bool expanded_fits(const LatentSizes& s, bool ragged) {
   const ExpandedPlan p = expanded_plan(s, ragged);
   return p.tiles * p.splits * p.heads <= kMaxGroups && expand_groups(s) <= kMaxGroups && s.m <= kMaxGroups;
