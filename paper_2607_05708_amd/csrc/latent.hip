@@ -126,7 +126,7 @@ struct LatentShape {
 // S^T = K Q^T and O^T = K^T P^T over the same rows of LDS, K the latent vectors (with the key part in the first product):
 // 2 (2 L + 64) operations a row and token for 2 bytes an element and less.  A unit is unpacked once for all rows of the tile,
 // into the third of three buffers, while the scores of one unit and the second product of the one before are made.
-// Bound by issue and the waits for LDS: 64 x 32,768 fp8 tokens, 128 heads of 512, 690 us (matrix cores busy 40 %); 16, 32
+// Bound by issue and the waits for LDS: 64 x 32,768 fp8 tokens, 128 heads of 512, 677 us (matrix cores busy 39 %); 16, 32
 // and 64 heads, in tiles of 16 to 64 rows, 279, 390 and 540.  Tiles of 256 rows (a wave with 64): 871 against 710 then.
 // Tiles of 32 RG rows: wave w has the 32 rows w / (4 / RG) of the tile and, of the second product, a share of the
 // columns; waves with the same rows make their scores each for itself.
@@ -473,7 +473,7 @@ constexpr int few_per_cu(int fmt, int latent) { return latent == 256 && fmt != M
 // from the page; unpacked, they are operands of the first product, and go through the wave's own LDS rows once to be
 // read back transposed for the second.  Each load is made again, for the wave's next unit, as soon as it has been used.
 // Weights go into the second product as two bf16 numbers.  Bound by HBM where contexts are long (4 x 131,072 bf16 tokens,
-// 16 heads: 115 us, 5.3 TB/s), else by its start and end: one token over 2,560, 3 units a workgroup, 16 us.
+// 16 heads: 116 us, 5.2 TB/s), else by its start and end: one token over 2,560, 4 units a workgroup, 16 us.
 template <int FMT, int L>
 __global__ __launch_bounds__(kThreads, few_per_cu(FMT, L)) void latent_few_kernel(LatentArgs x, int splits, int64_t tiles, int side,
                                                                              const uint16_t* __restrict__ query_rows,

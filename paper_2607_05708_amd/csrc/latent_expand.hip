@@ -69,8 +69,9 @@ constexpr int kGroupTokens = kGroupUnits * kUnit;  // 128
 // memory.  The order of a product's k is free as long as both operands have it: lane (row, half) takes 64 consecutive
 // bytes of each 128 of its row.  Keys and values are rounded to bf16 as the attention's operands: as two numbers each they
 // would take twice the memory and 1.7 to 1.8 times the attention's products.  Units that no row sees are made too.
-// Bound by the waits for its loads and stores, which leave in order (matrix cores busy 34 %): 4 x 8,192 tokens of 8 bits, 16 heads, 253 us with the latent vectors of a group loaded one after the other, 175
-// with all at once and W's and V's rows for the next head on their way.
+// Bound by the waits for its loads and stores, which leave in order (matrix cores busy 31 to 35 %): 4 x 8,192 tokens of 8
+// bits, 16 heads, 253 us with the latent vectors of a group loaded one after the other, 174 with all at once and W's and
+// V's rows for the next head on their way.
 template <int FMT, int L, int D>
 __global__ __launch_bounds__(kThreads, 1) void latent_expand_kernel(LatentArgs x, int64_t units,
                                                                  const Source* __restrict__ sources,
@@ -236,8 +237,8 @@ __device__ __forceinline__ void wait_for_lds() { asm volatile("s_waitcnt vmcnt(0
 // stands between its matrix products overlaps with them, and the exponentials are shared out over all of a step's.  They go by the
 // running maximum as it is; where a score turns out to be above it by more than the lag (rare: the largest score of a
 // unit is known at the end of its step), that unit's are made again.
-// Bound by issue and the waits at a step's end: 8,192 tokens behind 24,576, 32 heads of 128, 4,830 us, the matrix cores busy
-// in 45 % and the vector unit issuing in 42 % of the cycles.  5,320 with rows in a pitch and values transposed on their way
+// Bound by issue and the waits at a step's end: 8,192 tokens behind 24,576, 32 heads of 128, 4,830 us (5,150 on another
+// MI355X), the matrix cores busy in 45 % and the vector unit issuing in 42 % of the cycles.  5,320 with rows in a pitch and values transposed on their way
 // out of LDS (a quarter of whose cycles were bank conflicts); 5,170 with blocks as they lie in the workspace, through
 // registers, 13 of which were spilled.  Units loaded two steps ahead change nothing with heads of 64.
 template <int D>
