@@ -118,8 +118,8 @@ MEMATTN_API size_t mem_latent_attend_workspace_bytes(const mem_latent* cache, in
  * that is not finite among those that it does see makes its outputs so, however small
  * its weight (one of a key part counts as its score says: nothing at -inf).  An
  * element of V_h that is not finite makes the outputs that take it so, of rows that see
- * something, and may make the others of its head so; one of W_h counts as the scores
- * that it makes say.  q and t (device bf16, strides
+ * something with a score above -inf, and may make the others of its head so; one of W_h
+ * counts as the scores that it makes say.  q and t (device bf16, strides
  * in `q` and `t`, only read), out (device bf16 [total_q, heads, head_dim], contiguous,
  * 16-byte aligned) and lse (device fp32 [total_q, heads], nullable).  Rows that no
  * request owns are not written.  out, lse and the workspace must not overlap each
